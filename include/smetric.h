@@ -42,8 +42,8 @@
  *   - Host-detectable errors return immediately with nothing enqueued.
  *     Device-detectable errors (bad offsets, out-of-range tiers or loads, a
  *     full table) are latched in the index and reported by smetric_status.
- *   - Nothing here allocates device memory except smetric_index_create and
- *     smetric_index_set_lru.
+ *   - Nothing here allocates device memory except smetric_index_create,
+ *     smetric_index_set_lru and smetric_kv_create.
  */
 #ifndef SMETRIC_H
 #define SMETRIC_H
@@ -541,6 +541,149 @@ const char* smetric_profile_kernel_name(int32_t k);
 
 /* Kernels this index has launched since it was created. */
 int64_t smetric_launch_count(const smetric_index* idx);
+
+/* ---------------------------------------------------------------------------
+ * Paged KV$ blocks: what a serving instance does with the blocks that a route
+ * found. A prefix hit of c blocks leaves L - B*c tokens of the prompt to
+ * prefill (Figure 10(c)); on the instance their keys and values join the paged
+ * cache that holds the hit blocks, and their queries attend over both
+ * (Section 2: the KV$ of a prefix is reused by every later request with it).
+ * A page holds page_size tokens, so that a page is an index block when
+ * page_size is the index's block_size.
+ *
+ *   cache     keys and values of the same layout, [num_pages, page_size,
+ *             num_kv_heads, head_dim] with any page, token and head strides
+ *             (in elements) and contiguous head_dim.
+ *   batch     n_requests requests; request r's new tokens are rows
+ *             d_offsets[r] .. d_offsets[r+1] of q, k and v. Its length with
+ *             them is d_kv_lens[r], so new token j is at position
+ *             kv_len - (new tokens) + j, and position x is held at slot
+ *             x % page_size of page d_pages[r*pages_stride + x / page_size].
+ *
+ * A handle belongs to the device that was current at smetric_kv_create and
+ * holds one plan: the calls on one handle must not run concurrently on
+ * different streams. Errors as for an index: host-detectable ones return with
+ * nothing enqueued, device-detectable ones are latched in the handle and
+ * reported by smetric_kv_status. Arrays of heads and caches need 16-byte
+ * aligned pointers and strides that are multiples of 8 elements. */
+typedef struct smetric_kv smetric_kv; /* opaque, library-owned */
+
+#define SMETRIC_BF16 0
+#define SMETRIC_F16 1
+#define SMETRIC_KV_MAX_HEAD_DIM 128
+#define SMETRIC_KV_MAX_GROUP 128     /* query heads per key head */
+#define SMETRIC_KV_MAX_REQUESTS (1 << 20)
+#define SMETRIC_KV_MAX_TOKENS (1 << 26)
+#define SMETRIC_KV_INTERLEAVED 1     /* rotate pairs (2i, 2i+1) instead of (i, i + rot_dim/2) */
+
+typedef struct {
+  int32_t head_dim;           /* D, a multiple of 16, 16..SMETRIC_KV_MAX_HEAD_DIM */
+  int32_t num_q_heads;        /* a multiple of num_kv_heads; query head h reads key head h / (num_q_heads / num_kv_heads) */
+  int32_t num_kv_heads;       /* >= 1 */
+  int32_t page_size;          /* 16, 32, 64, 128 or 256 tokens */
+  int32_t dtype;              /* SMETRIC_BF16 or SMETRIC_F16, of q, k, v, the cache, the norm weights and the outputs */
+  int32_t flags;              /* 0 */
+  int64_t num_pages;          /* pages of the cache, 1..2^31-1 */
+  int64_t max_batch_requests; /* largest n_requests of a plan, <= SMETRIC_KV_MAX_REQUESTS */
+  int64_t max_batch_tokens;   /* largest n_tokens of a plan, <= SMETRIC_KV_MAX_TOKENS */
+} smetric_kv_config;
+
+/* Rows of heads: element d of head h of token t is at
+ * t*token_stride + h*head_stride + d. */
+typedef struct {
+  void* d_data;
+  int64_t token_stride;
+  int64_t head_stride;
+} smetric_heads;
+
+typedef struct {
+  void* d_k;
+  void* d_v;
+  int64_t page_stride;
+  int64_t token_stride;
+  int64_t head_stride;
+} smetric_kv_cache;
+
+/* What happens to a query or key head x on its way: with a norm weight,
+ * x <- x * rsqrt(mean(x^2) + eps) * weight over the head; then, with a table,
+ * the rotation of its first rot_dim elements by the token's position p:
+ * (a, b) <- (a cos - b sin, b cos + a sin) for the pairs (i, i + rot_dim/2)
+ * or, with SMETRIC_KV_INTERLEAVED, (2i, 2i+1). All in 32 bits, rounded once. */
+typedef struct {
+  const float* d_cos_sin;   /* NULL: no rotation; else [table_rows, rot_dim], 16-byte aligned: row p holds rot_dim/2 cosines, then as many sines */
+  int64_t table_rows;       /* a token at or past it latches OVERFLOW and is left out */
+  const void* d_q_norm;     /* NULL or [head_dim], 16-byte aligned */
+  const void* d_k_norm;
+  float eps;
+  int32_t rot_dim;          /* a multiple of 16, 0..head_dim */
+  int32_t flags;            /* SMETRIC_KV_INTERLEAVED or 0 */
+  int32_t reserved;         /* 0 */
+} smetric_kv_transform;
+
+/* Create a handle and its device memory on the current device: the plan (16
+ * bytes a token, 48 a request) and the partial results of sequences that
+ * several SMs share (2 * 256 * (head_dim + 2) floats an SM).
+ * Errors as smetric_index_create. */
+int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out);
+
+/* Free the handle and its device memory. Waits for the device first.
+ * NULL is accepted. */
+int smetric_kv_destroy(smetric_kv* kv);
+
+/* Plan a batch on the device, once for all layers of a model: where every new
+ * token goes and how the attention is shared out. The appends, norms and
+ * attention calls after it use this plan until the next one.
+ *   d_offsets  int64 [n_requests+1], non-decreasing, d_offsets[0] >= 0,
+ *              d_offsets[n_requests] <= n_tokens (tokens outside belong to no
+ *              request).
+ *   d_kv_lens  int32 [n_requests], at least the request's new tokens.
+ *   d_pages    int32 rows of max_pages page numbers (entries past a request's
+ *              length, and entries that lie before its window, are not
+ *              used), 4-byte aligned, row stride pages_stride >= max_pages.
+ *   window     0, or how many keys a query sees at most, its own among them.
+ * d_pages stays in use until the next plan: the attention reads it. Bad
+ * offsets or lengths latch INVALID_ARG and the batch counts as one of no
+ * requests; a page outside [0, num_pages) latches INVALID_ARG, an append
+ * leaves its tokens out, and the attention takes its keys and values as
+ * zeros. */
+int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests, int64_t n_tokens,
+                    const int32_t* d_kv_lens, const int32_t* d_pages, int32_t max_pages, int64_t pages_stride,
+                    int32_t window, smetric_stream_t stream);
+
+/* Append the planned batch's keys and values to the cache, the keys (and the
+ * queries, when q.d_data is not NULL, into q_out) transformed on the way.
+ * Two tokens with one slot are the caller's error (either may win). q_out may
+ * be q. A token that is left out keeps its slot and its q_out as they were. */
+int smetric_kv_append(smetric_kv* kv, smetric_kv_cache cache, smetric_heads k, smetric_heads v, smetric_heads q,
+                      smetric_heads q_out, smetric_kv_transform t, smetric_stream_t stream);
+
+/* The transform alone, for n_tokens tokens at d_positions (int32 [n_tokens];
+ * a negative one latches OVERFLOW and the token is left out), which need no
+ * plan. Outputs may be the inputs; q or k may be absent (d_data NULL). */
+int smetric_qk_norm_rope(smetric_kv* kv, smetric_heads q, smetric_heads k, const int32_t* d_positions,
+                         int64_t n_tokens, smetric_kv_transform t, smetric_heads q_out, smetric_heads k_out,
+                         smetric_stream_t stream);
+
+/* Attention of the planned batch's queries over the paged cache, which holds
+ * the new tokens' keys and values already: for a query at position p, over the
+ * keys of its request at positions max(0, p - window + 1) .. p,
+ *   out = sum_j softmax_j(scale * q.k_j) v_j,  lse = log sum_j exp(scale * q.k_j).
+ * Single tokens, chunks and whole prompts may share a batch. Scores, softmax
+ * and sums are held in 32 bits; the softmax's weights are rounded to dtype for
+ * the product with the values. A token of no request gets out = 0 and
+ * lse = -inf. scale is finite and > 0. d_lse: NULL or float [n_tokens,
+ * num_q_heads]. out must not overlap q. Values at masked positions of a
+ * request's own length must be finite; what lies past its length or before
+ * its window may be anything. */
+int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_heads q, float scale, smetric_heads out,
+                            float* d_lse, smetric_stream_t stream);
+
+/* Wait for `stream`, then return and clear the first error the device latched
+ * for this handle. */
+int smetric_kv_status(smetric_kv* kv, smetric_stream_t stream);
+
+/* Kernels this handle has launched since it was created. */
+int64_t smetric_kv_launch_count(const smetric_kv* kv);
 
 #ifdef __cplusplus
 }

@@ -7,7 +7,8 @@ torch.cuda.Stream, a raw cudaStream_t (int) or None for torch's current
 stream. Every computation runs in the library's CUDA kernels; there is no
 CPU fallback, and using the binding without the built library raises.
 
-SMetricIndex wraps one index and allocates output tensors for convenience.
+SMetricIndex wraps one index and SMetricKV one handle of the paged KV$
+operators; both allocate output tensors for convenience.
 """
 
 from __future__ import annotations
@@ -43,6 +44,13 @@ SMETRIC_IMBALANCE_MAX_REQUESTS = 1 << 26
 SMETRIC_IMBALANCE_MAX_CELLS = 1 << 31
 SMETRIC_SCORER_BAILIAN = 1
 SMETRIC_SCORER_LMETRIC = 2
+SMETRIC_BF16 = 0
+SMETRIC_F16 = 1
+SMETRIC_KV_MAX_HEAD_DIM = 128
+SMETRIC_KV_MAX_GROUP = 128
+SMETRIC_KV_MAX_REQUESTS = 1 << 20
+SMETRIC_KV_MAX_TOKENS = 1 << 26
+SMETRIC_KV_INTERLEAVED = 1
 
 EXPORTED = (
     "smetric_index_create", "smetric_index_destroy", "smetric_index_clear",
@@ -55,6 +63,8 @@ EXPORTED = (
     "smetric_route_batch_baseline", "smetric_route_batch_sequential", "smetric_reuse_workspace_bytes",
     "smetric_reuse_breakdown", "smetric_imbalance_workspace_bytes", "smetric_window_imbalance",
     "smetric_route_batches", "smetric_index_set_lru", "smetric_index_lru_sizes", "smetric_route_commit_batch",
+    "smetric_kv_create", "smetric_kv_destroy", "smetric_kv_plan", "smetric_kv_append", "smetric_qk_norm_rope",
+    "smetric_paged_attention", "smetric_kv_status", "smetric_kv_launch_count",
 )
 
 
@@ -85,6 +95,27 @@ class smetric_policy(C.Structure):
     _fields_ = [("c_lin", C.c_int64), ("c_att", C.c_int64), ("ttft_d0", C.c_int64),
                 ("ttft_d1", C.c_int64), ("hit_num", C.c_int64), ("hit_den", C.c_int64),
                 ("rr_base", C.c_int32), ("reserved", C.c_int32)]
+
+
+class smetric_kv_config(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32),
+                ("page_size", C.c_int32), ("dtype", C.c_int32), ("flags", C.c_int32), ("num_pages", C.c_int64),
+                ("max_batch_requests", C.c_int64), ("max_batch_tokens", C.c_int64)]
+
+
+class smetric_heads(C.Structure):
+    _fields_ = [("d_data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class smetric_kv_cache(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
+
+
+class smetric_kv_transform(C.Structure):
+    _fields_ = [("d_cos_sin", C.c_void_p), ("table_rows", C.c_int64), ("d_q_norm", C.c_void_p),
+                ("d_k_norm", C.c_void_p), ("eps", C.c_float), ("rot_dim", C.c_int32), ("flags", C.c_int32),
+                ("reserved", C.c_int32)]
 
 
 _lib = None
@@ -144,6 +175,17 @@ def lib():
             "smetric_profile_read": (C.c_int, [P, I32, P, P]),
             "smetric_profile_kernel_name": (C.c_char_p, [I32]),
             "smetric_launch_count": (I64, [P]),
+            "smetric_kv_create": (C.c_int, [C.POINTER(smetric_kv_config), C.POINTER(P)]),
+            "smetric_kv_destroy": (C.c_int, [P]),
+            "smetric_kv_plan": (C.c_int, [P, P, I32, I64, P, P, I32, I64, I32, P]),
+            "smetric_kv_append": (C.c_int, [P, smetric_kv_cache, smetric_heads, smetric_heads, smetric_heads,
+                                            smetric_heads, smetric_kv_transform, P]),
+            "smetric_qk_norm_rope": (C.c_int, [P, smetric_heads, smetric_heads, P, I64, smetric_kv_transform,
+                                               smetric_heads, smetric_heads, P]),
+            "smetric_paged_attention": (C.c_int, [P, smetric_kv_cache, smetric_heads, C.c_float, smetric_heads, P,
+                                                  P]),
+            "smetric_kv_status": (C.c_int, [P, P]),
+            "smetric_kv_launch_count": (I64, [P]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -417,8 +459,50 @@ def smetric_launch_count(idx: int) -> int:
     return int(lib().smetric_launch_count(idx))
 
 
+def smetric_kv_create(cfg: smetric_kv_config) -> int:
+    h = C.c_void_p()
+    _check(lib().smetric_kv_create(C.byref(cfg), C.byref(h)), "smetric_kv_create")
+    return h.value
+
+
+def smetric_kv_destroy(kv: int) -> None:
+    _check(lib().smetric_kv_destroy(kv), "smetric_kv_destroy")
+
+
+def smetric_kv_plan(kv: int, d_offsets, n_requests: int, n_tokens: int, d_kv_lens, d_pages, max_pages: int,
+                    pages_stride: int, window: int = 0, stream=None) -> None:
+    _check(lib().smetric_kv_plan(kv, _ptr(d_offsets), n_requests, n_tokens, _ptr(d_kv_lens), _ptr(d_pages), max_pages,
+                                 pages_stride, window, _stream(stream)), "smetric_kv_plan")
+
+
+def smetric_kv_append(kv: int, cache: smetric_kv_cache, k: smetric_heads, v: smetric_heads, q: smetric_heads,
+                      q_out: smetric_heads, transform: smetric_kv_transform, stream=None) -> None:
+    _check(lib().smetric_kv_append(kv, cache, k, v, q, q_out, transform, _stream(stream)), "smetric_kv_append")
+
+
+def smetric_qk_norm_rope(kv: int, q: smetric_heads, k: smetric_heads, d_positions, n_tokens: int,
+                         transform: smetric_kv_transform, q_out: smetric_heads, k_out: smetric_heads,
+                         stream=None) -> None:
+    _check(lib().smetric_qk_norm_rope(kv, q, k, _ptr(d_positions), n_tokens, transform, q_out, k_out,
+                                      _stream(stream)), "smetric_qk_norm_rope")
+
+
+def smetric_paged_attention(kv: int, cache: smetric_kv_cache, q: smetric_heads, scale: float, out: smetric_heads,
+                            d_lse=None, stream=None) -> None:
+    _check(lib().smetric_paged_attention(kv, cache, q, scale, out, _ptr(d_lse), _stream(stream)),
+           "smetric_paged_attention")
+
+
+def smetric_kv_status(kv: int, stream=None) -> int:
+    return int(lib().smetric_kv_status(kv, _stream(stream)))
+
+
+def smetric_kv_launch_count(kv: int) -> int:
+    return int(lib().smetric_kv_launch_count(kv))
+
+
 # ---------------------------------------------------------------------------
-# convenience wrapper
+# convenience wrappers
 # ---------------------------------------------------------------------------
 
 class SMetricIndex:
@@ -684,6 +768,160 @@ class SMetricIndex:
 
     def status(self, stream=None) -> int:
         return smetric_status(self.handle, stream)
+
+    def check(self, stream=None):
+        rc = self.status(stream)
+        if rc != SMETRIC_OK:
+            raise SmetricError(rc, "device")
+
+
+class SMetricKV:
+    """The paged KV$ operators for one layout of heads and pages, with torch
+    tensors. Caches are [num_pages, page_size, num_kv_heads, head_dim] views
+    (any strides but the last), heads [tokens, heads, head_dim] views.
+
+        kv = SMetricKV(head_dim=128, num_q_heads=32, num_kv_heads=4, page_size=32, num_pages=4096,
+                       max_batch_requests=64, max_batch_tokens=8192)
+        kv.plan(offsets_i64, kv_lens_i32, pages_i32, n_tokens)       # once a step
+        kv.append(k_cache, v_cache, k, v, q=q, q_out=q, cos_sin=table, q_norm=wq, k_norm=wk)
+        out = kv.paged_attention(q, k_cache, v_cache)
+        kv.check()
+    """
+
+    def __init__(self, head_dim: int, num_q_heads: int, num_kv_heads: int, page_size: int, num_pages: int,
+                 max_batch_requests: int, max_batch_tokens: int, dtype=None):
+        import torch
+        self.dtype = torch.bfloat16 if dtype is None else dtype
+        code = {torch.bfloat16: SMETRIC_BF16, torch.float16: SMETRIC_F16}.get(self.dtype)
+        if code is None:
+            raise ValueError("dtype must be torch.bfloat16 or torch.float16")
+        self.cfg = smetric_kv_config(head_dim, num_q_heads, num_kv_heads, page_size, code, 0, num_pages,
+                                     max_batch_requests, max_batch_tokens)
+        self.handle = smetric_kv_create(self.cfg)
+        self._n_tokens = None
+        self._kept = None
+
+    def close(self):
+        if getattr(self, "handle", None):
+            smetric_kv_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _heads(self, x, heads: int, n_tokens: int, name: str) -> smetric_heads:
+        if x is None:
+            return smetric_heads()
+        if x.dtype != self.dtype or tuple(x.shape) != (n_tokens, heads, self.cfg.head_dim):
+            raise ValueError(f"{name} must be {self.dtype} [{n_tokens}, {heads}, {self.cfg.head_dim}]")
+        if x.numel() and x.stride(2) != 1:
+            raise ValueError(f"{name}: the elements of a head must be contiguous")
+        # (the stride of a dimension of one is arbitrary)
+        return smetric_heads(x.data_ptr(), x.stride(0) if n_tokens > 1 else 0, x.stride(1) if heads > 1 else 0)
+
+    def _cache(self, k_cache, v_cache) -> smetric_kv_cache:
+        c = self.cfg
+        shape = (c.num_pages, c.page_size, c.num_kv_heads, c.head_dim)
+        for x in (k_cache, v_cache):
+            if x.dtype != self.dtype or tuple(x.shape) != shape:
+                raise ValueError(f"caches must be {self.dtype} {list(shape)}")
+        if k_cache.stride() != v_cache.stride() or k_cache.stride(3) != 1:
+            raise ValueError("caches must have equal strides and contiguous heads")
+        s = [st if n > 1 else 0 for st, n in zip(k_cache.stride(), shape)]
+        return smetric_kv_cache(k_cache.data_ptr(), v_cache.data_ptr(), s[0], s[1], s[2])
+
+    def _transform(self, cos_sin, interleaved, q_norm, k_norm, eps) -> smetric_kv_transform:
+        import torch
+        for w in (q_norm, k_norm):
+            if w is not None and (w.dtype != self.dtype or w.numel() != self.cfg.head_dim):
+                raise ValueError(f"norm weights must be {self.dtype} [{self.cfg.head_dim}]")
+        if cos_sin is not None and (cos_sin.dtype != torch.float32 or cos_sin.dim() != 2):
+            raise ValueError("cos_sin must be torch.float32 [positions, rot_dim]")
+        rows, rot = (0, 0) if cos_sin is None else cos_sin.shape
+        return smetric_kv_transform(_ptr(cos_sin), rows, _ptr(q_norm), _ptr(k_norm), eps, rot,
+                                    SMETRIC_KV_INTERLEAVED if interleaved else 0, 0)
+
+    def plan(self, offsets, kv_lens, pages, n_tokens: int, window: int = 0, stream=None):
+        """Plans a batch: offsets int64 [n+1], kv_lens int32 [n], pages int32
+        [n, max_pages] (row stride free). The tensors stay referenced until
+        the next plan."""
+        import torch
+        n = kv_lens.numel()
+        if offsets.dtype != torch.int64 or offsets.numel() != n + 1:
+            raise ValueError("offsets must be torch.int64 [requests + 1]")
+        if kv_lens.dtype != torch.int32 or pages.dtype != torch.int32 or pages.dim() != 2 or pages.shape[0] != n:
+            raise ValueError("kv_lens must be torch.int32 [requests] and pages torch.int32 [requests, max_pages]")
+        if pages.shape[1] > 1 and pages.stride(1) != 1:
+            raise ValueError("a request's pages must be contiguous")
+        most = pages.shape[1]
+        smetric_kv_plan(self.handle, offsets, n, n_tokens, kv_lens, pages.data_ptr() if pages.numel() else None, most,
+                        pages.stride(0) if n > 1 else most, window, stream)
+        self._n_tokens, self._kept = n_tokens, (offsets, kv_lens, pages)
+
+    def _planned(self) -> int:
+        if self._n_tokens is None:
+            raise SmetricError(SMETRIC_ERR_INVALID_ARG, "no batch is planned")
+        return self._n_tokens
+
+    def append(self, k_cache, v_cache, k, v, q=None, q_out=None, cos_sin=None, interleaved=False, q_norm=None,
+               k_norm=None, eps=1e-6, stream=None):
+        """Appends the planned batch's keys (normed with k_norm, rotated with
+        cos_sin where given) and values; with q, transforms the queries into
+        q_out (a new tensor by default) and returns it."""
+        import torch
+        t, c = self._planned(), self.cfg
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        smetric_kv_append(self.handle, self._cache(k_cache, v_cache), self._heads(k, c.num_kv_heads, t, "k"),
+                          self._heads(v, c.num_kv_heads, t, "v"), self._heads(q, c.num_q_heads, t, "q"),
+                          self._heads(q_out if q is not None else None, c.num_q_heads, t, "q_out"),
+                          self._transform(cos_sin, interleaved, q_norm, k_norm, eps), stream)
+        return q_out if q is not None else None
+
+    def qk_norm_rope(self, q, k, positions, cos_sin=None, interleaved=False, q_norm=None, k_norm=None, eps=1e-6,
+                     q_out=None, k_out=None, stream=None):
+        """The norms and the rotation alone, at int32 positions; q or k may be
+        None. Returns (q_out, k_out), new tensors unless given."""
+        import torch
+        t, c = positions.numel(), self.cfg
+        if positions.dtype != torch.int32:
+            raise ValueError("positions must be torch.int32")
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        smetric_qk_norm_rope(self.handle, self._heads(q, c.num_q_heads, t, "q"),
+                             self._heads(k, c.num_kv_heads, t, "k"), positions, t,
+                             self._transform(cos_sin, interleaved, q_norm, k_norm, eps),
+                             self._heads(q_out if q is not None else None, c.num_q_heads, t, "q_out"),
+                             self._heads(k_out if k is not None else None, c.num_kv_heads, t, "k_out"), stream)
+        return q_out, k_out
+
+    def paged_attention(self, q, k_cache, v_cache, scale=None, out=None, want_lse=False, stream=None):
+        """Attention of the planned batch's queries over the cache; scale is
+        head_dim ** -0.5 by default. Returns out, or (out, lse) with want_lse
+        (float32 [tokens, num_q_heads])."""
+        import torch
+        t, c = self._planned(), self.cfg
+        if out is None:
+            out = torch.empty((t, c.num_q_heads, c.head_dim), dtype=self.dtype, device=q.device)
+        lse = torch.empty((t, c.num_q_heads), dtype=torch.float32, device=q.device) if want_lse else None
+        smetric_paged_attention(self.handle, self._cache(k_cache, v_cache), self._heads(q, c.num_q_heads, t, "q"),
+                                c.head_dim ** -0.5 if scale is None else scale,
+                                self._heads(out, c.num_q_heads, t, "out"), lse, stream)
+        return (out, lse) if want_lse else out
+
+    def status(self, stream=None) -> int:
+        return smetric_kv_status(self.handle, stream)
 
     def check(self, stream=None):
         rc = self.status(stream)

@@ -1,6 +1,6 @@
 """Builds libsmetric.so in-tree for sm_103a with nvcc (no cmake, no torch).
 
-The two translation units compile in parallel and are linked with the CUDA
+The translation units compile in parallel and are linked with the CUDA
 runtime statically, so the library loads next to any PyTorch build.
 """
 
@@ -16,7 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libsmetric.so")
-SOURCES = ["index.cu", "route.cu", "imbalance.cu", "lru.cu"]
+SOURCES = ["index.cu", "route.cu", "imbalance.cu", "lru.cu", "kv.cu", "attention.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -1,0 +1,433 @@
+// The paged KV$ operators around the attention: the handle, the plan of a
+// batch, and the norm + rotation + append pass.
+//
+//   k_kv_plan      block 0 checks the batch; the other blocks find each new
+//                  token's request by bisection of the offsets, its position
+//                  and its slot in the cache.
+//   k_kv_heads     one pass over the new tokens' heads: queries and keys are
+//                  normed and rotated in registers, keys and values go to
+//                  their slots (or, for the transform alone, to rows).
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "call_range.cuh"
+#include "kv_impl.cuh"
+#include "launch.cuh"
+#include "smetric_impl.cuh"
+
+using namespace smetric;
+
+namespace {
+
+constexpr unsigned kFull = 0xffffffffu;
+constexpr int kPlanThreads = 1024;
+
+__global__ void __launch_bounds__(kPlanThreads)
+    k_kv_plan(const int64_t* __restrict__ off, int32_t n, int64_t n_tokens, const int32_t* __restrict__ kv_lens,
+              const int32_t* __restrict__ pages, int32_t max_pages, int64_t pages_stride, int32_t page_size,
+              int64_t num_pages, int32_t window, KvPlan* __restrict__ plan, KvToken* __restrict__ tokens,
+              int32_t* status) {
+  pdl_enter();
+  if (blockIdx.x == 0) {
+    int bad = 0;
+    for (int32_t r = threadIdx.x; r < n; r += blockDim.x) {
+      const int64_t a = off[r], b = off[r + 1], kv = kv_lens[r];
+      bad |= a < 0 || b < a || b > n_tokens || kv < b - a || kv > (int64_t)max_pages * page_size;
+    }
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) {
+      if (bad) latch_error(status, SMETRIC_ERR_INVALID_ARG);
+      plan->first = bad || n == 0 ? n_tokens : off[0];
+      plan->last = bad || n == 0 ? n_tokens : off[n];
+      plan->window = window > 0 ? window : INT32_MAX;
+      plan->valid = !bad;
+    }
+    return;
+  }
+  const int64_t t = (int64_t)(blockIdx.x - 1) * blockDim.x + threadIdx.x;
+  if (t >= n_tokens) return;
+  KvToken tok = {-1, -1, -1};
+  // the last request that starts at or before t (bad offsets may mislead the
+  // bisection, not past the array: the request's own bounds decide)
+  int32_t lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int32_t mid = lo + ((hi - lo) >> 1);
+    if (off[mid] <= t)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  if (n > 0) {
+    const int64_t a = off[lo], b = off[lo + 1], kv = kv_lens[lo];
+    if (a >= 0 && a <= t && t < b && kv >= b - a && kv <= (int64_t)max_pages * page_size) {
+      tok.req = lo;
+      tok.pos = (int32_t)(kv - (b - t));
+      const int32_t page = pages[lo * pages_stride + tok.pos / page_size];
+      if (page >= 0 && page < num_pages)
+        tok.slot = (int64_t)page * page_size + tok.pos % page_size;
+      else
+        latch_error(status, SMETRIC_ERR_INVALID_ARG);
+    }
+  }
+  tokens[t] = tok;
+}
+
+template <typename T>
+struct Pair;
+template <>
+struct Pair<__nv_bfloat16> {
+  static __device__ __forceinline__ float2 get(uint32_t x) {
+    return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+  }
+  static __device__ __forceinline__ uint32_t put(float a, float b) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+};
+template <>
+struct Pair<__half> {
+  static __device__ __forceinline__ float2 get(uint32_t x) { return __half22float2(*reinterpret_cast<__half2*>(&x)); }
+  static __device__ __forceinline__ uint32_t put(float a, float b) {
+    const __half2 p = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void unpack(uint4 x, float* f) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 p = Pair<T>::get(w[i]);
+    f[2 * i] = p.x;
+    f[2 * i + 1] = p.y;
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float* f) {
+  return make_uint4(Pair<T>::put(f[0], f[1]), Pair<T>::put(f[2], f[3]), Pair<T>::put(f[4], f[5]),
+                    Pair<T>::put(f[6], f[7]));
+}
+
+struct HeadsArgs {
+  smetric_heads q, k, v, q_out, k_out;  // absent: 0 heads
+  int32_t hq, hk, hv;
+  smetric_kv_cache cache;    // keys and values go here when tokens is not NULL
+  const KvToken* tokens;     // the plan's, or NULL: d_positions and k_out
+  const KvPlan* plan;
+  const int32_t* positions;
+  int64_t n_tokens;
+  int32_t D, page_shift, rot, lanes_shift, splits;
+  int64_t table_rows;
+  const float* table;
+  const void* q_norm;
+  const void* k_norm;
+  float eps;
+  int32_t* status;
+};
+
+// A warp takes a token (or one of `splits` shares of its heads) and a group of
+// 2^lanes_shift lanes a head at a time, 16 elements a lane in two 16-byte
+// pieces: the two halves of 8 rotation pairs (i, i + rot/2), 8 interleaved
+// pairs, or 16 elements past rot. So a rotation never leaves the lane, a norm
+// is a sum over the group's lanes, and the token's cosines and sines are
+// loaded once for all its heads.
+template <typename T, bool kInterleaved>
+__global__ void __launch_bounds__(256) k_kv_heads(const __grid_constant__ HeadsArgs a) {
+  pdl_enter();
+  const int lane = threadIdx.x & 31;
+  const int64_t w = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int64_t t = w / a.splits;
+  const int share = (int)(w - t * a.splits);
+  if (t >= a.n_tokens) return;
+  int64_t slot = 0;
+  int32_t pos;
+  if (a.tokens) {
+    const KvToken tok = a.tokens[t];
+    if (!a.plan->valid || tok.slot < 0) return;
+    slot = tok.slot;
+    pos = tok.pos;
+  } else {
+    pos = a.positions[t];
+  }
+  if (a.table && (pos < 0 || pos >= a.table_rows)) {
+    if (lane == 0 && share == 0) latch_error(a.status, SMETRIC_ERR_OVERFLOW);
+    return;
+  }
+  const int c = lane & ((1 << a.lanes_shift) - 1);
+  const bool held = 16 * c < a.D;  // (groups of 8 lanes hold heads of 96 elements)
+  const bool turned = held && a.table && 16 * c < a.rot;
+  const int e0 = turned && !kInterleaved ? 8 * c : 16 * c;
+  const int e1 = turned && !kInterleaved ? 8 * c + a.rot / 2 : 16 * c + 8;
+  float cs[8], sn[8];
+  if (turned) {
+    const float4* row = reinterpret_cast<const float4*>(a.table + (int64_t)pos * a.rot + 8 * c);
+    const float4* row2 = reinterpret_cast<const float4*>(a.table + (int64_t)pos * a.rot + a.rot / 2 + 8 * c);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 x = row[i], y = row2[i];
+      cs[4 * i] = x.x, cs[4 * i + 1] = x.y, cs[4 * i + 2] = x.z, cs[4 * i + 3] = x.w;
+      sn[4 * i] = y.x, sn[4 * i + 1] = y.y, sn[4 * i + 2] = y.z, sn[4 * i + 3] = y.w;
+    }
+  }
+  const int per = 32 >> a.lanes_shift;  // heads a warp takes at a time
+  const int total = a.hk + a.hv + a.hq;
+  const int64_t page = slot >> a.page_shift, place = slot & ((1 << a.page_shift) - 1);
+  const int64_t at = page * a.cache.page_stride + place * a.cache.token_stride;
+  for (int base = share * per; base < total; base += a.splits * per) {
+    const int h = base + (lane >> a.lanes_shift);
+    const bool on = held && h < total;
+    const bool is_k = h < a.hk, is_v = !is_k && h < a.hk + a.hv;
+    const T* src;
+    T* dst;
+    const T* norm = nullptr;
+    if (is_k) {
+      src = static_cast<const T*>(a.k.d_data) + t * a.k.token_stride + h * a.k.head_stride;
+      dst = a.tokens ? static_cast<T*>(a.cache.d_k) + at + h * a.cache.head_stride
+                     : static_cast<T*>(a.k_out.d_data) + t * a.k_out.token_stride + h * a.k_out.head_stride;
+      norm = static_cast<const T*>(a.k_norm);
+    } else if (is_v) {
+      src = static_cast<const T*>(a.v.d_data) + t * a.v.token_stride + (h - a.hk) * a.v.head_stride;
+      dst = static_cast<T*>(a.cache.d_v) + at + (h - a.hk) * a.cache.head_stride;
+    } else {
+      const int g = h - a.hk - a.hv;
+      src = static_cast<const T*>(a.q.d_data) + t * a.q.token_stride + g * a.q.head_stride;
+      dst = static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride + g * a.q_out.head_stride;
+      norm = static_cast<const T*>(a.q_norm);
+    }
+    uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
+    if (on) {
+      x0 = *reinterpret_cast<const uint4*>(src + e0);
+      x1 = *reinterpret_cast<const uint4*>(src + e1);
+    }
+    float f[16];
+    unpack<T>(x0, f);
+    unpack<T>(x1, f + 8);
+    if (a.q_norm || a.k_norm) {  // (the same for the warp: its lanes take part in the sum)
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ss = fmaf(f[i], f[i], ss);
+      for (int o = 1; o < 1 << a.lanes_shift; o <<= 1) ss += __shfl_xor_sync(kFull, ss, o);
+      if (on && norm) {
+        const float inv = 1.0f / sqrtf(ss / (float)a.D + a.eps);
+        float g[16];
+        unpack<T>(*reinterpret_cast<const uint4*>(norm + e0), g);
+        unpack<T>(*reinterpret_cast<const uint4*>(norm + e1), g + 8);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f[i] = f[i] * inv * g[i];
+      }
+    }
+    if (turned && !is_v) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int p = kInterleaved ? 2 * i : i, q = kInterleaved ? 2 * i + 1 : 8 + i;
+        const float u = f[p], v = f[q];
+        f[p] = u * cs[i] - v * sn[i];
+        f[q] = v * cs[i] + u * sn[i];
+      }
+    }
+    if (on) {
+      // (heads that nothing changes keep their bits, NaN payloads among them)
+      const bool same = is_v || (!norm && !turned);
+      *reinterpret_cast<uint4*>(dst + e0) = same ? x0 : pack<T>(f);
+      *reinterpret_cast<uint4*>(dst + e1) = same ? x1 : pack<T>(f + 8);
+    }
+  }
+}
+
+bool transform_ok(const smetric_kv* kv, const smetric_kv_transform& t) {
+  if (t.reserved || (t.flags & ~SMETRIC_KV_INTERLEAVED) || t.rot_dim < 0 || t.rot_dim > kv->cfg.head_dim ||
+      t.rot_dim % 16 || t.table_rows < 0)
+    return false;
+  if (t.d_cos_sin && (t.rot_dim == 0 || (reinterpret_cast<uintptr_t>(t.d_cos_sin) & 15))) return false;
+  if ((reinterpret_cast<uintptr_t>(t.d_q_norm) | reinterpret_cast<uintptr_t>(t.d_k_norm)) & 15) return false;
+  return (!t.d_q_norm && !t.d_k_norm) || (std::isfinite(t.eps) && t.eps >= 0.f);
+}
+
+int launch_heads(smetric_kv* kv, HeadsArgs& a, const smetric_kv_transform& t, cudaStream_t s) {
+  a.D = kv->cfg.head_dim;
+  a.page_shift = __builtin_ctz((unsigned)kv->cfg.page_size);
+  a.rot = t.rot_dim;
+  a.table = t.rot_dim ? t.d_cos_sin : nullptr;
+  a.table_rows = t.table_rows;
+  a.q_norm = a.hq ? t.d_q_norm : nullptr;
+  a.k_norm = a.hk ? t.d_k_norm : nullptr;
+  a.eps = t.eps;
+  a.status = kv->status;
+  a.lanes_shift = 0;
+  while (16 << a.lanes_shift < a.D) a.lanes_shift++;
+  // Warps that share a token's heads: as many as it has rounds of heads while
+  // there are too few tokens to fill the SMs (64 warps an SM), else one.
+  const int rounds = (a.hq + a.hk + a.hv + (32 >> a.lanes_shift) - 1) / (32 >> a.lanes_shift);
+  const int64_t room = (int64_t)kv->num_sms * 64 / std::max<int64_t>(1, a.n_tokens);
+  a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, room));
+  const int64_t grid = (a.n_tokens * a.splits + 7) / 8;
+  const bool il = t.flags & SMETRIC_KV_INTERLEAVED;
+  const bool bf = kv->cfg.dtype == SMETRIC_BF16;
+  auto kern = bf ? (il ? k_kv_heads<__nv_bfloat16, true> : k_kv_heads<__nv_bfloat16, false>)
+                 : (il ? k_kv_heads<__half, true> : k_kv_heads<__half, false>);
+  kv->launches++;
+  return launch_k(kern, dim3((unsigned)grid), dim3(256), 0, s, true, a);
+}
+
+void free_kv(smetric_kv* kv) {
+  cudaFree(kv->status);
+  cudaFree(kv->plan);
+  cudaFree(kv->tokens);
+}
+
+}  // namespace
+
+int smetric::check_device(const smetric_kv* kv) {
+  if (!kv) return SMETRIC_ERR_INVALID_ARG;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return cuda_status(cudaErrorUnknown);
+  return dev == kv->device ? SMETRIC_OK : SMETRIC_ERR_INVALID_ARG;
+}
+
+extern "C" {
+
+int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out) {
+  CallRange range("smetric_kv_create");
+  if (!cfg || !out) return SMETRIC_ERR_INVALID_ARG;
+  *out = nullptr;
+  const smetric_kv_config& c = *cfg;
+  if (c.head_dim < 16 || c.head_dim > SMETRIC_KV_MAX_HEAD_DIM || c.head_dim % 16 || c.num_kv_heads < 1 ||
+      c.num_kv_heads > 4096 || c.num_q_heads < c.num_kv_heads || c.num_q_heads % c.num_kv_heads ||
+      c.num_q_heads / c.num_kv_heads > SMETRIC_KV_MAX_GROUP || c.page_size < 16 || c.page_size > 256 ||
+      (c.page_size & (c.page_size - 1)) || (c.dtype != SMETRIC_BF16 && c.dtype != SMETRIC_F16) || c.flags ||
+      c.num_pages < 1 || c.num_pages > INT32_MAX || c.max_batch_requests < 0 ||
+      c.max_batch_requests > SMETRIC_KV_MAX_REQUESTS || c.max_batch_tokens < 0 ||
+      c.max_batch_tokens > SMETRIC_KV_MAX_TOKENS)
+    return SMETRIC_ERR_INVALID_ARG;
+  smetric_kv* kv = new (std::nothrow) smetric_kv{};
+  if (!kv) return SMETRIC_ERR_OOM;
+  kv->cfg = c;
+  kv->group = c.num_q_heads / c.num_kv_heads;
+  const bool ok =
+      cudaGetDevice(&kv->device) == cudaSuccess &&
+      cudaDeviceGetAttribute(&kv->num_sms, cudaDevAttrMultiProcessorCount, kv->device) == cudaSuccess &&
+      cudaMalloc(&kv->status, sizeof(int32_t)) == cudaSuccess && cudaMalloc(&kv->plan, sizeof(KvPlan)) == cudaSuccess &&
+      cudaMalloc(&kv->tokens, sizeof(KvToken) * (size_t)std::max<int64_t>(1, c.max_batch_tokens)) == cudaSuccess &&
+      cudaMemset(kv->status, 0, sizeof(int32_t)) == cudaSuccess && cudaDeviceSynchronize() == cudaSuccess;
+  if (!ok) {
+    (void)cudaGetLastError();
+    free_kv(kv);
+    delete kv;
+    return SMETRIC_ERR_OOM;
+  }
+  *out = kv;
+  return SMETRIC_OK;
+}
+
+int smetric_kv_destroy(smetric_kv* kv) {
+  CallRange range("smetric_kv_destroy");
+  if (!kv) return SMETRIC_OK;
+  int dev = -1;
+  cudaGetDevice(&dev);
+  if (dev != kv->device) cudaSetDevice(kv->device);
+  cudaDeviceSynchronize();
+  free_kv(kv);
+  int rc = cuda_status(cudaGetLastError());
+  if (dev >= 0 && dev != kv->device) cudaSetDevice(dev);
+  delete kv;
+  return rc;
+}
+
+int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests, int64_t n_tokens,
+                    const int32_t* d_kv_lens, const int32_t* d_pages, int32_t max_pages, int64_t pages_stride,
+                    int32_t window, smetric_stream_t stream) {
+  CallRange range("smetric_kv_plan");
+  int rc = check_device(kv);
+  if (rc) return rc;
+  if (n_requests < 0 || n_requests > kv->cfg.max_batch_requests || n_tokens < 0 ||
+      n_tokens > kv->cfg.max_batch_tokens || max_pages < 0 || pages_stride < max_pages || window < 0 ||
+      (n_requests > 0 && (!d_offsets || !d_kv_lens || (max_pages > 0 && !d_pages))))
+    return SMETRIC_ERR_INVALID_ARG;
+  kv->planned = false;
+  const unsigned grid = 1 + (unsigned)((n_tokens + kPlanThreads - 1) / kPlanThreads);
+  kv->launches++;
+  rc = launch_k(k_kv_plan, dim3(grid), dim3(kPlanThreads), 0, reinterpret_cast<cudaStream_t>(stream), true, d_offsets,
+                n_requests, n_tokens, d_kv_lens, d_pages, max_pages, pages_stride, kv->cfg.page_size,
+                kv->cfg.num_pages, window, kv->plan, kv->tokens, kv->status);
+  if (rc) return rc;
+  kv->planned = true;
+  kv->n_requests = n_requests;
+  kv->n_tokens = n_tokens;
+  kv->offsets = d_offsets;
+  kv->kv_lens = d_kv_lens;
+  kv->pages = d_pages;
+  kv->max_pages = max_pages;
+  kv->pages_stride = pages_stride;
+  return SMETRIC_OK;
+}
+
+int smetric_kv_append(smetric_kv* kv, smetric_kv_cache cache, smetric_heads k, smetric_heads v, smetric_heads q,
+                      smetric_heads q_out, smetric_kv_transform t, smetric_stream_t stream) {
+  CallRange range("smetric_kv_append");
+  int rc = check_device(kv);
+  if (rc) return rc;
+  if (!kv->planned || !transform_ok(kv, t) || !heads_ok(k, kv->n_tokens) || !heads_ok(v, kv->n_tokens) ||
+      (q.d_data && (!heads_ok(q, kv->n_tokens) || !heads_ok(q_out, kv->n_tokens))) || !cache_ok(cache))
+    return SMETRIC_ERR_INVALID_ARG;
+  if (kv->n_tokens == 0) return SMETRIC_OK;
+  HeadsArgs a = {};
+  a.k = k;
+  a.v = v;
+  a.q = q;
+  a.q_out = q_out;
+  a.hk = a.hv = kv->cfg.num_kv_heads;
+  a.hq = q.d_data ? kv->cfg.num_q_heads : 0;
+  a.cache = cache;
+  a.tokens = kv->tokens;
+  a.plan = kv->plan;
+  a.n_tokens = kv->n_tokens;
+  return launch_heads(kv, a, t, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int smetric_qk_norm_rope(smetric_kv* kv, smetric_heads q, smetric_heads k, const int32_t* d_positions,
+                         int64_t n_tokens, smetric_kv_transform t, smetric_heads q_out, smetric_heads k_out,
+                         smetric_stream_t stream) {
+  CallRange range("smetric_qk_norm_rope");
+  int rc = check_device(kv);
+  if (rc) return rc;
+  if (n_tokens < 0 || n_tokens > SMETRIC_KV_MAX_TOKENS || !transform_ok(kv, t) ||
+      (q.d_data && (!heads_ok(q, n_tokens) || !heads_ok(q_out, n_tokens))) ||
+      (k.d_data && (!heads_ok(k, n_tokens) || !heads_ok(k_out, n_tokens))) || (n_tokens > 0 && !d_positions))
+    return SMETRIC_ERR_INVALID_ARG;
+  if (n_tokens == 0 || (!q.d_data && !k.d_data)) return SMETRIC_OK;
+  HeadsArgs a = {};
+  a.k = k;
+  a.q = q;
+  a.k_out = k_out;
+  a.q_out = q_out;
+  a.hk = k.d_data ? kv->cfg.num_kv_heads : 0;
+  a.hq = q.d_data ? kv->cfg.num_q_heads : 0;
+  a.positions = d_positions;
+  a.n_tokens = n_tokens;
+  return launch_heads(kv, a, t, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int smetric_kv_status(smetric_kv* kv, smetric_stream_t stream) {
+  CallRange range("smetric_kv_status");
+  int rc = check_device(kv);
+  if (rc) return rc;
+  if (cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
+    return cuda_status(cudaErrorUnknown);
+  int32_t h = 0;
+  if (cudaMemcpy(&h, kv->status, sizeof(h), cudaMemcpyDeviceToHost) != cudaSuccess)
+    return cuda_status(cudaErrorUnknown);
+  if (h != 0 && cudaMemset(kv->status, 0, sizeof(int32_t)) != cudaSuccess) return cuda_status(cudaErrorUnknown);
+  return h;
+}
+
+int64_t smetric_kv_launch_count(const smetric_kv* kv) { return kv ? kv->launches : 0; }
+
+}  // extern "C"
