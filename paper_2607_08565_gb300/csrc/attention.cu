@@ -1,90 +1,782 @@
 // Attention of a planned batch's queries over the paged cache.
 //
-//   k_paged_attention  a warp for each (token, query head): the keys one after
-//                      another, the running maximum and sum of the softmax and
-//                      the output in registers, lane l holding elements
-//                      l, l + 32, ... of the head.
+//   k_paged_attention  one CTA an SM, each with the share of the batch that the
+//                      plan gave it; the sequences that several CTAs share are
+//                      joined by the one that finishes last.
+//
+// For a tile of 128 query rows (a row is a token and one of the query heads of
+// a key head) and a tile of 128 keys: S = Q K^T and O += P V on the tensor
+// cores (tcgen05, sums in TMEM), P = exp2(c S - ref) in between, c = scale *
+// log2(e). ref is the row's reference exponent: its largest c S when it was
+// last moved. It moves only when a score exceeds it by 2^kSlack, since a common
+// factor of P and its sum l cancels in O / l: so O is seldom rescaled.
+//
+// Two query tiles are in flight, so that one's softmax runs while the tensor
+// cores work on the other: a unit of more than 128 rows has its two halves
+// (both read the same keys), a smaller one has the even and the odd key tiles
+// of its rows, whose sums are joined at the end.
+//
+// Warps: 0 copies tiles with TMA (keys and values alternate in one ring of
+// buffers), 1 issues the matrix products, 4-7 and 8-11 are the two tiles'
+// softmax (a thread a row).
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "call_range.cuh"
 #include "kv_impl.cuh"
 #include "launch.cuh"
 #include "smetric_impl.cuh"
+#include "tensor_map.cuh"
 
 using namespace smetric;
 
 namespace {
 
+constexpr unsigned kFull = 0xffffffffu;
+constexpr uint32_t kSpinLimit = 1u << 24;  // bounded mbarrier waits
+constexpr int kThreads = 384;
+constexpr float kSlack = 8.f;     // log2 of how far scores may pass the reference
+constexpr uint32_t kHalf = 16384;  // bytes of 128 rows of 64 elements
+
+// Buffers of the ring: what 227 KB hold beside the two query tiles.
+__host__ __device__ constexpr int stages(int halves) { return halves == 2 ? 5 : 11; }
+
 struct AttentionArgs {
-  smetric_kv_cache cache;
-  smetric_heads q, out;
+  CUtensorMap q, k, v;
+  smetric_heads out;
   float* lse;
   const KvPlan* plan;
-  const KvToken* tokens;
+  const KvUnit* units;
+  const KvShare* shares;
+  int32_t* pieces;
+  float* part;
+  float2* part_ml;
   const int32_t* pages;
-  int64_t pages_stride, num_pages, n_tokens;
-  int32_t hq, group, D, page_size;
+  int64_t pages_stride, n_tokens;
+  int32_t num_pages, hq, kv_heads, group, tile_tokens, D, page_size, window;
   float scale;
   int32_t* status;
 };
 
-__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
-__device__ __forceinline__ void from_f(float x, __nv_bfloat16& y) { y = __float2bfloat16_rn(x); }
-__device__ __forceinline__ void from_f(float x, __half& y) { y = __float2half_rn(x); }
+// ---- shared memory, TMA, tensor cores ----
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_paged_attention(const __grid_constant__ AttentionArgs a) {
-  pdl_enter();
-  constexpr int E = SMETRIC_KV_MAX_HEAD_DIM / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t w = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const int64_t t = w / a.hq;
-  const int h = (int)(w - t * a.hq);
-  if (t >= a.n_tokens) return;
-  const KvToken tok = a.tokens[t];
-  float o[E] = {}, q[E], m = -INFINITY, l = 0.f;
-  if (a.plan->valid && tok.req >= 0) {
-    const T* qp = static_cast<const T*>(a.q.d_data) + t * a.q.token_stride + h * a.q.head_stride;
-#pragma unroll
-    for (int i = 0; i < E; ++i) q[i] = lane + 32 * i < a.D ? to_f(qp[lane + 32 * i]) * a.scale : 0.f;
-    const int64_t head = (int64_t)(h / a.group) * a.cache.head_stride;
-    const int32_t from = tok.pos >= a.plan->window ? tok.pos - a.plan->window + 1 : 0;
-    for (int32_t j = from; j <= tok.pos; ++j) {
-      const int32_t page = a.pages[tok.req * a.pages_stride + j / a.page_size];
-      const bool held = page >= 0 && page < a.num_pages;
-      if (!held && lane == 0) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
-      const int64_t at = (int64_t)page * a.cache.page_stride + (j % a.page_size) * a.cache.token_stride + head;
-      const T* kp = static_cast<const T*>(a.cache.d_k) + at;
-      const T* vp = static_cast<const T*>(a.cache.d_v) + at;
-      float x = 0.f;
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (held && lane + 32 * i < a.D) x = fmaf(q[i], to_f(kp[lane + 32 * i]), x);
-      for (int s = 16; s; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
-      const float top = fmaxf(m, x);
-      const float back = expf(m - top), p = expf(x - top);
-      l = l * back + p;
-      m = top;
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        o[i] = o[i] * back + (held && lane + 32 * i < a.D ? p * to_f(vp[lane + 32 * i]) : 0.f);
-    }
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+struct __align__(8) Barriers {
+  uint64_t full[16], empty[16];  // the ring's
+  uint64_t q_full, q_empty;
+  uint64_t s_full[2];  // scores in TMEM (and the products before them done)
+  uint64_t p_full[2];  // weights in TMEM, O rescaled
+  uint64_t o_full[2];  // the unit's last product with the values done
+  uint64_t odd_full, odd_empty;  // the odd key tiles' statistics
+  uint64_t drain;
+};
+
+struct Shared {
+  Barriers bar;
+  float2 odd[kTile];  // (reference, sum) of the odd key tiles
+  uint32_t tmem;
+  int32_t abort;      // a wait ran out: everybody stops waiting
+  int32_t joins[2];
+};
+
+__device__ __forceinline__ void mbar_init(uint64_t* b, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(smem_u32(b)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint64_t* b, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(done) : "r"(smem_u32(b)), "r"(parity) : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ bool stopped(const Shared* sh) { return *(const volatile int32_t*)&sh->abort != 0; }
+// Waits for the phase of the given parity; gives up after kSpinLimit tries, or
+// when another wait of the CTA has. Callers go on either way (every loop is
+// bounded by the plan); outputs are then undefined and the error is latched.
+__device__ __forceinline__ void mbar_wait(uint64_t* b, uint32_t parity, Shared* sh, int32_t* status) {
+  for (uint32_t i = 0; i < kSpinLimit; ++i) {
+    if (mbar_try(b, parity)) return;
+    if (stopped(sh)) return;
   }
-  T* op = static_cast<T*>(a.out.d_data) + t * a.out.token_stride + h * a.out.head_stride;
-#pragma unroll
-  for (int i = 0; i < E; ++i)
-    if (lane + 32 * i < a.D) from_f(l == 0.f ? 0.f : o[i] / l, op[lane + 32 * i]);
-  if (a.lse && lane == 0) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : m + logf(l);
+  *(volatile int32_t*)&sh->abort = 1;
+  latch_error(status, SMETRIC_ERR_CUDA);
 }
 
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* m, int32_t x, int32_t y, int32_t z, uint64_t* b) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::
+          "r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* m, int32_t x, int32_t y, int32_t z, int32_t w,
+                                       uint64_t* b) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}],"
+      " [%6];\n" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(b))
+      : "memory");
+}
+
+// Shared-memory descriptors of operands in rows of 128 bytes with the 128-byte
+// swizzle: groups of 8 rows 1,024 bytes apart. lbo: bytes between the 64-element
+// halves, where the rows run along the product's inner dimension (the values).
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo) {
+  return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 |
+         2ull << 61;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+// Arrives at b when the products issued so far are done.
+__device__ __forceinline__ void mma_commit(uint64_t* b) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(smem_u32(b))
+               : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
+// Waits for the warp's loads from TMEM; their registers are read after it.
+template <int N>
+__device__ __forceinline__ void wait_ld(uint32_t (&r)[N]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
+
+// 32 columns of the warp's 32 lanes (a row a thread).
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+      "[%16];\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16};\n" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <typename T>
+struct Type;
+template <>
+struct Type<__nv_bfloat16> {
+  static constexpr uint32_t kFormat = 1;  // of the tensor cores' operands
+  static constexpr float kLift = 0.f;
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+};
+template <>
+struct Type<__half> {
+  static constexpr uint32_t kFormat = 0;
+  // Weights up to 2^(kLift + kSlack) = 2^15: half precision's range ends at
+  // 65,504, and the small weights of long rows stay normal numbers longer.
+  static constexpr float kLift = 7.f;
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __half2 p = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+};
+
+// ---- a CTA's share ----
+
+struct Item {
+  KvUnit unit;
+  int32_t h, tb, te;  // key head, its key tiles in this CTA
+  bool whole;         // nobody else has key tiles of it
+  bool pair;          // two query tiles (else the even and the odd key tiles)
+  int32_t slot, c1, pieces;  // where !whole
+};
+
+struct Walk {
+  KvShare s;
+  int32_t u, h;
+  bool first, done;
+  __device__ __forceinline__ void start(const AttentionArgs& a) {
+    const int4* p = reinterpret_cast<const int4*>(a.shares + blockIdx.x);
+    const int4 x = p[0], y = p[1], z = p[2];
+    s.u0 = x.x, s.h0 = x.y, s.t0 = x.z, s.u1 = x.w, s.h1 = y.x, s.t1 = y.y, s.c1 = y.z, s.n_first = y.w, s.n_last = z.x;
+    u = s.u0, h = s.h0;
+    first = true;
+    done = u < 0;
+  }
+  __device__ __forceinline__ bool next(const AttentionArgs& a, Item& it) {
+    if (done) return false;
+    const int4* p = reinterpret_cast<const int4*>(a.units + u);
+    const int4 x = p[0], y = p[1];
+    it.unit.token = x.x, it.unit.tokens = x.y, it.unit.pos = x.z, it.unit.req = x.w, it.unit.tb = y.x, it.unit.te = y.y;
+    const bool last = u == s.u1 && h == s.h1;
+    it.h = h;
+    it.tb = first ? s.t0 : it.unit.tb;
+    it.te = last ? s.t1 : it.unit.te;
+    it.pair = it.unit.tokens > a.tile_tokens;
+    it.whole = it.tb == it.unit.tb && it.te == it.unit.te;
+    const bool inside = it.tb != it.unit.tb;
+    it.slot = 2 * (int32_t)blockIdx.x + !inside;
+    it.c1 = inside ? s.c1 : (int32_t)blockIdx.x;
+    it.pieces = inside ? s.n_first : s.n_last;
+    first = false;
+    done = last;
+    if (++h == a.kv_heads) h = 0, ++u;
+    return true;
+  }
+};
+
+// Places of an item's tiles in the ring, of n key tiles: K0 K1 V0 K2 V1 K3 ...
+__device__ __forceinline__ uint32_t place_k(int j) { return j < 2 ? j : 2 * j - 1; }
+__device__ __forceinline__ uint32_t place_v(int j, int n) { return min(2 + 2 * j, 2 * n - 1); }
+
+// ---- the warps ----
+
+template <int HALVES>
+__device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, uint32_t q_smem, uint32_t ring) {
+  constexpr int S = stages(HALVES);
+  Barriers& b = sh->bar;
+  const int lane = threadIdx.x & 31;
+  const int per = max(1, kTile / a.page_size);       // pages of a tile
+  const int rows = min(kTile, a.page_size);          // rows of a copy
+  const uint32_t q_bytes = (uint32_t)a.tile_tokens * a.group * 128 * HALVES;
+  uint32_t at = 0, items = 0;
+  Walk w;
+  Item it;
+  for (w.start(a); w.next(a, it); ++items) {
+    const int n = it.te - it.tb;
+    // the keys that some query of the unit sees
+    const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
+    const int32_t* pages = a.pages + it.unit.req * a.pages_stride;
+    // lane i < per: page i of a tile, -1 where nobody sees a key of it
+    const auto page_of = [&](int tile) {
+      const int64_t key = (int64_t)tile * kTile + lane * rows;
+      int32_t page = -1;
+      if (lane < per && tile < it.te && key < hi && key + rows > lo) {
+        page = pages[key / a.page_size];
+        if (page < 0 || page >= a.num_pages) {
+          latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
+          page = a.num_pages;  // outside the tensor map: zeros
+        }
+      }
+      return page;
+    };
+    if (items) mbar_wait(&b.q_empty, (items - 1) & 1, sh, a.status);
+    if (stopped(sh)) break;
+    if (lane == 0) {
+      mbar_expect(&b.q_full, q_bytes * (it.pair ? 2 : 1));
+      for (int t = 0; t < (it.pair ? 2 : 1); ++t)
+#pragma unroll
+        for (int e = 0; e < HALVES; ++e)
+          tma_3d(q_smem + (t * HALVES + e) * kHalf, &a.q, 64 * e, it.h * a.group, it.unit.token + t * a.tile_tokens,
+                 &b.q_full);
+    }
+    const auto copy = [&](const CUtensorMap* map, int tile, int32_t page) {
+      const uint32_t s = at % S, round = at / S;
+      if (round) mbar_wait(&b.empty[s], (round - 1) & 1, sh, a.status);
+      if (stopped(sh)) return;
+      const unsigned who = __ballot_sync(kFull, page >= 0);
+      if (lane == 0) mbar_expect(&b.full[s], __popc(who) * rows * 128 * HALVES);
+      __syncwarp();
+      if (page >= 0) {
+        const uint32_t dst = ring + s * HALVES * kHalf + lane * rows * 128;
+        const int32_t in = a.page_size > kTile ? tile * kTile % a.page_size : 0;
+#pragma unroll
+        for (int e = 0; e < HALVES; ++e) tma_4d(dst + e * kHalf, map, 64 * e, in, it.h, page, &b.full[s]);
+      }
+      ++at;
+    };
+    int32_t p0 = page_of(it.tb), p1 = page_of(it.tb + 1), p2;
+    copy(&a.k, it.tb, p0);
+    if (n > 1) copy(&a.k, it.tb + 1, p1);
+    for (int j = 0; j < n; ++j) {
+      p2 = page_of(it.tb + j + 2);
+      copy(&a.v, it.tb + j, p0);
+      if (j + 2 < n) copy(&a.k, it.tb + j + 2, p2);
+      p0 = p1, p1 = p2;
+    }
+  }
+  if (stopped(sh)) {  // copies in flight must land before the CTA ends
+    for (uint32_t i = at > S ? at - S : 0; i < at; ++i)
+      for (uint32_t k = 0; k < kSpinLimit && !mbar_try(&b.full[i % S], i / S & 1); ++k) {
+      }
+  }
+}
+
+template <typename T, int HALVES>
+__device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uint32_t q_smem, uint32_t ring) {
+  constexpr int S = stages(HALVES);
+  Barriers& b = sh->bar;
+  const int lane = threadIdx.x & 31;
+  const uint32_t tmem = sh->tmem;
+  constexpr uint32_t kType = 1u << 4 | Type<T>::kFormat << 7 | Type<T>::kFormat << 10 | (kTile >> 4) << 24;
+  constexpr uint32_t kScores = kType | (kTile >> 3) << 17;
+  const uint32_t values = kType | 1u << 16 | (uint32_t)(a.D >> 3) << 17;
+  uint32_t base = 0, items = 0, np[2] = {0, 0};
+  Walk w;
+  Item it;
+  for (w.start(a); w.next(a, it); ++items) {
+    const int n = it.te - it.tb;
+    const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
+    const auto stage = [&](uint32_t place) { return (base + place) % S; };
+    const auto wait_full = [&](uint32_t place) {
+      mbar_wait(&b.full[stage(place)], (base + place) / S & 1, sh, a.status);
+    };
+    const auto scores = [&](int t, int q, uint32_t place) {  // S_t = Q_q K^T
+      if (lane == 0) {
+        const uint32_t qa = q_smem + q * HALVES * kHalf, ka = ring + stage(place) * HALVES * kHalf;
+        for (int k = 0; k < a.D / 16; ++k) {
+          const uint32_t o = (k >> 2) * kHalf + (k & 3) * 32;
+          mma_ss(tmem + t * kTile, smem_desc(qa + o, 16), smem_desc(ka + o, 16), kScores, k > 0);
+        }
+        mma_commit(&b.s_full[t]);
+      }
+    };
+    const auto products = [&](int t, uint32_t place, bool add) {  // O_t += P_t V
+      mbar_wait(&b.p_full[t], np[t]++ & 1, sh, a.status);
+      fence_after();
+      if (lane == 0) {
+        const uint32_t va = ring + stage(place) * HALVES * kHalf;
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          mma_ts(tmem + 2 * kTile + t * kTile, tmem + t * kTile + 8 * k, smem_desc(va + k * 2048, kHalf), values,
+                 add || k > 0);
+      }
+    };
+    const auto release = [&](uint32_t place) {
+      if (lane == 0) mma_commit(&b.empty[stage(place)]);
+    };
+    // Rows of a tile's values that no key lies at become zeros: a weight of
+    // zero does not cancel what may lie there.
+    const auto clear = [&](uint32_t place, int j) {
+      const int32_t key = (it.tb + j) * kTile;
+      if (key >= lo && key + kTile <= hi) return;
+      for (int i = lane; i < kTile * 8 * HALVES; i += 32) {
+        const int row = i / 8 % kTile;
+        if (key + row < lo || key + row >= hi)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(
+                           ring + stage(place) * HALVES * kHalf + i / (8 * kTile) * kHalf + row * 128 + i % 8 * 16),
+                       "r"(0) : "memory");
+      }
+      asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+      __syncwarp();
+    };
+    mbar_wait(&b.q_full, items & 1, sh, a.status);
+    wait_full(0);
+    if (stopped(sh)) break;
+    fence_after();
+    if (it.pair) {
+      scores(0, 0, 0);
+      scores(1, 1, 0);
+      release(0);
+      if (n == 1 && lane == 0) mma_commit(&b.q_empty);
+      for (int j = 0; j < n; ++j) {
+        const uint32_t v = place_v(j, n), k = place_k(j + 1);
+        wait_full(v);
+        clear(v, j);
+        products(0, v, j > 0);
+        if (j + 1 < n) {
+          wait_full(k);
+          scores(0, 0, k);
+        } else if (lane == 0) {
+          mma_commit(&b.o_full[0]);
+        }
+        products(1, v, j > 0);
+        release(v);
+        if (j + 1 < n) {
+          scores(1, 1, k);
+          release(k);
+          if (j + 2 == n && lane == 0) mma_commit(&b.q_empty);
+        } else if (lane == 0) {
+          mma_commit(&b.o_full[1]);
+        }
+        if (stopped(sh)) break;
+      }
+    } else {
+      for (int j = 0; j < min(n, 2); ++j) {
+        if (j) wait_full(j);
+        scores(j, 0, j);
+        release(j);
+      }
+      if (n <= 2 && lane == 0) mma_commit(&b.q_empty);
+      for (int j = 0; j < n; ++j) {
+        const int t = j & 1;
+        const uint32_t v = place_v(j, n), k = place_k(j + 2);
+        wait_full(v);
+        clear(v, j);
+        products(t, v, j > 1);
+        release(v);
+        if (j + 2 < n) {
+          wait_full(k);
+          scores(t, 0, k);
+          release(k);
+          if (j + 3 == n && lane == 0) mma_commit(&b.q_empty);
+        } else if (lane == 0) {
+          mma_commit(&b.o_full[t]);
+        }
+        if (stopped(sh)) break;
+      }
+    }
+    base += 2 * n;
+    __syncwarp();
+  }
+  if (stopped(sh)) {  // products in flight must end before the CTA's memory goes
+    if (lane == 0) {
+      mma_commit(&b.drain);
+      for (uint32_t k = 0; k < kSpinLimit && !mbar_try(&b.drain, 0); ++k) {
+      }
+    }
+    __syncwarp();
+  }
+}
+
+template <int BAR>
+__device__ __forceinline__ void sync_tile() {
+  asm volatile("bar.sync %0, 128;\n" ::"n"(BAR) : "memory");
+}
+
+// Joins the pieces of a unit's query tile t, in their order whoever does it:
+// out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i.
+template <typename T>
+__device__ __forceinline__ void join(const AttentionArgs& a, const Item& it, int t, int n_rows, int64_t token) {
+  const int quads = a.D / 4;
+  const auto row_at = [&](int i, int row) {
+    const int64_t slot = i ? 2 * (it.c1 + i) : 2 * it.c1 + 1;
+    return slot * 2 * kTile + t * kTile + row;
+  };
+  for (int x = threadIdx.x & 127; x < n_rows * quads; x += 128) {
+    const int row = x / quads, c = x - row * quads;
+    float top = -INFINITY;
+#pragma unroll 8
+    for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, __ldcg(a.part_ml + row_at(i, row)).x);
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (top > -INFINITY) {
+#pragma unroll 8
+      for (int i = 0; i < it.pieces; ++i) {
+        const int64_t at = row_at(i, row);
+        const float2 ml = __ldcg(a.part_ml + at);
+        const float4 p = __ldcg(reinterpret_cast<const float4*>(a.part + at * a.D) + c);
+        const float f = ex2(ml.x - top);
+        l += f * ml.y;
+        o.x += f * p.x, o.y += f * p.y, o.z += f * p.z, o.w += f * p.w;
+      }
+    }
+    const float inv = l > 0.f ? 1.f / l : l;  // (NaN stays)
+    const int64_t tok = token + row / a.group;
+    const int head = it.h * a.group + row % a.group;
+    uint2 y = make_uint2(Type<T>::pack(o.x * inv, o.y * inv), Type<T>::pack(o.z * inv, o.w * inv));
+    *reinterpret_cast<uint2*>(static_cast<T*>(a.out.d_data) + tok * a.out.token_stride + head * a.out.head_stride + 4 * c) = y;
+    if (a.lse && c == 0) a.lse[tok * a.hq + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+  }
+}
+
+template <typename T, int TILE>
+__device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh) {
+  Barriers& b = sh->bar;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
+  const uint32_t lanes = (uint32_t)warp << 21;  // the warp's TMEM lanes
+  const uint32_t s_at = sh->tmem + TILE * kTile + lanes, o_at = sh->tmem + 2 * kTile + TILE * kTile + lanes;
+  const int row_token = row / a.group, row_head = row - row_token * a.group;
+  const float c = a.scale * 1.4426950408889634f;
+  uint32_t ns = 0, no = 0, n_other = 0, n_odd = 0;
+  Walk w;
+  Item it;
+  for (w.start(a); w.next(a, it);) {
+    const int n = it.te - it.tb;
+    const int token = it.pair ? TILE * a.tile_tokens : 0;           // the tile's first token in the unit
+    const int tokens = min(a.tile_tokens, it.unit.tokens - token);  // its tokens
+    const int n_rows = tokens * a.group;
+    const bool mine = row < n_rows;
+    const int32_t hi = mine ? it.unit.pos + token + row_token : INT32_MAX;  // last key that the row sees
+    const int32_t lo = mine && hi >= a.window ? hi - a.window + 1 : 0;      // first key
+    const bool busy = 32 * warp < n_rows;
+    const int step = it.pair ? 1 : 2;
+    float top = -INFINITY;  // largest score when the reference was last moved
+    float ref = 0.f;        // the reference exponent: c * top - kLift (0 before the first visible key)
+    float l = 0.f;
+    int count = 0;
+    for (int j = it.pair ? 0 : TILE; j < n; j += step, ++count) {
+      mbar_wait(&b.s_full[TILE], ns++ & 1, sh, a.status);
+      if (busy) {
+        fence_after();
+        uint32_t r[kTile];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, r + 32 * i);
+        wait_ld(r);
+        float s[kTile];
+#pragma unroll
+        for (int i = 0; i < kTile; ++i) s[i] = __uint_as_float(r[i]);
+        const int32_t key = (it.tb + j) * kTile;
+        if (__any_sync(kFull, key + kTile - 1 > hi || key < lo)) {
+#pragma unroll
+          for (int i = 0; i < kTile; ++i)
+            if (key + i > hi || key + i < lo) s[i] = -INFINITY;
+        }
+        float most = s[0];
+#pragma unroll
+        for (int i = 1; i < kTile; ++i) most = fmaxf(most, s[i]);
+        const bool move = (most - top) * c > kSlack;  // (false for -inf - -inf)
+        if (__any_sync(kFull, move)) {
+          float back = 1.f;
+          if (move) {
+            const float next = most * c - Type<T>::kLift;
+            back = top == -INFINITY ? 0.f : ex2(ref - next);
+            top = most;
+            ref = next;
+            l *= back;
+          }
+          if (count > 0) {
+            for (int d = 0; d < a.D; d += 16) {
+              uint32_t o[16];
+              tmem_ld16(o_at + d, o);
+              wait_ld(o);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * back);
+              tmem_st16(o_at + d, o);
+            }
+          }
+        }
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kTile; i += 32) {
+          uint32_t p[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float x = ex2(fmaf(s[i + 2 * k], c, -ref)), y = ex2(fmaf(s[i + 2 * k + 1], c, -ref));
+            sum[2 * k & 3] += x;
+            sum[2 * k + 1 & 3] += y;
+            p[k] = Type<T>::pack(x, y);
+          }
+          tmem_st16(s_at + i / 2, p);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        wait_st();
+        fence_before();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b.p_full[TILE]);
+    }
+    // ---- the unit's output ----
+    float ref2 = -INFINITY, w1 = 1.f, w2 = 0.f;  // the odd tiles' share
+    if (!it.pair) {
+      if (TILE == 1) {
+        sh->odd[row] = make_float2(top == -INFINITY ? -INFINITY : ref, l);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b.odd_full);
+        mbar_wait(&b.odd_empty, n_odd++ & 1, sh, a.status);  // until its sums are read
+        no += n > 1;
+        continue;
+      }
+      if (n > 1) mbar_wait(&b.o_full[1], n_other++ & 1, sh, a.status);
+      mbar_wait(&b.odd_full, n_odd++ & 1, sh, a.status);
+      const float2 odd = sh->odd[row];
+      ref2 = odd.x;
+      const float ref1 = top == -INFINITY ? -INFINITY : ref, both = fmaxf(ref1, ref2);
+      if (both > -INFINITY) {
+        w1 = ex2(ref1 - both);
+        w2 = ex2(ref2 - both);
+        l = l * w1 + odd.y * w2;
+        ref = both;
+        top = 0.f;  // (some key was seen)
+      }
+    } else if (TILE == 0) {
+      ++n_other;
+    }
+    mbar_wait(&b.o_full[TILE], no++ & 1, sh, a.status);
+    const bool two = !it.pair && n > 1;
+    const int64_t tok = it.unit.token + token;
+    if (busy) {
+      fence_after();
+      const float inv = it.whole ? (l > 0.f ? 1.f / l : l) : 1.f;
+      const int64_t at = (int64_t)it.slot * 2 * kTile + TILE * kTile + row;
+      T* out = static_cast<T*>(a.out.d_data) + (tok + row_token) * a.out.token_stride +
+               (it.h * a.group + row_head) * a.out.head_stride;
+      for (int d = 0; d < a.D; d += 16) {
+        uint32_t o[16], o2[16];
+        tmem_ld16(o_at + d, o);
+        if (two) tmem_ld16(o_at + kTile + d, o2);
+        wait_ld(o);
+        if (two) wait_ld(o2);
+        float f[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          f[i] = __uint_as_float(o[i]);
+          if (two) f[i] = f[i] * w1 + __uint_as_float(o2[i]) * w2;
+          f[i] *= inv;
+        }
+        if (mine) {
+          if (it.whole) {
+            uint32_t y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
+            *reinterpret_cast<uint4*>(out + d) = make_uint4(y[0], y[1], y[2], y[3]);
+            *reinterpret_cast<uint4*>(out + d + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+          } else {
+            float4* p = reinterpret_cast<float4*>(a.part + at * a.D + d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+          }
+        }
+      }
+      fence_before();
+      if (mine) {
+        if (!it.whole)
+          a.part_ml[at] = make_float2(top == -INFINITY ? -INFINITY : ref, l);
+        else if (a.lse)
+          a.lse[(tok + row_token) * a.hq + it.h * a.group + row_head] =
+              l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+      }
+    }
+    if (TILE == 0 && !it.pair) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b.odd_empty);
+    }
+    if (!it.whole) {
+      __threadfence();
+      sync_tile<1 + TILE>();
+      if (row == 0) {
+        int32_t* done = a.pieces + 2 * it.c1 + TILE;
+        const int32_t before = atomicAdd(done, 1);
+        if (before == it.pieces - 1) *done = 0;  // for the next call
+        sh->joins[TILE] = before == it.pieces - 1;
+        __threadfence();
+      }
+      sync_tile<1 + TILE>();
+      if (sh->joins[TILE]) join<T>(a, it, TILE, n_rows, tok);
+      sync_tile<1 + TILE>();
+    }
+  }
+}
+
+template <typename T, int HALVES>
+__global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_constant__ AttentionArgs a) {
+  constexpr int S = stages(HALVES);
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+  Shared* sh = reinterpret_cast<Shared*>(smem + (2 + S) * HALVES * kHalf);
+  const uint32_t q_smem = smem_u32(smem), ring = q_smem + 2 * HALVES * kHalf;
+  const int warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    Barriers& b = sh->bar;
+    for (int i = 0; i < S; ++i) mbar_init(&b.full[i], 1), mbar_init(&b.empty[i], 1);
+    mbar_init(&b.q_full, 1);
+    mbar_init(&b.q_empty, 1);
+    for (int t = 0; t < 2; ++t) mbar_init(&b.s_full[t], 1), mbar_init(&b.p_full[t], 4), mbar_init(&b.o_full[t], 1);
+    mbar_init(&b.odd_full, 4);
+    mbar_init(&b.odd_empty, 4);
+    mbar_init(&b.drain, 1);
+    sh->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.q)) : "memory");
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.k)) : "memory");
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.v)) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&sh->tmem))
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  pdl_enter();
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;\n");
+    if (warp == 0) {
+      copy_tiles<HALVES>(a, sh, q_smem, ring);
+    } else if (warp == 1) {
+      multiply<T, HALVES>(a, sh, q_smem, ring);
+    } else {
+      // tokens of no request
+      const int64_t first = a.plan->first, last = a.plan->last, none = first + a.n_tokens - last;
+      const int64_t pieces = none * a.hq * (a.D / 8);
+      for (int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x - 64; i < pieces; i += (int64_t)gridDim.x * 64) {
+        const int64_t x = i / (a.D / 8), h = x % a.hq;
+        int64_t t = x / a.hq;
+        if (t >= first) t += last - first;
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.out.d_data) + t * a.out.token_stride + h * a.out.head_stride +
+                                  i % (a.D / 8) * 8) = make_uint4(0, 0, 0, 0);
+        if (a.lse) a.lse[t * a.hq + h] = -INFINITY;
+      }
+    }
+  } else {
+    // (4 warps of 72 registers a thread and 8 of 216 are what the CTA was launched with: 12 of 168)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;\n");
+    if (warp < 8)
+      softmax<T, 0>(a, sh);
+    else
+      softmax<T, 1>(a, sh);
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(sh->tmem) : "memory");
+  }
+}
+
+constexpr size_t smem_bytes(int halves) { return 1024 + (size_t)(2 + stages(halves)) * halves * kHalf + sizeof(Shared); }
+static_assert(smem_bytes(1) <= 232448 && smem_bytes(2) <= 232448, "227 KB");
+
+bool encode(CUtensorMap* m, int32_t dtype, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+            const cuuint32_t* box) {
+  EncodeTiledFn enc = tensor_map_encoder();
+  const cuuint32_t one[5] = {1, 1, 1, 1, 1};
+  return enc && enc(m, dtype == SMETRIC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank,
+                    const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Bytes of a stride; a dimension of one entry may have any.
+cuuint64_t stride_of(int64_t elements, int64_t entries) { return entries > 1 ? (cuuint64_t)elements * 2 : 256; }
+
 }  // namespace
+
+bool smetric::attention_limits() {
+  const auto set = [](const void* f, int halves) {
+    return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(halves)) == cudaSuccess;
+  };
+  return set((const void*)k_paged_attention<__nv_bfloat16, 1>, 1) && set((const void*)k_paged_attention<__nv_bfloat16, 2>, 2) &&
+         set((const void*)k_paged_attention<__half, 1>, 1) && set((const void*)k_paged_attention<__half, 2>, 2);
+}
 
 extern "C" {
 
@@ -97,28 +789,53 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
       !heads_ok(out, kv->n_tokens) || (reinterpret_cast<uintptr_t>(d_lse) & 3))
     return SMETRIC_ERR_INVALID_ARG;
   if (kv->n_tokens == 0) return SMETRIC_OK;
-  AttentionArgs a = {};
-  a.cache = cache;
-  a.q = q;
+  const smetric_kv_config& c = kv->cfg;
+  static thread_local AttentionArgs a;
+  {
+    const cuuint64_t dims[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.num_q_heads, (cuuint64_t)kv->n_tokens};
+    const cuuint64_t strides[2] = {stride_of(q.head_stride, c.num_q_heads), stride_of(q.token_stride, kv->n_tokens)};
+    const cuuint32_t box[3] = {64, (cuuint32_t)kv->group, (cuuint32_t)kv->tile_tokens};
+    if (!encode(&a.q, c.dtype, 3, q.d_data, dims, strides, box)) return SMETRIC_ERR_INVALID_ARG;
+  }
+  {
+    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.num_kv_heads,
+                                (cuuint64_t)c.num_pages};
+    const cuuint64_t strides[3] = {stride_of(cache.token_stride, c.page_size),
+                                   stride_of(cache.head_stride, c.num_kv_heads),
+                                   stride_of(cache.page_stride, c.num_pages)};
+    const cuuint32_t box[4] = {64, (cuuint32_t)std::min(c.page_size, kTile), 1, 1};
+    if (!encode(&a.k, c.dtype, 4, cache.d_k, dims, strides, box) ||
+        !encode(&a.v, c.dtype, 4, cache.d_v, dims, strides, box))
+      return SMETRIC_ERR_INVALID_ARG;
+  }
   a.out = out;
   a.lse = d_lse;
   a.plan = kv->plan;
-  a.tokens = kv->tokens;
+  a.units = kv->units;
+  a.shares = kv->shares;
+  a.pieces = kv->pieces;
+  a.part = kv->part;
+  a.part_ml = kv->part_ml;
   a.pages = kv->pages;
   a.pages_stride = kv->pages_stride;
-  a.num_pages = kv->cfg.num_pages;
   a.n_tokens = kv->n_tokens;
-  a.hq = kv->cfg.num_q_heads;
+  a.num_pages = (int32_t)c.num_pages;
+  a.hq = c.num_q_heads;
+  a.kv_heads = c.num_kv_heads;
   a.group = kv->group;
-  a.D = kv->cfg.head_dim;
-  a.page_size = kv->cfg.page_size;
+  a.tile_tokens = kv->tile_tokens;
+  a.D = c.head_dim;
+  a.page_size = c.page_size;
+  a.window = kv->window;
   a.scale = scale;
   a.status = kv->status;
+  const int halves = c.head_dim > 64 ? 2 : 1;
+  auto kern = c.dtype == SMETRIC_BF16
+                  ? (halves == 2 ? k_paged_attention<__nv_bfloat16, 2> : k_paged_attention<__nv_bfloat16, 1>)
+                  : (halves == 2 ? k_paged_attention<__half, 2> : k_paged_attention<__half, 1>);
   kv->launches++;
-  auto kern = kv->cfg.dtype == SMETRIC_BF16 ? k_paged_attention<__nv_bfloat16> : k_paged_attention<__half>;
-  const int64_t grid = (kv->n_tokens * a.hq + 7) / 8;
-  if (grid > INT32_MAX) return SMETRIC_ERR_INVALID_ARG;
-  return launch_k(kern, dim3((unsigned)grid), dim3(256), 0, reinterpret_cast<cudaStream_t>(stream), true, a);
+  return launch_k(kern, dim3((unsigned)kv->num_sms), dim3(kThreads), smem_bytes(halves),
+                  reinterpret_cast<cudaStream_t>(stream), true, a);
 }
 
 }  // extern "C"

@@ -1,9 +1,9 @@
 // The paged KV$ operators around the attention: the handle, the plan of a
 // batch, and the norm + rotation + append pass.
 //
-//   k_kv_plan      block 0 checks the batch; the other blocks find each new
-//                  token's request by bisection of the offsets, its position
-//                  and its slot in the cache.
+//   k_kv_plan      block 0 checks the batch and shares its attention out;
+//                  the other blocks find each new token's request by bisection
+//                  of the offsets, its position and its slot in the cache.
 //   k_kv_heads     one pass over the new tokens' heads: queries and keys are
 //                  normed and rotated in registers, keys and values go to
 //                  their slots (or, for the transform alone, to rows).
@@ -28,55 +28,203 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kPlanThreads = 1024;
+constexpr int kMaxCtas = 1024;  // attention CTAs that a plan shares work out to
 
-__global__ void __launch_bounds__(kPlanThreads)
-    k_kv_plan(const int64_t* __restrict__ off, int32_t n, int64_t n_tokens, const int32_t* __restrict__ kv_lens,
-              const int32_t* __restrict__ pages, int32_t max_pages, int64_t pages_stride, int32_t page_size,
-              int64_t num_pages, int32_t window, KvPlan* __restrict__ plan, KvToken* __restrict__ tokens,
-              int32_t* status) {
-  pdl_enter();
-  if (blockIdx.x == 0) {
-    int bad = 0;
-    for (int32_t r = threadIdx.x; r < n; r += blockDim.x) {
-      const int64_t a = off[r], b = off[r + 1], kv = kv_lens[r];
-      bad |= a < 0 || b < a || b > n_tokens || kv < b - a || kv > (int64_t)max_pages * page_size;
-    }
-    bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) {
-      if (bad) latch_error(status, SMETRIC_ERR_INVALID_ARG);
-      plan->first = bad || n == 0 ? n_tokens : off[0];
-      plan->last = bad || n == 0 ? n_tokens : off[n];
-      plan->window = window > 0 ? window : INT32_MAX;
-      plan->valid = !bad;
-    }
-    return;
+// A unit's cost is its key tiles and kUnitCost for what it does once (its
+// queries' load, the first scores, its output). A CTA takes at least kUnitCost
+// + kMinTiles, and a unit is cut at least kMinTiles from its ends.
+constexpr int kUnitCost = 2;
+constexpr int kMinTiles = 2;
+
+struct PlanArgs {
+  const int64_t* off;
+  int32_t n;
+  int64_t n_tokens;
+  const int32_t* kv_lens;
+  const int32_t* pages;
+  int32_t max_pages, page_size;
+  int64_t pages_stride, num_pages;
+  int32_t window, tile_tokens, kv_heads, ctas;
+  KvPlan* plan;
+  KvToken* tokens;
+  KvUnit* units;
+  int64_t* unit_cost;
+  int32_t* unit_base;
+  KvShare* shares;
+  int32_t* pieces;
+  int32_t* status;
+};
+
+// Exclusive prefix sum over the block; total receives the sum.
+template <typename S>
+__device__ S block_scan(S x, S* warp_sums, S& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  S y = x;
+  for (int o = 1; o < 32; o <<= 1) {
+    const S z = __shfl_up_sync(kFull, y, o);
+    if (lane >= o) y += z;
   }
-  const int64_t t = (int64_t)(blockIdx.x - 1) * blockDim.x + threadIdx.x;
-  if (t >= n_tokens) return;
-  KvToken tok = {-1, -1, -1};
-  // the last request that starts at or before t (bad offsets may mislead the
-  // bisection, not past the array: the request's own bounds decide)
+  if (lane == 31) warp_sums[warp] = y;
+  __syncthreads();
+  if (warp == 0) {
+    S v = warp_sums[lane];
+    for (int o = 1; o < 32; o <<= 1) {
+      const S z = __shfl_up_sync(kFull, v, o);
+      if (lane >= o) v += z;
+    }
+    warp_sums[lane] = v;
+  }
+  __syncthreads();
+  total = warp_sums[31];
+  const S before = warp ? warp_sums[warp - 1] : 0;
+  __syncthreads();
+  return before + y - x;
+}
+
+// Largest i in [0, n) with a[i] * scale <= x (a non-decreasing, a[0] = 0, x >= 0).
+template <typename S>
+__device__ int32_t last_at_most(const S* a, int32_t n, int64_t x, int64_t scale) {
   int32_t lo = 0, hi = n;
   while (hi - lo > 1) {
     const int32_t mid = lo + ((hi - lo) >> 1);
-    if (off[mid] <= t)
+    if ((int64_t)a[mid] * scale <= x)
       lo = mid;
     else
       hi = mid;
   }
-  if (n > 0) {
-    const int64_t a = off[lo], b = off[lo + 1], kv = kv_lens[lo];
-    if (a >= 0 && a <= t && t < b && kv >= b - a && kv <= (int64_t)max_pages * page_size) {
-      tok.req = lo;
-      tok.pos = (int32_t)(kv - (b - t));
-      const int32_t page = pages[lo * pages_stride + tok.pos / page_size];
-      if (page >= 0 && page < num_pages)
-        tok.slot = (int64_t)page * page_size + tok.pos % page_size;
+  return lo;
+}
+
+// Shares the batch's attention out: the key tiles of all (unit, key head)
+// pairs in a row, cut into one stretch of equal cost for each CTA, so that one
+// long sequence and many short ones load the SMs alike.
+__device__ void plan_units(const PlanArgs& a) {
+  __shared__ int64_t sums[32];
+  __shared__ int32_t su[kMaxCtas + 1], sh[kMaxCtas + 1], st[kMaxCtas + 1];
+  const int per = 2 * a.tile_tokens;
+  int64_t base = 0;
+  for (int32_t r0 = 0; r0 < a.n; r0 += kPlanThreads) {
+    const int32_t r = r0 + threadIdx.x;
+    const int64_t mine = r < a.n ? (a.off[r + 1] - a.off[r] + per - 1) / per : 0;
+    int64_t total;
+    const int64_t at = block_scan(mine, sums, total);
+    if (r < a.n) a.unit_base[r] = (int32_t)(base + at);
+    base += total;
+  }
+  const int32_t U = (int32_t)base;
+  __syncthreads();
+  int64_t cost = 0;
+  for (int32_t u0 = 0; u0 < U; u0 += kPlanThreads) {
+    const int32_t u = u0 + threadIdx.x;
+    int64_t mine = 0;
+    if (u < U) {
+      const int32_t r = last_at_most(a.unit_base, a.n, u, 1);
+      const int64_t first = (int64_t)(u - a.unit_base[r]) * per, lq = a.off[r + 1] - a.off[r];
+      KvUnit x = {};
+      x.token = (int32_t)(a.off[r] + first);
+      x.tokens = (int32_t)min((int64_t)per, lq - first);
+      x.pos = (int32_t)(a.kv_lens[r] - lq + first);
+      x.req = r;
+      x.tb = x.pos >= a.window ? (x.pos - a.window + 1) / kTile : 0;
+      x.te = (x.pos + x.tokens - 1) / kTile + 1;
+      a.units[u] = x;
+      mine = x.te - x.tb + kUnitCost;
+    }
+    int64_t total;
+    const int64_t at = block_scan(mine, sums, total);
+    if (u < U) a.unit_cost[u] = cost + at;
+    cost += total;
+  }
+  __syncthreads();
+  cost *= a.kv_heads;
+  const int ctas = (int)max((int64_t)1, min((int64_t)a.ctas, cost / (kUnitCost + kMinTiles)));
+  for (int c = threadIdx.x; c <= ctas; c += kPlanThreads) {
+    int32_t u = U, h = 0, t = 0;
+    if (c < ctas && U > 0) {
+      const int64_t x = cost / ctas * c + cost % ctas * c / ctas;
+      u = last_at_most(a.unit_cost, U, x, a.kv_heads);
+      const KvUnit unit = a.units[u];
+      const int64_t one = unit.te - unit.tb + kUnitCost, in = x - a.unit_cost[u] * a.kv_heads;
+      h = (int32_t)(in / one);
+      t = unit.tb + (int32_t)max((int64_t)0, in % one - kUnitCost);
+      if (t - unit.tb < kMinTiles) {
+        t = unit.tb;
+      } else if (unit.te - t < kMinTiles) {
+        if (++h == a.kv_heads) h = 0, ++u;
+        t = u < U ? a.units[u].tb : 0;
+      }
+    }
+    su[c] = u, sh[c] = h, st[c] = t;
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.ctas; c += kPlanThreads) {
+    KvShare s = {};
+    s.u0 = -1;
+    if (c < ctas && (su[c] != su[c + 1] || sh[c] != sh[c + 1] || st[c] != st[c + 1])) {
+      s.u0 = su[c], s.h0 = sh[c], s.t0 = st[c];
+      s.u1 = su[c + 1], s.h1 = sh[c + 1], s.t1 = st[c + 1];
+      const bool cut = s.u1 < U && s.t1 > a.units[s.u1].tb;
+      if (!cut) {
+        if (--s.h1 < 0) s.h1 = a.kv_heads - 1, --s.u1;
+        s.t1 = a.units[s.u1].te;
+      }
+      const auto same = [&](int i, int32_t u, int32_t h) {
+        return i <= ctas && su[i] == u && sh[i] == h && u < U && st[i] > a.units[u].tb;
+      };
+      if (s.t0 > a.units[s.u0].tb) {
+        s.c1 = c;
+        while (same(s.c1, s.u0, s.h0)) --s.c1;
+        s.n_first = 1;
+        while (same(s.c1 + s.n_first, s.u0, s.h0)) ++s.n_first;
+      }
+      s.n_last = 1;
+      while (same(c + s.n_last, s.u1, s.h1)) ++s.n_last;
+    }
+    a.shares[c] = s;
+  }
+}
+
+__global__ void __launch_bounds__(kPlanThreads) k_kv_plan(const __grid_constant__ PlanArgs a) {
+  pdl_enter();
+  if (blockIdx.x == 0) {
+    int bad = 0;
+    for (int32_t r = threadIdx.x; r < a.n; r += blockDim.x) {
+      const int64_t lo = a.off[r], hi = a.off[r + 1], kv = a.kv_lens[r];
+      bad |= lo < 0 || hi < lo || hi > a.n_tokens || kv < hi - lo || kv > (int64_t)a.max_pages * a.page_size;
+    }
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) {
+      if (bad) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
+      a.plan->first = bad || a.n == 0 ? a.n_tokens : a.off[0];
+      a.plan->last = bad || a.n == 0 ? a.n_tokens : a.off[a.n];
+      a.plan->valid = !bad;
+    }
+    for (int i = threadIdx.x; i < 2 * a.ctas; i += kPlanThreads) a.pieces[i] = 0;
+    if (!bad) {
+      plan_units(a);
+    } else {
+      for (int i = threadIdx.x; i < a.ctas; i += kPlanThreads) a.shares[i].u0 = -1;
+    }
+    return;
+  }
+  const int64_t t = (int64_t)(blockIdx.x - 1) * blockDim.x + threadIdx.x;
+  if (t >= a.n_tokens) return;
+  KvToken tok = {-1, -1, 0};
+  if (a.n > 0) {
+    // the last request that starts at or before t (bad offsets may mislead the
+    // bisection, not past the array: the request's own bounds decide)
+    const int32_t r = last_at_most(a.off, a.n, t, 1);
+    const int64_t lo = a.off[r], hi = a.off[r + 1], kv = a.kv_lens[r];
+    if (lo >= 0 && lo <= t && t < hi && kv >= hi - lo && kv <= (int64_t)a.max_pages * a.page_size) {
+      tok.pos = (int32_t)(kv - (hi - t));
+      const int32_t page = a.pages[r * a.pages_stride + tok.pos / a.page_size];
+      if (page >= 0 && page < a.num_pages)
+        tok.slot = (int64_t)page * a.page_size + tok.pos % a.page_size;
       else
-        latch_error(status, SMETRIC_ERR_INVALID_ARG);
+        latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
     }
   }
-  tokens[t] = tok;
+  a.tokens[t] = tok;
 }
 
 template <typename T>
@@ -281,6 +429,13 @@ void free_kv(smetric_kv* kv) {
   cudaFree(kv->status);
   cudaFree(kv->plan);
   cudaFree(kv->tokens);
+  cudaFree(kv->units);
+  cudaFree(kv->unit_cost);
+  cudaFree(kv->unit_base);
+  cudaFree(kv->shares);
+  cudaFree(kv->pieces);
+  cudaFree(kv->part);
+  cudaFree(kv->part_ml);
 }
 
 }  // namespace
@@ -311,12 +466,26 @@ int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out) {
   if (!kv) return SMETRIC_ERR_OOM;
   kv->cfg = c;
   kv->group = c.num_q_heads / c.num_kv_heads;
-  const bool ok =
-      cudaGetDevice(&kv->device) == cudaSuccess &&
-      cudaDeviceGetAttribute(&kv->num_sms, cudaDevAttrMultiProcessorCount, kv->device) == cudaSuccess &&
-      cudaMalloc(&kv->status, sizeof(int32_t)) == cudaSuccess && cudaMalloc(&kv->plan, sizeof(KvPlan)) == cudaSuccess &&
-      cudaMalloc(&kv->tokens, sizeof(KvToken) * (size_t)std::max<int64_t>(1, c.max_batch_tokens)) == cudaSuccess &&
-      cudaMemset(kv->status, 0, sizeof(int32_t)) == cudaSuccess && cudaDeviceSynchronize() == cudaSuccess;
+  kv->tile_tokens = kTile / kv->group;
+  const size_t tokens = (size_t)c.max_batch_tokens, requests = (size_t)c.max_batch_requests;
+  const size_t units = tokens / (2 * kv->tile_tokens) + requests + 1;
+  bool ok = cudaGetDevice(&kv->device) == cudaSuccess &&
+            cudaDeviceGetAttribute(&kv->num_sms, cudaDevAttrMultiProcessorCount, kv->device) == cudaSuccess;
+  if (ok) {
+    kv->num_sms = std::min(kv->num_sms, kMaxCtas);
+    const size_t slots = 2 * (size_t)kv->num_sms * 2 * kTile;
+    ok = cudaMalloc(&kv->status, sizeof(int32_t)) == cudaSuccess &&
+         cudaMalloc(&kv->plan, sizeof(KvPlan)) == cudaSuccess &&
+         cudaMalloc(&kv->tokens, sizeof(KvToken) * (tokens + 1)) == cudaSuccess &&
+         cudaMalloc(&kv->units, sizeof(KvUnit) * units) == cudaSuccess &&
+         cudaMalloc(&kv->unit_cost, sizeof(int64_t) * (units + 1)) == cudaSuccess &&
+         cudaMalloc(&kv->unit_base, sizeof(int32_t) * (requests + 1)) == cudaSuccess &&
+         cudaMalloc(&kv->shares, sizeof(KvShare) * kv->num_sms) == cudaSuccess &&
+         cudaMalloc(&kv->pieces, sizeof(int32_t) * 2 * kv->num_sms) == cudaSuccess &&
+         cudaMalloc(&kv->part, sizeof(float) * slots * c.head_dim) == cudaSuccess &&
+         cudaMalloc(&kv->part_ml, sizeof(float2) * slots) == cudaSuccess && attention_limits() &&
+         cudaMemset(kv->status, 0, sizeof(int32_t)) == cudaSuccess && cudaDeviceSynchronize() == cudaSuccess;
+  }
   if (!ok) {
     (void)cudaGetLastError();
     free_kv(kv);
@@ -352,20 +521,37 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
       (n_requests > 0 && (!d_offsets || !d_kv_lens || (max_pages > 0 && !d_pages))))
     return SMETRIC_ERR_INVALID_ARG;
   kv->planned = false;
+  PlanArgs a = {};
+  a.off = d_offsets;
+  a.n = n_requests;
+  a.n_tokens = n_tokens;
+  a.kv_lens = d_kv_lens;
+  a.pages = d_pages;
+  a.max_pages = max_pages;
+  a.page_size = kv->cfg.page_size;
+  a.pages_stride = pages_stride;
+  a.num_pages = kv->cfg.num_pages;
+  a.window = window > 0 ? window : INT32_MAX;
+  a.tile_tokens = kv->tile_tokens;
+  a.kv_heads = kv->cfg.num_kv_heads;
+  a.ctas = kv->num_sms;
+  a.plan = kv->plan;
+  a.tokens = kv->tokens;
+  a.units = kv->units;
+  a.unit_cost = kv->unit_cost;
+  a.unit_base = kv->unit_base;
+  a.shares = kv->shares;
+  a.pieces = kv->pieces;
+  a.status = kv->status;
   const unsigned grid = 1 + (unsigned)((n_tokens + kPlanThreads - 1) / kPlanThreads);
   kv->launches++;
-  rc = launch_k(k_kv_plan, dim3(grid), dim3(kPlanThreads), 0, reinterpret_cast<cudaStream_t>(stream), true, d_offsets,
-                n_requests, n_tokens, d_kv_lens, d_pages, max_pages, pages_stride, kv->cfg.page_size,
-                kv->cfg.num_pages, window, kv->plan, kv->tokens, kv->status);
+  rc = launch_k(k_kv_plan, dim3(grid), dim3(kPlanThreads), 0, reinterpret_cast<cudaStream_t>(stream), true, a);
   if (rc) return rc;
   kv->planned = true;
-  kv->n_requests = n_requests;
   kv->n_tokens = n_tokens;
-  kv->offsets = d_offsets;
-  kv->kv_lens = d_kv_lens;
   kv->pages = d_pages;
-  kv->max_pages = max_pages;
   kv->pages_stride = pages_stride;
+  kv->window = a.window;
   return SMETRIC_OK;
 }
 

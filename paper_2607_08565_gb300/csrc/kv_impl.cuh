@@ -13,15 +13,41 @@ namespace smetric {
 struct KvToken {
   int64_t slot;
   int32_t pos;
-  int32_t req;
+  int32_t reserved;
 };
 
 // The plan's device-side summary.
 struct KvPlan {
   int64_t first, last;  // tokens [first, last) belong to requests
-  int32_t window;       // keys a query sees at most (INT32_MAX: all)
   int32_t valid;        // 0: the batch's offsets or lengths were refused
+  int32_t reserved[3];
+};
+
+// Keys go through the attention in tiles of kTile, queries in tiles of kTile
+// rows (a row is a token and one of the query heads that share a key head).
+constexpr int kTile = 128;
+
+// Up to two query tiles of one request's consecutive tokens, for one key head
+// at a time: the attention's unit of work.
+struct __align__(16) KvUnit {
+  int32_t token;   // its first token's row in q
+  int32_t tokens;
+  int32_t pos;     // its first token's position
+  int32_t req;
+  int32_t tb, te;  // key tiles that it sees
   int32_t reserved[2];
+};
+
+// A CTA's share: the key tiles of (unit u0, key head h0) from t0, the units
+// and heads that follow, and (u1, h1) up to t1, exclusive. A unit that several
+// CTAs share has n pieces: piece 0 is the end of CTA c1's share, piece i > 0
+// the start of CTA c1 + i's.
+struct __align__(16) KvShare {
+  int32_t u0, h0, t0;  // u0 < 0: nothing
+  int32_t u1, h1, t1;
+  int32_t c1, n_first;  // of the first unit, where the share starts inside it
+  int32_t n_last;       // pieces of the last unit, where the share starts it
+  int32_t reserved[3];
 };
 
 }  // namespace smetric
@@ -31,24 +57,31 @@ struct smetric_kv {
   int device;
   int num_sms;
   int group;        // query heads per key head
+  int tile_tokens;  // tokens of a query tile: kTile / group
   int32_t* status;  // device: first latched error
   smetric::KvPlan* plan;
   smetric::KvToken* tokens;  // max_batch_tokens
+  smetric::KvUnit* units;    // max_batch_tokens / (2 * tile_tokens) + max_batch_requests
+  int64_t* unit_cost;        // as many + 1: cost of the units before, for one key head
+  int32_t* unit_base;        // max_batch_requests + 1: a request's first unit
+  smetric::KvShare* shares;  // num_sms
+  int32_t* pieces;           // 2 * num_sms: pieces done of a unit's two query tiles, by the CTA that starts it
+  float* part;               // 2 * num_sms slots of 2 * kTile rows of head_dim sums
+  float2* part_ml;           // and of (reference exponent, sum)
   // of the last plan
   bool planned;
-  int32_t n_requests;
   int64_t n_tokens;
-  const int64_t* offsets;
-  const int32_t* kv_lens;
   const int32_t* pages;
   int64_t pages_stride;
-  int32_t max_pages;
+  int32_t window;  // keys a query sees at most (INT32_MAX: all)
   int64_t launches;
 };
 
 namespace smetric {
 // Returns SMETRIC_OK if the handle is usable from the current device.
 int check_device(const smetric_kv* kv);
+// Sets the attention kernels' shared-memory limits; false on a CUDA error.
+bool attention_limits();
 // A row of heads that a kernel can address: 16-byte aligned, strides of whole
 // 16-byte pieces.
 inline bool heads_ok(const smetric_heads& h, int64_t n_tokens) {

@@ -46,6 +46,7 @@
 #include "smetric_impl.cuh"
 #include "commit.cuh"
 #include "launch.cuh"
+#include "tensor_map.cuh"
 
 using namespace smetric;
 
@@ -2532,25 +2533,6 @@ void profile_mark(smetric_index* idx, int k, cudaStream_t s);
 struct Overlap {
   cudaEvent_t after_chain;
 };
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-// The driver's tensor-map encoder, looked up once (thread-safe static init).
-EncodeTiledFn tensor_map_encoder() {
-  static const EncodeTiledFn fn = [] {
-    EncodeTiledFn f = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", reinterpret_cast<void**>(&f), 12000,
-                                         cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      f = nullptr;
-    return f;
-  }();
-  return fn;
-}
 
 // The maps of a token buffer: as many rows as fit inside it from each map's base.
 template <int HB>
