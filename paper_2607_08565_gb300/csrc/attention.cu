@@ -194,6 +194,27 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float m;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(m) : "f"(x), "f"(y), "f"(z));
+  return m;
+}
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  float2 r;
+  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+      " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y), "f"(z.x), "f"(z.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 r;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 d, a, b;\n"
+      " mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+  return r;
+}
+
 template <typename T>
 struct Type;
 template <>
@@ -465,10 +486,7 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
   }
 }
 
-template <int BAR>
-__device__ __forceinline__ void sync_tile() {
-  asm volatile("bar.sync %0, 128;\n" ::"n"(BAR) : "memory");
-}
+__device__ __forceinline__ void sync_tile(int bar) { asm volatile("bar.sync %0, 128;\n" ::"r"(bar) : "memory"); }
 
 // Joins the pieces of a unit's query tile t, in their order whoever does it:
 // out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i.
@@ -506,12 +524,13 @@ __device__ __forceinline__ void join(const AttentionArgs& a, const Item& it, int
   }
 }
 
-template <typename T, int TILE>
-__device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh) {
+// (One code for both tiles: two copies miss the instruction cache.)
+template <typename T>
+__device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, const int tile) {
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)warp << 21;  // the warp's TMEM lanes
-  const uint32_t s_at = sh->tmem + TILE * kTile + lanes, o_at = sh->tmem + 2 * kTile + TILE * kTile + lanes;
+  const uint32_t s_at = sh->tmem + tile * kTile + lanes, o_at = sh->tmem + 2 * kTile + tile * kTile + lanes;
   const int row_token = row / a.group, row_head = row - row_token * a.group;
   const float c = a.scale * 1.4426950408889634f;
   uint32_t ns = 0, no = 0, n_other = 0, n_odd = 0;
@@ -519,7 +538,7 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh) {
   Item it;
   for (w.start(a); w.next(a, it);) {
     const int n = it.te - it.tb;
-    const int token = it.pair ? TILE * a.tile_tokens : 0;           // the tile's first token in the unit
+    const int token = it.pair ? tile * a.tile_tokens : 0;           // the tile's first token in the unit
     const int tokens = min(a.tile_tokens, it.unit.tokens - token);  // its tokens
     const int n_rows = tokens * a.group;
     const bool mine = row < n_rows;
@@ -531,8 +550,8 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh) {
     float ref = 0.f;        // the reference exponent: c * top - kLift (0 before the first visible key)
     float l = 0.f;
     int count = 0;
-    for (int j = it.pair ? 0 : TILE; j < n; j += step, ++count) {
-      mbar_wait(&b.s_full[TILE], ns++ & 1, sh, a.status);
+    for (int j = it.pair ? 0 : tile; j < n; j += step, ++count) {
+      mbar_wait(&b.s_full[tile], ns++ & 1, sh, a.status);
       if (busy) {
         fence_after();
         uint32_t r[kTile];
@@ -548,9 +567,14 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh) {
           for (int i = 0; i < kTile; ++i)
             if (key + i > hi || key + i < lo) s[i] = -INFINITY;
         }
-        float most = s[0];
+        float m[8];
 #pragma unroll
-        for (int i = 1; i < kTile; ++i) most = fmaxf(most, s[i]);
+        for (int i = 0; i < 8; ++i) m[i] = s[i];
+#pragma unroll
+        for (int i = 8; i < kTile; i += 16)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) m[k] = i + 8 + k < kTile ? max3(m[k], s[i + k], s[i + 8 + k]) : fmaxf(m[k], s[i + k]);
+        const float most = max3(max3(m[0], m[1], m[2]), max3(m[3], m[4], m[5]), fmaxf(m[6], m[7]));
         const bool move = (most - top) * c > kSlack;  // (false for -inf - -inf)
         if (__any_sync(kFull, move)) {
           float back = 1.f;
@@ -572,30 +596,32 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh) {
             }
           }
         }
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        float2 sum[4] = {};
+        const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
 #pragma unroll
         for (int i = 0; i < kTile; i += 32) {
           uint32_t p[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            const float x = ex2(fmaf(s[i + 2 * k], c, -ref)), y = ex2(fmaf(s[i + 2 * k + 1], c, -ref));
-            sum[2 * k & 3] += x;
-            sum[2 * k + 1 & 3] += y;
-            p[k] = Type<T>::pack(x, y);
+            float2 x = fma2(make_float2(s[i + 2 * k], s[i + 2 * k + 1]), c2, ref2);
+            x = make_float2(ex2(x.x), ex2(x.y));
+            sum[k & 3] = add2(sum[k & 3], x);
+            p[k] = Type<T>::pack(x.x, x.y);
           }
           tmem_st16(s_at + i / 2, p);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        const float2 all = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+        l += all.x + all.y;
         wait_st();
         fence_before();
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&b.p_full[TILE]);
+      if (lane == 0) mbar_arrive(&b.p_full[tile]);
     }
     // ---- the unit's output ----
-    float ref2 = -INFINITY, w1 = 1.f, w2 = 0.f;  // the odd tiles' share
+    float w1 = 1.f, w2 = 0.f;  // the even and the odd tiles' shares
     if (!it.pair) {
-      if (TILE == 1) {
+      if (tile == 1) {
         sh->odd[row] = make_float2(top == -INFINITY ? -INFINITY : ref, l);
         __syncwarp();
         if (lane == 0) mbar_arrive(&b.odd_full);
@@ -606,25 +632,24 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh) {
       if (n > 1) mbar_wait(&b.o_full[1], n_other++ & 1, sh, a.status);
       mbar_wait(&b.odd_full, n_odd++ & 1, sh, a.status);
       const float2 odd = sh->odd[row];
-      ref2 = odd.x;
-      const float ref1 = top == -INFINITY ? -INFINITY : ref, both = fmaxf(ref1, ref2);
+      const float even = top == -INFINITY ? -INFINITY : ref, both = fmaxf(even, odd.x);
       if (both > -INFINITY) {
-        w1 = ex2(ref1 - both);
-        w2 = ex2(ref2 - both);
+        w1 = ex2(even - both);
+        w2 = ex2(odd.x - both);
         l = l * w1 + odd.y * w2;
         ref = both;
         top = 0.f;  // (some key was seen)
       }
-    } else if (TILE == 0) {
+    } else if (tile == 0) {
       ++n_other;
     }
-    mbar_wait(&b.o_full[TILE], no++ & 1, sh, a.status);
+    mbar_wait(&b.o_full[tile], no++ & 1, sh, a.status);
     const bool two = !it.pair && n > 1;
     const int64_t tok = it.unit.token + token;
     if (busy) {
       fence_after();
       const float inv = it.whole ? (l > 0.f ? 1.f / l : l) : 1.f;
-      const int64_t at = (int64_t)it.slot * 2 * kTile + TILE * kTile + row;
+      const int64_t at = (int64_t)it.slot * 2 * kTile + tile * kTile + row;
       T* out = static_cast<T*>(a.out.d_data) + (tok + row_token) * a.out.token_stride +
                (it.h * a.group + row_head) * a.out.head_stride;
       for (int d = 0; d < a.D; d += 16) {
@@ -663,23 +688,23 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh) {
               l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
       }
     }
-    if (TILE == 0 && !it.pair) {
+    if (tile == 0 && !it.pair) {
       __syncwarp();
       if (lane == 0) mbar_arrive(&b.odd_empty);
     }
     if (!it.whole) {
       __threadfence();
-      sync_tile<1 + TILE>();
+      sync_tile(1 + tile);
       if (row == 0) {
-        int32_t* done = a.pieces + 2 * it.c1 + TILE;
+        int32_t* done = a.pieces + 2 * it.c1 + tile;
         const int32_t before = atomicAdd(done, 1);
         if (before == it.pieces - 1) *done = 0;  // for the next call
-        sh->joins[TILE] = before == it.pieces - 1;
+        sh->joins[tile] = before == it.pieces - 1;
         __threadfence();
       }
-      sync_tile<1 + TILE>();
-      if (sh->joins[TILE]) join<T>(a, it, TILE, n_rows, tok);
-      sync_tile<1 + TILE>();
+      sync_tile(1 + tile);
+      if (sh->joins[tile]) join<T>(a, it, tile, n_rows, tok);
+      sync_tile(1 + tile);
     }
   }
 }
@@ -738,10 +763,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   } else {
     // (4 warps of 72 registers a thread and 8 of 216 are what the CTA was launched with: 12 of 168)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;\n");
-    if (warp < 8)
-      softmax<T, 0>(a, sh);
-    else
-      softmax<T, 1>(a, sh);
+    softmax<T>(a, sh, (warp >> 2) - 1);
   }
   __syncwarp();
   fence_before();
