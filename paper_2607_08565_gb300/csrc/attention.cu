@@ -129,6 +129,15 @@ __device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* m, int32
       : "memory");
 }
 
+// One lane of a converged warp, the same one each time. (Under a condition on
+// the lane number the compiler cannot tell that one thread issues, and a matrix
+// product took 120 cycles to issue.)
+__device__ __forceinline__ bool elect() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p) : : "memory");
+  return p != 0;
+}
+
 // Shared-memory descriptors of operands in rows of 128 bytes with the 128-byte
 // swizzle: groups of 8 rows 1,024 bytes apart. lbo: bytes between the 64-element
 // halves, where the rows run along the product's inner dimension (the values).
@@ -368,6 +377,9 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
   constexpr uint32_t kType = 1u << 4 | Type<T>::kFormat << 7 | Type<T>::kFormat << 10 | (kTile >> 4) << 24;
   constexpr uint32_t kScores = kType | (kTile >> 3) << 17;
   const uint32_t values = kType | 1u << 16 | (uint32_t)(a.D >> 3) << 17;
+  const int steps = a.D / 16;
+  // (an operand's address is the descriptor's low bits, in units of 16 bytes)
+  const uint64_t q_desc = smem_desc(q_smem, 16), k_desc = smem_desc(ring, 16), v_desc = smem_desc(ring, kHalf);
   uint32_t base = 0, items = 0, np[2] = {0, 0};
   Walk w;
   Item it;
@@ -379,11 +391,12 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
       mbar_wait(&b.full[stage(place)], (base + place) / S & 1, sh, a.status);
     };
     const auto scores = [&](int t, int q, uint32_t place) {  // S_t = Q_q K^T
-      if (lane == 0) {
-        const uint32_t qa = q_smem + q * HALVES * kHalf, ka = ring + stage(place) * HALVES * kHalf;
-        for (int k = 0; k < a.D / 16; ++k) {
-          const uint32_t o = (k >> 2) * kHalf + (k & 3) * 32;
-          mma_ss(tmem + t * kTile, smem_desc(qa + o, 16), smem_desc(ka + o, 16), kScores, k > 0);
+      if (elect()) {
+        const uint64_t qd = q_desc + (uint64_t)(q * HALVES * kHalf >> 4), kd = k_desc + stage(place) * (HALVES * kHalf >> 4);
+#pragma unroll
+        for (int k = 0; k < 4 * HALVES; ++k) {
+          const uint32_t o = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
+          if (k < steps) mma_ss(tmem + t * kTile, qd + o, kd + o, kScores, k > 0);
         }
         mma_commit(&b.s_full[t]);
       }
@@ -391,16 +404,15 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
     const auto products = [&](int t, uint32_t place, bool add) {  // O_t += P_t V
       mbar_wait(&b.p_full[t], np[t]++ & 1, sh, a.status);
       fence_after();
-      if (lane == 0) {
-        const uint32_t va = ring + stage(place) * HALVES * kHalf;
+      if (elect()) {
+        const uint64_t vd = v_desc + stage(place) * (HALVES * kHalf >> 4);
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)
-          mma_ts(tmem + 2 * kTile + t * kTile, tmem + t * kTile + 8 * k, smem_desc(va + k * 2048, kHalf), values,
-                 add || k > 0);
+          mma_ts(tmem + 2 * kTile + t * kTile, tmem + t * kTile + 8 * k, vd + k * (2048 >> 4), values, add || k > 0);
       }
     };
     const auto release = [&](uint32_t place) {
-      if (lane == 0) mma_commit(&b.empty[stage(place)]);
+      if (elect()) mma_commit(&b.empty[stage(place)]);
     };
     // Rows of a tile's values that no key lies at become zeros: a weight of
     // zero does not cancel what may lie there.
@@ -425,7 +437,7 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
       scores(0, 0, 0);
       scores(1, 1, 0);
       release(0);
-      if (n == 1 && lane == 0) mma_commit(&b.q_empty);
+      if (n == 1 && elect()) mma_commit(&b.q_empty);
       for (int j = 0; j < n; ++j) {
         const uint32_t v = place_v(j, n), k = place_k(j + 1);
         wait_full(v);
@@ -434,7 +446,7 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
         if (j + 1 < n) {
           wait_full(k);
           scores(0, 0, k);
-        } else if (lane == 0) {
+        } else if (elect()) {
           mma_commit(&b.o_full[0]);
         }
         products(1, v, j > 0);
@@ -442,8 +454,8 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
         if (j + 1 < n) {
           scores(1, 1, k);
           release(k);
-          if (j + 2 == n && lane == 0) mma_commit(&b.q_empty);
-        } else if (lane == 0) {
+          if (j + 2 == n && elect()) mma_commit(&b.q_empty);
+        } else if (elect()) {
           mma_commit(&b.o_full[1]);
         }
         if (stopped(sh)) break;
@@ -454,7 +466,7 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
         scores(j, 0, j);
         release(j);
       }
-      if (n <= 2 && lane == 0) mma_commit(&b.q_empty);
+      if (n <= 2 && elect()) mma_commit(&b.q_empty);
       for (int j = 0; j < n; ++j) {
         const int t = j & 1;
         const uint32_t v = place_v(j, n), k = place_k(j + 2);
@@ -466,8 +478,8 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
           wait_full(k);
           scores(t, 0, k);
           release(k);
-          if (j + 3 == n && lane == 0) mma_commit(&b.q_empty);
-        } else if (lane == 0) {
+          if (j + 3 == n && elect()) mma_commit(&b.q_empty);
+        } else if (elect()) {
           mma_commit(&b.o_full[t]);
         }
         if (stopped(sh)) break;
@@ -477,7 +489,7 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
     __syncwarp();
   }
   if (stopped(sh)) {  // products in flight must end before the CTA's memory goes
-    if (lane == 0) {
+    if (elect()) {
       mma_commit(&b.drain);
       for (uint32_t k = 0; k < kSpinLimit && !mbar_try(&b.drain, 0); ++k) {
       }
