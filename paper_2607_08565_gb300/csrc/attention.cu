@@ -1,8 +1,8 @@
 // Attention of a planned batch's queries over the paged cache.
 //
 //   k_paged_attention  one CTA an SM, each with the share of the batch that the
-//                      plan gave it; the sequences that several CTAs share are
-//                      joined by the one that finishes last.
+//                      plan gave it.
+//   k_paged_join       joins the pieces of the units that several CTAs share.
 //
 // For a tile of 128 query rows (a row is a token and one of the query heads of
 // a key head) and a tile of 128 keys: S = Q K^T and O += P V on the tensor
@@ -55,13 +55,13 @@ struct AttentionArgs {
   const KvPlan* plan;
   const KvUnit* units;
   const KvShare* shares;
-  int32_t* pieces;
   float* part;
   float2* part_ml;
   const int32_t* pages;
   int64_t pages_stride, n_tokens;
   int32_t num_pages, hq, kv_heads, group, tile_tokens, D, page_size, window;
   float scale;
+  bool wide;  // outputs can be stored in pieces of 32 bytes
   int32_t* status;
 };
 
@@ -84,7 +84,6 @@ struct Shared {
   float2 odd[kTile];  // (reference, sum) of the odd key tiles
   uint32_t tmem;
   int32_t abort;      // a wait ran out: everybody stops waiting
-  int32_t joins[2];
 };
 
 __device__ __forceinline__ void mbar_init(uint64_t* b, uint32_t count) {
@@ -224,6 +223,11 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
   return r;
 }
 
+__device__ __forceinline__ void st_global32(void* p, const uint32_t* r) {  // 32-byte aligned
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+
 template <typename T>
 struct Type;
 template <>
@@ -254,7 +258,7 @@ struct Item {
   int32_t h, tb, te;  // key head, its key tiles in this CTA
   bool whole;         // nobody else has key tiles of it
   bool pair;          // two query tiles (else the even and the odd key tiles)
-  int32_t slot, c1, pieces;  // where !whole
+  int32_t slot;       // of its partial sums, where !whole
 };
 
 struct Walk {
@@ -263,8 +267,8 @@ struct Walk {
   bool first, done;
   __device__ __forceinline__ void start(const AttentionArgs& a) {
     const int4* p = reinterpret_cast<const int4*>(a.shares + blockIdx.x);
-    const int4 x = p[0], y = p[1], z = p[2];
-    s.u0 = x.x, s.h0 = x.y, s.t0 = x.z, s.u1 = x.w, s.h1 = y.x, s.t1 = y.y, s.c1 = y.z, s.n_first = y.w, s.n_last = z.x;
+    const int4 x = p[0], y = p[1];
+    s.u0 = x.x, s.h0 = x.y, s.t0 = x.z, s.u1 = x.w, s.h1 = y.x, s.t1 = y.y;
     u = s.u0, h = s.h0;
     first = true;
     done = u < 0;
@@ -280,16 +284,20 @@ struct Walk {
     it.te = last ? s.t1 : it.unit.te;
     it.pair = it.unit.tokens > a.tile_tokens;
     it.whole = it.tb == it.unit.tb && it.te == it.unit.te;
-    const bool inside = it.tb != it.unit.tb;
-    it.slot = 2 * (int32_t)blockIdx.x + !inside;
-    it.c1 = inside ? s.c1 : (int32_t)blockIdx.x;
-    it.pieces = inside ? s.n_first : s.n_last;
+    it.slot = 2 * (int32_t)blockIdx.x + (it.tb == it.unit.tb);
     first = false;
     done = last;
     if (++h == a.kv_heads) h = 0, ++u;
     return true;
   }
 };
+
+// Partial sums: a slot's two query tiles, each D/4 columns of kTile rows of four
+// sums, so that the threads of a warp (a row each) store in whole lines. The
+// place of a column's first row, in units of four sums.
+__device__ __forceinline__ int64_t part_at(int D, int64_t slot, int tile, int column) {
+  return ((slot * 2 + tile) * (D / 4) + column) * kTile;
+}
 
 // Places of an item's tiles in the ring, of n key tiles: K0 K1 V0 K2 V1 K3 ...
 __device__ __forceinline__ uint32_t place_k(int j) { return j < 2 ? j : 2 * j - 1; }
@@ -498,44 +506,6 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
   }
 }
 
-__device__ __forceinline__ void sync_tile(int bar) { asm volatile("bar.sync %0, 128;\n" ::"r"(bar) : "memory"); }
-
-// Joins the pieces of a unit's query tile t, in their order whoever does it:
-// out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i.
-template <typename T>
-__device__ __forceinline__ void join(const AttentionArgs& a, const Item& it, int t, int n_rows, int64_t token) {
-  const int quads = a.D / 4;
-  const auto row_at = [&](int i, int row) {
-    const int64_t slot = i ? 2 * (it.c1 + i) : 2 * it.c1 + 1;
-    return slot * 2 * kTile + t * kTile + row;
-  };
-  for (int x = threadIdx.x & 127; x < n_rows * quads; x += 128) {
-    const int row = x / quads, c = x - row * quads;
-    float top = -INFINITY;
-#pragma unroll 8
-    for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, __ldcg(a.part_ml + row_at(i, row)).x);
-    float l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (top > -INFINITY) {
-#pragma unroll 8
-      for (int i = 0; i < it.pieces; ++i) {
-        const int64_t at = row_at(i, row);
-        const float2 ml = __ldcg(a.part_ml + at);
-        const float4 p = __ldcg(reinterpret_cast<const float4*>(a.part + at * a.D) + c);
-        const float f = ex2(ml.x - top);
-        l += f * ml.y;
-        o.x += f * p.x, o.y += f * p.y, o.z += f * p.z, o.w += f * p.w;
-      }
-    }
-    const float inv = l > 0.f ? 1.f / l : l;  // (NaN stays)
-    const int64_t tok = token + row / a.group;
-    const int head = it.h * a.group + row % a.group;
-    uint2 y = make_uint2(Type<T>::pack(o.x * inv, o.y * inv), Type<T>::pack(o.z * inv, o.w * inv));
-    *reinterpret_cast<uint2*>(static_cast<T*>(a.out.d_data) + tok * a.out.token_stride + head * a.out.head_stride + 4 * c) = y;
-    if (a.lse && c == 0) a.lse[tok * a.hq + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
-  }
-}
-
 // (One code for both tiles: two copies miss the instruction cache.)
 template <typename T>
 __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, const int tile) {
@@ -661,7 +631,6 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, cons
     if (busy) {
       fence_after();
       const float inv = it.whole ? (l > 0.f ? 1.f / l : l) : 1.f;
-      const int64_t at = (int64_t)it.slot * 2 * kTile + tile * kTile + row;
       T* out = static_cast<T*>(a.out.d_data) + (tok + row_token) * a.out.token_stride +
                (it.h * a.group + row_head) * a.out.head_stride;
       for (int d = 0; d < a.D; d += 16) {
@@ -682,19 +651,24 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, cons
             uint32_t y[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
-            *reinterpret_cast<uint4*>(out + d) = make_uint4(y[0], y[1], y[2], y[3]);
-            *reinterpret_cast<uint4*>(out + d + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+            if (a.wide) {
+              st_global32(out + d, y);
+            } else {
+              *reinterpret_cast<uint4*>(out + d) = make_uint4(y[0], y[1], y[2], y[3]);
+              *reinterpret_cast<uint4*>(out + d + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+            }
           } else {
-            float4* p = reinterpret_cast<float4*>(a.part + at * a.D + d);
+            float4* p = reinterpret_cast<float4*>(a.part) + part_at(a.D, it.slot, tile, d / 4) + row;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+            for (int i = 0; i < 4; ++i)
+              p[i * kTile] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
           }
         }
       }
       fence_before();
       if (mine) {
         if (!it.whole)
-          a.part_ml[at] = make_float2(top == -INFINITY ? -INFINITY : ref, l);
+          a.part_ml[(int64_t)it.slot * 2 * kTile + tile * kTile + row] = make_float2(top == -INFINITY ? -INFINITY : ref, l);
         else if (a.lse)
           a.lse[(tok + row_token) * a.hq + it.h * a.group + row_head] =
               l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
@@ -703,20 +677,6 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, cons
     if (tile == 0 && !it.pair) {
       __syncwarp();
       if (lane == 0) mbar_arrive(&b.odd_empty);
-    }
-    if (!it.whole) {
-      __threadfence();
-      sync_tile(1 + tile);
-      if (row == 0) {
-        int32_t* done = a.pieces + 2 * it.c1 + tile;
-        const int32_t before = atomicAdd(done, 1);
-        if (before == it.pieces - 1) *done = 0;  // for the next call
-        sh->joins[tile] = before == it.pieces - 1;
-        __threadfence();
-      }
-      sync_tile(1 + tile);
-      if (sh->joins[tile]) join<T>(a, it, tile, n_rows, tok);
-      sync_tile(1 + tile);
     }
   }
 }
@@ -786,6 +746,64 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   }
 }
 
+// A block for a share of the elements of a unit that starts in CTA blockIdx.x's
+// share and that others go on with. With top = max_i ref_i over the pieces,
+// out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i, in the order of
+// the pieces. The loads of kAtOnce pieces are in
+// flight at a time.
+constexpr int kJoinThreads = 128;
+constexpr int kJoinBlocks = 8;
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_constant__ AttentionArgs a) {
+  pdl_enter();
+  const KvShare s = a.shares[blockIdx.x];
+  if (s.u0 < 0) return;
+  const KvUnit unit = a.units[s.u1];
+  const bool starts = s.u0 != s.u1 || s.h0 != s.h1 || s.t0 == unit.tb;
+  if (!starts || s.t1 == unit.te) return;
+  const int pieces = s.n_last, n_rows = unit.tokens * a.group, tile_rows = a.tile_tokens * a.group;
+  constexpr int kAtOnce = 8;
+  for (int x = blockIdx.y * kJoinThreads + threadIdx.x; x < n_rows * (a.D / 4); x += kJoinBlocks * kJoinThreads) {
+    const int column = x / n_rows, r = x - column * n_rows;
+    const int tile = r >= tile_rows, row = r - tile * tile_rows;
+    float top = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < pieces; i0 += kAtOnce) {
+      float2 ml[kAtOnce];
+      float4 p[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int i = min(i0 + k, pieces - 1);
+        const int64_t slot = i ? 2 * ((int64_t)blockIdx.x + i) : 2 * (int64_t)blockIdx.x + 1;
+        ml[k] = a.part_ml[slot * 2 * kTile + tile * kTile + row];
+        p[k] = reinterpret_cast<const float4*>(a.part)[part_at(a.D, slot, tile, column) + row];
+      }
+      float next = top;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
+      if (next == -INFINITY) continue;  // no key so far
+      const float back = ex2(top - next);
+      top = next;
+      l *= back;
+      o.x *= back, o.y *= back, o.z *= back, o.w *= back;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const float f = i0 + k < pieces ? ex2(ml[k].x - top) : 0.f;
+        l += f * ml[k].y;
+        o.x += f * p[k].x, o.y += f * p[k].y, o.z += f * p[k].z, o.w += f * p[k].w;
+      }
+    }
+    const float inv = l > 0.f ? 1.f / l : l;  // (NaN stays)
+    const int64_t token = unit.token + r / a.group;
+    const int head = s.h1 * a.group + r % a.group;
+    *reinterpret_cast<uint2*>(static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride +
+                              4 * column) =
+        make_uint2(Type<T>::pack(o.x * inv, o.y * inv), Type<T>::pack(o.z * inv, o.w * inv));
+    if (a.lse && column == 0)
+      a.lse[token * a.hq + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+  }
+}
+
 constexpr size_t smem_bytes(int halves) { return 1024 + (size_t)(2 + stages(halves)) * halves * kHalf + sizeof(Shared); }
 static_assert(smem_bytes(1) <= 232448 && smem_bytes(2) <= 232448, "227 KB");
 
@@ -847,7 +865,6 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
   a.plan = kv->plan;
   a.units = kv->units;
   a.shares = kv->shares;
-  a.pieces = kv->pieces;
   a.part = kv->part;
   a.part_ml = kv->part_ml;
   a.pages = kv->pages;
@@ -862,13 +879,18 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
   a.page_size = c.page_size;
   a.window = kv->window;
   a.scale = scale;
+  a.wide = !(reinterpret_cast<uintptr_t>(out.d_data) & 31) && out.token_stride % 16 == 0 && out.head_stride % 16 == 0;
   a.status = kv->status;
   const int halves = c.head_dim > 64 ? 2 : 1;
   auto kern = c.dtype == SMETRIC_BF16
                   ? (halves == 2 ? k_paged_attention<__nv_bfloat16, 2> : k_paged_attention<__nv_bfloat16, 1>)
                   : (halves == 2 ? k_paged_attention<__half, 2> : k_paged_attention<__half, 1>);
-  kv->launches++;
-  return launch_k(kern, dim3((unsigned)kv->num_sms), dim3(kThreads), smem_bytes(halves),
+  kv->launches += 2;
+  rc = launch_k(kern, dim3((unsigned)kv->num_sms), dim3(kThreads), smem_bytes(halves),
+                reinterpret_cast<cudaStream_t>(stream), true, a);
+  if (rc) return rc;
+  auto join = c.dtype == SMETRIC_BF16 ? k_paged_join<__nv_bfloat16> : k_paged_join<__half>;
+  return launch_k(join, dim3((unsigned)kv->num_sms, kJoinBlocks), dim3(kJoinThreads), 0,
                   reinterpret_cast<cudaStream_t>(stream), true, a);
 }
 

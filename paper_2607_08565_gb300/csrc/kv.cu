@@ -51,7 +51,6 @@ struct PlanArgs {
   int64_t* unit_cost;
   int32_t* unit_base;
   KvShare* shares;
-  int32_t* pieces;
   int32_t* status;
 };
 
@@ -171,12 +170,6 @@ __device__ void plan_units(const PlanArgs& a) {
       const auto same = [&](int i, int32_t u, int32_t h) {
         return i <= ctas && su[i] == u && sh[i] == h && u < U && st[i] > a.units[u].tb;
       };
-      if (s.t0 > a.units[s.u0].tb) {
-        s.c1 = c;
-        while (same(s.c1, s.u0, s.h0)) --s.c1;
-        s.n_first = 1;
-        while (same(s.c1 + s.n_first, s.u0, s.h0)) ++s.n_first;
-      }
       s.n_last = 1;
       while (same(c + s.n_last, s.u1, s.h1)) ++s.n_last;
     }
@@ -199,7 +192,6 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(const __grid_constant_
       a.plan->last = bad || a.n == 0 ? a.n_tokens : a.off[a.n];
       a.plan->valid = !bad;
     }
-    for (int i = threadIdx.x; i < 2 * a.ctas; i += kPlanThreads) a.pieces[i] = 0;
     if (!bad) {
       plan_units(a);
     } else {
@@ -433,7 +425,6 @@ void free_kv(smetric_kv* kv) {
   cudaFree(kv->unit_cost);
   cudaFree(kv->unit_base);
   cudaFree(kv->shares);
-  cudaFree(kv->pieces);
   cudaFree(kv->part);
   cudaFree(kv->part_ml);
 }
@@ -481,7 +472,6 @@ int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out) {
          cudaMalloc(&kv->unit_cost, sizeof(int64_t) * (units + 1)) == cudaSuccess &&
          cudaMalloc(&kv->unit_base, sizeof(int32_t) * (requests + 1)) == cudaSuccess &&
          cudaMalloc(&kv->shares, sizeof(KvShare) * kv->num_sms) == cudaSuccess &&
-         cudaMalloc(&kv->pieces, sizeof(int32_t) * 2 * kv->num_sms) == cudaSuccess &&
          cudaMalloc(&kv->part, sizeof(float) * slots * c.head_dim) == cudaSuccess &&
          cudaMalloc(&kv->part_ml, sizeof(float2) * slots) == cudaSuccess && attention_limits() &&
          cudaMemset(kv->status, 0, sizeof(int32_t)) == cudaSuccess && cudaDeviceSynchronize() == cudaSuccess;
@@ -541,7 +531,6 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
   a.unit_cost = kv->unit_cost;
   a.unit_base = kv->unit_base;
   a.shares = kv->shares;
-  a.pieces = kv->pieces;
   a.status = kv->status;
   const unsigned grid = 1 + (unsigned)((n_tokens + kPlanThreads - 1) / kPlanThreads);
   kv->launches++;

@@ -40,14 +40,13 @@ struct __align__(16) KvUnit {
 
 // A CTA's share: the key tiles of (unit u0, key head h0) from t0, the units
 // and heads that follow, and (u1, h1) up to t1, exclusive. A unit that several
-// CTAs share has n pieces: piece 0 is the end of CTA c1's share, piece i > 0
-// the start of CTA c1 + i's.
+// CTAs share has pieces: the first is the end of a CTA's share, the others the
+// starts of the next CTAs'.
 struct __align__(16) KvShare {
   int32_t u0, h0, t0;  // u0 < 0: nothing
   int32_t u1, h1, t1;
-  int32_t c1, n_first;  // of the first unit, where the share starts inside it
-  int32_t n_last;       // pieces of the last unit, where the share starts it
-  int32_t reserved[3];
+  int32_t n_last;      // pieces of the last unit, where the share starts it
+  int32_t reserved;
 };
 
 }  // namespace smetric
@@ -65,9 +64,8 @@ struct smetric_kv {
   int64_t* unit_cost;        // as many + 1: cost of the units before, for one key head
   int32_t* unit_base;        // max_batch_requests + 1: a request's first unit
   smetric::KvShare* shares;  // num_sms
-  int32_t* pieces;           // 2 * num_sms: pieces done of a unit's two query tiles, by the CTA that starts it
-  float* part;               // 2 * num_sms slots of 2 * kTile rows of head_dim sums
-  float2* part_ml;           // and of (reference exponent, sum)
+  float* part;               // 2 * num_sms slots of partial sums: a CTA's first unit's, its last's
+  float2* part_ml;           // and their rows' (reference exponent, sum of weights)
   // of the last plan
   bool planned;
   int64_t n_tokens;
