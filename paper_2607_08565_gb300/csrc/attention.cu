@@ -17,8 +17,9 @@
 // of its rows, whose sums are joined at the end.
 //
 // Warps: 0 copies tiles with TMA (keys and values alternate in one ring of
-// buffers), 1 issues the matrix products, 4-7 and 8-11 are the two tiles'
-// softmax (a thread a row).
+// buffers, query tiles in one of two), 1 issues the matrix products, 4-7 and
+// 8-11 are the two tiles' softmax (a thread a row), 12-15 write a unit's output
+// while the softmax of the next one runs.
 
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -40,8 +41,9 @@ using namespace smetric;
 namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
-constexpr uint32_t kSpinLimit = 1u << 24;  // bounded mbarrier waits
-constexpr int kThreads = 384;
+constexpr long long kWaitCycles = 1ll << 32;  // bounded mbarrier waits: about 2 s
+constexpr uint32_t kNap = 20000;
+constexpr int kThreads = 512;
 constexpr float kSlack = 8.f;     // log2 of how far scores may pass the reference
 constexpr uint32_t kHalf = 16384;  // bytes of 128 rows of 64 elements
 
@@ -70,20 +72,21 @@ struct AttentionArgs {
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 struct __align__(8) Barriers {
-  uint64_t full[16], empty[16];  // the ring's
-  uint64_t q_full, q_empty;
+  uint64_t full[11], empty[11];   // the ring's
+  uint64_t q_full[2], q_empty[2];
   uint64_t s_full[2];  // scores in TMEM (and the products before them done)
   uint64_t p_full[2];  // weights in TMEM, O rescaled
   uint64_t o_full[2];  // the unit's last product with the values done
-  uint64_t odd_full, odd_empty;  // the odd key tiles' statistics
+  uint64_t o_free[2];  // its sums and statistics read
+  uint64_t stat_full[2];
   uint64_t drain;
 };
 
 struct Shared {
   Barriers bar;
-  float2 odd[kTile];  // (reference, sum) of the odd key tiles
+  float2 stat[2][kTile];  // a unit's (reference exponent, sum of weights), rows of the two tiles
   uint32_t tmem;
-  int32_t abort;      // a wait ran out: everybody stops waiting
+  int32_t abort;          // a wait ran out: everybody stops waiting
 };
 
 __device__ __forceinline__ void mbar_init(uint64_t* b, uint32_t count) {
@@ -95,24 +98,36 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* b) {
 __device__ __forceinline__ void mbar_expect(uint64_t* b, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
 }
+// One try for the phase of the given parity, asleep for up to kNap ns: four
+// warps that only polled for a unit's end took a tenth of the softmax's speed.
 __device__ __forceinline__ bool mbar_try(uint64_t* b, uint32_t parity) {
   uint32_t done;
   asm volatile(
-      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-      : "=r"(done) : "r"(smem_u32(b)), "r"(parity) : "memory");
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(done) : "r"(smem_u32(b)), "r"(parity), "r"(kNap) : "memory");
   return done != 0;
 }
 __device__ __forceinline__ bool stopped(const Shared* sh) { return *(const volatile int32_t*)&sh->abort != 0; }
-// Waits for the phase of the given parity; gives up after kSpinLimit tries, or
-// when another wait of the CTA has. Callers go on either way (every loop is
-// bounded by the plan); outputs are then undefined and the error is latched.
+// Waits for the phase of the given parity; gives up after kWaitCycles, or when
+// another wait of the CTA has. Callers go on either way (every loop is bounded
+// by the plan); outputs are then undefined and the error is latched.
 __device__ __forceinline__ void mbar_wait(uint64_t* b, uint32_t parity, Shared* sh, int32_t* status) {
-  for (uint32_t i = 0; i < kSpinLimit; ++i) {
-    if (mbar_try(b, parity)) return;
+  if (mbar_try(b, parity)) return;
+  const long long start = clock64();
+  while (!mbar_try(b, parity)) {
     if (stopped(sh)) return;
+    if (clock64() - start > kWaitCycles) {
+      *(volatile int32_t*)&sh->abort = 1;
+      latch_error(status, SMETRIC_ERR_CUDA);
+      return;
+    }
   }
-  *(volatile int32_t*)&sh->abort = 1;
-  latch_error(status, SMETRIC_ERR_CUDA);
+}
+// The same for what is in flight when the CTA gives up.
+__device__ __forceinline__ void mbar_drain(uint64_t* b, uint32_t parity) {
+  const long long start = clock64();
+  while (!mbar_try(b, parity) && clock64() - start < kWaitCycles) {
+  }
 }
 
 __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* m, int32_t x, int32_t y, int32_t z, uint64_t* b) {
@@ -138,21 +153,28 @@ __device__ __forceinline__ bool elect() {
 }
 
 // Shared-memory descriptors of operands in rows of 128 bytes with the 128-byte
-// swizzle: groups of 8 rows 1,024 bytes apart. lbo: bytes between the 64-element
-// halves, where the rows run along the product's inner dimension (the values).
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo) {
-  return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 |
-         2ull << 61;
+// swizzle: groups of 8 rows 1,024 bytes apart (the high half says that). The
+// low half has the address in units of 16 bytes and lbo, the bytes between the
+// 64-element halves where the rows run along the product's inner dimension
+// (the values).
+constexpr uint32_t kDescHigh = 1024 >> 4 | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lbo) {
+  return (addr & 0x3ffff) >> 4 | lbo >> 4 << 16;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.u32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(add),
+      "n"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+      "{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.u32 p, %4, 0;\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(add),
+      "n"(kDescHigh) : "memory");
+}
+__device__ __forceinline__ void zero16(uint32_t addr) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(addr), "r"(0) : "memory");
 }
 // Arrives at b when the products issued so far are done.
 __device__ __forceinline__ void mma_commit(uint64_t* b) {
@@ -262,32 +284,39 @@ struct Item {
 };
 
 struct Walk {
-  KvShare s;
-  int32_t u, h;
+  KvUnit unit;  // the next item's
+  int32_t u, h, t0, u1, h1, t1;
   bool first, done;
+  __device__ __forceinline__ void load(const KvUnit* p) {
+    const int4 x = reinterpret_cast<const int4*>(p)[0];
+    const int2 y = reinterpret_cast<const int2*>(p)[2];
+    unit.token = x.x, unit.tokens = x.y, unit.pos = x.z, unit.req = x.w, unit.tb = y.x, unit.te = y.y;
+  }
   __device__ __forceinline__ void start(const AttentionArgs& a) {
-    const int4* p = reinterpret_cast<const int4*>(a.shares + blockIdx.x);
-    const int4 x = p[0], y = p[1];
-    s.u0 = x.x, s.h0 = x.y, s.t0 = x.z, s.u1 = x.w, s.h1 = y.x, s.t1 = y.y;
-    u = s.u0, h = s.h0;
+    const KvShare* s = a.shares + blockIdx.x;
+    const int4 x = reinterpret_cast<const int4*>(s)[0];
+    const int2 y = reinterpret_cast<const int2*>(s)[2];
+    load(&s->first);
+    u = x.x, h = x.y, t0 = x.z, u1 = x.w, h1 = y.x, t1 = y.y;
     first = true;
     done = u < 0;
   }
   __device__ __forceinline__ bool next(const AttentionArgs& a, Item& it) {
     if (done) return false;
-    const int4* p = reinterpret_cast<const int4*>(a.units + u);
-    const int4 x = p[0], y = p[1];
-    it.unit.token = x.x, it.unit.tokens = x.y, it.unit.pos = x.z, it.unit.req = x.w, it.unit.tb = y.x, it.unit.te = y.y;
-    const bool last = u == s.u1 && h == s.h1;
+    const bool last = u == u1 && h == h1;
+    it.unit = unit;
     it.h = h;
-    it.tb = first ? s.t0 : it.unit.tb;
-    it.te = last ? s.t1 : it.unit.te;
-    it.pair = it.unit.tokens > a.tile_tokens;
-    it.whole = it.tb == it.unit.tb && it.te == it.unit.te;
-    it.slot = 2 * (int32_t)blockIdx.x + (it.tb == it.unit.tb);
+    it.tb = first ? t0 : unit.tb;
+    it.te = last ? t1 : unit.te;
+    it.pair = unit.tokens > a.tile_tokens;
+    it.whole = it.tb == unit.tb && it.te == unit.te;
+    it.slot = 2 * (int32_t)blockIdx.x + (it.tb == unit.tb);
     first = false;
     done = last;
-    if (++h == a.kv_heads) h = 0, ++u;
+    if (++h == a.kv_heads && !done) {
+      h = 0;
+      load(a.units + ++u);  // (ahead of its use)
+    }
     return true;
   }
 };
@@ -313,10 +342,10 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, u
   const int per = max(1, kTile / a.page_size);       // pages of a tile
   const int rows = min(kTile, a.page_size);          // rows of a copy
   const uint32_t q_bytes = (uint32_t)a.tile_tokens * a.group * 128 * HALVES;
-  uint32_t at = 0, items = 0;
+  uint32_t at = 0, nq = 0;
   Walk w;
   Item it;
-  for (w.start(a); w.next(a, it); ++items) {
+  for (w.start(a); w.next(a, it);) {
     const int n = it.te - it.tb;
     // the keys that some query of the unit sees
     const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
@@ -334,16 +363,6 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, u
       }
       return page;
     };
-    if (items) mbar_wait(&b.q_empty, (items - 1) & 1, sh, a.status);
-    if (stopped(sh)) break;
-    if (lane == 0) {
-      mbar_expect(&b.q_full, q_bytes * (it.pair ? 2 : 1));
-      for (int t = 0; t < (it.pair ? 2 : 1); ++t)
-#pragma unroll
-        for (int e = 0; e < HALVES; ++e)
-          tma_3d(q_smem + (t * HALVES + e) * kHalf, &a.q, 64 * e, it.h * a.group, it.unit.token + t * a.tile_tokens,
-                 &b.q_full);
-    }
     const auto copy = [&](const CUtensorMap* map, int tile, int32_t page) {
       const uint32_t s = at % S, round = at / S;
       if (round) mbar_wait(&b.empty[s], (round - 1) & 1, sh, a.status);
@@ -361,6 +380,18 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, u
     };
     int32_t p0 = page_of(it.tb), p1 = page_of(it.tb + 1), p2;
     copy(&a.k, it.tb, p0);
+    for (int t = 0; t < (it.pair ? 2 : 1); ++t, ++nq) {
+      uint64_t* full = &b.q_full[nq & 1];
+      if (nq > 1) mbar_wait(&b.q_empty[nq & 1], (nq / 2 - 1) & 1, sh, a.status);
+      if (lane == 0 && !stopped(sh)) {
+        mbar_expect(full, q_bytes);
+#pragma unroll
+        for (int e = 0; e < HALVES; ++e)
+          tma_3d(q_smem + ((nq & 1) * HALVES + e) * kHalf, &a.q, 64 * e, it.h * a.group,
+                 it.unit.token + t * a.tile_tokens, full);
+      }
+      __syncwarp();
+    }
     if (n > 1) copy(&a.k, it.tb + 1, p1);
     for (int j = 0; j < n; ++j) {
       p2 = page_of(it.tb + j + 2);
@@ -368,11 +399,11 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, u
       if (j + 2 < n) copy(&a.k, it.tb + j + 2, p2);
       p0 = p1, p1 = p2;
     }
+    if (stopped(sh)) break;
   }
   if (stopped(sh)) {  // copies in flight must land before the CTA ends
-    for (uint32_t i = at > S ? at - S : 0; i < at; ++i)
-      for (uint32_t k = 0; k < kSpinLimit && !mbar_try(&b.full[i % S], i / S & 1); ++k) {
-      }
+    for (uint32_t i = at > S ? at - S : 0; i < at; ++i) mbar_drain(&b.full[i % S], i / S & 1);
+    for (uint32_t i = nq > 2 ? nq - 2 : 0; i < nq; ++i) mbar_drain(&b.q_full[i & 1], i / 2 & 1);
   }
 }
 
@@ -387,8 +418,8 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
   const uint32_t values = kType | 1u << 16 | (uint32_t)(a.D >> 3) << 17;
   const int steps = a.D / 16;
   // (an operand's address is the descriptor's low bits, in units of 16 bytes)
-  const uint64_t q_desc = smem_desc(q_smem, 16), k_desc = smem_desc(ring, 16), v_desc = smem_desc(ring, kHalf);
-  uint32_t base = 0, items = 0, np[2] = {0, 0};
+  const uint32_t q_desc = desc_low(q_smem, 16), k_desc = desc_low(ring, 16), v_desc = desc_low(ring, kHalf);
+  uint32_t base = 0, items = 0, nq = 0, np[2] = {0, 0};
   Walk w;
   Item it;
   for (w.start(a); w.next(a, it); ++items) {
@@ -398,9 +429,13 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
     const auto wait_full = [&](uint32_t place) {
       mbar_wait(&b.full[stage(place)], (base + place) / S & 1, sh, a.status);
     };
-    const auto scores = [&](int t, int q, uint32_t place) {  // S_t = Q_q K^T
+    const auto wait_q = [&](uint32_t i) { mbar_wait(&b.q_full[i & 1], i / 2 & 1, sh, a.status); };
+    const auto release_q = [&](uint32_t i) {
+      if (elect()) mma_commit(&b.q_empty[i & 1]);
+    };
+    const auto scores = [&](int t, uint32_t q, uint32_t place) {  // S_t = Q_q K^T
       if (elect()) {
-        const uint64_t qd = q_desc + (uint64_t)(q * HALVES * kHalf >> 4), kd = k_desc + stage(place) * (HALVES * kHalf >> 4);
+        const uint32_t qd = q_desc + (q & 1) * (HALVES * kHalf >> 4), kd = k_desc + stage(place) * (HALVES * kHalf >> 4);
 #pragma unroll
         for (int k = 0; k < 4 * HALVES; ++k) {
           const uint32_t o = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
@@ -409,101 +444,114 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
         mma_commit(&b.s_full[t]);
       }
     };
-    const auto products = [&](int t, uint32_t place, bool add) {  // O_t += P_t V
+    // O_t (+)= P_t V; `next`, if not 0, is a place that is needed after it.
+    const auto products = [&](int t, uint32_t place, bool add, uint32_t next) {
+      const uint32_t vd = v_desc + stage(place) * (HALVES * kHalf >> 4);
+      if (!add && items) mbar_wait(&b.o_free[t], (items - 1) & 1, sh, a.status);
       mbar_wait(&b.p_full[t], np[t]++ & 1, sh, a.status);
       fence_after();
       if (elect()) {
-        const uint64_t vd = v_desc + stage(place) * (HALVES * kHalf >> 4);
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)
           mma_ts(tmem + 2 * kTile + t * kTile, tmem + t * kTile + 8 * k, vd + k * (2048 >> 4), values, add || k > 0);
       }
+      if (next) wait_full(next);
     };
     const auto release = [&](uint32_t place) {
       if (elect()) mma_commit(&b.empty[stage(place)]);
     };
     // Rows of a tile's values that no key lies at become zeros: a weight of
-    // zero does not cancel what may lie there.
+    // zero does not cancel what may lie there. (A row's 128 bytes are its own
+    // under the swizzle.)
     const auto clear = [&](uint32_t place, int j) {
       const int32_t key = (it.tb + j) * kTile;
       if (key >= lo && key + kTile <= hi) return;
-      for (int i = lane; i < kTile * 8 * HALVES; i += 32) {
-        const int row = i / 8 % kTile;
-        if (key + row < lo || key + row >= hi)
-          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(
-                           ring + stage(place) * HALVES * kHalf + i / (8 * kTile) * kHalf + row * 128 + i % 8 * 16),
-                       "r"(0) : "memory");
+      const uint32_t at = ring + stage(place) * HALVES * kHalf;
+      const int before = max(lo - key, 0), after = min(hi - key, kTile);
+#pragma unroll
+      for (int e = 0; e < HALVES; ++e) {
+        for (int i = lane * 16; i < before * 128; i += 512) zero16(at + e * kHalf + i);
+        for (int i = after * 128 + lane * 16; i < kTile * 128; i += 512) zero16(at + e * kHalf + i);
       }
       asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
       __syncwarp();
     };
-    mbar_wait(&b.q_full, items & 1, sh, a.status);
     wait_full(0);
+    wait_q(nq);
     if (stopped(sh)) break;
     fence_after();
     if (it.pair) {
-      scores(0, 0, 0);
-      scores(1, 1, 0);
+      scores(0, nq, 0);
+      wait_q(nq + 1);
+      scores(1, nq + 1, 0);
       release(0);
-      if (n == 1 && elect()) mma_commit(&b.q_empty);
+      if (n == 1) release_q(nq), release_q(nq + 1);
       for (int j = 0; j < n; ++j) {
-        const uint32_t v = place_v(j, n), k = place_k(j + 1);
+        const uint32_t v = place_v(j, n), k = j + 1 < n ? place_k(j + 1) : 0;
         wait_full(v);
         clear(v, j);
-        products(0, v, j > 0);
-        if (j + 1 < n) {
-          wait_full(k);
-          scores(0, 0, k);
+        products(0, v, j > 0, k);
+        if (k) {
+          scores(0, nq, k);
+          if (j + 2 == n) release_q(nq);
         } else if (elect()) {
           mma_commit(&b.o_full[0]);
         }
-        products(1, v, j > 0);
+        products(1, v, j > 0, 0);
         release(v);
-        if (j + 1 < n) {
-          scores(1, 1, k);
+        if (k) {
+          scores(1, nq + 1, k);
           release(k);
-          if (j + 2 == n && elect()) mma_commit(&b.q_empty);
+          if (j + 2 == n) release_q(nq + 1);
         } else if (elect()) {
           mma_commit(&b.o_full[1]);
         }
         if (stopped(sh)) break;
       }
+      nq += 2;
     } else {
       for (int j = 0; j < min(n, 2); ++j) {
         if (j) wait_full(j);
-        scores(j, 0, j);
+        scores(j, nq, j);
         release(j);
       }
-      if (n <= 2 && elect()) mma_commit(&b.q_empty);
+      if (n <= 2) release_q(nq);
       for (int j = 0; j < n; ++j) {
         const int t = j & 1;
-        const uint32_t v = place_v(j, n), k = place_k(j + 2);
+        const uint32_t v = place_v(j, n), k = j + 2 < n ? place_k(j + 2) : 0;
         wait_full(v);
         clear(v, j);
-        products(t, v, j > 1);
+        products(t, v, j > 1, k);
         release(v);
-        if (j + 2 < n) {
-          wait_full(k);
-          scores(t, 0, k);
+        if (k) {
+          scores(t, nq, k);
           release(k);
-          if (j + 3 == n && elect()) mma_commit(&b.q_empty);
+          if (j + 3 == n) release_q(nq);
         } else if (elect()) {
           mma_commit(&b.o_full[t]);
         }
         if (stopped(sh)) break;
       }
+      // (every unit's is waited for, so that no two have one parity)
+      if (n == 1 && items) mbar_wait(&b.o_free[1], (items - 1) & 1, sh, a.status);
+      nq += 1;
     }
     base += 2 * n;
     __syncwarp();
   }
   if (stopped(sh)) {  // products in flight must end before the CTA's memory goes
-    if (elect()) {
-      mma_commit(&b.drain);
-      for (uint32_t k = 0; k < kSpinLimit && !mbar_try(&b.drain, 0); ++k) {
-      }
-    }
+    if (elect()) mma_commit(&b.drain);
+    mbar_drain(&b.drain, 0);
     __syncwarp();
   }
+}
+
+// A tile's first token in its unit, and its rows.
+__device__ __forceinline__ int tile_token(const AttentionArgs& a, const Item& it, int tile) {
+  return it.pair ? tile * a.tile_tokens : 0;
+}
+__device__ __forceinline__ int tile_rows(const AttentionArgs& a, const Item& it, int tile) {
+  return min(a.tile_tokens, it.unit.tokens - tile_token(a, it, tile)) * a.group;
 }
 
 // (One code for both tiles: two copies miss the instruction cache.)
@@ -513,170 +561,183 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, cons
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)warp << 21;  // the warp's TMEM lanes
   const uint32_t s_at = sh->tmem + tile * kTile + lanes, o_at = sh->tmem + 2 * kTile + tile * kTile + lanes;
-  const int row_token = row / a.group, row_head = row - row_token * a.group;
+  const int row_token = row / a.group;
   const float c = a.scale * 1.4426950408889634f;
-  uint32_t ns = 0, no = 0, n_other = 0, n_odd = 0;
+  uint32_t ns = 0, items = 0;
   Walk w;
   Item it;
-  for (w.start(a); w.next(a, it);) {
+  for (w.start(a); w.next(a, it); ++items) {
     const int n = it.te - it.tb;
-    const int token = it.pair ? tile * a.tile_tokens : 0;           // the tile's first token in the unit
-    const int tokens = min(a.tile_tokens, it.unit.tokens - token);  // its tokens
-    const int n_rows = tokens * a.group;
+    const int n_rows = tile_rows(a, it, tile);
     const bool mine = row < n_rows;
-    const int32_t hi = mine ? it.unit.pos + token + row_token : INT32_MAX;  // last key that the row sees
-    const int32_t lo = mine && hi >= a.window ? hi - a.window + 1 : 0;      // first key
+    const int32_t hi = mine ? it.unit.pos + tile_token(a, it, tile) + row_token : INT32_MAX;  // last key that the row sees
+    const int32_t lo = mine && hi >= a.window ? hi - a.window + 1 : 0;                        // first key
     const bool busy = 32 * warp < n_rows;
-    const int step = it.pair ? 1 : 2;
     float top = -INFINITY;  // largest score when the reference was last moved
     float ref = 0.f;        // the reference exponent: c * top - kLift (0 before the first visible key)
     float l = 0.f;
-    int count = 0;
-    for (int j = it.pair ? 0 : tile; j < n; j += step, ++count) {
+    for (int j = it.pair ? 0 : tile; j < n; j += it.pair ? 1 : 2) {
       mbar_wait(&b.s_full[tile], ns++ & 1, sh, a.status);
-      if (busy) {
-        fence_after();
-        uint32_t r[kTile];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, r + 32 * i);
-        wait_ld(r);
-        float s[kTile];
-#pragma unroll
-        for (int i = 0; i < kTile; ++i) s[i] = __uint_as_float(r[i]);
-        const int32_t key = (it.tb + j) * kTile;
-        if (__any_sync(kFull, key + kTile - 1 > hi || key < lo)) {
-#pragma unroll
-          for (int i = 0; i < kTile; ++i)
-            if (key + i > hi || key + i < lo) s[i] = -INFINITY;
-        }
-        float m[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m[i] = s[i];
-#pragma unroll
-        for (int i = 8; i < kTile; i += 16)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) m[k] = i + 8 + k < kTile ? max3(m[k], s[i + k], s[i + 8 + k]) : fmaxf(m[k], s[i + k]);
-        const float most = max3(max3(m[0], m[1], m[2]), max3(m[3], m[4], m[5]), fmaxf(m[6], m[7]));
-        const bool move = (most - top) * c > kSlack;  // (false for -inf - -inf)
-        if (__any_sync(kFull, move)) {
-          float back = 1.f;
-          if (move) {
-            const float next = most * c - Type<T>::kLift;
-            back = top == -INFINITY ? 0.f : ex2(ref - next);
-            top = most;
-            ref = next;
-            l *= back;
-          }
-          if (count > 0) {
-            for (int d = 0; d < a.D; d += 16) {
-              uint32_t o[16];
-              tmem_ld16(o_at + d, o);
-              wait_ld(o);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * back);
-              tmem_st16(o_at + d, o);
-            }
-          }
-        }
-        float2 sum[4] = {};
-        const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
-#pragma unroll
-        for (int i = 0; i < kTile; i += 32) {
-          uint32_t p[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            float2 x = fma2(make_float2(s[i + 2 * k], s[i + 2 * k + 1]), c2, ref2);
-            x = make_float2(ex2(x.x), ex2(x.y));
-            sum[k & 3] = add2(sum[k & 3], x);
-            p[k] = Type<T>::pack(x.x, x.y);
-          }
-          tmem_st16(s_at + i / 2, p);
-        }
-        const float2 all = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
-        l += all.x + all.y;
-        wait_st();
-        fence_before();
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&b.p_full[tile]);
-    }
-    // ---- the unit's output ----
-    float w1 = 1.f, w2 = 0.f;  // the even and the odd tiles' shares
-    if (!it.pair) {
-      if (tile == 1) {
-        sh->odd[row] = make_float2(top == -INFINITY ? -INFINITY : ref, l);
+      if (!busy) {
         __syncwarp();
-        if (lane == 0) mbar_arrive(&b.odd_full);
-        mbar_wait(&b.odd_empty, n_odd++ & 1, sh, a.status);  // until its sums are read
-        no += n > 1;
+        if (lane == 0) mbar_arrive(&b.p_full[tile]);
         continue;
       }
-      if (n > 1) mbar_wait(&b.o_full[1], n_other++ & 1, sh, a.status);
-      mbar_wait(&b.odd_full, n_odd++ & 1, sh, a.status);
-      const float2 odd = sh->odd[row];
-      const float even = top == -INFINITY ? -INFINITY : ref, both = fmaxf(even, odd.x);
-      if (both > -INFINITY) {
-        w1 = ex2(even - both);
-        w2 = ex2(odd.x - both);
-        l = l * w1 + odd.y * w2;
-        ref = both;
-        top = 0.f;  // (some key was seen)
-      }
-    } else if (tile == 0) {
-      ++n_other;
-    }
-    mbar_wait(&b.o_full[tile], no++ & 1, sh, a.status);
-    const bool two = !it.pair && n > 1;
-    const int64_t tok = it.unit.token + token;
-    if (busy) {
       fence_after();
-      const float inv = it.whole ? (l > 0.f ? 1.f / l : l) : 1.f;
-      T* out = static_cast<T*>(a.out.d_data) + (tok + row_token) * a.out.token_stride +
-               (it.h * a.group + row_head) * a.out.head_stride;
-      for (int d = 0; d < a.D; d += 16) {
-        uint32_t o[16], o2[16];
-        tmem_ld16(o_at + d, o);
-        if (two) tmem_ld16(o_at + kTile + d, o2);
-        wait_ld(o);
-        if (two) wait_ld(o2);
-        float f[16];
+      uint32_t r[kTile];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          f[i] = __uint_as_float(o[i]);
-          if (two) f[i] = f[i] * w1 + __uint_as_float(o2[i]) * w2;
-          f[i] *= inv;
+      for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, r + 32 * i);
+      wait_ld(r);
+      float s[kTile];
+#pragma unroll
+      for (int i = 0; i < kTile; ++i) s[i] = __uint_as_float(r[i]);
+      const int32_t key = (it.tb + j) * kTile;
+      if (__any_sync(kFull, key + kTile - 1 > hi || key < lo)) {
+#pragma unroll
+        for (int i = 0; i < kTile; ++i)
+          if (key + i > hi || key + i < lo) s[i] = -INFINITY;
+      }
+      float m[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[i] = s[i];
+#pragma unroll
+      for (int i = 8; i < kTile; i += 16)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m[k] = i + 8 + k < kTile ? max3(m[k], s[i + k], s[i + 8 + k]) : fmaxf(m[k], s[i + k]);
+      const float most = max3(max3(m[0], m[1], m[2]), max3(m[3], m[4], m[5]), fmaxf(m[6], m[7]));
+      const bool move = (most - top) * c > kSlack;  // (false for -inf - -inf)
+      if (__any_sync(kFull, move)) {
+        float back = 1.f;
+        if (move) {
+          const float next = most * c - Type<T>::kLift;
+          back = top == -INFINITY ? 0.f : ex2(ref - next);
+          top = most;
+          ref = next;
+          l *= back;
         }
-        if (mine) {
-          if (it.whole) {
-            uint32_t y[8];
+        if (j > (it.pair ? 0 : tile)) {
+          for (int d = 0; d < a.D; d += 16) {
+            uint32_t o[16];
+            tmem_ld16(o_at + d, o);
+            wait_ld(o);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
-            if (a.wide) {
-              st_global32(out + d, y);
-            } else {
-              *reinterpret_cast<uint4*>(out + d) = make_uint4(y[0], y[1], y[2], y[3]);
-              *reinterpret_cast<uint4*>(out + d + 8) = make_uint4(y[4], y[5], y[6], y[7]);
-            }
-          } else {
-            float4* p = reinterpret_cast<float4*>(a.part) + part_at(a.D, it.slot, tile, d / 4) + row;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              p[i * kTile] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * back);
+            tmem_st16(o_at + d, o);
           }
         }
       }
-      fence_before();
-      if (mine) {
-        if (!it.whole)
-          a.part_ml[(int64_t)it.slot * 2 * kTile + tile * kTile + row] = make_float2(top == -INFINITY ? -INFINITY : ref, l);
-        else if (a.lse)
-          a.lse[(tok + row_token) * a.hq + it.h * a.group + row_head] =
-              l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+      float2 sum[4] = {};
+      const float2 c2 = make_float2(c, c), ref2 = make_float2(-ref, -ref);
+#pragma unroll
+      for (int i = 0; i < kTile; i += 32) {
+        uint32_t p[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          float2 x = fma2(make_float2(s[i + 2 * k], s[i + 2 * k + 1]), c2, ref2);
+          x = make_float2(ex2(x.x), ex2(x.y));
+          sum[k & 3] = add2(sum[k & 3], x);
+          p[k] = Type<T>::pack(x.x, x.y);
+        }
+        tmem_st16(s_at + i / 2, p);
       }
-    }
-    if (tile == 0 && !it.pair) {
+      wait_st();
+      fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&b.odd_empty);
+      if (lane == 0) mbar_arrive(&b.p_full[tile]);
+      const float2 all = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+      l += all.x + all.y;
+    }
+    if (items) mbar_wait(&b.o_free[tile], (items - 1) & 1, sh, a.status);
+    sh->stat[tile][row] = make_float2(top == -INFINITY ? -INFINITY : ref, l);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&b.stat_full[tile]);
+  }
+}
+
+// A unit's output: O / l, or its sums and statistics where other CTAs have
+// pieces of it.
+template <typename T>
+__device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh) {
+  Barriers& b = sh->bar;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
+  const uint32_t o_all = sh->tmem + 2 * kTile + ((uint32_t)warp << 21);
+  const int row_token = row / a.group, row_head = row - row_token * a.group;
+  uint32_t items = 0, no[2] = {0, 0};
+  Walk w;
+  Item it;
+  for (w.start(a); w.next(a, it); ++items) {
+    const bool two = !it.pair && it.te - it.tb > 1;  // sums of even and of odd key tiles
+    for (int tile = 0; tile < (it.pair ? 2 : 1); ++tile) {
+      const int n_rows = tile_rows(a, it, tile);
+      mbar_wait(&b.stat_full[tile], items & 1, sh, a.status);
+      float2 st = sh->stat[tile][row];
+      float w1 = 1.f, w2 = 0.f;  // the even and the odd tiles' shares
+      if (!it.pair) {
+        mbar_wait(&b.stat_full[1], items & 1, sh, a.status);
+        const float2 odd = sh->stat[1][row];
+        const float both = fmaxf(st.x, odd.x);
+        if (both > -INFINITY) {
+          w1 = ex2(st.x - both);
+          w2 = ex2(odd.x - both);
+          st = make_float2(both, st.y * w1 + odd.y * w2);
+        }
+        if (two) mbar_wait(&b.o_full[1], no[1]++ & 1, sh, a.status);
+      }
+      mbar_wait(&b.o_full[tile], no[tile]++ & 1, sh, a.status);
+      if (32 * warp < n_rows) {
+        fence_after();
+        const bool mine = row < n_rows;
+        const int64_t token = it.unit.token + tile_token(a, it, tile) + row_token;
+        const int head = it.h * a.group + row_head;
+        const float inv = it.whole ? (st.y > 0.f ? 1.f / st.y : st.y) : 1.f;  // (NaN stays)
+        w1 *= inv, w2 *= inv;
+        const uint32_t o_at = o_all + tile * kTile;
+        T* out = static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride;
+        for (int d = 0; d < a.D; d += 16) {
+          uint32_t o[16];
+          float f[16];
+          tmem_ld16(o_at + d, o);
+          wait_ld(o);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(o[i]) * w1;
+          if (two) {
+            tmem_ld16(o_at + kTile + d, o);
+            wait_ld(o);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f[i] += __uint_as_float(o[i]) * w2;
+          }
+          if (mine) {
+            if (it.whole) {
+              uint32_t y[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
+              if (a.wide) {
+                st_global32(out + d, y);
+              } else {
+                *reinterpret_cast<uint4*>(out + d) = make_uint4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<uint4*>(out + d + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+              }
+            } else {
+              float4* p = reinterpret_cast<float4*>(a.part) + part_at(a.D, it.slot, tile, d / 4) + row;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                p[i * kTile] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+            }
+          }
+        }
+        fence_before();
+        if (mine) {
+          if (!it.whole)
+            a.part_ml[(int64_t)it.slot * 2 * kTile + tile * kTile + row] = st;
+          else if (a.lse)
+            a.lse[token * a.hq + head] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * 0.6931471805599453f;
+        }
+      }
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&b.o_free[tile]);
+        if (!it.pair) mbar_arrive(&b.o_free[1]);
+      }
     }
   }
 }
@@ -685,18 +746,25 @@ template <typename T, int HALVES>
 __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_constant__ AttentionArgs a) {
   constexpr int S = stages(HALVES);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-  Shared* sh = reinterpret_cast<Shared*>(smem + (2 + S) * HALVES * kHalf);
-  const uint32_t q_smem = smem_u32(smem), ring = q_smem + 2 * HALVES * kHalf;
+  Shared* sh = reinterpret_cast<Shared*>(smem_raw + (2 + S) * HALVES * kHalf);
+  if (smem_u32(smem_raw) & 1023) {  // (the swizzle's groups of 8 rows)
+    latch_error(a.status, SMETRIC_ERR_CUDA);
+    return;
+  }
+  const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + 2 * HALVES * kHalf;
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     Barriers& b = sh->bar;
     for (int i = 0; i < S; ++i) mbar_init(&b.full[i], 1), mbar_init(&b.empty[i], 1);
-    mbar_init(&b.q_full, 1);
-    mbar_init(&b.q_empty, 1);
-    for (int t = 0; t < 2; ++t) mbar_init(&b.s_full[t], 1), mbar_init(&b.p_full[t], 4), mbar_init(&b.o_full[t], 1);
-    mbar_init(&b.odd_full, 4);
-    mbar_init(&b.odd_empty, 4);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&b.q_full[t], 1);
+      mbar_init(&b.q_empty[t], 1);
+      mbar_init(&b.s_full[t], 1);
+      mbar_init(&b.p_full[t], 4);  // (a lane of each warp)
+      mbar_init(&b.o_full[t], 1);
+      mbar_init(&b.o_free[t], 4);
+      mbar_init(&b.stat_full[t], 4);
+    }
     mbar_init(&b.drain, 1);
     sh->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -713,8 +781,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   __syncthreads();
   fence_after();
   pdl_enter();
+  // Registers a thread: 4 warps of 80, 8 of 176 and 4 of 80 are what the CTA was
+  // launched with, 16 of 128.
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;\n");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
     if (warp == 0) {
       copy_tiles<HALVES>(a, sh, q_smem, ring);
     } else if (warp == 1) {
@@ -732,10 +802,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         if (a.lse) a.lse[t * a.hq + h] = -INFINITY;
       }
     }
-  } else {
-    // (4 warps of 72 registers a thread and 8 of 216 are what the CTA was launched with: 12 of 168)
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;\n");
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;\n");
     softmax<T>(a, sh, (warp >> 2) - 1);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
+    write_out<T>(a, sh);
   }
   __syncwarp();
   fence_before();
@@ -761,11 +833,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
   const KvUnit unit = a.units[s.u1];
   const bool starts = s.u0 != s.u1 || s.h0 != s.h1 || s.t0 == unit.tb;
   if (!starts || s.t1 == unit.te) return;
-  const int pieces = s.n_last, n_rows = unit.tokens * a.group, tile_rows = a.tile_tokens * a.group;
+  const int pieces = s.n_last, n_rows = unit.tokens * a.group, full_rows = a.tile_tokens * a.group;
   constexpr int kAtOnce = 8;
   for (int x = blockIdx.y * kJoinThreads + threadIdx.x; x < n_rows * (a.D / 4); x += kJoinBlocks * kJoinThreads) {
     const int column = x / n_rows, r = x - column * n_rows;
-    const int tile = r >= tile_rows, row = r - tile * tile_rows;
+    const int tile = r >= full_rows, row = r - tile * full_rows;
     float top = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i0 = 0; i0 < pieces; i0 += kAtOnce) {
@@ -804,7 +876,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
   }
 }
 
-constexpr size_t smem_bytes(int halves) { return 1024 + (size_t)(2 + stages(halves)) * halves * kHalf + sizeof(Shared); }
+constexpr size_t smem_bytes(int halves) { return (size_t)(2 + stages(halves)) * halves * kHalf + sizeof(Shared); }
 static_assert(smem_bytes(1) <= 232448 && smem_bytes(2) <= 232448, "227 KB");
 
 bool encode(CUtensorMap* m, int32_t dtype, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,

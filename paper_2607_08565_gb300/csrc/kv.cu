@@ -161,6 +161,7 @@ __device__ void plan_units(const PlanArgs& a) {
     s.u0 = -1;
     if (c < ctas && (su[c] != su[c + 1] || sh[c] != sh[c + 1] || st[c] != st[c + 1])) {
       s.u0 = su[c], s.h0 = sh[c], s.t0 = st[c];
+      s.first = a.units[s.u0];
       s.u1 = su[c + 1], s.h1 = sh[c + 1], s.t1 = st[c + 1];
       const bool cut = s.u1 < U && s.t1 > a.units[s.u1].tb;
       if (!cut) {
