@@ -16,9 +16,9 @@
 // (both read the same keys), a smaller one has the even and the odd key tiles
 // of its rows, whose sums are joined at the end.
 //
-// Warps: 0 copies tiles with TMA (keys and values alternate in one ring of
-// buffers, query tiles in one of two), 1 issues the matrix products, 4-7 and
-// 8-11 are the two tiles' softmax (a thread a row), 12-15 write a unit's output
+// Warps: 0 and 2 copy tiles with TMA (keys and values alternate in one ring of
+// buffers, query tiles in one of two), 1 issues the matrix products, 3 writes
+// zeros for tokens of no request, 4-7 and 8-11 are the two tiles' softmax (a thread a row), 12-15 write a unit's output
 // while the softmax of the next one runs.
 
 #include <cuda.h>
@@ -123,7 +123,7 @@ __device__ __forceinline__ void mbar_wait(uint64_t* b, uint32_t parity, Shared* 
     }
   }
 }
-// The same for what is in flight when the CTA gives up.
+// The same for the products in flight when the CTA gives up.
 __device__ __forceinline__ void mbar_drain(uint64_t* b, uint32_t parity) {
   const long long start = clock64();
   while (!mbar_try(b, parity) && clock64() - start < kWaitCycles) {
@@ -334,15 +334,22 @@ __device__ __forceinline__ uint32_t place_v(int j, int n) { return min(2 + 2 * j
 
 // ---- the warps ----
 
+// One warp copies the query tiles and the keys, another the values (a tile of
+// 16-token pages is 16 copies, and one warp issues them no faster than memory
+// delivers half of them). A lane has a page and a half of the elements.
 template <int HALVES>
-__device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, uint32_t q_smem, uint32_t ring) {
+__device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, uint32_t q_smem, uint32_t ring,
+                                           const bool values) {
   constexpr int S = stages(HALVES);
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31;
-  const int per = max(1, kTile / a.page_size);       // pages of a tile
-  const int rows = min(kTile, a.page_size);          // rows of a copy
+  const int rows = min(kTile, a.page_size), per = kTile / rows;  // of a copy, and pages of a tile
+  const int page_shift = __ffs(a.page_size) - 1;
+  const int mine = lane % per, half = lane / per;
+  const bool copies = half < HALVES;
   const uint32_t q_bytes = (uint32_t)a.tile_tokens * a.group * 128 * HALVES;
-  uint32_t at = 0, nq = 0;
+  const CUtensorMap* const map = values ? &a.v : &a.k;
+  uint32_t base = 0, nq = 0;
   Walk w;
   Item it;
   for (w.start(a); w.next(a, it);) {
@@ -350,60 +357,53 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, u
     // the keys that some query of the unit sees
     const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
     const int32_t* pages = a.pages + it.unit.req * a.pages_stride;
-    // lane i < per: page i of a tile, -1 where nobody sees a key of it
-    const auto page_of = [&](int tile) {
-      const int64_t key = (int64_t)tile * kTile + lane * rows;
-      int32_t page = -1;
-      if (lane < per && tile < it.te && key < hi && key + rows > lo) {
-        page = pages[key / a.page_size];
+    // the lane's page of a tile, -1 where nobody sees a key of it
+    const auto page_of = [&](int j) {
+      const int64_t key = (int64_t)(it.tb + j) * kTile + mine * rows;
+      return copies && j < n && key < hi && key + rows > lo ? pages[key >> page_shift] : INT32_MIN;
+    };
+    int32_t next = page_of(0);
+    for (int j = 0; j < n; ++j) {
+      int32_t page = next;
+      next = page_of(j + 1);
+      const uint32_t at = base + (values ? place_v(j, n) : place_k(j)), s = at % S;
+      if (at >= S) mbar_wait(&b.empty[s], (at / S - 1) & 1, sh, a.status);
+      if (stopped(sh)) break;
+      const bool held = page != INT32_MIN;
+      const unsigned who = __ballot_sync(kFull, held);
+      if (lane == 0) mbar_expect(&b.full[s], __popc(who) * rows * 128);
+      __syncwarp();
+      if (held) {
         if (page < 0 || page >= a.num_pages) {
           latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
           page = a.num_pages;  // outside the tensor map: zeros
         }
+        tma_4d(ring + (s * HALVES + half) * kHalf + mine * rows * 128, map, 64 * half,
+               a.page_size > kTile ? (it.tb + j) * kTile % a.page_size : 0, it.h, page, &b.full[s]);
       }
-      return page;
-    };
-    const auto copy = [&](const CUtensorMap* map, int tile, int32_t page) {
-      const uint32_t s = at % S, round = at / S;
-      if (round) mbar_wait(&b.empty[s], (round - 1) & 1, sh, a.status);
-      if (stopped(sh)) return;
-      const unsigned who = __ballot_sync(kFull, page >= 0);
-      if (lane == 0) mbar_expect(&b.full[s], __popc(who) * rows * 128 * HALVES);
-      __syncwarp();
-      if (page >= 0) {
-        const uint32_t dst = ring + s * HALVES * kHalf + lane * rows * 128;
-        const int32_t in = a.page_size > kTile ? tile * kTile % a.page_size : 0;
+      if (j == 0 && !values) {
+        for (int t = 0; t < (it.pair ? 2 : 1); ++t, ++nq) {
+          uint64_t* full = &b.q_full[nq & 1];
+          if (nq > 1) mbar_wait(&b.q_empty[nq & 1], (nq / 2 - 1) & 1, sh, a.status);
+          if (lane == 0 && !stopped(sh)) {
+            mbar_expect(full, q_bytes);
 #pragma unroll
-        for (int e = 0; e < HALVES; ++e) tma_4d(dst + e * kHalf, map, 64 * e, in, it.h, page, &b.full[s]);
+            for (int e = 0; e < HALVES; ++e)
+              tma_3d(q_smem + ((nq & 1) * HALVES + e) * kHalf, &a.q, 64 * e, it.h * a.group,
+                     it.unit.token + t * a.tile_tokens, full);
+          }
+          __syncwarp();
+        }
       }
-      ++at;
-    };
-    int32_t p0 = page_of(it.tb), p1 = page_of(it.tb + 1), p2;
-    copy(&a.k, it.tb, p0);
-    for (int t = 0; t < (it.pair ? 2 : 1); ++t, ++nq) {
-      uint64_t* full = &b.q_full[nq & 1];
-      if (nq > 1) mbar_wait(&b.q_empty[nq & 1], (nq / 2 - 1) & 1, sh, a.status);
-      if (lane == 0 && !stopped(sh)) {
-        mbar_expect(full, q_bytes);
-#pragma unroll
-        for (int e = 0; e < HALVES; ++e)
-          tma_3d(q_smem + ((nq & 1) * HALVES + e) * kHalf, &a.q, 64 * e, it.h * a.group,
-                 it.unit.token + t * a.tile_tokens, full);
-      }
-      __syncwarp();
     }
-    if (n > 1) copy(&a.k, it.tb + 1, p1);
-    for (int j = 0; j < n; ++j) {
-      p2 = page_of(it.tb + j + 2);
-      copy(&a.v, it.tb + j, p0);
-      if (j + 2 < n) copy(&a.k, it.tb + j + 2, p2);
-      p0 = p1, p1 = p2;
-    }
+    base += 2 * n;
     if (stopped(sh)) break;
   }
   if (stopped(sh)) {  // copies in flight must land before the CTA ends
-    for (uint32_t i = at > S ? at - S : 0; i < at; ++i) mbar_drain(&b.full[i % S], i / S & 1);
-    for (uint32_t i = nq > 2 ? nq - 2 : 0; i < nq; ++i) mbar_drain(&b.q_full[i & 1], i / 2 & 1);
+    // (which stages have one pending is another warp's to know: a pause that is
+    // a thousand times as long as any copy takes)
+    const long long start = clock64();
+    while (clock64() - start < kWaitCycles / 1024) __nanosleep(1000);
   }
 }
 
@@ -786,14 +786,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
     if (warp == 0) {
-      copy_tiles<HALVES>(a, sh, q_smem, ring);
+      copy_tiles<HALVES>(a, sh, q_smem, ring, false);
     } else if (warp == 1) {
       multiply<T, HALVES>(a, sh, q_smem, ring);
+    } else if (warp == 2) {
+      copy_tiles<HALVES>(a, sh, q_smem, ring, true);
     } else {
       // tokens of no request
       const int64_t first = a.plan->first, last = a.plan->last, none = first + a.n_tokens - last;
       const int64_t pieces = none * a.hq * (a.D / 8);
-      for (int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x - 64; i < pieces; i += (int64_t)gridDim.x * 64) {
+      for (int64_t i = (int64_t)blockIdx.x * 32 + threadIdx.x - 96; i < pieces; i += (int64_t)gridDim.x * 32) {
         const int64_t x = i / (a.D / 8), h = x % a.hq;
         int64_t t = x / a.hq;
         if (t >= first) t += last - first;
