@@ -820,62 +820,92 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   }
 }
 
-// A block for a share of the elements of a unit that starts in CTA blockIdx.x's
-// share and that others go on with. With top = max_i ref_i over the pieces,
-// out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i, in the order of
-// the pieces. The loads of kAtOnce pieces are in
-// flight at a time.
+// With top = max_i ref_i over the pieces, out = sum_i 2^(ref_i - top) O_i /
+// sum_i 2^(ref_i - top) l_i, in the order of the pieces. A thread has X quads of
+// a row's elements at a time; the loads of P pieces of each are in flight.
 constexpr int kJoinThreads = 128;
-constexpr int kJoinBlocks = 8;
+constexpr int kJoinBlocks = 16;  // of a unit
+template <typename T, int P, int X>
+__device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit, int h, int pieces) {
+  const int n_rows = unit.tokens * a.group, full_rows = a.tile_tokens * a.group;
+  constexpr int kStep = kJoinBlocks * kJoinThreads;
+  const int n = n_rows * (a.D / 4);
+  for (int x0 = blockIdx.y * kJoinThreads + threadIdx.x; x0 < n; x0 += X * kStep) {
+    float top[X], l[X];
+    float4 o[X];
+    int column[X], r[X];
+#pragma unroll
+    for (int j = 0; j < X; ++j) {
+      const int x = min(x0 + j * kStep, n - 1);
+      column[j] = x / n_rows;
+      r[j] = x - column[j] * n_rows;
+      top[j] = -INFINITY;
+      l[j] = 0.f;
+      o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int i0 = 0; i0 < pieces; i0 += P) {
+      float2 ml[X][P];
+      float4 p[X][P];
+#pragma unroll
+      for (int j = 0; j < X; ++j) {
+        const int tile = r[j] >= full_rows, row = r[j] - tile * full_rows;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          if (i0 + k >= pieces) continue;
+          const int64_t slot = 2 * ((int64_t)blockIdx.x + i0 + k) + (i0 + k == 0);
+          ml[j][k] = a.part_ml[slot * 2 * kTile + tile * kTile + row];
+          p[j][k] = reinterpret_cast<const float4*>(a.part)[part_at(a.D, slot, tile, column[j]) + row];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < X; ++j) {
+        float next = top[j];
+#pragma unroll
+        for (int k = 0; k < P; ++k)
+          if (i0 + k < pieces) next = fmaxf(next, ml[j][k].x);
+        if (next == -INFINITY) continue;  // no key so far
+        const float back = ex2(top[j] - next);
+        top[j] = next;
+        l[j] *= back;
+        o[j].x *= back, o[j].y *= back, o[j].z *= back, o[j].w *= back;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          if (i0 + k >= pieces) continue;
+          const float f = ex2(ml[j][k].x - next);
+          l[j] += f * ml[j][k].y;
+          o[j].x += f * p[j][k].x, o[j].y += f * p[j][k].y, o[j].z += f * p[j][k].z, o[j].w += f * p[j][k].w;
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < X; ++j) {
+      if (x0 + j * kStep >= n) continue;
+      const float inv = l[j] > 0.f ? 1.f / l[j] : l[j];  // (NaN stays)
+      const int64_t token = unit.token + r[j] / a.group;
+      const int head = h * a.group + r[j] % a.group;
+      *reinterpret_cast<uint2*>(static_cast<T*>(a.out.d_data) + token * a.out.token_stride +
+                                head * a.out.head_stride + 4 * column[j]) =
+          make_uint2(Type<T>::pack(o[j].x * inv, o[j].y * inv), Type<T>::pack(o[j].z * inv, o[j].w * inv));
+      if (a.lse && column[j] == 0)
+        a.lse[token * a.hq + head] = l[j] == 0.f ? -INFINITY : (top[j] + log2f(l[j])) * 0.6931471805599453f;
+    }
+  }
+}
+
+// kJoinBlocks blocks for the unit that starts in CTA blockIdx.x's share and that
+// others go on with.
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_constant__ AttentionArgs a) {
   pdl_enter();
   const KvShare s = a.shares[blockIdx.x];
-  if (s.u0 < 0) return;
+  if (s.u0 < 0 || s.n_last < 2) return;
   const KvUnit unit = a.units[s.u1];
-  const bool starts = s.u0 != s.u1 || s.h0 != s.h1 || s.t0 == unit.tb;
-  if (!starts || s.t1 == unit.te) return;
-  const int pieces = s.n_last, n_rows = unit.tokens * a.group, full_rows = a.tile_tokens * a.group;
-  constexpr int kAtOnce = 8;
-  for (int x = blockIdx.y * kJoinThreads + threadIdx.x; x < n_rows * (a.D / 4); x += kJoinBlocks * kJoinThreads) {
-    const int column = x / n_rows, r = x - column * n_rows;
-    const int tile = r >= full_rows, row = r - tile * full_rows;
-    float top = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = 0; i0 < pieces; i0 += kAtOnce) {
-      float2 ml[kAtOnce];
-      float4 p[kAtOnce];
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        const int i = min(i0 + k, pieces - 1);
-        const int64_t slot = i ? 2 * ((int64_t)blockIdx.x + i) : 2 * (int64_t)blockIdx.x + 1;
-        ml[k] = a.part_ml[slot * 2 * kTile + tile * kTile + row];
-        p[k] = reinterpret_cast<const float4*>(a.part)[part_at(a.D, slot, tile, column) + row];
-      }
-      float next = top;
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
-      if (next == -INFINITY) continue;  // no key so far
-      const float back = ex2(top - next);
-      top = next;
-      l *= back;
-      o.x *= back, o.y *= back, o.z *= back, o.w *= back;
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        const float f = i0 + k < pieces ? ex2(ml[k].x - top) : 0.f;
-        l += f * ml[k].y;
-        o.x += f * p[k].x, o.y += f * p[k].y, o.z += f * p[k].z, o.w += f * p[k].w;
-      }
-    }
-    const float inv = l > 0.f ? 1.f / l : l;  // (NaN stays)
-    const int64_t token = unit.token + r / a.group;
-    const int head = s.h1 * a.group + r % a.group;
-    *reinterpret_cast<uint2*>(static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride +
-                              4 * column) =
-        make_uint2(Type<T>::pack(o.x * inv, o.y * inv), Type<T>::pack(o.z * inv, o.w * inv));
-    if (a.lse && column == 0)
-      a.lse[token * a.hq + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
-  }
+  if (s.u0 == s.u1 && s.h0 == s.h1 && s.t0 != unit.tb) return;  // started before this share
+  // Chunks have two or three pieces of many rows, single tokens many of few.
+  if (s.n_last <= 2)
+    join<T, 2, 4>(a, unit, s.h1, 2);
+  else
+    join<T, 8, 1>(a, unit, s.h1, s.n_last);
 }
 
 constexpr size_t smem_bytes(int halves) { return (size_t)(2 + stages(halves)) * halves * kHalf + sizeof(Shared); }

@@ -30,10 +30,13 @@ constexpr unsigned kFull = 0xffffffffu;
 constexpr int kPlanThreads = 1024;
 constexpr int kMaxCtas = 1024;  // attention CTAs that a plan shares work out to
 
-// A unit's cost is its key tiles and kUnitCost for what it does once (its
-// queries' load, the first scores, its output). A CTA takes at least kUnitCost
-// + kMinTiles, and a unit is cut at least kMinTiles from its ends.
-constexpr int kUnitCost = 2;
+// A unit's cost, in 1,000 cycles as measured: for each key tile, where it has
+// two query tiles or one, and for what it does once (its queries' load, the
+// first scores, its output). A CTA takes at least kMinCost, and a unit is cut
+// at least kMinTiles from its ends.
+__device__ __forceinline__ int tile_cost(const KvUnit& u, int tile_tokens) { return u.tokens > tile_tokens ? 3 : 2; }
+__device__ __forceinline__ int once_cost(const KvUnit& u, int tile_tokens) { return u.tokens > tile_tokens ? 6 : 4; }
+constexpr int kMinCost = 8;
 constexpr int kMinTiles = 2;
 
 struct PlanArgs {
@@ -127,7 +130,7 @@ __device__ void plan_units(const PlanArgs& a) {
       x.tb = x.pos >= a.window ? (x.pos - a.window + 1) / kTile : 0;
       x.te = (x.pos + x.tokens - 1) / kTile + 1;
       a.units[u] = x;
-      mine = x.te - x.tb + kUnitCost;
+      mine = (x.te - x.tb) * tile_cost(x, a.tile_tokens) + once_cost(x, a.tile_tokens);
     }
     int64_t total;
     const int64_t at = block_scan(mine, sums, total);
@@ -136,16 +139,17 @@ __device__ void plan_units(const PlanArgs& a) {
   }
   __syncthreads();
   cost *= a.kv_heads;
-  const int ctas = (int)max((int64_t)1, min((int64_t)a.ctas, cost / (kUnitCost + kMinTiles)));
+  const int ctas = (int)max((int64_t)1, min((int64_t)a.ctas, cost / kMinCost));
   for (int c = threadIdx.x; c <= ctas; c += kPlanThreads) {
     int32_t u = U, h = 0, t = 0;
     if (c < ctas && U > 0) {
       const int64_t x = cost / ctas * c + cost % ctas * c / ctas;
       u = last_at_most(a.unit_cost, U, x, a.kv_heads);
       const KvUnit unit = a.units[u];
-      const int64_t one = unit.te - unit.tb + kUnitCost, in = x - a.unit_cost[u] * a.kv_heads;
+      const int per_tile = tile_cost(unit, a.tile_tokens), once = once_cost(unit, a.tile_tokens);
+      const int64_t one = (int64_t)(unit.te - unit.tb) * per_tile + once, in = x - a.unit_cost[u] * a.kv_heads;
       h = (int32_t)(in / one);
-      t = unit.tb + (int32_t)max((int64_t)0, in % one - kUnitCost);
+      t = unit.tb + (int32_t)(max((int64_t)0, in % one - once) / per_tile);
       if (t - unit.tb < kMinTiles) {
         t = unit.tb;
       } else if (unit.te - t < kMinTiles) {
