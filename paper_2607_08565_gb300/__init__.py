@@ -215,7 +215,7 @@ def _ptr(x) -> Optional[int]:
 def _stream(s) -> Optional[int]:
     if s is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(s, int):
         return s
     return s.cuda_stream
@@ -775,6 +775,9 @@ class SMetricIndex:
             raise SmetricError(rc, "device")
 
 
+_NO_HEADS = smetric_heads()
+
+
 class SMetricKV:
     """The paged KV$ operators for one layout of heads and pages, with torch
     tensors. Caches are [num_pages, page_size, num_kv_heads, head_dim] views
@@ -800,6 +803,8 @@ class SMetricKV:
         self.handle = smetric_kv_create(self.cfg)
         self._n_tokens = None
         self._kept = None
+        self._dim, self._f32, self._i32 = head_dim, torch.float32, torch.int32
+        self._cache_shape = (num_pages, page_size, num_kv_heads, head_dim)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -820,34 +825,40 @@ class SMetricKV:
 
     def _heads(self, x, heads: int, n_tokens: int, name: str) -> smetric_heads:
         if x is None:
-            return smetric_heads()
-        if x.dtype != self.dtype or tuple(x.shape) != (n_tokens, heads, self.cfg.head_dim):
-            raise ValueError(f"{name} must be {self.dtype} [{n_tokens}, {heads}, {self.cfg.head_dim}]")
-        if x.numel() and x.stride(2) != 1:
+            return _NO_HEADS
+        if x.dtype != self.dtype or x.shape != (n_tokens, heads, self._dim):
+            raise ValueError(f"{name} must be {self.dtype} [{n_tokens}, {heads}, {self._dim}]")
+        token, head, one = x.stride()
+        if one != 1 and x.numel():
             raise ValueError(f"{name}: the elements of a head must be contiguous")
         # (the stride of a dimension of one is arbitrary)
-        return smetric_heads(x.data_ptr(), x.stride(0) if n_tokens > 1 else 0, x.stride(1) if heads > 1 else 0)
+        return smetric_heads(x.data_ptr(), token if n_tokens > 1 else 0, head if heads > 1 else 0)
 
     def _cache(self, k_cache, v_cache) -> smetric_kv_cache:
-        c = self.cfg
-        shape = (c.num_pages, c.page_size, c.num_kv_heads, c.head_dim)
-        for x in (k_cache, v_cache):
-            if x.dtype != self.dtype or tuple(x.shape) != shape:
-                raise ValueError(f"caches must be {self.dtype} {list(shape)}")
-        if k_cache.stride() != v_cache.stride() or k_cache.stride(3) != 1:
+        shape = self._cache_shape
+        if k_cache.dtype != self.dtype or v_cache.dtype != self.dtype or k_cache.shape != shape or v_cache.shape != shape:
+            raise ValueError(f"caches must be {self.dtype} {list(shape)}")
+        strides = k_cache.stride()
+        if v_cache.stride() != strides or strides[3] != 1:
             raise ValueError("caches must have equal strides and contiguous heads")
-        s = [st if n > 1 else 0 for st, n in zip(k_cache.stride(), shape)]
-        return smetric_kv_cache(k_cache.data_ptr(), v_cache.data_ptr(), s[0], s[1], s[2])
+        return smetric_kv_cache(k_cache.data_ptr(), v_cache.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1],
+                                strides[2] if shape[2] > 1 else 0)
+
+    def _norm(self, w) -> Optional[int]:
+        if w is None:
+            return None
+        if w.dtype != self.dtype or w.numel() != self._dim:
+            raise ValueError(f"norm weights must be {self.dtype} [{self._dim}]")
+        return _ptr(w)
 
     def _transform(self, cos_sin, interleaved, q_norm, k_norm, eps) -> smetric_kv_transform:
-        import torch
-        for w in (q_norm, k_norm):
-            if w is not None and (w.dtype != self.dtype or w.numel() != self.cfg.head_dim):
-                raise ValueError(f"norm weights must be {self.dtype} [{self.cfg.head_dim}]")
-        if cos_sin is not None and (cos_sin.dtype != torch.float32 or cos_sin.dim() != 2):
-            raise ValueError("cos_sin must be torch.float32 [positions, rot_dim]")
-        rows, rot = (0, 0) if cos_sin is None else cos_sin.shape
-        return smetric_kv_transform(_ptr(cos_sin), rows, _ptr(q_norm), _ptr(k_norm), eps, rot,
+        if cos_sin is None:
+            rows = rot = 0
+        else:
+            if cos_sin.dtype != self._f32 or cos_sin.dim() != 2:
+                raise ValueError("cos_sin must be torch.float32 [positions, rot_dim]")
+            rows, rot = cos_sin.shape
+        return smetric_kv_transform(_ptr(cos_sin), rows, self._norm(q_norm), self._norm(k_norm), eps, rot,
                                     SMETRIC_KV_INTERLEAVED if interleaved else 0, 0)
 
     def plan(self, offsets, kv_lens, pages, n_tokens: int, window: int = 0, stream=None):
@@ -877,47 +888,49 @@ class SMetricKV:
         """Appends the planned batch's keys (normed with k_norm, rotated with
         cos_sin where given) and values; with q, transforms the queries into
         q_out (a new tensor by default) and returns it."""
-        import torch
         t, c = self._planned(), self.cfg
-        if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        smetric_kv_append(self.handle, self._cache(k_cache, v_cache), self._heads(k, c.num_kv_heads, t, "k"),
-                          self._heads(v, c.num_kv_heads, t, "v"), self._heads(q, c.num_q_heads, t, "q"),
-                          self._heads(q_out if q is not None else None, c.num_q_heads, t, "q_out"),
+        if q is None:
+            q_out = None
+        elif q_out is None:
+            q_out = q.new_empty(q.shape)
+        hk, hq = c.num_kv_heads, c.num_q_heads
+        smetric_kv_append(self.handle, self._cache(k_cache, v_cache), self._heads(k, hk, t, "k"),
+                          self._heads(v, hk, t, "v"), self._heads(q, hq, t, "q"), self._heads(q_out, hq, t, "q_out"),
                           self._transform(cos_sin, interleaved, q_norm, k_norm, eps), stream)
-        return q_out if q is not None else None
+        return q_out
 
     def qk_norm_rope(self, q, k, positions, cos_sin=None, interleaved=False, q_norm=None, k_norm=None, eps=1e-6,
                      q_out=None, k_out=None, stream=None):
         """The norms and the rotation alone, at int32 positions; q or k may be
         None. Returns (q_out, k_out), new tensors unless given."""
-        import torch
         t, c = positions.numel(), self.cfg
-        if positions.dtype != torch.int32:
+        if positions.dtype != self._i32:
             raise ValueError("positions must be torch.int32")
-        if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if k is not None and k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        smetric_qk_norm_rope(self.handle, self._heads(q, c.num_q_heads, t, "q"),
-                             self._heads(k, c.num_kv_heads, t, "k"), positions, t,
+        if q is None:
+            q_out = None
+        elif q_out is None:
+            q_out = q.new_empty(q.shape)
+        if k is None:
+            k_out = None
+        elif k_out is None:
+            k_out = k.new_empty(k.shape)
+        hk, hq = c.num_kv_heads, c.num_q_heads
+        smetric_qk_norm_rope(self.handle, self._heads(q, hq, t, "q"), self._heads(k, hk, t, "k"), positions, t,
                              self._transform(cos_sin, interleaved, q_norm, k_norm, eps),
-                             self._heads(q_out if q is not None else None, c.num_q_heads, t, "q_out"),
-                             self._heads(k_out if k is not None else None, c.num_kv_heads, t, "k_out"), stream)
+                             self._heads(q_out, hq, t, "q_out"), self._heads(k_out, hk, t, "k_out"), stream)
         return q_out, k_out
 
     def paged_attention(self, q, k_cache, v_cache, scale=None, out=None, want_lse=False, stream=None):
         """Attention of the planned batch's queries over the cache; scale is
         head_dim ** -0.5 by default. Returns out, or (out, lse) with want_lse
         (float32 [tokens, num_q_heads])."""
-        import torch
-        t, c = self._planned(), self.cfg
+        t, hq = self._planned(), self.cfg.num_q_heads
         if out is None:
-            out = torch.empty((t, c.num_q_heads, c.head_dim), dtype=self.dtype, device=q.device)
-        lse = torch.empty((t, c.num_q_heads), dtype=torch.float32, device=q.device) if want_lse else None
-        smetric_paged_attention(self.handle, self._cache(k_cache, v_cache), self._heads(q, c.num_q_heads, t, "q"),
-                                c.head_dim ** -0.5 if scale is None else scale,
-                                self._heads(out, c.num_q_heads, t, "out"), lse, stream)
+            out = q.new_empty((t, hq, self._dim))
+        lse = q.new_empty((t, hq), dtype=self._f32) if want_lse else None
+        smetric_paged_attention(self.handle, self._cache(k_cache, v_cache), self._heads(q, hq, t, "q"),
+                                self._dim ** -0.5 if scale is None else scale, self._heads(out, hq, t, "out"), lse,
+                                stream)
         return (out, lse) if want_lse else out
 
     def status(self, stream=None) -> int:

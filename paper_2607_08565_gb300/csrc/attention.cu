@@ -338,7 +338,7 @@ __device__ __forceinline__ uint32_t place_v(int j, int n) { return min(2 + 2 * j
 // 16-token pages is 16 copies, and one warp issues them no faster than memory
 // delivers half of them). A lane has a page and a half of the elements.
 template <int HALVES>
-__device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, uint32_t q_smem, uint32_t ring,
+__device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, Walk w, uint32_t q_smem, uint32_t ring,
                                            const bool values) {
   constexpr int S = stages(HALVES);
   Barriers& b = sh->bar;
@@ -350,9 +350,8 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, u
   const uint32_t q_bytes = (uint32_t)a.tile_tokens * a.group * 128 * HALVES;
   const CUtensorMap* const map = values ? &a.v : &a.k;
   uint32_t base = 0, nq = 0;
-  Walk w;
   Item it;
-  for (w.start(a); w.next(a, it);) {
+  while (w.next(a, it)) {
     const int n = it.te - it.tb;
     // the keys that some query of the unit sees
     const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
@@ -408,7 +407,7 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, u
 }
 
 template <typename T, int HALVES>
-__device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uint32_t q_smem, uint32_t ring) {
+__device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Walk w, uint32_t q_smem, uint32_t ring) {
   constexpr int S = stages(HALVES);
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31;
@@ -420,9 +419,8 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, uin
   // (an operand's address is the descriptor's low bits, in units of 16 bytes)
   const uint32_t q_desc = desc_low(q_smem, 16), k_desc = desc_low(ring, 16), v_desc = desc_low(ring, kHalf);
   uint32_t base = 0, items = 0, nq = 0, np[2] = {0, 0};
-  Walk w;
   Item it;
-  for (w.start(a); w.next(a, it); ++items) {
+  for (; w.next(a, it); ++items) {
     const int n = it.te - it.tb;
     const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
     const auto stage = [&](uint32_t place) { return (base + place) % S; };
@@ -556,7 +554,7 @@ __device__ __forceinline__ int tile_rows(const AttentionArgs& a, const Item& it,
 
 // (One code for both tiles: two copies miss the instruction cache.)
 template <typename T>
-__device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, const int tile) {
+__device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk w, const int tile) {
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)warp << 21;  // the warp's TMEM lanes
@@ -564,9 +562,8 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, cons
   const int row_token = row / a.group;
   const float c = a.scale * 1.4426950408889634f;
   uint32_t ns = 0, items = 0;
-  Walk w;
   Item it;
-  for (w.start(a); w.next(a, it); ++items) {
+  for (; w.next(a, it); ++items) {
     const int n = it.te - it.tb;
     const int n_rows = tile_rows(a, it, tile);
     const bool mine = row < n_rows;
@@ -657,15 +654,14 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, cons
 // A unit's output: O / l, or its sums and statistics where other CTAs have
 // pieces of it.
 template <typename T>
-__device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh) {
+__device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Walk w) {
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
   const uint32_t o_all = sh->tmem + 2 * kTile + ((uint32_t)warp << 21);
   const int row_token = row / a.group, row_head = row - row_token * a.group;
   uint32_t items = 0, no[2] = {0, 0};
-  Walk w;
   Item it;
-  for (w.start(a); w.next(a, it); ++items) {
+  for (; w.next(a, it); ++items) {
     const bool two = !it.pair && it.te - it.tb > 1;  // sums of even and of odd key tiles
     for (int tile = 0; tile < (it.pair ? 2 : 1); ++tile) {
       const int n_rows = tile_rows(a, it, tile);
@@ -777,20 +773,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
+  pdl_enter();
+  Walk w;
+  w.start(a);  // (its loads run while the CTA is set up)
   fence_before();
   __syncthreads();
   fence_after();
-  pdl_enter();
   // Registers a thread: 4 warps of 80, 8 of 176 and 4 of 80 are what the CTA was
   // launched with, 16 of 128.
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
     if (warp == 0) {
-      copy_tiles<HALVES>(a, sh, q_smem, ring, false);
+      copy_tiles<HALVES>(a, sh, w, q_smem, ring, false);
     } else if (warp == 1) {
-      multiply<T, HALVES>(a, sh, q_smem, ring);
+      multiply<T, HALVES>(a, sh, w, q_smem, ring);
     } else if (warp == 2) {
-      copy_tiles<HALVES>(a, sh, q_smem, ring, true);
+      copy_tiles<HALVES>(a, sh, w, q_smem, ring, true);
     } else {
       // tokens of no request
       const int64_t first = a.plan->first, last = a.plan->last, none = first + a.n_tokens - last;
@@ -806,10 +804,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     }
   } else if (warp < 12) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 176;\n");
-    softmax<T>(a, sh, (warp >> 2) - 1);
+    softmax<T>(a, sh, w, (warp >> 2) - 1);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
-    write_out<T>(a, sh);
+    write_out<T>(a, sh, w);
   }
   __syncwarp();
   fence_before();
@@ -820,30 +818,41 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   }
 }
 
-// With top = max_i ref_i over the pieces, out = sum_i 2^(ref_i - top) O_i /
-// sum_i 2^(ref_i - top) l_i, in the order of the pieces. A thread has X quads of
-// a row's elements at a time; the loads of P pieces of each are in flight.
+// The pieces of four elements of a row, so far.
+struct Joined {
+  float top = -INFINITY, l = 0.f;  // largest reference exponent; sum of weights, to it
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void add(float ref, float weights, float4 p) {
+    const float next = fmaxf(top, ref);
+    if (next == -INFINITY) return;  // no key so far
+    const float f = ex2(top - next), g = ex2(ref - next);
+    top = next;
+    l = l * f + weights * g;
+    o.x = o.x * f + p.x * g, o.y = o.y * f + p.y * g, o.z = o.z * f + p.z * g, o.w = o.w * f + p.w * g;
+  }
+};
+
+// out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i over a unit's
+// pieces. G threads share four elements of a row, thread g taking pieces g, g +
+// G, ..., P of them in flight, and join in pairs; a thread has X such fours at a
+// time. So the order of the sums depends on the number of pieces alone.
 constexpr int kJoinThreads = 128;
 constexpr int kJoinBlocks = 16;  // of a unit
-template <typename T, int P, int X>
+template <typename T, int G, int P, int X>
 __device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit, int h, int pieces) {
   const int n_rows = unit.tokens * a.group, full_rows = a.tile_tokens * a.group;
-  constexpr int kStep = kJoinBlocks * kJoinThreads;
-  const int n = n_rows * (a.D / 4);
-  for (int x0 = blockIdx.y * kJoinThreads + threadIdx.x; x0 < n; x0 += X * kStep) {
-    float top[X], l[X];
-    float4 o[X];
+  constexpr int kStep = kJoinBlocks * kJoinThreads / G;
+  const int n = n_rows * (a.D / 4), g = threadIdx.x % G;
+  for (int x0 = blockIdx.y * (kJoinThreads / G) + threadIdx.x / G; x0 - (threadIdx.x % 32) / G < n; x0 += X * kStep) {
+    Joined sum[X];
     int column[X], r[X];
 #pragma unroll
     for (int j = 0; j < X; ++j) {
       const int x = min(x0 + j * kStep, n - 1);
       column[j] = x / n_rows;
       r[j] = x - column[j] * n_rows;
-      top[j] = -INFINITY;
-      l[j] = 0.f;
-      o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    for (int i0 = 0; i0 < pieces; i0 += P) {
+    for (int i0 = g; i0 < pieces; i0 += P * G) {
       float2 ml[X][P];
       float4 p[X][P];
 #pragma unroll
@@ -851,43 +860,49 @@ __device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit,
         const int tile = r[j] >= full_rows, row = r[j] - tile * full_rows;
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          if (i0 + k >= pieces) continue;
-          const int64_t slot = 2 * ((int64_t)blockIdx.x + i0 + k) + (i0 + k == 0);
+          const int i = i0 + k * G;
+          if (i >= pieces) continue;
+          const int64_t slot = 2 * ((int64_t)blockIdx.x + i) + (i == 0);
           ml[j][k] = a.part_ml[slot * 2 * kTile + tile * kTile + row];
           p[j][k] = reinterpret_cast<const float4*>(a.part)[part_at(a.D, slot, tile, column[j]) + row];
         }
       }
 #pragma unroll
-      for (int j = 0; j < X; ++j) {
-        float next = top[j];
+      for (int j = 0; j < X; ++j)
 #pragma unroll
         for (int k = 0; k < P; ++k)
-          if (i0 + k < pieces) next = fmaxf(next, ml[j][k].x);
-        if (next == -INFINITY) continue;  // no key so far
-        const float back = ex2(top[j] - next);
-        top[j] = next;
-        l[j] *= back;
-        o[j].x *= back, o[j].y *= back, o[j].z *= back, o[j].w *= back;
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-          if (i0 + k >= pieces) continue;
-          const float f = ex2(ml[j][k].x - next);
-          l[j] += f * ml[j][k].y;
-          o[j].x += f * p[j][k].x, o[j].y += f * p[j][k].y, o[j].z += f * p[j][k].z, o[j].w += f * p[j][k].w;
-        }
-      }
+          if (i0 + k * G < pieces) sum[j].add(ml[j][k].x, ml[j][k].y, p[j][k]);
     }
 #pragma unroll
     for (int j = 0; j < X; ++j) {
-      if (x0 + j * kStep >= n) continue;
-      const float inv = l[j] > 0.f ? 1.f / l[j] : l[j];  // (NaN stays)
+      Joined& s = sum[j];
+#pragma unroll
+      for (int o = 1; o < G; o <<= 1) {
+        // (both lanes of a pair add the lower one's sums first)
+        const bool low = !(g & o);
+        Joined t;
+        t.top = __shfl_xor_sync(kFull, s.top, o);
+        t.l = __shfl_xor_sync(kFull, s.l, o);
+        t.o.x = __shfl_xor_sync(kFull, s.o.x, o);
+        t.o.y = __shfl_xor_sync(kFull, s.o.y, o);
+        t.o.z = __shfl_xor_sync(kFull, s.o.z, o);
+        t.o.w = __shfl_xor_sync(kFull, s.o.w, o);
+        if (low) {
+          s.add(t.top, t.l, t.o);
+        } else {
+          t.add(s.top, s.l, s.o);
+          s = t;
+        }
+      }
+      if (x0 + j * kStep >= n || g) continue;
+      const float inv = s.l > 0.f ? 1.f / s.l : s.l;  // (NaN stays)
       const int64_t token = unit.token + r[j] / a.group;
       const int head = h * a.group + r[j] % a.group;
       *reinterpret_cast<uint2*>(static_cast<T*>(a.out.d_data) + token * a.out.token_stride +
                                 head * a.out.head_stride + 4 * column[j]) =
-          make_uint2(Type<T>::pack(o[j].x * inv, o[j].y * inv), Type<T>::pack(o[j].z * inv, o[j].w * inv));
+          make_uint2(Type<T>::pack(s.o.x * inv, s.o.y * inv), Type<T>::pack(s.o.z * inv, s.o.w * inv));
       if (a.lse && column[j] == 0)
-        a.lse[token * a.hq + head] = l[j] == 0.f ? -INFINITY : (top[j] + log2f(l[j])) * 0.6931471805599453f;
+        a.lse[token * a.hq + head] = s.l == 0.f ? -INFINITY : (s.top + log2f(s.l)) * 0.6931471805599453f;
     }
   }
 }
@@ -899,13 +914,13 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
   pdl_enter();
   const KvShare s = a.shares[blockIdx.x];
   if (s.u0 < 0 || s.n_last < 2) return;
-  const KvUnit unit = a.units[s.u1];
+  const KvUnit unit = s.last;
   if (s.u0 == s.u1 && s.h0 == s.h1 && s.t0 != unit.tb) return;  // started before this share
   // Chunks have two or three pieces of many rows, single tokens many of few.
-  if (s.n_last <= 2)
-    join<T, 2, 4>(a, unit, s.h1, 2);
+  if (s.n_last <= 4)
+    join<T, 1, 2, 4>(a, unit, s.h1, s.n_last);
   else
-    join<T, 8, 1>(a, unit, s.h1, s.n_last);
+    join<T, 8, 5, 1>(a, unit, s.h1, s.n_last);
 }
 
 constexpr size_t smem_bytes(int halves) { return (size_t)(2 + stages(halves)) * halves * kHalf + sizeof(Shared); }

@@ -175,6 +175,7 @@ __device__ void plan_units(const PlanArgs& a) {
       const auto same = [&](int i, int32_t u, int32_t h) {
         return i <= ctas && su[i] == u && sh[i] == h && u < U && st[i] > a.units[u].tb;
       };
+      s.last = a.units[s.u1];
       s.n_last = 1;
       while (same(c + s.n_last, s.u1, s.h1)) ++s.n_last;
     }

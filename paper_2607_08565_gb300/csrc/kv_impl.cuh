@@ -47,7 +47,7 @@ struct __align__(16) KvShare {
   int32_t u1, h1, t1;
   int32_t n_last;      // pieces of the last unit, where the share starts it
   int32_t reserved;
-  KvUnit first;        // unit u0
+  KvUnit first, last;  // units u0 and u1
 };
 
 }  // namespace smetric
