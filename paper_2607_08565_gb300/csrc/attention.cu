@@ -552,6 +552,9 @@ __device__ __forceinline__ int tile_rows(const AttentionArgs& a, const Item& it,
   return min(a.tile_tokens, it.unit.tokens - tile_token(a, it, tile)) * a.group;
 }
 
+// The lowest n bits, none or all where n is outside 0..32.
+__device__ __forceinline__ uint32_t below(int32_t n) { return n <= 0 ? 0 : n >= 32 ? kFull : (1u << n) - 1; }
+
 // (One code for both tiles: two copies miss the instruction cache.)
 template <typename T>
 __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk w, const int tile) {
@@ -567,7 +570,7 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
     const int n = it.te - it.tb;
     const int n_rows = tile_rows(a, it, tile);
     const bool mine = row < n_rows;
-    const int32_t hi = mine ? it.unit.pos + tile_token(a, it, tile) + row_token : INT32_MAX;  // last key that the row sees
+    const int32_t hi = mine ? it.unit.pos + tile_token(a, it, tile) + row_token : INT32_MAX / 2;  // last key that the row sees
     const int32_t lo = mine && hi >= a.window ? hi - a.window + 1 : 0;                        // first key
     const bool busy = 32 * warp < n_rows;
     float top = -INFINITY;  // largest score when the reference was last moved
@@ -591,8 +594,11 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
       const int32_t key = (it.tb + j) * kTile;
       if (__any_sync(kFull, key + kTile - 1 > hi || key < lo)) {
 #pragma unroll
-        for (int i = 0; i < kTile; ++i)
-          if (key + i > hi || key + i < lo) s[i] = -INFINITY;
+        for (int i = 0; i < kTile; i += 32) {  // a bit a column
+          const uint32_t seen = below(hi + 1 - (key + i)) & ~below(lo - (key + i));
+#pragma unroll
+          for (int k = 0; k < 32; ++k) s[i + k] = seen & 1u << k ? s[i + k] : -INFINITY;
+        }
       }
       float m[8];
 #pragma unroll
