@@ -279,20 +279,140 @@ struct HeadsArgs {
   int32_t* status;
 };
 
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  float2 r;
+  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+      " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y), "f"(z.x), "f"(z.y));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+  float2 r;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 d, a, b;\n"
+      " mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+  return r;
+}
+
+// A lane's part of the transform: 16 elements in two pieces of 8.
+struct Lane {
+  bool held, turned;  // it has elements of a head; they are rotated
+  int e0, e1;         // the pieces' first elements
+  int lanes_shift, D;
+  float eps;
+  float2 cs[4], sn[4];  // of its 8 pairs
+};
+
+// A lane's two pieces of head h of a token (src is at that head).
+template <typename T>
+__device__ __forceinline__ void load_head(const Lane& l, const T* src, int h, int heads, uint4 (&x)[2]) {
+  if (l.held && h < heads) {
+    x[0] = *reinterpret_cast<const uint4*>(src + l.e0);
+    x[1] = *reinterpret_cast<const uint4*>(src + l.e1);
+  }
+}
+
+// heads h, h + step, ... < heads of a token, from src to dst (both at head h);
+// x: the first of them. (A round's heads are loaded while the round before is
+// computed.)
+template <typename T, bool kInterleaved>
+__device__ __forceinline__ void transform_heads(const Lane& l, const T* src, int64_t src_step, T* dst, int64_t dst_step,
+                                                int h, int step, int heads, int rounds, const T* norm, uint4 (&x)[2]) {
+  for (int r = 0; r < rounds; ++r, h += step, dst += dst_step) {
+    const bool on = l.held && h < heads;
+    const uint4 y[2] = {x[0], x[1]};
+    src += src_step;
+    load_head(l, src, h + step, heads, x);
+    if (!norm && !l.turned) {  // (nothing changes: its bits are kept, a NaN's among them)
+      if (on) {
+        *reinterpret_cast<uint4*>(dst + l.e0) = y[0];
+        *reinterpret_cast<uint4*>(dst + l.e1) = y[1];
+      }
+      continue;
+    }
+    float2 f[8];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) unpack<T>(y[e], &f[4 * e].x);
+    if (norm) {  // (the same for the warp: its lanes take part in the sum)
+      float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s2 = fma2(f[k], f[k], s2);
+      float ss = on ? s2.x + s2.y : 0.f;
+      for (int o = 1; o < 1 << l.lanes_shift; o <<= 1) ss += __shfl_xor_sync(kFull, ss, o);
+      if (on) {
+        const float inv = 1.0f / sqrtf(ss / (float)l.D + l.eps);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float2 g[4];
+          unpack<T>(*reinterpret_cast<const uint4*>(norm + (e ? l.e1 : l.e0)), &g[0].x);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) f[4 * e + k] = mul2(mul2(f[4 * e + k], make_float2(inv, inv)), g[k]);
+        }
+      }
+    }
+    if (l.turned) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (kInterleaved) {  // pairs 2k and 2k + 1, as (a, b) each
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float c = i ? l.cs[k].y : l.cs[k].x, s = i ? l.sn[k].y : l.sn[k].x;
+            const float2 u = f[2 * k + i];
+            f[2 * k + i] = make_float2(u.x * c - u.y * s, u.y * c + u.x * s);
+          }
+        } else {
+          const float2 u = f[k], v = f[4 + k];
+          f[k] = fma2(u, l.cs[k], mul2(v, make_float2(-l.sn[k].x, -l.sn[k].y)));
+          f[4 + k] = fma2(v, l.cs[k], mul2(u, l.sn[k]));
+        }
+      }
+    }
+    if (on) {
+      *reinterpret_cast<uint4*>(dst + l.e0) = pack<T>(&f[0].x);
+      *reinterpret_cast<uint4*>(dst + l.e1) = pack<T>(&f[4].x);
+    }
+  }
+}
+
 // A warp takes a token (or one of `splits` shares of its heads) and a group of
 // 2^lanes_shift lanes a head at a time, 16 elements a lane in two 16-byte
 // pieces: the two halves of 8 rotation pairs (i, i + rot/2), 8 interleaved
 // pairs, or 16 elements past rot. So a rotation never leaves the lane, a norm
 // is a sum over the group's lanes, and the token's cosines and sines are
-// loaded once for all its heads.
+// loaded once for all its heads. Bound by memory; the registers of 24 warps an
+// SM hold the bytes in flight.
 template <typename T, bool kInterleaved>
-__global__ void __launch_bounds__(256) k_kv_heads(const __grid_constant__ HeadsArgs a) {
+__global__ void __launch_bounds__(256, 3) k_kv_heads(const __grid_constant__ HeadsArgs a) {
   pdl_enter();
   const int lane = threadIdx.x & 31;
   const int64_t w = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int64_t t = w / a.splits;
   const int share = (int)(w - t * a.splits);
   if (t >= a.n_tokens) return;
+  Lane l;
+  const int c = lane & ((1 << a.lanes_shift) - 1);
+  l.held = 16 * c < a.D;  // (groups of 8 lanes hold heads of 96 elements)
+  l.turned = l.held && a.table && 16 * c < a.rot;
+  l.e0 = l.turned && !kInterleaved ? 8 * c : 16 * c;
+  l.e1 = l.turned && !kInterleaved ? 8 * c + a.rot / 2 : 16 * c + 8;
+  l.lanes_shift = a.lanes_shift;
+  l.D = a.D;
+  l.eps = a.eps;
+  const int per = 32 >> a.lanes_shift;  // heads a warp takes at a time
+  const int step = per * a.splits, first = lane >> a.lanes_shift;
+  // rounds of heads: the keys', then the values', then the queries'; the share
+  // has every splits-th, from rounds k0, v0, q0 of each
+  const int rk = (a.hk + per - 1) / per, rv = (a.hv + per - 1) / per, rq = (a.hq + per - 1) / per;
+  const auto start = [&](int before) { return (share - before % a.splits + a.splits) % a.splits; };
+  const int k0 = share, v0 = start(rk), q0 = start(rk + rv);
+  const auto source = [&](const smetric_heads& src, int r) {
+    return static_cast<const T*>(src.d_data) + t * src.token_stride + (r * per + first) * src.head_stride;
+  };
+  // (the first loads run while the token's place is found)
+  uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)}, y[2] = {x[0], x[1]};
+  if (v0 < rv) load_head(l, source(a.v, v0), v0 * per + first, a.hv, y);
+  if (k0 < rk) load_head(l, source(a.k, k0), k0 * per + first, a.hk, x);
   int64_t slot = 0;
   int32_t pos;
   if (a.tokens) {
@@ -307,85 +427,35 @@ __global__ void __launch_bounds__(256) k_kv_heads(const __grid_constant__ HeadsA
     if (lane == 0 && share == 0) latch_error(a.status, SMETRIC_ERR_OVERFLOW);
     return;
   }
-  const int c = lane & ((1 << a.lanes_shift) - 1);
-  const bool held = 16 * c < a.D;  // (groups of 8 lanes hold heads of 96 elements)
-  const bool turned = held && a.table && 16 * c < a.rot;
-  const int e0 = turned && !kInterleaved ? 8 * c : 16 * c;
-  const int e1 = turned && !kInterleaved ? 8 * c + a.rot / 2 : 16 * c + 8;
-  float cs[8], sn[8];
+  const bool turned = l.turned;
   if (turned) {
     const float4* row = reinterpret_cast<const float4*>(a.table + (int64_t)pos * a.rot + 8 * c);
     const float4* row2 = reinterpret_cast<const float4*>(a.table + (int64_t)pos * a.rot + a.rot / 2 + 8 * c);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float4 x = row[i], y = row2[i];
-      cs[4 * i] = x.x, cs[4 * i + 1] = x.y, cs[4 * i + 2] = x.z, cs[4 * i + 3] = x.w;
-      sn[4 * i] = y.x, sn[4 * i + 1] = y.y, sn[4 * i + 2] = y.z, sn[4 * i + 3] = y.w;
+      const float4 u = row[i], v = row2[i];
+      l.cs[2 * i] = make_float2(u.x, u.y), l.cs[2 * i + 1] = make_float2(u.z, u.w);
+      l.sn[2 * i] = make_float2(v.x, v.y), l.sn[2 * i + 1] = make_float2(v.z, v.w);
     }
   }
-  const int per = 32 >> a.lanes_shift;  // heads a warp takes at a time
-  const int total = a.hk + a.hv + a.hq;
-  const int64_t page = slot >> a.page_shift, place = slot & ((1 << a.page_shift) - 1);
-  const int64_t at = page * a.cache.page_stride + place * a.cache.token_stride;
-  for (int base = share * per; base < total; base += a.splits * per) {
-    const int h = base + (lane >> a.lanes_shift);
-    const bool on = held && h < total;
-    const bool is_k = h < a.hk, is_v = !is_k && h < a.hk + a.hv;
-    const T* src;
-    T* dst;
-    const T* norm = nullptr;
-    if (is_k) {
-      src = static_cast<const T*>(a.k.d_data) + t * a.k.token_stride + h * a.k.head_stride;
-      dst = a.tokens ? static_cast<T*>(a.cache.d_k) + at + h * a.cache.head_stride
-                     : static_cast<T*>(a.k_out.d_data) + t * a.k_out.token_stride + h * a.k_out.head_stride;
-      norm = static_cast<const T*>(a.k_norm);
-    } else if (is_v) {
-      src = static_cast<const T*>(a.v.d_data) + t * a.v.token_stride + (h - a.hk) * a.v.head_stride;
-      dst = static_cast<T*>(a.cache.d_v) + at + (h - a.hk) * a.cache.head_stride;
-    } else {
-      const int g = h - a.hk - a.hv;
-      src = static_cast<const T*>(a.q.d_data) + t * a.q.token_stride + g * a.q.head_stride;
-      dst = static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride + g * a.q_out.head_stride;
-      norm = static_cast<const T*>(a.q_norm);
-    }
-    uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
-    if (on) {
-      x0 = *reinterpret_cast<const uint4*>(src + e0);
-      x1 = *reinterpret_cast<const uint4*>(src + e1);
-    }
-    float f[16];
-    unpack<T>(x0, f);
-    unpack<T>(x1, f + 8);
-    if (a.q_norm || a.k_norm) {  // (the same for the warp: its lanes take part in the sum)
-      float ss = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) ss = fmaf(f[i], f[i], ss);
-      for (int o = 1; o < 1 << a.lanes_shift; o <<= 1) ss += __shfl_xor_sync(kFull, ss, o);
-      if (on && norm) {
-        const float inv = 1.0f / sqrtf(ss / (float)a.D + a.eps);
-        float g[16];
-        unpack<T>(*reinterpret_cast<const uint4*>(norm + e0), g);
-        unpack<T>(*reinterpret_cast<const uint4*>(norm + e1), g + 8);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) f[i] = f[i] * inv * g[i];
-      }
-    }
-    if (turned && !is_v) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int p = kInterleaved ? 2 * i : i, q = kInterleaved ? 2 * i + 1 : 8 + i;
-        const float u = f[p], v = f[q];
-        f[p] = u * cs[i] - v * sn[i];
-        f[q] = v * cs[i] + u * sn[i];
-      }
-    }
-    if (on) {
-      // (heads that nothing changes keep their bits, NaN payloads among them)
-      const bool same = is_v || (!norm && !turned);
-      *reinterpret_cast<uint4*>(dst + e0) = same ? x0 : pack<T>(f);
-      *reinterpret_cast<uint4*>(dst + e1) = same ? x1 : pack<T>(f + 8);
-    }
-  }
+  const auto heads = [&](const smetric_heads& src, T* dst, int64_t head_stride, int r, int rounds, int n_heads,
+                         const void* norm, uint4(&z)[2]) {
+    if (r < rounds)
+      transform_heads<T, kInterleaved>(l, source(src, r), step * src.head_stride,
+                                       dst + (r * per + first) * head_stride, step * head_stride, r * per + first, step,
+                                       n_heads, (rounds - r + a.splits - 1) / a.splits, static_cast<const T*>(norm), z);
+  };
+  const int64_t at = (slot >> a.page_shift) * a.cache.page_stride +
+                     (slot & ((1 << a.page_shift) - 1)) * a.cache.token_stride;
+  l.turned = false;
+  heads(a.v, static_cast<T*>(a.cache.d_v) + at, a.cache.head_stride, v0, rv, a.hv, nullptr, y);
+  l.turned = turned;
+  if (q0 < rq) load_head(l, source(a.q, q0), q0 * per + first, a.hq, y);
+  if (a.tokens)
+    heads(a.k, static_cast<T*>(a.cache.d_k) + at, a.cache.head_stride, k0, rk, a.hk, a.k_norm, x);
+  else
+    heads(a.k, static_cast<T*>(a.k_out.d_data) + t * a.k_out.token_stride, a.k_out.head_stride, k0, rk, a.hk, a.k_norm, x);
+  heads(a.q, static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride, a.q_out.head_stride, q0, rq, a.hq, a.q_norm, y);
 }
 
 bool transform_ok(const smetric_kv* kv, const smetric_kv_transform& t) {
@@ -410,9 +480,9 @@ int launch_heads(smetric_kv* kv, HeadsArgs& a, const smetric_kv_transform& t, cu
   a.lanes_shift = 0;
   while (16 << a.lanes_shift < a.D) a.lanes_shift++;
   // Warps that share a token's heads: as many as it has rounds of heads while
-  // there are too few tokens to fill the SMs (64 warps an SM), else one.
+  // there are too few tokens to fill the SMs (24 warps an SM), else one.
   const int rounds = (a.hq + a.hk + a.hv + (32 >> a.lanes_shift) - 1) / (32 >> a.lanes_shift);
-  const int64_t room = (int64_t)kv->num_sms * 64 / std::max<int64_t>(1, a.n_tokens);
+  const int64_t room = (int64_t)kv->num_sms * 24 / std::max<int64_t>(1, a.n_tokens);
   a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, room));
   const int64_t grid = (a.n_tokens * a.splits + 7) / 8;
   const bool il = t.flags & SMETRIC_KV_INTERLEAVED;
