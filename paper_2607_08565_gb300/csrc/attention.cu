@@ -245,11 +245,6 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
   return r;
 }
 
-__device__ __forceinline__ void st_global32(void* p, const uint32_t* r) {  // 32-byte aligned
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
-               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
-}
-
 template <typename T>
 struct Type;
 template <>
@@ -544,6 +539,17 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Wal
   }
 }
 
+// 16 elements of an output.
+__device__ __forceinline__ void store16(const AttentionArgs& a, void* p, const uint32_t* r) {
+  if (a.wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+  } else {
+    static_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+  }
+}
+
 // A tile's first token in its unit, and its rows.
 __device__ __forceinline__ int tile_token(const AttentionArgs& a, const Item& it, int tile) {
   return it.pair ? tile * a.tile_tokens : 0;
@@ -713,12 +719,7 @@ __device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Wa
               uint32_t y[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
-              if (a.wide) {
-                st_global32(out + d, y);
-              } else {
-                *reinterpret_cast<uint4*>(out + d) = make_uint4(y[0], y[1], y[2], y[3]);
-                *reinterpret_cast<uint4*>(out + d + 8) = make_uint4(y[4], y[5], y[6], y[7]);
-              }
+              store16(a, out + d, y);
             } else {
               float4* p = reinterpret_cast<float4*>(a.part) + part_at(a.D, it.slot, tile, d / 4) + row;
 #pragma unroll
@@ -824,92 +825,89 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   }
 }
 
-// The pieces of four elements of a row, so far.
+// The pieces of 16 elements of a row, so far.
 struct Joined {
   float top = -INFINITY, l = 0.f;  // largest reference exponent; sum of weights, to it
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  __device__ __forceinline__ void add(float ref, float weights, float4 p) {
+  float4 o[4] = {};
+  __device__ __forceinline__ void add(float ref, float weights, const float4 (&p)[4]) {
     const float next = fmaxf(top, ref);
     if (next == -INFINITY) return;  // no key so far
     const float f = ex2(top - next), g = ex2(ref - next);
     top = next;
     l = l * f + weights * g;
-    o.x = o.x * f + p.x * g, o.y = o.y * f + p.y * g, o.z = o.z * f + p.z * g, o.w = o.w * f + p.w * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[i].x = o[i].x * f + p[i].x * g, o[i].y = o[i].y * f + p[i].y * g;
+      o[i].z = o[i].z * f + p[i].z * g, o[i].w = o[i].w * f + p[i].w * g;
+    }
   }
 };
 
 // out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i over a unit's
-// pieces. G threads share four elements of a row, thread g taking pieces g, g +
-// G, ..., P of them in flight, and join in pairs; a thread has X such fours at a
-// time. So the order of the sums depends on the number of pieces alone.
+// pieces. G threads share 16 elements of a row (a whole sector of the output),
+// thread g taking pieces g, g + G, ..., two of them in flight, and join in
+// pairs: the order of the sums depends on the number of pieces alone.
 constexpr int kJoinThreads = 128;
 constexpr int kJoinBlocks = 16;  // of a unit
-template <typename T, int G, int P, int X>
+template <typename T, int G>
 __device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit, int h, int pieces) {
   const int n_rows = unit.tokens * a.group, full_rows = a.tile_tokens * a.group;
-  constexpr int kStep = kJoinBlocks * kJoinThreads / G;
-  const int n = n_rows * (a.D / 4), g = threadIdx.x % G;
-  for (int x0 = blockIdx.y * (kJoinThreads / G) + threadIdx.x / G; x0 - (threadIdx.x % 32) / G < n; x0 += X * kStep) {
-    Joined sum[X];
-    int column[X], r[X];
-#pragma unroll
-    for (int j = 0; j < X; ++j) {
-      const int x = min(x0 + j * kStep, n - 1);
-      column[j] = x / n_rows;
-      r[j] = x - column[j] * n_rows;
-    }
+  constexpr int kStep = kJoinBlocks * kJoinThreads / G, P = 2;
+  const int n = n_rows * (a.D / 16), g = threadIdx.x % G;
+  for (int x = blockIdx.y * (kJoinThreads / G) + threadIdx.x / G; x - (int)(threadIdx.x % 32) / G < n; x += kStep) {
+    const int column = min(x, n - 1) / n_rows, r = min(x, n - 1) - column * n_rows;
+    const int tile = r >= full_rows, row = r - tile * full_rows;
+    Joined s;
     for (int i0 = g; i0 < pieces; i0 += P * G) {
-      float2 ml[X][P];
-      float4 p[X][P];
+      float2 ml[P];
+      float4 p[P][4];
 #pragma unroll
-      for (int j = 0; j < X; ++j) {
-        const int tile = r[j] >= full_rows, row = r[j] - tile * full_rows;
+      for (int k = 0; k < P; ++k) {
+        const int i = i0 + k * G;
+        if (i >= pieces) continue;
+        const int64_t slot = 2 * ((int64_t)blockIdx.x + i) + (i == 0);
+        ml[k] = a.part_ml[slot * 2 * kTile + tile * kTile + row];
+        const float4* from = reinterpret_cast<const float4*>(a.part) + part_at(a.D, slot, tile, 4 * column) + row;
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-          const int i = i0 + k * G;
-          if (i >= pieces) continue;
-          const int64_t slot = 2 * ((int64_t)blockIdx.x + i) + (i == 0);
-          ml[j][k] = a.part_ml[slot * 2 * kTile + tile * kTile + row];
-          p[j][k] = reinterpret_cast<const float4*>(a.part)[part_at(a.D, slot, tile, column[j]) + row];
-        }
+        for (int q = 0; q < 4; ++q) p[k][q] = from[q * kTile];
       }
 #pragma unroll
-      for (int j = 0; j < X; ++j)
-#pragma unroll
-        for (int k = 0; k < P; ++k)
-          if (i0 + k * G < pieces) sum[j].add(ml[j][k].x, ml[j][k].y, p[j][k]);
+      for (int k = 0; k < P; ++k)
+        if (i0 + k * G < pieces) s.add(ml[k].x, ml[k].y, p[k]);
     }
 #pragma unroll
-    for (int j = 0; j < X; ++j) {
-      Joined& s = sum[j];
+    for (int o = 1; o < G; o <<= 1) {
+      // (both lanes of a pair add the lower one's sums first)
+      Joined t;
+      t.top = __shfl_xor_sync(kFull, s.top, o);
+      t.l = __shfl_xor_sync(kFull, s.l, o);
 #pragma unroll
-      for (int o = 1; o < G; o <<= 1) {
-        // (both lanes of a pair add the lower one's sums first)
-        const bool low = !(g & o);
-        Joined t;
-        t.top = __shfl_xor_sync(kFull, s.top, o);
-        t.l = __shfl_xor_sync(kFull, s.l, o);
-        t.o.x = __shfl_xor_sync(kFull, s.o.x, o);
-        t.o.y = __shfl_xor_sync(kFull, s.o.y, o);
-        t.o.z = __shfl_xor_sync(kFull, s.o.z, o);
-        t.o.w = __shfl_xor_sync(kFull, s.o.w, o);
-        if (low) {
-          s.add(t.top, t.l, t.o);
-        } else {
-          t.add(s.top, s.l, s.o);
-          s = t;
-        }
+      for (int q = 0; q < 4; ++q) {
+        t.o[q].x = __shfl_xor_sync(kFull, s.o[q].x, o);
+        t.o[q].y = __shfl_xor_sync(kFull, s.o[q].y, o);
+        t.o[q].z = __shfl_xor_sync(kFull, s.o[q].z, o);
+        t.o[q].w = __shfl_xor_sync(kFull, s.o[q].w, o);
       }
-      if (x0 + j * kStep >= n || g) continue;
-      const float inv = s.l > 0.f ? 1.f / s.l : s.l;  // (NaN stays)
-      const int64_t token = unit.token + r[j] / a.group;
-      const int head = h * a.group + r[j] % a.group;
-      *reinterpret_cast<uint2*>(static_cast<T*>(a.out.d_data) + token * a.out.token_stride +
-                                head * a.out.head_stride + 4 * column[j]) =
-          make_uint2(Type<T>::pack(s.o.x * inv, s.o.y * inv), Type<T>::pack(s.o.z * inv, s.o.w * inv));
-      if (a.lse && column[j] == 0)
-        a.lse[token * a.hq + head] = s.l == 0.f ? -INFINITY : (s.top + log2f(s.l)) * 0.6931471805599453f;
+      if (!(g & o)) {
+        s.add(t.top, t.l, t.o);
+      } else {
+        t.add(s.top, s.l, s.o);
+        s = t;
+      }
     }
+    if (x >= n || g) continue;
+    const float inv = s.l > 0.f ? 1.f / s.l : s.l;  // (NaN stays)
+    const int64_t token = unit.token + r / a.group;
+    const int head = h * a.group + r % a.group;
+    uint32_t y[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      y[2 * q] = Type<T>::pack(s.o[q].x * inv, s.o[q].y * inv);
+      y[2 * q + 1] = Type<T>::pack(s.o[q].z * inv, s.o[q].w * inv);
+    }
+    store16(a, static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride + 16 * column, y);
+    if (a.lse && column == 0)
+      a.lse[token * a.hq + head] = s.l == 0.f ? -INFINITY : (s.top + log2f(s.l)) * 0.6931471805599453f;
   }
 }
 
@@ -924,9 +922,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
   if (s.u0 == s.u1 && s.h0 == s.h1 && s.t0 != unit.tb) return;  // started before this share
   // Chunks have two or three pieces of many rows, single tokens many of few.
   if (s.n_last <= 4)
-    join<T, 1, 2, 4>(a, unit, s.h1, s.n_last);
+    join<T, 1>(a, unit, s.h1, s.n_last);
+  else if (s.n_last <= 16)
+    join<T, 8>(a, unit, s.h1, s.n_last);
   else
-    join<T, 8, 5, 1>(a, unit, s.h1, s.n_last);
+    join<T, 32>(a, unit, s.h1, s.n_last);
 }
 
 constexpr size_t smem_bytes(int halves) { return (size_t)(2 + stages(halves)) * halves * kHalf + sizeof(Shared); }
