@@ -781,6 +781,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
   pdl_enter();
+  // (the join's blocks find no room beside this CTA, but are ready when it ends)
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   Walk w;
   w.start(a);  // (its loads run while the CTA is set up)
   fence_before();
@@ -915,10 +917,10 @@ __device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit,
 // others go on with.
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_constant__ AttentionArgs a) {
-  pdl_enter();
-  const KvShare s = a.shares[blockIdx.x];
-  if (s.u0 < 0 || s.n_last < 2) return;
+  const KvShare s = a.shares[blockIdx.x];  // (the plan was done before the kernel that this one waits for)
   const KvUnit unit = s.last;
+  pdl_enter();
+  if (s.u0 < 0 || s.n_last < 2) return;
   if (s.u0 == s.u1 && s.h0 == s.h1 && s.t0 != unit.tb) return;  // started before this share
   // Chunks have two or three pieces of many rows, single tokens many of few.
   if (s.n_last <= 4)
