@@ -621,8 +621,9 @@ typedef struct {
 } smetric_kv_transform;
 
 /* Create a handle and its device memory on the current device: the plan (16
- * bytes a token, 48 a request) and the partial results of sequences that
- * several SMs share (2 * 256 * (head_dim + 2) floats an SM).
+ * bytes a token, and 40 for every 2 * (128 / group) of them, group =
+ * num_q_heads / num_kv_heads; 44 bytes a request) and the partial results of
+ * sequences that several SMs share (4 * 128 * (head_dim + 2) floats an SM).
  * Errors as smetric_index_create. */
 int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out);
 
