@@ -509,6 +509,9 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Wal
         release(j);
       }
       if (n <= 2) release_q(nq);
+      // (waited for by every unit, so that no two have one parity, and before the
+      // product that lets the unit's own phase end)
+      if (n == 1 && items) mbar_wait(&b.o_free[1], (items - 1) & 1, sh, a.status);
       for (int j = 0; j < n; ++j) {
         const int t = j & 1;
         const uint32_t v = place_v(j, n), k = j + 2 < n ? place_k(j + 2) : 0;
@@ -525,8 +528,6 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Wal
         }
         if (stopped(sh)) break;
       }
-      // (every unit's is waited for, so that no two have one parity)
-      if (n == 1 && items) mbar_wait(&b.o_free[1], (items - 1) & 1, sh, a.status);
       nq += 1;
     }
     base += 2 * n;
