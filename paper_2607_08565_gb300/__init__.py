@@ -803,7 +803,8 @@ class SMetricKV:
         self.handle = smetric_kv_create(self.cfg)
         self._n_tokens = None
         self._kept = None
-        self._dim, self._f32, self._i32, self._empty = head_dim, torch.float32, torch.int32, torch.empty
+        self._dim, self._f32, self._i32 = head_dim, torch.float32, torch.int32
+        self._empty, self._like = torch.empty, torch.empty_like
         self._cache_shape = (num_pages, page_size, num_kv_heads, head_dim)
 
     def close(self):
@@ -892,7 +893,7 @@ class SMetricKV:
         if q is None:
             q_out = None
         elif q_out is None:
-            q_out = self._empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = self._like(q)
         hk, hq = c.num_kv_heads, c.num_q_heads
         smetric_kv_append(self.handle, self._cache(k_cache, v_cache), self._heads(k, hk, t, "k"),
                           self._heads(v, hk, t, "v"), self._heads(q, hq, t, "q"), self._heads(q_out, hq, t, "q_out"),
@@ -909,11 +910,11 @@ class SMetricKV:
         if q is None:
             q_out = None
         elif q_out is None:
-            q_out = self._empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = self._like(q)
         if k is None:
             k_out = None
         elif k_out is None:
-            k_out = self._empty(k.shape, dtype=k.dtype, device=k.device)
+            k_out = self._like(k)
         hk, hq = c.num_kv_heads, c.num_q_heads
         smetric_qk_norm_rope(self.handle, self._heads(q, hq, t, "q"), self._heads(k, hk, t, "k"), positions, t,
                              self._transform(cos_sin, interleaved, q_norm, k_norm, eps),
@@ -926,7 +927,7 @@ class SMetricKV:
         (float32 [tokens, num_q_heads])."""
         t, hq = self._planned(), self.cfg.num_q_heads
         if out is None:
-            out = self._empty((t, hq, self._dim), dtype=self.dtype, device=q.device)
+            out = self._like(q)
         lse = self._empty((t, hq), dtype=self._f32, device=q.device) if want_lse else None
         smetric_paged_attention(self.handle, self._cache(k_cache, v_cache), self._heads(q, hq, t, "q"),
                                 self._dim ** -0.5 if scale is None else scale, self._heads(out, hq, t, "out"), lse,

@@ -380,10 +380,10 @@ __device__ __forceinline__ void transform_heads(const Lane& l, const T* src, int
 // pieces: the two halves of 8 rotation pairs (i, i + rot/2), 8 interleaved
 // pairs, or 16 elements past rot. So a rotation never leaves the lane, a norm
 // is a sum over the group's lanes, and the token's cosines and sines are
-// loaded once for all its heads. Bound by memory; the registers of 24 warps an
+// loaded once for all its heads. Bound by memory; the registers of 28 warps an
 // SM hold the bytes in flight.
 template <typename T, bool kInterleaved>
-__global__ void __launch_bounds__(256, 3) k_kv_heads(const __grid_constant__ HeadsArgs a) {
+__global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ HeadsArgs a) {
   pdl_enter();
   const int lane = threadIdx.x & 31;
   const int64_t w = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
@@ -480,17 +480,17 @@ int launch_heads(smetric_kv* kv, HeadsArgs& a, const smetric_kv_transform& t, cu
   a.lanes_shift = 0;
   while (16 << a.lanes_shift < a.D) a.lanes_shift++;
   // Warps that share a token's heads: as many as it has rounds of heads while
-  // there are too few tokens to fill the SMs (24 warps an SM), else one.
+  // there are too few tokens to fill the SMs (28 warps an SM), else one.
   const int rounds = (a.hq + a.hk + a.hv + (32 >> a.lanes_shift) - 1) / (32 >> a.lanes_shift);
-  const int64_t room = (int64_t)kv->num_sms * 24 / std::max<int64_t>(1, a.n_tokens);
+  const int64_t room = (int64_t)kv->num_sms * 28 / std::max<int64_t>(1, a.n_tokens);
   a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, room));
-  const int64_t grid = (a.n_tokens * a.splits + 7) / 8;
+  const int64_t grid = (a.n_tokens * a.splits + 3) / 4;
   const bool il = t.flags & SMETRIC_KV_INTERLEAVED;
   const bool bf = kv->cfg.dtype == SMETRIC_BF16;
   auto kern = bf ? (il ? k_kv_heads<__nv_bfloat16, true> : k_kv_heads<__nv_bfloat16, false>)
                  : (il ? k_kv_heads<__half, true> : k_kv_heads<__half, false>);
   kv->launches++;
-  return launch_k(kern, dim3((unsigned)grid), dim3(256), 0, s, true, a);
+  return launch_k(kern, dim3((unsigned)grid), dim3(128), 0, s, true, a);
 }
 
 void free_kv(smetric_kv* kv) {
