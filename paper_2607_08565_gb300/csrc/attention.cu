@@ -57,6 +57,7 @@ struct AttentionArgs {
   const KvPlan* plan;
   const KvUnit* units;
   const KvShare* shares;
+  const int32_t* split;
   float* part;
   float2* part_ml;
   const int32_t* pages;
@@ -850,14 +851,16 @@ struct Joined {
 // pieces. G threads share 16 elements of a row (a whole sector of the output),
 // thread g taking pieces g, g + G, ..., two of them in flight, and join in
 // pairs: the order of the sums depends on the number of pieces alone.
+// CTA c1's share starts the unit; the block is one of `blocks` for it.
 constexpr int kJoinThreads = 128;
-constexpr int kJoinBlocks = 16;  // of a unit
+constexpr int kJoinBlocks = 16;  // an SM
 template <typename T, int G>
-__device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit, int h, int pieces) {
+__device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit, int h, int c1, int pieces, int block,
+                                     int blocks) {
   const int n_rows = unit.tokens * a.group, full_rows = a.tile_tokens * a.group;
-  constexpr int kStep = kJoinBlocks * kJoinThreads / G, P = 2;
-  const int n = n_rows * (a.D / 16), g = threadIdx.x % G;
-  for (int x = blockIdx.y * (kJoinThreads / G) + threadIdx.x / G; x - (int)(threadIdx.x % 32) / G < n; x += kStep) {
+  constexpr int P = 2;
+  const int n = n_rows * (a.D / 16), g = threadIdx.x % G, step = blocks * (kJoinThreads / G);
+  for (int x = block * (kJoinThreads / G) + threadIdx.x / G; x - (int)(threadIdx.x % 32) / G < n; x += step) {
     const int column = min(x, n - 1) / n_rows, r = min(x, n - 1) - column * n_rows;
     const int tile = r >= full_rows, row = r - tile * full_rows;
     Joined s;
@@ -868,7 +871,7 @@ __device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit,
       for (int k = 0; k < P; ++k) {
         const int i = i0 + k * G;
         if (i >= pieces) continue;
-        const int64_t slot = 2 * ((int64_t)blockIdx.x + i) + (i == 0);
+        const int64_t slot = 2 * ((int64_t)c1 + i) + (i == 0);
         ml[k] = a.part_ml[slot * 2 * kTile + tile * kTile + row];
         const float4* from = reinterpret_cast<const float4*>(a.part) + part_at(a.D, slot, tile, 4 * column) + row;
 #pragma unroll
@@ -914,22 +917,28 @@ __device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit,
   }
 }
 
-// kJoinBlocks blocks for the unit that starts in CTA blockIdx.x's share and that
-// others go on with.
+// The blocks in turn for the units that several CTAs share, so that one such
+// unit (a chunk over a long sequence: 9 MB of pieces) has them all.
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_constant__ AttentionArgs a) {
-  const KvShare s = a.shares[blockIdx.x];  // (the plan was done before the kernel that this one waits for)
-  const KvUnit unit = s.last;
+  // (the plan was done before the kernel that this one waits for)
+  const int units = a.plan->n_split, blocks = units ? gridDim.x / units : 0;
+  const int block = units ? blockIdx.x / units : 0;
+  KvShare s = {};
+  int c1 = 0;
+  if (block < blocks) {
+    c1 = a.split[blockIdx.x % units];
+    s = a.shares[c1];
+  }
   pdl_enter();
-  if (s.u0 < 0 || s.n_last < 2) return;
-  if (s.u0 == s.u1 && s.h0 == s.h1 && s.t0 != unit.tb) return;  // started before this share
+  if (block >= blocks) return;
   // Chunks have two or three pieces of many rows, single tokens many of few.
   if (s.n_last <= 4)
-    join<T, 1>(a, unit, s.h1, s.n_last);
+    join<T, 1>(a, s.last, s.h1, c1, s.n_last, block, blocks);
   else if (s.n_last <= 16)
-    join<T, 8>(a, unit, s.h1, s.n_last);
+    join<T, 8>(a, s.last, s.h1, c1, s.n_last, block, blocks);
   else
-    join<T, 32>(a, unit, s.h1, s.n_last);
+    join<T, 32>(a, s.last, s.h1, c1, s.n_last, block, blocks);
 }
 
 constexpr size_t smem_bytes(int halves) { return (size_t)(2 + stages(halves)) * halves * kHalf + sizeof(Shared); }
@@ -993,6 +1002,7 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
   a.plan = kv->plan;
   a.units = kv->units;
   a.shares = kv->shares;
+  a.split = kv->split;
   a.part = kv->part;
   a.part_ml = kv->part_ml;
   a.pages = kv->pages;
@@ -1018,7 +1028,7 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
                 reinterpret_cast<cudaStream_t>(stream), true, a);
   if (rc) return rc;
   auto join = c.dtype == SMETRIC_BF16 ? k_paged_join<__nv_bfloat16> : k_paged_join<__half>;
-  return launch_k(join, dim3((unsigned)kv->num_sms, kJoinBlocks), dim3(kJoinThreads), 0,
+  return launch_k(join, dim3((unsigned)kv->num_sms * kJoinBlocks), dim3(kJoinThreads), 0,
                   reinterpret_cast<cudaStream_t>(stream), true, a);
 }
 

@@ -54,6 +54,7 @@ struct PlanArgs {
   int64_t* unit_cost;
   int32_t* unit_base;
   KvShare* shares;
+  int32_t* split;
   int32_t* status;
 };
 
@@ -103,6 +104,7 @@ __device__ int32_t last_at_most(const S* a, int32_t n, int64_t x, int64_t scale)
 __device__ void plan_units(const PlanArgs& a) {
   __shared__ int64_t sums[32];
   __shared__ int32_t su[kMaxCtas + 1], sh[kMaxCtas + 1], st[kMaxCtas + 1];
+  __shared__ int32_t n_split;
   const int per = 2 * a.tile_tokens;
   int64_t base = 0;
   for (int32_t r0 = 0; r0 < a.n; r0 += kPlanThreads) {
@@ -159,6 +161,7 @@ __device__ void plan_units(const PlanArgs& a) {
     }
     su[c] = u, sh[c] = h, st[c] = t;
   }
+  if (threadIdx.x == 0) n_split = 0;
   __syncthreads();
   for (int c = threadIdx.x; c < a.ctas; c += kPlanThreads) {
     KvShare s = {};
@@ -178,9 +181,13 @@ __device__ void plan_units(const PlanArgs& a) {
       s.last = a.units[s.u1];
       s.n_last = 1;
       while (same(c + s.n_last, s.u1, s.h1)) ++s.n_last;
+      // (their order decides which blocks join them, not how)
+      if (s.n_last > 1 && !same(c, s.u1, s.h1)) a.split[atomicAdd(&n_split, 1)] = c;
     }
     a.shares[c] = s;
   }
+  __syncthreads();
+  if (threadIdx.x == 0) a.plan->n_split = n_split;
 }
 
 __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(const __grid_constant__ PlanArgs a) {
@@ -202,6 +209,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(const __grid_constant_
       plan_units(a);
     } else {
       for (int i = threadIdx.x; i < a.ctas; i += kPlanThreads) a.shares[i].u0 = -1;
+      if (threadIdx.x == 0) a.plan->n_split = 0;
     }
     return;
   }
@@ -501,6 +509,7 @@ void free_kv(smetric_kv* kv) {
   cudaFree(kv->unit_cost);
   cudaFree(kv->unit_base);
   cudaFree(kv->shares);
+  cudaFree(kv->split);
   cudaFree(kv->part);
   cudaFree(kv->part_ml);
 }
@@ -548,6 +557,7 @@ int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out) {
          cudaMalloc(&kv->unit_cost, sizeof(int64_t) * (units + 1)) == cudaSuccess &&
          cudaMalloc(&kv->unit_base, sizeof(int32_t) * (requests + 1)) == cudaSuccess &&
          cudaMalloc(&kv->shares, sizeof(KvShare) * kv->num_sms) == cudaSuccess &&
+         cudaMalloc(&kv->split, sizeof(int32_t) * kv->num_sms) == cudaSuccess &&
          cudaMalloc(&kv->part, sizeof(float) * slots * c.head_dim) == cudaSuccess &&
          cudaMalloc(&kv->part_ml, sizeof(float2) * slots) == cudaSuccess && attention_limits() &&
          cudaMemset(kv->status, 0, sizeof(int32_t)) == cudaSuccess && cudaDeviceSynchronize() == cudaSuccess;
@@ -607,6 +617,7 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
   a.unit_cost = kv->unit_cost;
   a.unit_base = kv->unit_base;
   a.shares = kv->shares;
+  a.split = kv->split;
   a.status = kv->status;
   const unsigned grid = 1 + (unsigned)((n_tokens + kPlanThreads - 1) / kPlanThreads);
   kv->launches++;

@@ -20,7 +20,8 @@ struct KvToken {
 struct KvPlan {
   int64_t first, last;  // tokens [first, last) belong to requests
   int32_t valid;        // 0: the batch's offsets or lengths were refused
-  int32_t reserved[3];
+  int32_t n_split;      // units that several CTAs share
+  int32_t reserved[2];
 };
 
 // Keys go through the attention in tiles of kTile, queries in tiles of kTile
@@ -65,6 +66,7 @@ struct smetric_kv {
   int64_t* unit_cost;        // as many + 1: cost of the units before, for one key head
   int32_t* unit_base;        // max_batch_requests + 1: a request's first unit
   smetric::KvShare* shares;  // num_sms
+  int32_t* split;            // num_sms: the CTAs that start a unit which others go on with
   float* part;               // 2 * num_sms slots of partial sums: a CTA's first unit's, its last's
   float2* part_ml;           // and their rows' (reference exponent, sum of weights)
   // of the last plan
