@@ -108,12 +108,20 @@ __device__ __forceinline__ bool mbar_try(uint64_t* b, uint32_t parity) {
       : "=r"(done) : "r"(smem_u32(b)), "r"(parity), "r"(kNap) : "memory");
   return done != 0;
 }
+// One look.
+__device__ __forceinline__ bool mbar_test(uint64_t* b, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(done) : "r"(smem_u32(b)), "r"(parity) : "memory");
+  return done != 0;
+}
 __device__ __forceinline__ bool stopped(const Shared* sh) { return *(const volatile int32_t*)&sh->abort != 0; }
 // Waits for the phase of the given parity; gives up after kWaitCycles, or when
 // another wait of the CTA has. Callers go on either way (every loop is bounded
 // by the plan); outputs are then undefined and the error is latched.
 __device__ __forceinline__ void mbar_wait(uint64_t* b, uint32_t parity, Shared* sh, int32_t* status) {
-  if (mbar_try(b, parity)) return;
+  if (mbar_test(b, parity)) return;
   const long long start = clock64();
   while (!mbar_try(b, parity)) {
     if (stopped(sh)) return;
@@ -427,32 +435,26 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Wal
     const auto release_q = [&](uint32_t i) {
       if (elect()) mma_commit(&b.q_empty[i & 1]);
     };
-    const auto scores = [&](int t, uint32_t q, uint32_t place) {  // S_t = Q_q K^T
-      if (elect()) {
-        const uint32_t qd = q_desc + (q & 1) * (HALVES * kHalf >> 4), kd = k_desc + stage(place) * (HALVES * kHalf >> 4);
+    // (one elected lane, from here to the commit)
+    const auto issue_scores = [&](int t, uint32_t q, uint32_t at) {  // S_t = Q_q K^T
+      const uint32_t qd = q_desc + (q & 1) * (HALVES * kHalf >> 4), kd = k_desc + at * (HALVES * kHalf >> 4);
 #pragma unroll
-        for (int k = 0; k < 4 * HALVES; ++k) {
-          const uint32_t o = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
-          if (k < steps) mma_ss(tmem + t * kTile, qd + o, kd + o, kScores, k > 0);
-        }
-        mma_commit(&b.s_full[t]);
+      for (int k = 0; k < 4 * HALVES; ++k) {
+        const uint32_t o = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
+        if (k < steps) mma_ss(tmem + t * kTile, qd + o, kd + o, kScores, k > 0);
       }
+      mma_commit(&b.s_full[t]);
     };
-    // O_t (+)= P_t V; `next`, if not 0, is a place that is needed after it.
-    const auto products = [&](int t, uint32_t place, bool add, uint32_t next) {
-      const uint32_t vd = v_desc + stage(place) * (HALVES * kHalf >> 4);
-      if (!add && items) mbar_wait(&b.o_free[t], (items - 1) & 1, sh, a.status);
+    const auto issue_products = [&](int t, uint32_t at, bool add) {  // O_t (+)= P_t V
+      const uint32_t vd = v_desc + at * (HALVES * kHalf >> 4);
+#pragma unroll
+      for (int k = 0; k < kTile / 16; ++k)
+        mma_ts(tmem + 2 * kTile + t * kTile, tmem + t * kTile + 8 * k, vd + k * (2048 >> 4), values, add || k > 0);
+    };
+    const auto wait_weights = [&](int t, bool first) {
+      if (first && items) mbar_wait(&b.o_free[t], (items - 1) & 1, sh, a.status);
       mbar_wait(&b.p_full[t], np[t]++ & 1, sh, a.status);
       fence_after();
-      if (elect()) {
-#pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-          mma_ts(tmem + 2 * kTile + t * kTile, tmem + t * kTile + 8 * k, vd + k * (2048 >> 4), values, add || k > 0);
-      }
-      if (next) wait_full(next);
-    };
-    const auto release = [&](uint32_t place) {
-      if (elect()) mma_commit(&b.empty[stage(place)]);
     };
     // Rows of a tile's values that no key lies at become zeros: a weight of
     // zero does not cancel what may lie there. (A row's 128 bytes are its own
@@ -475,39 +477,53 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Wal
     if (stopped(sh)) break;
     fence_after();
     if (it.pair) {
-      scores(0, nq, 0);
+      if (elect()) issue_scores(0, nq, stage(0));
       wait_q(nq + 1);
-      scores(1, nq + 1, 0);
-      release(0);
-      if (n == 1) release_q(nq), release_q(nq + 1);
-      for (int j = 0; j < n; ++j) {
-        const uint32_t v = place_v(j, n), k = j + 1 < n ? place_k(j + 1) : 0;
+      if (elect()) {
+        issue_scores(1, nq + 1, stage(0));
+        mma_commit(&b.empty[stage(0)]);
+      }
+      for (int j = 0; j + 1 < n; ++j) {
+        const uint32_t v = place_v(j, n), k = place_k(j + 1), vs = stage(v), ks = stage(k);
         wait_full(v);
-        clear(v, j);
-        products(0, v, j > 0, k);
-        if (k) {
-          scores(0, nq, k);
-          if (j + 2 == n) release_q(nq);
-        } else if (elect()) {
-          mma_commit(&b.o_full[0]);
+        if (j == 0) clear(v, j);
+        wait_full(k);
+        wait_weights(0, j == 0);
+        if (elect()) {
+          issue_products(0, vs, j > 0);
+          issue_scores(0, nq, ks);
         }
-        products(1, v, j > 0, 0);
-        release(v);
-        if (k) {
-          scores(1, nq + 1, k);
-          release(k);
-          if (j + 2 == n) release_q(nq + 1);
-        } else if (elect()) {
-          mma_commit(&b.o_full[1]);
+        wait_weights(1, j == 0);
+        if (elect()) {
+          issue_products(1, vs, j > 0);
+          mma_commit(&b.empty[vs]);
+          issue_scores(1, nq + 1, ks);
+          mma_commit(&b.empty[ks]);
         }
-        if (stopped(sh)) break;
+      }
+      release_q(nq), release_q(nq + 1);
+      const uint32_t v = place_v(n - 1, n), vs = stage(v);
+      wait_full(v);
+      clear(v, n - 1);
+      wait_weights(0, n == 1);
+      if (elect()) {
+        issue_products(0, vs, n > 1);
+        mma_commit(&b.o_full[0]);
+      }
+      wait_weights(1, n == 1);
+      if (elect()) {
+        issue_products(1, vs, n > 1);
+        mma_commit(&b.o_full[1]);
+        mma_commit(&b.empty[vs]);
       }
       nq += 2;
     } else {
       for (int j = 0; j < min(n, 2); ++j) {
         if (j) wait_full(j);
-        scores(j, nq, j);
-        release(j);
+        if (elect()) {
+          issue_scores(j, nq, stage(j));
+          mma_commit(&b.empty[stage(j)]);
+        }
       }
       if (n <= 2) release_q(nq);
       // (waited for by every unit, so that no two have one parity, and before the
@@ -515,19 +531,23 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Wal
       if (n == 1 && items) mbar_wait(&b.o_free[1], (items - 1) & 1, sh, a.status);
       for (int j = 0; j < n; ++j) {
         const int t = j & 1;
-        const uint32_t v = place_v(j, n), k = j + 2 < n ? place_k(j + 2) : 0;
+        const bool more = j + 2 < n;
+        const uint32_t v = place_v(j, n), k = place_k(j + 2), vs = stage(v), ks = stage(k);
         wait_full(v);
         clear(v, j);
-        products(t, v, j > 1, k);
-        release(v);
-        if (k) {
-          scores(t, nq, k);
-          release(k);
-          if (j + 3 == n) release_q(nq);
-        } else if (elect()) {
-          mma_commit(&b.o_full[t]);
+        if (more) wait_full(k);
+        wait_weights(t, j < 2);
+        if (elect()) {
+          issue_products(t, vs, j > 1);
+          mma_commit(&b.empty[vs]);
+          if (more) {
+            issue_scores(t, nq, ks);
+            mma_commit(&b.empty[ks]);
+            if (j + 3 == n) mma_commit(&b.q_empty[nq & 1]);
+          } else {
+            mma_commit(&b.o_full[t]);
+          }
         }
-        if (stopped(sh)) break;
       }
       nq += 1;
     }

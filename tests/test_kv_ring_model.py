@@ -108,24 +108,25 @@ def run(seed, stages, units):
                 products.extend(q_empty[nq + t & 1].arrive for t in range(2 if pair else 1))
             if not pair and n == 1 and u:
                 yield from wait(o_free[1], u - 1 & 1)
+            ahead = 1 if pair else 2  # steps between a tile's product and the next scores in its half
             for j in range(n):
-                v, ahead = place_v(j, n), 1 if pair else 2
+                v, k = place_v(j, n), place_k(j + ahead)
                 yield from wait_full(v)
+                if j + ahead < n:
+                    yield from wait_full(k)
                 for t in (0, 1) if pair else (j & 1,):
                     yield from weigh(t, v, (u, "v", j), j < ahead)
                     if not pair or t:
                         release(v)
                     if j + ahead < n:
-                        k = place_k(j + ahead)
-                        yield from wait_full(k)
                         scores(t, nq + (t if pair else 0), k, (u, "k", j + ahead))
                         if not pair or t:
                             release(k)
-                        if j + ahead + 1 == n:
-                            products.append(q_empty[nq + (t if pair else 0) & 1].arrive)
                     else:
                         products.append(o_full[t].arrive)
                     yield
+                if j + ahead + 1 == n and n > ahead:
+                    products.extend(q_empty[nq + t & 1].arrive for t in range(2 if pair else 1))
             nq += 2 if pair else 1
             base += 2 * n
 
