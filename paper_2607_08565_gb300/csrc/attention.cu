@@ -601,6 +601,8 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
     const int32_t hi = mine ? it.unit.pos + tile_token(a, it, tile) + row_token : INT32_MAX / 2;  // last key that the row sees
     const int32_t lo = mine && hi >= a.window ? hi - a.window + 1 : 0;                        // first key
     const bool busy = 32 * warp < n_rows;
+    // every row of the warp sees all keys of [all_lo, all_hi]
+    const int32_t all_lo = __reduce_max_sync(kFull, lo), all_hi = __reduce_min_sync(kFull, hi);
     float top = -INFINITY;  // largest score when the reference was last moved
     float ref = 0.f;        // the reference exponent: c * top - kLift (0 before the first visible key)
     float l = 0.f;
@@ -620,7 +622,7 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
 #pragma unroll
       for (int i = 0; i < kTile; ++i) s[i] = __uint_as_float(r[i]);
       const int32_t key = (it.tb + j) * kTile;
-      if (__any_sync(kFull, key + kTile - 1 > hi || key < lo)) {
+      if (key + kTile - 1 > all_hi || key < all_lo) {
 #pragma unroll
         for (int i = 0; i < kTile; i += 32) {  // a bit a column
           const uint32_t seen = below(hi + 1 - (key + i)) & ~below(lo - (key + i));
