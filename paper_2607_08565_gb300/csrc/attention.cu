@@ -18,8 +18,16 @@
 //
 // Warps: 0 and 2 copy tiles with TMA (keys and values alternate in one ring of
 // buffers, query tiles in one of two), 1 issues the matrix products, 3 writes
-// zeros for tokens of no request, 4-7 and 8-11 are the two tiles' softmax (a thread a row), 12-15 write a unit's output
-// while the softmax of the next one runs.
+// zeros for tokens of no request, 4-7 and 8-11 are the two tiles' softmax (a
+// thread a row), 12-15 write a unit's output while the softmax of the next one
+// runs.
+//
+// Single tokens are bound by memory: 64 of them over 2k to 48k keys (4 key heads
+// of 128, 3.2 GB) take 464 us, 6.9 TB/s, the rate of a copy. Chunks are bound by
+// the chain of a tile's softmax (1,300 cycles), its product with the values and
+// its half's next scores (2 x 512 on the tensor cores): 2,840 cycles for two query
+// tiles and a key tile, and by the power cap: 2,048 tokens over 65,000 (32 query
+// heads) 1,440 us, 1,540 TFLOP/s, 1,560 us where the cap holds.
 
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -42,7 +50,7 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr long long kWaitCycles = 1ll << 32;  // bounded mbarrier waits: about 2 s
-constexpr uint32_t kNap = 20000;
+constexpr uint32_t kNap = 20000;  // ns that a waiting warp sleeps between looks at most
 constexpr int kThreads = 512;
 constexpr float kSlack = 8.f;     // log2 of how far scores may pass the reference
 constexpr uint32_t kHalf = 16384;  // bytes of 128 rows of 64 elements
@@ -360,7 +368,7 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
     // the keys that some query of the unit sees
     const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
     const int32_t* pages = a.pages + it.unit.req * a.pages_stride;
-    // the lane's page of a tile, -1 where nobody sees a key of it
+    // the lane's page of a tile, INT32_MIN where nobody sees a key of it
     const auto page_of = [&](int j) {
       const int64_t key = (int64_t)(it.tb + j) * kTile + mine * rows;
       return copies && j < n && key < hi && key + rows > lo ? pages[key >> page_shift] : INT32_MIN;
@@ -410,6 +418,9 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
   }
 }
 
+// Issues the products, a step's (weights with values, then the half's next
+// scores) by one elected lane in one go: this warp is close to the limit, a wait
+// that is ready costs it 60 to 160 cycles. The two halves take turns.
 template <typename T, int HALVES>
 __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Walk w, uint32_t q_smem, uint32_t ring) {
   constexpr int S = stages(HALVES);
@@ -940,7 +951,9 @@ __device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit,
 }
 
 // The blocks in turn for the units that several CTAs share, so that one such
-// unit (a chunk over a long sequence: 9 MB of pieces) has them all.
+// unit (a chunk over a long sequence: 9 MB of pieces) has them all. Bound by the
+// latency of its reads: 10 us for 150 units of 252 rows in two pieces (49 MB), 6
+// for 4 units of 8 rows in 38, 3.5 for none.
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_constant__ AttentionArgs a) {
   // (the plan was done before the kernel that this one waits for)
