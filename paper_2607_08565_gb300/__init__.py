@@ -803,6 +803,8 @@ class SMetricKV:
         self.handle = smetric_kv_create(self.cfg)
         self._n_tokens = None
         self._kept = None
+        # (what the calls use each time: a step's few tokens are bound by the host)
+        self._lib, self._raw_stream, self._device = lib(), torch._C._cuda_getCurrentRawStream, torch.cuda.current_device()
         self._dim, self._f32, self._i32 = head_dim, torch.float32, torch.int32
         self._empty, self._like = torch.empty, torch.empty_like
         self._cache_shape = (num_pages, page_size, num_kv_heads, head_dim)
@@ -845,21 +847,30 @@ class SMetricKV:
         return smetric_kv_cache(k_cache.data_ptr(), v_cache.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1],
                                 strides[2] if shape[2] > 1 else 0)
 
+    def _new_heads(self, like):
+        """A tensor like `like` for a call to fill, and its description."""
+        out = self._like(like)
+        token, head, _ = out.stride()
+        return out, smetric_heads(out.data_ptr(), token, head)
+
+    def _stream(self, stream) -> Optional[int]:
+        return self._raw_stream(self._device) if stream is None else _stream(stream)
+
     def _norm(self, w) -> Optional[int]:
         if w is None:
             return None
-        if w.dtype != self.dtype or w.numel() != self._dim:
-            raise ValueError(f"norm weights must be {self.dtype} [{self._dim}]")
-        return _ptr(w)
+        if w.dtype != self.dtype or w.numel() != self._dim or not w.is_contiguous():
+            raise ValueError(f"norm weights must be {self.dtype} [{self._dim}], contiguous")
+        return w.data_ptr()
 
     def _transform(self, cos_sin, interleaved, q_norm, k_norm, eps) -> smetric_kv_transform:
-        if cos_sin is None:
-            rows = rot = 0
-        else:
-            if cos_sin.dtype != self._f32 or cos_sin.dim() != 2:
-                raise ValueError("cos_sin must be torch.float32 [positions, rot_dim]")
+        rows = rot = table = None
+        if cos_sin is not None:
+            if cos_sin.dtype != self._f32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
+                raise ValueError("cos_sin must be torch.float32 [positions, rot_dim], contiguous")
             rows, rot = cos_sin.shape
-        return smetric_kv_transform(_ptr(cos_sin), rows, self._norm(q_norm), self._norm(k_norm), eps, rot,
+            table = cos_sin.data_ptr() if rows and rot else None
+        return smetric_kv_transform(table, rows or 0, self._norm(q_norm), self._norm(k_norm), eps, rot or 0,
                                     SMETRIC_KV_INTERLEAVED if interleaved else 0, 0)
 
     def plan(self, offsets, kv_lens, pages, n_tokens: int, window: int = 0, stream=None):
@@ -890,14 +901,18 @@ class SMetricKV:
         cos_sin where given) and values; with q, transforms the queries into
         q_out (a new tensor by default) and returns it."""
         t, c = self._planned(), self.cfg
+        hk, hq = c.num_kv_heads, c.num_q_heads
+        caches, kh, vh, qh = (self._cache(k_cache, v_cache), self._heads(k, hk, t, "k"), self._heads(v, hk, t, "v"),
+                              self._heads(q, hq, t, "q"))
         if q is None:
             q_out = None
-        elif q_out is None:
-            q_out = self._like(q)
-        hk, hq = c.num_kv_heads, c.num_q_heads
-        smetric_kv_append(self.handle, self._cache(k_cache, v_cache), self._heads(k, hk, t, "k"),
-                          self._heads(v, hk, t, "v"), self._heads(q, hq, t, "q"), self._heads(q_out, hq, t, "q_out"),
-                          self._transform(cos_sin, interleaved, q_norm, k_norm, eps), stream)
+        if q is not None and q_out is None:
+            q_out, oh = self._new_heads(q)
+        else:
+            oh = self._heads(q_out, hq, t, "q_out")
+        _check(self._lib.smetric_kv_append(self.handle, caches, kh, vh, qh, oh,
+                                           self._transform(cos_sin, interleaved, q_norm, k_norm, eps),
+                                           self._stream(stream)), "smetric_kv_append")
         return q_out
 
     def qk_norm_rope(self, q, k, positions, cos_sin=None, interleaved=False, q_norm=None, k_norm=None, eps=1e-6,
@@ -905,20 +920,25 @@ class SMetricKV:
         """The norms and the rotation alone, at int32 positions; q or k may be
         None. Returns (q_out, k_out), new tensors unless given."""
         t, c = positions.numel(), self.cfg
-        if positions.dtype != self._i32:
-            raise ValueError("positions must be torch.int32")
+        if positions.dtype != self._i32 or not positions.is_contiguous():
+            raise ValueError("positions must be torch.int32, contiguous")
+        hk, hq = c.num_kv_heads, c.num_q_heads
+        qh, kh = self._heads(q, hq, t, "q"), self._heads(k, hk, t, "k")
         if q is None:
             q_out = None
-        elif q_out is None:
-            q_out = self._like(q)
         if k is None:
             k_out = None
-        elif k_out is None:
-            k_out = self._like(k)
-        hk, hq = c.num_kv_heads, c.num_q_heads
-        smetric_qk_norm_rope(self.handle, self._heads(q, hq, t, "q"), self._heads(k, hk, t, "k"), positions, t,
-                             self._transform(cos_sin, interleaved, q_norm, k_norm, eps),
-                             self._heads(q_out, hq, t, "q_out"), self._heads(k_out, hk, t, "k_out"), stream)
+        if q is not None and q_out is None:
+            q_out, qo = self._new_heads(q)
+        else:
+            qo = self._heads(q_out, hq, t, "q_out")
+        if k is not None and k_out is None:
+            k_out, ko = self._new_heads(k)
+        else:
+            ko = self._heads(k_out, hk, t, "k_out")
+        _check(self._lib.smetric_qk_norm_rope(self.handle, qh, kh, positions.data_ptr() if t else None, t,
+                                              self._transform(cos_sin, interleaved, q_norm, k_norm, eps), qo, ko,
+                                              self._stream(stream)), "smetric_qk_norm_rope")
         return q_out, k_out
 
     def paged_attention(self, q, k_cache, v_cache, scale=None, out=None, want_lse=False, stream=None):
@@ -926,12 +946,16 @@ class SMetricKV:
         head_dim ** -0.5 by default. Returns out, or (out, lse) with want_lse
         (float32 [tokens, num_q_heads])."""
         t, hq = self._planned(), self.cfg.num_q_heads
+        caches, qh = self._cache(k_cache, v_cache), self._heads(q, hq, t, "q")
         if out is None:
-            out = self._like(q)
+            out, oh = self._new_heads(q)
+        else:
+            oh = self._heads(out, hq, t, "out")
         lse = self._empty((t, hq), dtype=self._f32, device=q.device) if want_lse else None
-        smetric_paged_attention(self.handle, self._cache(k_cache, v_cache), self._heads(q, hq, t, "q"),
-                                self._dim ** -0.5 if scale is None else scale, self._heads(out, hq, t, "out"), lse,
-                                stream)
+        _check(self._lib.smetric_paged_attention(self.handle, caches, qh,
+                                                 self._dim ** -0.5 if scale is None else scale, oh,
+                                                 lse.data_ptr() if want_lse and t else None, self._stream(stream)),
+               "smetric_paged_attention")
         return (out, lse) if want_lse else out
 
     def status(self, stream=None) -> int:
