@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 #include "call_range.cuh"
 #include "kv_impl.cuh"
@@ -507,17 +508,29 @@ int launch_heads(smetric_kv* kv, HeadsArgs& a, const smetric_kv_transform& t, cu
   return launch_k(kern, dim3((unsigned)grid), dim3(128), 0, s, true, a);
 }
 
-void free_kv(smetric_kv* kv) {
-  cudaFree(kv->status);
-  cudaFree(kv->plan);
-  cudaFree(kv->tokens);
-  cudaFree(kv->units);
-  cudaFree(kv->unit_cost);
-  cudaFree(kv->unit_base);
-  cudaFree(kv->shares);
-  cudaFree(kv->split);
-  cudaFree(kv->part);
-  cudaFree(kv->part_ml);
+// Device memory of a handle: one allocation (each costs the host some 30 us),
+// its parts 256-byte aligned. Sets the parts' pointers within `mem` (NULL: only
+// counts) and returns its size.
+size_t lay_out(smetric_kv* kv, unsigned char* mem) {
+  const size_t tokens = (size_t)kv->cfg.max_batch_tokens, requests = (size_t)kv->cfg.max_batch_requests;
+  const size_t units = tokens / (2 * kv->tile_tokens) + requests + 1;
+  const size_t slots = 2 * (size_t)kv->num_sms * 2 * kTile;
+  size_t at = 0;
+  const auto part = [&](auto*& p, size_t n) {
+    p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(mem ? mem + at : nullptr);
+    at += (n * sizeof(*p) + 255) / 256 * 256;
+  };
+  part(kv->status, 1);
+  part(kv->plan, 1);
+  part(kv->tokens, tokens + 1);
+  part(kv->units, units);
+  part(kv->unit_cost, units + 1);
+  part(kv->unit_base, requests + 1);
+  part(kv->shares, kv->num_sms);
+  part(kv->split, kv->num_sms);
+  part(kv->part, slots * kv->cfg.head_dim);
+  part(kv->part_ml, slots);
+  return at;
 }
 
 }  // namespace
@@ -549,28 +562,21 @@ int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out) {
   kv->cfg = c;
   kv->group = c.num_q_heads / c.num_kv_heads;
   kv->tile_tokens = kTile / kv->group;
-  const size_t tokens = (size_t)c.max_batch_tokens, requests = (size_t)c.max_batch_requests;
-  const size_t units = tokens / (2 * kv->tile_tokens) + requests + 1;
+  unsigned char* mem = nullptr;
   bool ok = cudaGetDevice(&kv->device) == cudaSuccess &&
             cudaDeviceGetAttribute(&kv->num_sms, cudaDevAttrMultiProcessorCount, kv->device) == cudaSuccess;
   if (ok) {
     kv->num_sms = std::min(kv->num_sms, kMaxCtas);
-    const size_t slots = 2 * (size_t)kv->num_sms * 2 * kTile;
-    ok = cudaMalloc(&kv->status, sizeof(int32_t)) == cudaSuccess &&
-         cudaMalloc(&kv->plan, sizeof(KvPlan)) == cudaSuccess &&
-         cudaMalloc(&kv->tokens, sizeof(KvToken) * (tokens + 1)) == cudaSuccess &&
-         cudaMalloc(&kv->units, sizeof(KvUnit) * units) == cudaSuccess &&
-         cudaMalloc(&kv->unit_cost, sizeof(int64_t) * (units + 1)) == cudaSuccess &&
-         cudaMalloc(&kv->unit_base, sizeof(int32_t) * (requests + 1)) == cudaSuccess &&
-         cudaMalloc(&kv->shares, sizeof(KvShare) * kv->num_sms) == cudaSuccess &&
-         cudaMalloc(&kv->split, sizeof(int32_t) * kv->num_sms) == cudaSuccess &&
-         cudaMalloc(&kv->part, sizeof(float) * slots * c.head_dim) == cudaSuccess &&
-         cudaMalloc(&kv->part_ml, sizeof(float2) * slots) == cudaSuccess && attention_limits() &&
-         cudaMemset(kv->status, 0, sizeof(int32_t)) == cudaSuccess && cudaDeviceSynchronize() == cudaSuccess;
+    ok = cudaMalloc(&mem, lay_out(kv, nullptr)) == cudaSuccess;
+  }
+  if (ok) {
+    lay_out(kv, mem);
+    ok = attention_limits() && cudaMemset(kv->status, 0, sizeof(int32_t)) == cudaSuccess &&
+         cudaDeviceSynchronize() == cudaSuccess;
   }
   if (!ok) {
     (void)cudaGetLastError();
-    free_kv(kv);
+    cudaFree(mem);
     delete kv;
     return SMETRIC_ERR_OOM;
   }
@@ -585,7 +591,7 @@ int smetric_kv_destroy(smetric_kv* kv) {
   cudaGetDevice(&dev);
   if (dev != kv->device) cudaSetDevice(kv->device);
   cudaDeviceSynchronize();
-  free_kv(kv);
+  cudaFree(kv->status);  // (the first part: the whole)
   int rc = cuda_status(cudaGetLastError());
   if (dev >= 0 && dev != kv->device) cudaSetDevice(dev);
   delete kv;
