@@ -882,8 +882,8 @@ struct Joined {
 
 // out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i over a unit's
 // pieces. G threads share 16 elements of a row (a whole sector of the output),
-// thread g taking pieces g, g + G, ..., two of them in flight, and join in
-// pairs: the order of the sums depends on the number of pieces alone.
+// thread g taking pieces g, g + G, ..., two of them in flight: the order of the
+// sums depends on the number of pieces alone.
 // CTA c1's share starts the unit; the block is one of `blocks` for it.
 constexpr int kJoinThreads = 128;
 constexpr int kJoinBlocks = 16;  // an SM
@@ -914,39 +914,53 @@ __device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit,
       for (int k = 0; k < P; ++k)
         if (i0 + k * G < pieces) s.add(ml[k].x, ml[k].y, p[k]);
     }
+    // The G threads' sums: their exponents to the largest, then in pairs, each of
+    // a pair going on with half of the elements: 15 to 16 exchanges of elements
+    // instead of 16 a step, and the stores spread over the threads (18.6 us against
+    // 19.3 for single tokens of 19 sequences of up to 900 keys, 192 against 196 for
+    // chunks in a window).
+    float top = s.top;
+#pragma unroll
+    for (int o = 1; o < G; o <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+    const float f = s.top == -INFINITY ? 0.f : ex2(s.top - top);
+    float l = s.l * f, v[16];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      v[4 * q] = s.o[q].x * f, v[4 * q + 1] = s.o[q].y * f, v[4 * q + 2] = s.o[q].z * f, v[4 * q + 3] = s.o[q].w * f;
+    int first = 0;  // of the elements that the thread has
 #pragma unroll
     for (int o = 1; o < G; o <<= 1) {
-      // (both lanes of a pair add the lower one's sums first)
-      Joined t;
-      t.top = __shfl_xor_sync(kFull, s.top, o);
-      t.l = __shfl_xor_sync(kFull, s.l, o);
+      l += __shfl_xor_sync(kFull, l, o);
+      const bool high = g & o;
+      const int m = 8 / o;  // elements to go on with
+      if (m > 0) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        t.o[q].x = __shfl_xor_sync(kFull, s.o[q].x, o);
-        t.o[q].y = __shfl_xor_sync(kFull, s.o[q].y, o);
-        t.o[q].z = __shfl_xor_sync(kFull, s.o[q].z, o);
-        t.o[q].w = __shfl_xor_sync(kFull, s.o[q].w, o);
-      }
-      if (!(g & o)) {
-        s.add(t.top, t.l, t.o);
+        for (int i = 0; i < m; ++i) v[i] = (high ? v[i + m] : v[i]) + __shfl_xor_sync(kFull, high ? v[i] : v[i + m], o);
+        first += high ? m : 0;
       } else {
-        t.add(s.top, s.l, s.o);
-        s = t;
+        v[0] += __shfl_xor_sync(kFull, v[0], o);
       }
     }
-    if (x >= n || g) continue;
-    const float inv = s.l > 0.f ? 1.f / s.l : s.l;  // (NaN stays)
+    if (x >= n) continue;
+    const float inv = l > 0.f ? 1.f / l : l;  // (NaN stays)
     const int64_t token = unit.token + r / a.group;
     const int head = h * a.group + r % a.group;
-    uint32_t y[8];
+    T* out = static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride + 16 * column;
+    if constexpr (G == 1) {
+      uint32_t y[8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      y[2 * q] = Type<T>::pack(s.o[q].x * inv, s.o[q].y * inv);
-      y[2 * q + 1] = Type<T>::pack(s.o[q].z * inv, s.o[q].w * inv);
+      for (int q = 0; q < 8; ++q) y[q] = Type<T>::pack(v[2 * q] * inv, v[2 * q + 1] * inv);
+      store16(a, out, y);
+    } else if constexpr (G <= 8) {
+#pragma unroll
+      for (int q = 0; q < 8 / G; ++q)
+        reinterpret_cast<uint32_t*>(out + first)[q] = Type<T>::pack(v[2 * q] * inv, v[2 * q + 1] * inv);
+    } else if (g < 16) {
+      // (element 0 is the low half)
+      reinterpret_cast<uint16_t*>(out)[first] = (uint16_t)Type<T>::pack(v[0] * inv, 0.f);
     }
-    store16(a, static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride + 16 * column, y);
-    if (a.lse && column == 0)
-      a.lse[token * a.hq + head] = s.l == 0.f ? -INFINITY : (s.top + log2f(s.l)) * 0.6931471805599453f;
+    if (a.lse && column == 0 && g == 0)
+      a.lse[token * a.hq + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
   }
 }
 
