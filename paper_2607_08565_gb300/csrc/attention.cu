@@ -692,7 +692,9 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
       l += all.x + all.y;
     }
     if (items) mbar_wait(&b.o_free[tile], (items - 1) & 1, sh, a.status);
-    sh->stat[tile][row] = make_float2(top == -INFINITY ? -INFINITY : ref, l);
+    // (scores that are all NaN leave top where it was, but not l: the row is not
+    // one without keys, and what joins its pieces must not pass over it)
+    sh->stat[tile][row] = make_float2(top == -INFINITY && l == 0.f ? -INFINITY : ref, l);
     __syncwarp();
     if (lane == 0) mbar_arrive(&b.stat_full[tile]);
   }

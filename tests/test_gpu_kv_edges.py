@@ -1,0 +1,45 @@
+"""Edges of the paged KV$ operators: NaN rows, positions and lengths at the ends
+of their ranges, tables without rows, views of one token or one head, and calls
+on another stream than torch's current one."""
+
+import pytest
+import torch
+
+import paper_2607_08565_gb300 as pkg
+from kv_util import BF, DEV, HF, UNIT, Batch, table
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    import __graft_entry__
+    __graft_entry__.build()
+    torch.cuda.set_device(0)
+
+
+@pytest.mark.parametrize("hq,hk,d,new,lens", [
+    (8, 2, 64, [1, 1], [100, 3]),             # nobody shares them
+    (8, 2, 64, [300], [300]),                 # two tiles of queries
+    (64, 64, 128, [1], [24577]),              # some two pieces each (of 152 SMs)
+    (32, 16, 64, [1], [24577]),               # nine or ten
+    (32, 4, 128, [1], [24577]),               # 38
+    (16, 2, 128, [40], [30000]),              # of many rows
+])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_a_nan_query_stays_nan(hq, hk, d, new, lens, dtype):
+    """However many SMs share its keys; the rows beside it are as without it."""
+    b = Batch(new, lens, hq, hk, d, 64, dtype, seed=hk).fill()
+    kv = b.handle()
+    good, good_lse = kv.paged_attention(b.q, b.k_cache, b.v_cache, want_lse=True)
+    kv.check()
+    b.assert_attends(good, good_lse)
+    for token, head in ((0, 0), (b.t - 1, hq - 1), (b.t // 2, hq // 2)):
+        q = b.q.clone()
+        q[token, head, d // 2] = float("nan")
+        out, lse = kv.paged_attention(q, b.k_cache, b.v_cache, want_lse=True)
+        kv.check()
+        assert bool(out[token, head].isnan().all()) and bool(lse[token, head].isnan())
+        out[token, head], lse[token, head] = good[token, head], good_lse[token, head]
+        assert torch.equal(out, good) and torch.equal(lse, good_lse)
+    kv.close()
