@@ -869,7 +869,9 @@ class SMetricKV:
             if cos_sin.dtype != self._f32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
                 raise ValueError("cos_sin must be torch.float32 [positions, rot_dim], contiguous")
             rows, rot = cos_sin.shape
-            table = cos_sin.data_ptr() if rows and rot else None
+            # (a table without rows has no address, but NULL would say that there is no table: every token is
+            # past its end, and no row is read)
+            table = (cos_sin.data_ptr() if rows else 16) if rot else None
         return smetric_kv_transform(table, rows or 0, self._norm(q_norm), self._norm(k_norm), eps, rot or 0,
                                     SMETRIC_KV_INTERLEAVED if interleaved else 0, 0)
 

@@ -43,3 +43,20 @@ def test_a_nan_query_stays_nan(hq, hk, d, new, lens, dtype):
         out[token, head], lse[token, head] = good[token, head], good_lse[token, head]
         assert torch.equal(out, good) and torch.equal(lse, good_lse)
     kv.close()
+
+
+@pytest.mark.parametrize("tokens", [0, 1, 5])
+def test_a_table_without_rows_latches_every_token(tokens):
+    """Every position is past its end: nothing is left unrotated without a word."""
+    b = Batch([tokens], [tokens + 20], 4, 2, 64, 16, junk=9.0)
+    kv = b.handle()
+    k, empty, late = b.q[:, :2] + 1, table(0, 64), pkg.SMETRIC_ERR_OVERFLOW if tokens else pkg.SMETRIC_OK
+    q_out = torch.full_like(b.q, 5.0)
+    kv.append(b.k_cache, b.v_cache, k, k, q=b.q, q_out=q_out, cos_sin=empty)
+    assert kv.status() == late
+    assert bool((b.k_cache == 9).all()) and bool((b.v_cache == 9).all()) and bool((q_out == 5).all())
+    kv.qk_norm_rope(b.q, None, torch.arange(tokens, dtype=torch.int32, device=DEV), cos_sin=empty, q_out=q_out)
+    assert kv.status() == late and bool((q_out == 5).all())
+    kv.append(b.k_cache, b.v_cache, k, k, cos_sin=table(30, 0))  # a rotation of no elements is none
+    assert kv.status() == pkg.SMETRIC_OK and int((b.k_cache != 9).any(-1).sum()) == 2 * tokens
+    kv.close()
