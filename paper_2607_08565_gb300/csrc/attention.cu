@@ -472,7 +472,7 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Wal
     // under the swizzle.)
     const auto clear = [&](uint32_t place, int j) {
       const int32_t key = (it.tb + j) * kTile;
-      if (key >= lo && key + kTile <= hi) return;
+      if (key >= lo && hi - key >= kTile) return;  // (key + kTile may pass 32 bits)
       const uint32_t at = ring + stage(place) * HALVES * kHalf;
       const int before = max(lo - key, 0), after = min(hi - key, kTile);
 #pragma unroll

@@ -60,3 +60,38 @@ def test_a_table_without_rows_latches_every_token(tokens):
     kv.append(b.k_cache, b.v_cache, k, k, cos_sin=table(30, 0))  # a rotation of no elements is none
     assert kv.status() == pkg.SMETRIC_OK and int((b.k_cache != 9).any(-1).sum()) == 2 * tokens
     kv.close()
+
+
+@pytest.mark.parametrize("window", [100, 400])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_the_longest_sequence(window, dtype):
+    """A request of 2^31 - 1 tokens, of which a window is seen: NaN in the one
+    slot past its end and before the window."""
+    d, page, new, kv_len = 16, 256, 3, 2 ** 31 - 1
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, generator=g, device=DEV).to(dtype)  # noqa: E731
+    pages = torch.full((1, 2 ** 31 // page), -7, dtype=torch.int32, device=DEV)
+    pages[0, -2:] = torch.tensor([1, 2], dtype=torch.int32)
+    k_cache, v_cache = (torch.full((4, page, 1, d), float("nan"), dtype=dtype, device=DEV) for _ in range(2))
+    last = 2 * page - 1  # places in the two pages that are seen, in a row: the one past the end
+    for c in (k_cache, v_cache):
+        c[1:3].view(2 * page, 1, d)[last - new - window + 1:last - new] = rnd(window - 1, 1, d)
+    k, v, q = rnd(new, 1, d), rnd(new, 1, d), rnd(new, 2, d)
+    kv = pkg.SMetricKV(d, 2, 1, page, 4, 1, new, dtype=dtype)
+    kv.plan(torch.tensor([0, new], device=DEV), torch.tensor([kv_len], dtype=torch.int32, device=DEV), pages, new, window=window)
+    kv.append(k_cache, v_cache, k, v)
+    out, lse = kv.paged_attention(q, k_cache, v_cache, want_lse=True)
+    kv.check()
+    keys, values = (c[1:3].view(2 * page, d) for c in (k_cache, v_cache))
+    for x, y in ((keys, k), (values, v)):
+        assert torch.equal(x[last - new:last], y[:, 0]) and bool(x[last].isnan().all())
+    for i in range(new):
+        end = last - new + i + 1  # past its own place
+        x = q[i].double() @ keys[end - window:end].double().T * d ** -0.5
+        p = x.softmax(-1)
+        want, mag = p @ values[end - window:end].double(), p @ values[end - window:end].double().abs()
+        u = UNIT[dtype]  # (the bound that the other attention tests use)
+        assert bool(((out[i].double() - want).abs() <= u * want.abs() + (u + 2.0 ** -12) * mag).all())
+        assert bool(((lse[i].double() - x.logsumexp(-1)).abs() <= 2.0 ** -12).all())
+    kv.close()
