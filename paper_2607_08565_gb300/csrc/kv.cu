@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   } else {
     pos = a.positions[t];
   }
-  if (a.table && (pos < 0 || pos >= a.table_rows)) {
+  if (pos < 0 || (a.table && pos >= a.table_rows)) {
     if (lane == 0 && share == 0) latch_error(a.status, SMETRIC_ERR_OVERFLOW);
     return;
   }

@@ -95,3 +95,20 @@ def test_the_longest_sequence(window, dtype):
         assert bool(((out[i].double() - want).abs() <= u * want.abs() + (u + 2.0 ** -12) * mag).all())
         assert bool(((lse[i].double() - x.logsumexp(-1)).abs() <= 2.0 ** -12).all())
     kv.close()
+
+
+@pytest.mark.parametrize("cos_sin", [False, True])
+def test_negative_positions_are_left_out(cos_sin):
+    """With a table and without one."""
+    q = torch.randn(4, 2, 64, device=DEV).to(BF)
+    w = torch.ones(64, dtype=BF, device=DEV)
+    kv = pkg.SMetricKV(64, 2, 2, 16, 1, 1, 1)
+    for pos in ([0, -1, 17, 3], [-2 ** 31, 1, 2, 3]):
+        at = torch.tensor(pos, dtype=torch.int32, device=DEV)
+        q_out, k_out = torch.full_like(q, 9.0), torch.full_like(q, 9.0)
+        kv.qk_norm_rope(q, q, at, cos_sin=table(18, 64) if cos_sin else None, q_norm=w, q_out=q_out, k_out=k_out)
+        assert kv.status() == pkg.SMETRIC_ERR_OVERFLOW
+        left = torch.tensor(pos, device=DEV) < 0
+        for out in (q_out, k_out):
+            assert torch.equal((out == 9).all(-1).all(-1), left)
+    kv.close()
