@@ -848,10 +848,11 @@ class SMetricKV:
                                 strides[2] if shape[2] > 1 else 0)
 
     def _new_heads(self, like):
-        """A tensor like `like` for a call to fill, and its description."""
+        """A tensor like `like` for a call to fill, and its description (as for _heads)."""
         out = self._like(like)
+        tokens, heads, _ = out.shape
         token, head, _ = out.stride()
-        return out, smetric_heads(out.data_ptr(), token, head)
+        return out, smetric_heads(out.data_ptr(), token if tokens > 1 else 0, head if heads > 1 else 0)
 
     def _stream(self, stream) -> Optional[int]:
         return self._raw_stream(self._device) if stream is None else _stream(stream)

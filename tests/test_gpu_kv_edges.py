@@ -112,3 +112,42 @@ def test_negative_positions_are_left_out(cos_sin):
         for out in (q_out, k_out):
             assert torch.equal((out == 9).all(-1).all(-1), left)
     kv.close()
+
+
+def _views(tokens, heads, d, seed=0):
+    """Random [tokens, heads, d] tensors whose dimension of one, if any, comes first, second or last in memory."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    flat = torch.randn(tokens * heads, d, generator=g, device=DEV).to(BF)
+    if tokens == 1:
+        yield flat.unsqueeze(2).permute(2, 0, 1)  # a token stride of 1
+        yield flat.unsqueeze(1).transpose(0, 1)
+        yield torch.randn(heads, 9, d, generator=g, device=DEV).to(BF)[:, 4:5].transpose(0, 1)
+    if heads == 1:
+        yield flat.unsqueeze(2).transpose(1, 2)  # a head stride of 1
+        yield flat.unsqueeze(0).transpose(0, 1)
+        yield torch.randn(tokens, 3 * d, generator=g, device=DEV).to(BF)[:, d:2 * d].unsqueeze(1)
+
+
+@pytest.mark.parametrize("tokens,hq", [(1, 1), (1, 4), (7, 1)])
+def test_views_of_one_token_or_one_head(tokens, hq):
+    """The stride of a dimension of one is arbitrary, and torch gives a new tensor the same one."""
+    b = Batch([tokens], [tokens + 300], hq, 1, 64, 16).fill()
+    kv = b.handle()
+    pos = torch.arange(tokens, dtype=torch.int32, device=DEV)
+    kw = dict(cos_sin=table(400, 64), q_norm=torch.ones(64, dtype=BF, device=DEV))
+    for q in _views(tokens, hq, 64):
+        plain = q.contiguous().view(-1).view(tokens, hq, 64).clone()
+        for k in _views(tokens, 1, 64, seed=1) if tokens > 1 else [torch.ones(1, 1, 64, dtype=BF, device=DEV)]:
+            got = kv.qk_norm_rope(q, k, pos, **kw)
+            want = kv.qk_norm_rope(plain, k.contiguous().view(-1).view(tokens, 1, 64).clone(), pos, **kw)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+            caches = [(b.k_cache.clone(), b.v_cache.clone()) for _ in range(2)]
+            got = kv.append(*caches[0], k, k, q=q, **kw)
+            want = kv.append(*caches[1], k.contiguous().clone(), k.contiguous().clone(), q=plain, **kw)
+            assert torch.equal(got, want)
+            assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip(*caches))
+        got, want = (kv.paged_attention(x, b.k_cache, b.v_cache, want_lse=True) for x in (q, plain))
+        kv.check()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    kv.close()
