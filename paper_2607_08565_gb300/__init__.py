@@ -789,6 +789,9 @@ class SMetricKV:
         kv.append(k_cache, v_cache, k, v, q=q, q_out=q, cos_sin=table, q_norm=wq, k_norm=wk)
         out = kv.paged_attention(q, k_cache, v_cache)
         kv.check()
+
+    A call on another stream than torch's current one (stream=) allocates its
+    new outputs there; the caller orders the two streams, as for its inputs.
     """
 
     def __init__(self, head_dim: int, num_q_heads: int, num_kv_heads: int, page_size: int, num_pages: int,
@@ -807,6 +810,7 @@ class SMetricKV:
         self._lib, self._raw_stream, self._device = lib(), torch._C._cuda_getCurrentRawStream, torch.cuda.current_device()
         self._dim, self._f32, self._i32 = head_dim, torch.float32, torch.int32
         self._empty, self._like = torch.empty, torch.empty_like
+        self._others = {}  # torch's objects for streams given by a call, by their raw ones
         self._cache_shape = (num_pages, page_size, num_kv_heads, head_dim)
 
     def close(self):
@@ -847,15 +851,41 @@ class SMetricKV:
         return smetric_kv_cache(k_cache.data_ptr(), v_cache.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1],
                                 strides[2] if shape[2] > 1 else 0)
 
-    def _new_heads(self, like):
+    def _stream(self, stream):
+        """A call's stream: (raw, None), or (raw, torch's object for it) where it is not torch's current one."""
+        now = self._raw_stream(self._device)
+        if stream is None:
+            return now, None
+        raw = _stream(stream)
+        if raw == 1:  # (the legacy default stream by its other name)
+            raw = 0
+        if raw == now:
+            return raw, None
+        other = self._others.get(raw)
+        if other is None:
+            import torch
+            other = self._others[raw] = torch.cuda.ExternalStream(raw, device=self._device)
+        return raw, other
+
+    def _new(self, other, make, *args, **kw):
+        """A new tensor for a call on the stream `other` to fill (None: torch's
+        current one). Its memory is that stream's, as what was done with it
+        before may still wait on the current one; and goes back to it only when
+        the current stream is done with it too."""
+        if other is None:
+            return make(*args, **kw)
+        import torch
+        with torch.cuda.stream(other):
+            x = make(*args, **kw)
+        x.record_stream(torch.cuda.current_stream(self._device))
+        return x
+
+    def _new_heads(self, like, other):
         """A tensor like `like` for a call to fill, and its description (as for _heads)."""
-        out = self._like(like)
+        out = self._like(like) if other is None else self._new(other, self._like, like)
         tokens, heads, _ = out.shape
         token, head, _ = out.stride()
         return out, smetric_heads(out.data_ptr(), token if tokens > 1 else 0, head if heads > 1 else 0)
-
-    def _stream(self, stream) -> Optional[int]:
-        return self._raw_stream(self._device) if stream is None else _stream(stream)
 
     def _norm(self, w) -> Optional[int]:
         if w is None:
@@ -907,15 +937,16 @@ class SMetricKV:
         hk, hq = c.num_kv_heads, c.num_q_heads
         caches, kh, vh, qh = (self._cache(k_cache, v_cache), self._heads(k, hk, t, "k"), self._heads(v, hk, t, "v"),
                               self._heads(q, hq, t, "q"))
+        raw, other = self._stream(stream)
         if q is None:
             q_out = None
         if q is not None and q_out is None:
-            q_out, oh = self._new_heads(q)
+            q_out, oh = self._new_heads(q, other)
         else:
             oh = self._heads(q_out, hq, t, "q_out")
         _check(self._lib.smetric_kv_append(self.handle, caches, kh, vh, qh, oh,
-                                           self._transform(cos_sin, interleaved, q_norm, k_norm, eps),
-                                           self._stream(stream)), "smetric_kv_append")
+                                           self._transform(cos_sin, interleaved, q_norm, k_norm, eps), raw),
+               "smetric_kv_append")
         return q_out
 
     def qk_norm_rope(self, q, k, positions, cos_sin=None, interleaved=False, q_norm=None, k_norm=None, eps=1e-6,
@@ -927,21 +958,22 @@ class SMetricKV:
             raise ValueError("positions must be torch.int32, contiguous")
         hk, hq = c.num_kv_heads, c.num_q_heads
         qh, kh = self._heads(q, hq, t, "q"), self._heads(k, hk, t, "k")
+        raw, other = self._stream(stream)
         if q is None:
             q_out = None
         if k is None:
             k_out = None
         if q is not None and q_out is None:
-            q_out, qo = self._new_heads(q)
+            q_out, qo = self._new_heads(q, other)
         else:
             qo = self._heads(q_out, hq, t, "q_out")
         if k is not None and k_out is None:
-            k_out, ko = self._new_heads(k)
+            k_out, ko = self._new_heads(k, other)
         else:
             ko = self._heads(k_out, hk, t, "k_out")
         _check(self._lib.smetric_qk_norm_rope(self.handle, qh, kh, positions.data_ptr() if t else None, t,
                                               self._transform(cos_sin, interleaved, q_norm, k_norm, eps), qo, ko,
-                                              self._stream(stream)), "smetric_qk_norm_rope")
+                                              raw), "smetric_qk_norm_rope")
         return q_out, k_out
 
     def paged_attention(self, q, k_cache, v_cache, scale=None, out=None, want_lse=False, stream=None):
@@ -950,14 +982,15 @@ class SMetricKV:
         (float32 [tokens, num_q_heads])."""
         t, hq = self._planned(), self.cfg.num_q_heads
         caches, qh = self._cache(k_cache, v_cache), self._heads(q, hq, t, "q")
+        raw, other = self._stream(stream)
         if out is None:
-            out, oh = self._new_heads(q)
+            out, oh = self._new_heads(q, other)
         else:
             oh = self._heads(out, hq, t, "out")
-        lse = self._empty((t, hq), dtype=self._f32, device=q.device) if want_lse else None
+        lse = self._new(other, self._empty, (t, hq), dtype=self._f32, device=q.device) if want_lse else None
         _check(self._lib.smetric_paged_attention(self.handle, caches, qh,
                                                  self._dim ** -0.5 if scale is None else scale, oh,
-                                                 lse.data_ptr() if want_lse and t else None, self._stream(stream)),
+                                                 lse.data_ptr() if want_lse and t else None, raw),
                "smetric_paged_attention")
         return (out, lse) if want_lse else out
 

@@ -151,3 +151,83 @@ def test_views_of_one_token_or_one_head(tokens, hq):
         kv.check()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     kv.close()
+
+
+SLEEP = 200_000_000  # cycles: about 0.1 s, longer than the host takes to go on
+
+
+def _calls(kv, b, stream):
+    """Every call that allocates, on a stream: its new tensors."""
+    pos = torch.arange(b.t, dtype=torch.int32, device=DEV)
+    k, v = (torch.cat([x[-n:] for x, n in zip(xs, b.new)]) for xs in (b.keys, b.values))
+    torch.cuda.synchronize()
+    return [
+        lambda: list(kv.paged_attention(b.q, b.k_cache, b.v_cache, want_lse=True, stream=stream)),
+        lambda: [kv.append(b.k_cache, b.v_cache, k, v, q=b.q, stream=stream)],
+        lambda: list(kv.qk_norm_rope(b.q, k, pos, stream=stream)),
+    ]
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_new_outputs_on_another_stream(raw):
+    """Their memory is not handed out again before that stream has written it,
+    nor written before the current stream is done with its last owner."""
+    b = Batch([40, 1], [300, 70], 8, 2, 64, 16).fill()
+    s = torch.cuda.Stream()
+    kv = b.handle()
+    for call in _calls(kv, b, s.cuda_stream if raw else s):
+        got = call()
+        torch.cuda.synchronize()
+        like = [x.clone() for x in got]
+        del got
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        # dropped before they are written
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(SLEEP)
+        call()
+        others = [torch.full_like(x, 7.0) for x in like for _ in range(2)]
+        torch.cuda.synchronize()
+        assert all(bool((x == 7).all()) for x in others)
+        del others
+        torch.cuda.empty_cache()
+        # memory whose last owner is still being read
+        owners = [torch.full_like(x, 3.0) for x in like for _ in range(2)]
+        copies = [torch.empty_like(x) for x in owners]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(SLEEP)
+        for c, x in zip(copies, owners):
+            c.copy_(x)
+        del owners, x
+        got = call()
+        torch.cuda.synchronize()
+        assert all(bool((c == 3).all()) for c in copies)
+        assert all(torch.equal(x, y) for x, y in zip(got, like))
+        del got, copies, like
+    kv.check()
+    kv.close()
+
+
+def test_new_outputs_used_on_the_current_stream():
+    """Read there while the stream that wrote them allocates again."""
+    b = Batch([40, 1], [300, 70], 8, 2, 64, 16).fill()
+    s = torch.cuda.Stream()
+    kv = b.handle()
+    for call in _calls(kv, b, s):
+        got = call()
+        torch.cuda.current_stream().wait_stream(s)
+        torch.cuda.synchronize()
+        want = [x.clone() for x in got]
+        copies = [torch.empty_like(x) for x in got]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(SLEEP)
+        for c, x in zip(copies, got):
+            c.copy_(x)
+        del got, x
+        with torch.cuda.stream(s):
+            others = [torch.full_like(x, 7.0) for x in want for _ in range(2)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(c, w) for c, w in zip(copies, want))
+        del others, want, copies
+    kv.check()
+    kv.close()
