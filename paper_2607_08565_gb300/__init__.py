@@ -872,12 +872,16 @@ class SMetricKV:
         current one). Its memory is that stream's, as what was done with it
         before may still wait on the current one; and goes back to it only when
         the current stream is done with it too."""
-        if other is None:
-            return make(*args, **kw)
         import torch
-        with torch.cuda.stream(other):
+        if other is None or torch.cuda.current_device() != self._device:  # (a call that is refused)
+            return make(*args, **kw)
+        now = torch.cuda.current_stream(self._device)
+        torch.cuda.set_stream(other)  # (the context manager costs the host 5 us more)
+        try:
             x = make(*args, **kw)
-        x.record_stream(torch.cuda.current_stream(self._device))
+        finally:
+            torch.cuda.set_stream(now)
+        x.record_stream(now)
         return x
 
     def _new_heads(self, like, other):
