@@ -805,7 +805,9 @@ class SMetricKV:
                                      max_batch_requests, max_batch_tokens)
         self.handle = smetric_kv_create(self.cfg)
         self._n_tokens = None
-        self._kept = None
+        # the plan's tensors; torch's current stream when they were given; reads of them on others, as events
+        # after the last one; and the tensors of plans before, with such events
+        self._kept, self._home, self._reads, self._dropped = None, None, {}, []
         # (what the calls use each time: a step's few tokens are bound by the host)
         self._lib, self._raw_stream, self._device = lib(), torch._C._cuda_getCurrentRawStream, torch.cuda.current_device()
         self._dim, self._f32, self._i32 = head_dim, torch.float32, torch.int32
@@ -815,8 +817,9 @@ class SMetricKV:
 
     def close(self):
         if getattr(self, "handle", None):
-            smetric_kv_destroy(self.handle)
+            smetric_kv_destroy(self.handle)  # (waits for the device)
             self.handle = None
+            self._kept, self._reads, self._dropped = None, {}, []
 
     def __enter__(self):
         return self
@@ -861,11 +864,43 @@ class SMetricKV:
             raw = 0
         if raw == now:
             return raw, None
-        other = self._others.get(raw)
-        if other is None:
+        return raw, self._object(raw)
+
+    def _object(self, raw: int):
+        s = self._others.get(raw)
+        if s is None:
             import torch
-            other = self._others[raw] = torch.cuda.ExternalStream(raw, device=self._device)
-        return raw, other
+            s = self._others[raw] = torch.cuda.ExternalStream(raw, device=self._device)
+        return s
+
+    def _read(self, raw: int, other):
+        """Notes that a call on a stream reads the plan's tensors. Where it is not
+        the one that they were given on, they are to outlive the call."""
+        if raw == self._home:
+            return
+        import torch
+        now = torch.cuda.current_stream(self._device)
+        if other is not None:
+            torch.cuda.set_stream(other)
+        try:
+            if not torch.cuda.is_current_stream_capturing():
+                done = self._reads.get(raw)
+                if done is None:
+                    done = self._reads[raw] = torch.cuda.Event()
+                done.record(self._object(raw))
+        finally:
+            if other is not None:
+                torch.cuda.set_stream(now)
+
+    def _keep(self, tensors):
+        """Holds a plan's tensors, and those of plans before it that are still read on another stream."""
+        import torch
+        if self._reads:
+            self._dropped.append((self._kept, list(self._reads.values())))
+            self._reads = {}
+        if self._dropped and not torch.cuda.is_current_stream_capturing():
+            self._dropped = [x for x in self._dropped if not all(e.query() for e in x[1])]
+        self._kept, self._home = tensors, self._raw_stream(self._device)
 
     def _new(self, other, make, *args, **kw):
         """A new tensor for a call on the stream `other` to fill (None: torch's
@@ -912,8 +947,10 @@ class SMetricKV:
 
     def plan(self, offsets, kv_lens, pages, n_tokens: int, window: int = 0, stream=None):
         """Plans a batch: offsets int64 [n+1], kv_lens int32 [n], pages int32
-        [n, max_pages] (row stride free). The tensors stay referenced until
-        the next plan."""
+        [n, max_pages] (row stride free). The handle keeps the tensors until
+        the next plan, and until what read them on another stream than torch's
+        current one at this call is done; those that a captured call reads are
+        the graph's owner's to keep."""
         import torch
         n = kv_lens.numel()
         if offsets.dtype != torch.int64 or offsets.numel() != n + 1:
@@ -923,9 +960,12 @@ class SMetricKV:
         if pages.shape[1] > 1 and pages.stride(1) != 1:
             raise ValueError("a request's pages must be contiguous")
         most = pages.shape[1]
+        raw, other = self._stream(stream)
         smetric_kv_plan(self.handle, offsets, n, n_tokens, kv_lens, pages.data_ptr() if pages.numel() else None, most,
-                        pages.stride(0) if n > 1 else most, window, stream)
-        self._n_tokens, self._kept = n_tokens, (offsets, kv_lens, pages)
+                        pages.stride(0) if n > 1 else most, window, raw)
+        self._n_tokens = n_tokens
+        self._keep((offsets, kv_lens, pages))
+        self._read(raw, other)
 
     def _planned(self) -> int:
         if self._n_tokens is None:
@@ -996,6 +1036,7 @@ class SMetricKV:
                                                  self._dim ** -0.5 if scale is None else scale, oh,
                                                  lse.data_ptr() if want_lse and t else None, raw),
                "smetric_paged_attention")
+        self._read(raw, other)
         return (out, lse) if want_lse else out
 
     def status(self, stream=None) -> int:

@@ -231,3 +231,36 @@ def test_new_outputs_used_on_the_current_stream():
         del others, want, copies
     kv.check()
     kv.close()
+
+
+@pytest.mark.parametrize("how", ["stream", "raw", "current"])
+def test_a_plans_tensors_outlive_the_attention_on_another_stream(how):
+    """A new plan drops them: their memory is not handed out again before an
+    attention that still waits on that stream has read the page numbers."""
+    b = Batch([1, 40, 1], [300, 800, 70], 8, 2, 64, 16).fill()
+    kv = b.handle()
+    want = kv.paged_attention(b.q, b.k_cache, b.v_cache)
+    kv.check()
+    s = torch.cuda.Stream()
+    out = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    offsets, lens, pages = b.offsets.clone(), b.kv_lens.clone(), b.pages.contiguous().clone()
+    stream = s.cuda_stream if how == "raw" else s
+    torch.cuda.synchronize()
+    kv.plan(offsets, lens, pages, b.t, stream=stream)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(SLEEP)
+    if how == "current":
+        with torch.cuda.stream(s):
+            kv.paged_attention(b.q, b.k_cache, b.v_cache, out=out)
+    else:
+        kv.paged_attention(b.q, b.k_cache, b.v_cache, out=out, stream=stream)
+    kv.plan(b.offsets, b.kv_lens, b.pages, b.t, stream=stream)
+    like = pages.shape
+    del offsets, lens, pages
+    others = [torch.zeros(like, dtype=torch.int32, device=DEV) for _ in range(4)]  # (a page that there is)
+    torch.cuda.synchronize()
+    kv.check()
+    assert torch.equal(out, want) and all(bool((x == 0).all()) for x in others)
+    kv.close()
