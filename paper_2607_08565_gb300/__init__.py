@@ -790,8 +790,9 @@ class SMetricKV:
         out = kv.paged_attention(q, k_cache, v_cache)
         kv.check()
 
-    A call on another stream than torch's current one (stream=) allocates its
-    new outputs there; the caller orders the two streams, as for its inputs.
+    Tensors are on the device that was current when the object was made. A call
+    on another stream than torch's current one (stream=) allocates its new
+    outputs there; the caller orders the two streams, as for its inputs.
     """
 
     def __init__(self, head_dim: int, num_q_heads: int, num_kv_heads: int, page_size: int, num_pages: int,
@@ -836,8 +837,8 @@ class SMetricKV:
     def _heads(self, x, heads: int, n_tokens: int, name: str) -> smetric_heads:
         if x is None:
             return _NO_HEADS
-        if x.dtype != self.dtype or x.shape != (n_tokens, heads, self._dim):
-            raise ValueError(f"{name} must be {self.dtype} [{n_tokens}, {heads}, {self._dim}]")
+        if x.dtype != self.dtype or x.shape != (n_tokens, heads, self._dim) or x.get_device() != self._device:
+            raise ValueError(f"{name} must be {self.dtype} [{n_tokens}, {heads}, {self._dim}] on cuda:{self._device}")
         token, head, one = x.stride()
         if one != 1 and x.numel():
             raise ValueError(f"{name}: the elements of a head must be contiguous")
@@ -846,8 +847,10 @@ class SMetricKV:
 
     def _cache(self, k_cache, v_cache) -> smetric_kv_cache:
         shape = self._cache_shape
-        if k_cache.dtype != self.dtype or v_cache.dtype != self.dtype or k_cache.shape != shape or v_cache.shape != shape:
-            raise ValueError(f"caches must be {self.dtype} {list(shape)}")
+        here = self._device
+        if (k_cache.dtype != self.dtype or v_cache.dtype != self.dtype or k_cache.shape != shape or v_cache.shape != shape or
+                k_cache.get_device() != here or v_cache.get_device() != here):
+            raise ValueError(f"caches must be {self.dtype} {list(shape)} on cuda:{here}")
         strides = k_cache.stride()
         if v_cache.stride() != strides or strides[3] != 1:
             raise ValueError("caches must have equal strides and contiguous heads")
@@ -929,15 +932,16 @@ class SMetricKV:
     def _norm(self, w) -> Optional[int]:
         if w is None:
             return None
-        if w.dtype != self.dtype or w.numel() != self._dim or not w.is_contiguous():
-            raise ValueError(f"norm weights must be {self.dtype} [{self._dim}], contiguous")
+        if w.dtype != self.dtype or w.numel() != self._dim or not w.is_contiguous() or w.get_device() != self._device:
+            raise ValueError(f"norm weights must be {self.dtype} [{self._dim}], contiguous, on cuda:{self._device}")
         return w.data_ptr()
 
     def _transform(self, cos_sin, interleaved, q_norm, k_norm, eps) -> smetric_kv_transform:
         rows = rot = table = None
         if cos_sin is not None:
-            if cos_sin.dtype != self._f32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
-                raise ValueError("cos_sin must be torch.float32 [positions, rot_dim], contiguous")
+            if (cos_sin.dtype != self._f32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous() or
+                    cos_sin.get_device() != self._device):
+                raise ValueError(f"cos_sin must be torch.float32 [positions, rot_dim], contiguous, on cuda:{self._device}")
             rows, rot = cos_sin.shape
             # (a table without rows has no address, but NULL would say that there is no table: every token is
             # past its end, and no row is read)
@@ -957,6 +961,8 @@ class SMetricKV:
             raise ValueError("offsets must be torch.int64 [requests + 1]")
         if kv_lens.dtype != torch.int32 or pages.dtype != torch.int32 or pages.dim() != 2 or pages.shape[0] != n:
             raise ValueError("kv_lens must be torch.int32 [requests] and pages torch.int32 [requests, max_pages]")
+        if any(x.get_device() != self._device for x in (offsets, kv_lens, pages)):
+            raise ValueError(f"offsets, kv_lens and pages must be on cuda:{self._device}")
         if pages.shape[1] > 1 and pages.stride(1) != 1:
             raise ValueError("a request's pages must be contiguous")
         most = pages.shape[1]
@@ -998,8 +1004,8 @@ class SMetricKV:
         """The norms and the rotation alone, at int32 positions; q or k may be
         None. Returns (q_out, k_out), new tensors unless given."""
         t, c = positions.numel(), self.cfg
-        if positions.dtype != self._i32 or not positions.is_contiguous():
-            raise ValueError("positions must be torch.int32, contiguous")
+        if positions.dtype != self._i32 or not positions.is_contiguous() or positions.get_device() != self._device:
+            raise ValueError(f"positions must be torch.int32, contiguous, on cuda:{self._device}")
         hk, hq = c.num_kv_heads, c.num_q_heads
         qh, kh = self._heads(q, hq, t, "q"), self._heads(k, hk, t, "k")
         raw, other = self._stream(stream)
