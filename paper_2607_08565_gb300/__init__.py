@@ -922,12 +922,11 @@ class SMetricKV:
         x.record_stream(now)
         return x
 
-    def _new_heads(self, like, other):
+    def _new_heads(self, like, heads: int, n_tokens: int, other):
         """A tensor like `like` for a call to fill, and its description (as for _heads)."""
         out = self._like(like) if other is None else self._new(other, self._like, like)
-        tokens, heads, _ = out.shape
         token, head, _ = out.stride()
-        return out, smetric_heads(out.data_ptr(), token if tokens > 1 else 0, head if heads > 1 else 0)
+        return out, smetric_heads(out.data_ptr(), token if n_tokens > 1 else 0, head if heads > 1 else 0)
 
     def _norm(self, w) -> Optional[int]:
         if w is None:
@@ -991,7 +990,7 @@ class SMetricKV:
         if q is None:
             q_out = None
         if q is not None and q_out is None:
-            q_out, oh = self._new_heads(q, other)
+            q_out, oh = self._new_heads(q, hq, t, other)
         else:
             oh = self._heads(q_out, hq, t, "q_out")
         _check(self._lib.smetric_kv_append(self.handle, caches, kh, vh, qh, oh,
@@ -1014,11 +1013,11 @@ class SMetricKV:
         if k is None:
             k_out = None
         if q is not None and q_out is None:
-            q_out, qo = self._new_heads(q, other)
+            q_out, qo = self._new_heads(q, hq, t, other)
         else:
             qo = self._heads(q_out, hq, t, "q_out")
         if k is not None and k_out is None:
-            k_out, ko = self._new_heads(k, other)
+            k_out, ko = self._new_heads(k, hk, t, other)
         else:
             ko = self._heads(k_out, hk, t, "k_out")
         _check(self._lib.smetric_qk_norm_rope(self.handle, qh, kh, positions.data_ptr() if t else None, t,
@@ -1034,7 +1033,7 @@ class SMetricKV:
         caches, qh = self._cache(k_cache, v_cache), self._heads(q, hq, t, "q")
         raw, other = self._stream(stream)
         if out is None:
-            out, oh = self._new_heads(q, other)
+            out, oh = self._new_heads(q, hq, t, other)
         else:
             oh = self._heads(out, hq, t, "out")
         lse = self._new(other, self._empty, (t, hq), dtype=self._f32, device=q.device) if want_lse else None
