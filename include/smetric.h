@@ -565,7 +565,8 @@ int64_t smetric_launch_count(const smetric_index* idx);
  * different streams. Errors as for an index: host-detectable ones return with
  * nothing enqueued, device-detectable ones are latched in the handle and
  * reported by smetric_kv_status. Arrays of heads and caches need 16-byte
- * aligned pointers and strides that are multiples of 8 elements. */
+ * aligned pointers and strides that are multiples of 8 elements, arrays of
+ * whole numbers and d_lse the alignment of their elements. */
 typedef struct smetric_kv smetric_kv; /* opaque, library-owned */
 
 #define SMETRIC_BF16 0
@@ -640,7 +641,7 @@ int smetric_kv_destroy(smetric_kv* kv);
  *   d_kv_lens  int32 [n_requests], at least the request's new tokens.
  *   d_pages    int32 rows of max_pages page numbers (entries past a request's
  *              length, and entries that lie before its window, are not
- *              used), 4-byte aligned, row stride pages_stride >= max_pages.
+ *              used), row stride pages_stride >= max_pages.
  *   window     0, or how many keys a query sees at most, its own among them.
  * d_pages stays in use until the next plan: the attention reads it. Bad
  * offsets or lengths latch INVALID_ARG and the batch counts as one of no

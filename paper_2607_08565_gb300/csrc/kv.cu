@@ -473,6 +473,12 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   heads(a.q, static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride, a.q_out.head_stride, q0, rq, a.hq, a.q_norm, y);
 }
 
+// At a whole number of its elements, as loads need.
+template <typename E>
+bool aligned(const E* p) {
+  return reinterpret_cast<uintptr_t>(p) % sizeof(E) == 0;
+}
+
 bool transform_ok(const smetric_kv* kv, const smetric_kv_transform& t) {
   if (t.reserved || (t.flags & ~SMETRIC_KV_INTERLEAVED) || t.rot_dim < 0 || t.rot_dim > kv->cfg.head_dim ||
       t.rot_dim % 16 || t.table_rows < 0)
@@ -606,7 +612,8 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
   if (rc) return rc;
   if (n_requests < 0 || n_requests > kv->cfg.max_batch_requests || n_tokens < 0 ||
       n_tokens > kv->cfg.max_batch_tokens || max_pages < 0 || pages_stride < max_pages || window < 0 ||
-      (n_requests > 0 && (!d_offsets || !d_kv_lens || (max_pages > 0 && !d_pages))))
+      (n_requests > 0 && (!d_offsets || !d_kv_lens || (max_pages > 0 && !d_pages))) || !aligned(d_offsets) ||
+      !aligned(d_kv_lens) || !aligned(d_pages))
     return SMETRIC_ERR_INVALID_ARG;
   kv->planned = false;
   PlanArgs a = {};
@@ -674,7 +681,8 @@ int smetric_qk_norm_rope(smetric_kv* kv, smetric_heads q, smetric_heads k, const
   if (rc) return rc;
   if (n_tokens < 0 || n_tokens > SMETRIC_KV_MAX_TOKENS || !transform_ok(kv, t) ||
       (q.d_data && (!heads_ok(q, n_tokens) || !heads_ok(q_out, n_tokens))) ||
-      (k.d_data && (!heads_ok(k, n_tokens) || !heads_ok(k_out, n_tokens))) || (n_tokens > 0 && !d_positions))
+      (k.d_data && (!heads_ok(k, n_tokens) || !heads_ok(k_out, n_tokens))) || (n_tokens > 0 && !d_positions) ||
+      !aligned(d_positions))
     return SMETRIC_ERR_INVALID_ARG;
   if (n_tokens == 0 || (!q.d_data && !k.d_data)) return SMETRIC_OK;
   HeadsArgs a = {};

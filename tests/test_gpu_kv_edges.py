@@ -264,3 +264,23 @@ def test_a_plans_tensors_outlive_the_attention_on_another_stream(how):
     kv.check()
     assert torch.equal(out, want) and all(bool((x == 0).all()) for x in others)
     kv.close()
+
+
+def test_unaligned_arrays_of_whole_numbers_are_refused():
+    b = Batch([3], [40], 4, 2, 64, 16).fill()
+    kv = b.handle()
+    arrays = [b.offsets, b.kv_lens, b.pages]
+    good = kv.paged_attention(b.q, b.k_cache, b.v_cache)
+    for i, by in ((0, 4), (0, 1), (1, 2), (2, 2), (2, 1)):
+        at = [x.data_ptr() for x in arrays]
+        at[i] += by
+        with pytest.raises(pkg.SmetricError):
+            pkg.smetric_kv_plan(kv.handle, at[0], 1, 3, at[1], at[2], 3, 3)
+    q = pkg.smetric_heads(b.q.data_ptr(), 4 * 64, 64)
+    for by in (1, 2, 3):
+        with pytest.raises(pkg.SmetricError):
+            pkg.smetric_qk_norm_rope(kv.handle, q, pkg.smetric_heads(), b.kv_lens.data_ptr() + by, 1, pkg.smetric_kv_transform(), q,
+                                     pkg.smetric_heads())
+    kv.check()
+    assert torch.equal(kv.paged_attention(b.q, b.k_cache, b.v_cache), good)  # the plan stands
+    kv.close()
