@@ -124,21 +124,27 @@ __device__ __forceinline__ bool mbar_test(uint64_t* b, uint32_t parity) {
       : "=r"(done) : "r"(smem_u32(b)), "r"(parity) : "memory");
   return done != 0;
 }
-__device__ __forceinline__ bool stopped(const Shared* sh) { return *(const volatile int32_t*)&sh->abort != 0; }
-// Waits for the phase of the given parity; gives up after kWaitCycles, or when
-// another wait of the CTA has. Callers go on either way (every loop is bounded
-// by the plan); outputs are then undefined and the error is latched.
+// Whether a wait of the CTA has run out. The warp votes: its lanes may read the
+// flag before and after another warp sets it, and have to go the same way.
+__device__ __forceinline__ bool stopped(const Shared* sh) {
+  return __any_sync(kFull, *(const volatile int32_t*)&sh->abort != 0);
+}
+// The warp waits for the phase of the given parity; gives up after kWaitCycles,
+// or when another wait of the CTA has. Callers go on either way (every loop is
+// bounded by the plan); outputs are then undefined and the error is latched.
 __device__ __forceinline__ void mbar_wait(uint64_t* b, uint32_t parity, Shared* sh, int32_t* status) {
-  if (mbar_test(b, parity)) return;
-  const long long start = clock64();
-  while (!mbar_try(b, parity)) {
-    if (stopped(sh)) return;
-    if (clock64() - start > kWaitCycles) {
-      *(volatile int32_t*)&sh->abort = 1;
-      latch_error(status, SMETRIC_ERR_CUDA);
-      return;
+  if (!mbar_test(b, parity)) {
+    const long long start = clock64();
+    while (!mbar_try(b, parity)) {
+      if (*(const volatile int32_t*)&sh->abort != 0) break;
+      if (clock64() - start > kWaitCycles) {
+        *(volatile int32_t*)&sh->abort = 1;
+        latch_error(status, SMETRIC_ERR_CUDA);
+        break;
+      }
     }
   }
+  __syncwarp();
 }
 // The same for the products in flight when the CTA gives up.
 __device__ __forceinline__ void mbar_drain(uint64_t* b, uint32_t parity) {
@@ -396,7 +402,8 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
         for (int t = 0; t < (it.pair ? 2 : 1); ++t, ++nq) {
           uint64_t* full = &b.q_full[nq & 1];
           if (nq > 1) mbar_wait(&b.q_empty[nq & 1], (nq / 2 - 1) & 1, sh, a.status);
-          if (lane == 0 && !stopped(sh)) {
+          const bool stop = stopped(sh);
+          if (lane == 0 && !stop) {
             mbar_expect(full, q_bytes);
 #pragma unroll
             for (int e = 0; e < HALVES; ++e)
