@@ -417,12 +417,6 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
     base += 2 * n;
     if (stopped(sh)) break;
   }
-  if (stopped(sh)) {  // copies in flight must land before the CTA ends
-    // (which stages have one pending is another warp's to know: a pause that is
-    // a thousand times as long as any copy takes)
-    const long long start = clock64();
-    while (clock64() - start < kWaitCycles / 1024) __nanosleep(1000);
-  }
 }
 
 // Issues the products, a step's (weights with values, then the half's next
@@ -865,6 +859,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   __syncwarp();
   fence_before();
   __syncthreads();
+  if (stopped(sh)) {
+    // Copies and products in flight must end before the CTA's memory goes. Which
+    // are pending is for the warps to know that have given up, or have issued them
+    // and gone on: a pause that is a thousand times as long as any takes.
+    const long long start = clock64();
+    while (clock64() - start < kWaitCycles / 1024) __nanosleep(1000);
+    __syncwarp();
+  }
   if (warp == 1) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(sh->tmem) : "memory");

@@ -58,3 +58,11 @@ def test_all_lanes_vote(source):
 def test_a_wait_ends_with_the_warp_together(source):
     inside = body(source, "void mbar_wait(")
     assert inside.rstrip(" \n}").endswith("__syncwarp();") and "return;" not in inside
+
+
+def test_what_is_in_flight_lands_before_the_memory_goes(source):
+    """The pause comes after every warp has stopped issuing, and before the CTA frees what copies and products write."""
+    kernel = body(source, "k_paged_attention(const")
+    together, pause, free = kernel.rindex("__syncthreads();"), kernel.index("__nanosleep"), kernel.index("tcgen05.dealloc")
+    assert together < kernel.index("stopped(") < pause < free
+    assert "__nanosleep" not in body(source, "void copy_tiles(")
