@@ -286,7 +286,7 @@ struct HeadsArgs {
   const int32_t* positions;
   int64_t n_tokens;
   int32_t D, page_shift, rot, lanes_shift, splits;
-  int64_t table_rows;
+  uint32_t rows;  // positions below it are taken: the table's rows, all that are not negative without one
   const float* table;
   const void* q_norm;
   const void* k_norm;
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   } else {
     pos = a.positions[t];
   }
-  if (pos < 0 || (a.table && pos >= a.table_rows)) {
+  if ((uint32_t)pos >= a.rows) {
     if (lane == 0 && share == 0) latch_error(a.status, SMETRIC_ERR_OVERFLOW);
     return;
   }
@@ -493,7 +493,7 @@ int launch_heads(smetric_kv* kv, HeadsArgs& a, const smetric_kv_transform& t, cu
   a.page_shift = __builtin_ctz((unsigned)kv->cfg.page_size);
   a.rot = t.rot_dim;
   a.table = t.rot_dim ? t.d_cos_sin : nullptr;
-  a.table_rows = t.table_rows;
+  a.rows = (uint32_t)(a.table ? std::min<int64_t>(t.table_rows, 1ll << 31) : 1ll << 31);
   a.q_norm = a.hq ? t.d_q_norm : nullptr;
   a.k_norm = a.hk ? t.d_k_norm : nullptr;
   a.eps = t.eps;
