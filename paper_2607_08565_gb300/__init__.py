@@ -967,7 +967,7 @@ class SMetricKV:
         most = pages.shape[1]
         raw, other = self._stream(stream)
         smetric_kv_plan(self.handle, offsets, n, n_tokens, kv_lens, pages.data_ptr() if pages.numel() else None, most,
-                        pages.stride(0) if n > 1 else most, window, raw)
+                        pages.stride(0) if n > 1 else most, max(-1 << 31, min(window, (1 << 31) - 1)), raw)
         self._n_tokens = n_tokens
         self._keep((offsets, kv_lens, pages))
         self._read(raw, other)

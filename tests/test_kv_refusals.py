@@ -1,6 +1,6 @@
-"""What the paged KV$ binding refuses before it reaches the library, without a GPU:
-tensors that are not on the handle's device, whose addresses the kernels must not
-get."""
+"""What the paged KV$ binding passes on to the library and what it refuses, without a
+GPU: tensors that are not on the handle's device, whose addresses the kernels must
+not get, and windows of any size."""
 
 import pytest
 import torch
@@ -11,13 +11,17 @@ BF = torch.bfloat16
 
 
 class Library:
-    """Counts the calls that come through."""
+    """Notes the calls that come through."""
 
     def __init__(self):
-        self.calls = []
+        self.calls, self.args = [], None
 
     def __getattr__(self, name):
-        return lambda *a: self.calls.append(name) or 0
+        def call(*args):
+            self.calls.append(name)
+            self.args = args
+            return 0
+        return call
 
 
 class Elsewhere(torch.Tensor):
@@ -86,3 +90,11 @@ def test_a_plans_tensors_elsewhere_are_refused(kv, which, device):
     with pytest.raises(ValueError, match="device|cuda"):
         kv.plan(*args, 4)
     assert not kv.library.calls
+
+
+@pytest.mark.parametrize("window,passed", [(0, 0), (5, 5), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 2 ** 31 - 1), (2 ** 32 + 5, 2 ** 31 - 1),
+                                           (2 ** 63 - 1, 2 ** 31 - 1), (-1, -1), (-2 ** 32, -2 ** 31)])
+def test_windows_past_32_bits_are_as_wide_as_any_sequence(kv, window, passed):
+    """And negative ones stay negative, which the library refuses."""
+    kv.plan(*(on(x, 0) for x in plan()), 4, window=window)
+    assert kv.library.args[8] == passed
