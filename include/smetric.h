@@ -642,7 +642,8 @@ int smetric_kv_destroy(smetric_kv* kv);
  *   d_pages    int32 rows of max_pages page numbers (entries past a request's
  *              length, and entries that lie before its window, are not
  *              used), row stride pages_stride >= max_pages.
- *   window     0, or how many keys a query sees at most, its own among them.
+ *   window     0, or how many keys a query sees at most, its own among them
+ *              (layers of different windows need a plan each, or a handle).
  * d_pages stays in use until the next plan: the attention reads it. Bad
  * offsets or lengths latch INVALID_ARG and the batch counts as one of no
  * requests; a page outside [0, num_pages) latches INVALID_ARG, an append

@@ -950,7 +950,8 @@ class SMetricKV:
 
     def plan(self, offsets, kv_lens, pages, n_tokens: int, window: int = 0, stream=None):
         """Plans a batch: offsets int64 [n+1], kv_lens int32 [n], pages int32
-        [n, max_pages] (row stride free). The handle keeps the tensors until
+        [n, max_pages] (row stride free). The window is the plan's: layers that
+        alternate need two plans or handles. The handle keeps the tensors until
         the next plan, and until what read them on another stream than torch's
         current one at this call is done; those that a captured call reads are
         the graph's owner's to keep."""

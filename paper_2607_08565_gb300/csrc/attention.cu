@@ -22,12 +22,19 @@
 // thread a row), 12-15 write a unit's output while the softmax of the next one
 // runs.
 //
+// Scores, statistics, sums and the join are in 32 bits. P is rounded to the
+// type of the values, as the tensor cores multiply operands of one type of 16
+// bits (its sum l is taken before that): against 64 bits the output's error is
+// 1.2 to 1.5 times that of its own rounding.
+//
 // Single tokens are bound by memory: 64 of them over 2k to 48k keys (4 key heads
 // of 128, 3.2 GB) take 464 us, 6.9 TB/s, the rate of a copy. Chunks are bound by
-// the chain of a tile's softmax (1,300 cycles), its product with the values and
-// its half's next scores (2 x 512 on the tensor cores): 2,840 cycles for two query
-// tiles and a key tile, and by the power cap: 2,048 tokens over 65,000 (32 query
-// heads) 1,440 us, 1,540 TFLOP/s, 1,560 us where the cap holds.
+// the power cap and by the chain of a tile's softmax (1,300 cycles), its product
+// with the values and its half's next scores (2 x 512 on the tensor cores), 2,840
+// cycles for two query tiles and a key tile: 2,048 tokens over 65,000 (32 query
+// heads) take 1,566 us, 1,415 TFLOP/s, with the cap, and 1,360 to 1,440 us in
+// runs too short for it. A thread spills 108 bytes and loads 152 (of all roles:
+// 60 and 56 without the softmax, 88 and 120 without the issuing warp).
 
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -819,7 +826,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
   pdl_enter();
-  // (the join's blocks find no room beside this CTA, but are ready when it ends)
+  // The join's blocks find no room beside this CTA, but are ready when it ends.
+  // Not before the wait above: they read the plan before their own.
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   Walk w;
   w.start(a);  // (its loads run while the CTA is set up)

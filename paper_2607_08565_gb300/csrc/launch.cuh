@@ -12,8 +12,9 @@ namespace smetric {
 // Programmatic dependent launch: a kernel launched with programmatic stream
 // serialisation is set up while its predecessor still runs and waits here
 // until that predecessor has finished and its writes are visible (a no-op for
-// an ordinary launch). No kernel triggers its successor early: successors
-// waiting on the SMs during a kernel's run measured slower.
+// an ordinary launch). But for k_paged_attention, whose CTAs leave no room for
+// its successor's, no kernel triggers its successor early: successors waiting on
+// the SMs during a kernel's run measured slower.
 __device__ __forceinline__ void pdl_enter() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
 
 // Launches a kernel; with pdl the launch may begin while the previous kernel
