@@ -566,7 +566,16 @@ int64_t smetric_launch_count(const smetric_index* idx);
  * nothing enqueued, device-detectable ones are latched in the handle and
  * reported by smetric_kv_status. Arrays of heads and caches need 16-byte
  * aligned pointers and strides that are multiples of 8 elements, arrays of
- * whole numbers and d_lse the alignment of their elements. */
+ * whole numbers and d_lse the alignment of their elements.
+ *
+ * A cache in 4 bits holds 3.6 times the tokens. Of each head of each token it
+ * has head_dim codes, two a byte (the even element in the low four bits): a
+ * sign, two bits of exponent and one of mantissa (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4
+ * and 6); and for every 16 elements a scale of 8 bits (e4m3). An element is
+ *   code * scale * 2^exp,
+ * with one exp for all keys and one for all values. smetric_kvq_append writes
+ * it, smetric_kvq_attention attends over it and smetric_kvq_read reads it back;
+ * they need a handle with SMETRIC_KV_4BIT and share its plan. */
 typedef struct smetric_kv smetric_kv; /* opaque, library-owned */
 
 #define SMETRIC_BF16 0
@@ -575,15 +584,18 @@ typedef struct smetric_kv smetric_kv; /* opaque, library-owned */
 #define SMETRIC_KV_MAX_GROUP 128     /* query heads per key head */
 #define SMETRIC_KV_MAX_REQUESTS (1 << 20)
 #define SMETRIC_KV_MAX_TOKENS (1 << 26)
+#define SMETRIC_KV_4BIT 2            /* smetric_kv_config.flags: the handle's caches are in 4 bits */
+#define SMETRIC_KVQ_MAX_EXP 64
+#define SMETRIC_KVQ_MAX_ROWS (1 << 30) /* of a read */
 #define SMETRIC_KV_INTERLEAVED 1     /* rotate pairs (2i, 2i+1) instead of (i, i + rot_dim/2) */
 
 typedef struct {
-  int32_t head_dim;           /* D, a multiple of 16, 16..SMETRIC_KV_MAX_HEAD_DIM */
+  int32_t head_dim;           /* D, a multiple of 16 (of 32 for caches in 4 bits), 16..SMETRIC_KV_MAX_HEAD_DIM */
   int32_t num_q_heads;        /* a multiple of num_kv_heads; query head h reads key head h / (num_q_heads / num_kv_heads) */
   int32_t num_kv_heads;       /* >= 1 */
   int32_t page_size;          /* 16, 32, 64, 128 or 256 tokens */
   int32_t dtype;              /* SMETRIC_BF16 or SMETRIC_F16, of q, k, v, the cache, the norm weights and the outputs */
-  int32_t flags;              /* 0 */
+  int32_t flags;              /* 0 or SMETRIC_KV_4BIT */
   int64_t num_pages;          /* pages of the cache, 1..2^31-1 */
   int64_t max_batch_requests; /* largest n_requests of a plan, <= SMETRIC_KV_MAX_REQUESTS */
   int64_t max_batch_tokens;   /* largest n_tokens of a plan, <= SMETRIC_KV_MAX_TOKENS */
@@ -604,6 +616,24 @@ typedef struct {
   int64_t token_stride;
   int64_t head_stride;
 } smetric_kv_cache;
+
+/* Keys or values in 4 bits: [num_pages, page_size, num_kv_heads] rows of
+ * head_dim / 2 bytes of codes and of 4 (head_dim <= 64) or 8 bytes of scales,
+ * of which the first head_dim / 16 are used. Strides in bytes, any but that
+ * d_codes and its strides are multiples of 16 and d_scales and its strides
+ * of 4 (head_dim <= 64) or 8. */
+typedef struct {
+  void* d_codes;
+  void* d_scales;
+  int64_t page_stride;
+  int64_t token_stride;
+  int64_t head_stride;
+  int64_t scale_page_stride;
+  int64_t scale_token_stride;
+  int64_t scale_head_stride;
+  int32_t exp;                /* -SMETRIC_KVQ_MAX_EXP..SMETRIC_KVQ_MAX_EXP */
+  int32_t reserved;           /* 0 */
+} smetric_kvq_cache;
 
 /* What happens to a query or key head x on its way: with a norm weight,
  * x <- x * rsqrt(mean(x^2) + eps) * weight over the head; then, with a table,
@@ -680,6 +710,37 @@ int smetric_qk_norm_rope(smetric_kv* kv, smetric_heads q, smetric_heads k, const
  * its window may be anything. */
 int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_heads q, float scale, smetric_heads out,
                             float* d_lse, smetric_stream_t stream);
+
+/* smetric_kv_append into caches in 4 bits: the transformed keys, in 32 bits,
+ * and the values are quantised as they are written. For 16 elements x with
+ * y = x / 2^exp, the scale s is the e4m3 number nearest to max|y| / 6 (at most
+ * 448), and a code the e2m1 number nearest to y / s (at most 6 in magnitude;
+ * where s is 0 the codes are), halves to even in both. So elements up to 2,688 *
+ * 2^exp are held to within a sixth of their group's largest. A NaN makes its 16
+ * elements NaN; an infinite one is held as 2,688 * 2^exp. */
+int smetric_kvq_append(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cache v_cache, smetric_heads k,
+                       smetric_heads v, smetric_heads q, smetric_heads q_out, smetric_kv_transform t,
+                       smetric_stream_t stream);
+
+/* Read keys and values back: rows d_offsets[r] .. d_offsets[r+1] of k and v (of
+ * the handle's dtype, [n_rows, num_kv_heads, head_dim]; either may be absent)
+ * get what the caches hold for request r at positions d_first[r], d_first[r]+1,
+ * ... (d_first NULL: from 0), rounded once. It needs no plan: offsets and pages
+ * are as for smetric_kv_plan, with as few rows of pages as requests. Bad offsets,
+ * a position outside its row of pages, and a page outside the cache latch
+ * INVALID_ARG; such positions read as zeros. Rows of no request stay as they
+ * were. */
+int smetric_kvq_read(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cache v_cache, const int64_t* d_offsets,
+                     int32_t n_requests, int64_t n_rows, const int32_t* d_first, const int32_t* d_pages,
+                     int32_t max_pages, int64_t pages_stride, smetric_heads k, smetric_heads v,
+                     smetric_stream_t stream);
+
+/* smetric_paged_attention over caches in 4 bits. Codes times scales are exact
+ * in 16 bits, and so are scores of the values that the caches stand for, up to
+ * the sums' 32 bits. scale * 2^exp of the keys is finite and > 0. Masked
+ * positions of a request's own length may hold anything too. */
+int smetric_kvq_attention(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cache v_cache, smetric_heads q,
+                          float scale, smetric_heads out, float* d_lse, smetric_stream_t stream);
 
 /* Wait for `stream`, then return and clear the first error the device latched
  * for this handle. */

@@ -7,15 +7,16 @@ torch.cuda.Stream, a raw cudaStream_t (int) or None for torch's current
 stream. Every computation runs in the library's CUDA kernels; there is no
 CPU fallback, and using the binding without the built library raises.
 
-SMetricIndex wraps one index and SMetricKV one handle of the paged KV$
-operators; both allocate output tensors for convenience.
+SMetricIndex wraps one index, SMetricKV one handle of the paged KV$
+operators and SMetricKV4 one with its caches in 4 bits; they allocate output
+tensors for convenience.
 """
 
 from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional
+from typing import Any, NamedTuple, Optional
 
 from .build_lib import LIB as _LIB_PATH
 
@@ -51,6 +52,9 @@ SMETRIC_KV_MAX_GROUP = 128
 SMETRIC_KV_MAX_REQUESTS = 1 << 20
 SMETRIC_KV_MAX_TOKENS = 1 << 26
 SMETRIC_KV_INTERLEAVED = 1
+SMETRIC_KV_4BIT = 2
+SMETRIC_KVQ_MAX_EXP = 64
+SMETRIC_KVQ_MAX_ROWS = 1 << 30
 
 EXPORTED = (
     "smetric_index_create", "smetric_index_destroy", "smetric_index_clear",
@@ -65,6 +69,7 @@ EXPORTED = (
     "smetric_route_batches", "smetric_index_set_lru", "smetric_index_lru_sizes", "smetric_route_commit_batch",
     "smetric_kv_create", "smetric_kv_destroy", "smetric_kv_plan", "smetric_kv_append", "smetric_qk_norm_rope",
     "smetric_paged_attention", "smetric_kv_status", "smetric_kv_launch_count",
+    "smetric_kvq_append", "smetric_kvq_read", "smetric_kvq_attention",
 )
 
 
@@ -110,6 +115,12 @@ class smetric_heads(C.Structure):
 class smetric_kv_cache(C.Structure):
     _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
                 ("head_stride", C.c_int64)]
+
+
+class smetric_kvq_cache(C.Structure):
+    _fields_ = [("d_codes", C.c_void_p), ("d_scales", C.c_void_p), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("scale_page_stride", C.c_int64), ("scale_token_stride", C.c_int64),
+                ("scale_head_stride", C.c_int64), ("exp", C.c_int32), ("reserved", C.c_int32)]
 
 
 class smetric_kv_transform(C.Structure):
@@ -184,6 +195,12 @@ def lib():
                                                smetric_heads, smetric_heads, P]),
             "smetric_paged_attention": (C.c_int, [P, smetric_kv_cache, smetric_heads, C.c_float, smetric_heads, P,
                                                   P]),
+            "smetric_kvq_append": (C.c_int, [P, smetric_kvq_cache, smetric_kvq_cache, smetric_heads, smetric_heads,
+                                             smetric_heads, smetric_heads, smetric_kv_transform, P]),
+            "smetric_kvq_read": (C.c_int, [P, smetric_kvq_cache, smetric_kvq_cache, P, I32, I64, P, P, I32, I64,
+                                           smetric_heads, smetric_heads, P]),
+            "smetric_kvq_attention": (C.c_int, [P, smetric_kvq_cache, smetric_kvq_cache, smetric_heads, C.c_float,
+                                                smetric_heads, P, P]),
             "smetric_kv_status": (C.c_int, [P, P]),
             "smetric_kv_launch_count": (I64, [P]),
         }
@@ -493,6 +510,24 @@ def smetric_paged_attention(kv: int, cache: smetric_kv_cache, q: smetric_heads, 
            "smetric_paged_attention")
 
 
+def smetric_kvq_append(kv: int, k_cache: smetric_kvq_cache, v_cache: smetric_kvq_cache, k: smetric_heads, v: smetric_heads,
+                       q: smetric_heads, q_out: smetric_heads, transform: smetric_kv_transform, stream=None) -> None:
+    _check(lib().smetric_kvq_append(kv, k_cache, v_cache, k, v, q, q_out, transform, _stream(stream)), "smetric_kvq_append")
+
+
+def smetric_kvq_read(kv: int, k_cache: smetric_kvq_cache, v_cache: smetric_kvq_cache, d_offsets, n_requests: int, n_rows: int,
+                     d_first, d_pages, max_pages: int, pages_stride: int, k: smetric_heads, v: smetric_heads,
+                     stream=None) -> None:
+    _check(lib().smetric_kvq_read(kv, k_cache, v_cache, _ptr(d_offsets), n_requests, n_rows, _ptr(d_first), _ptr(d_pages),
+                                  max_pages, pages_stride, k, v, _stream(stream)), "smetric_kvq_read")
+
+
+def smetric_kvq_attention(kv: int, k_cache: smetric_kvq_cache, v_cache: smetric_kvq_cache, q: smetric_heads, scale: float,
+                          out: smetric_heads, d_lse=None, stream=None) -> None:
+    _check(lib().smetric_kvq_attention(kv, k_cache, v_cache, q, scale, out, _ptr(d_lse), _stream(stream)),
+           "smetric_kvq_attention")
+
+
 def smetric_kv_status(kv: int, stream=None) -> int:
     return int(lib().smetric_kv_status(kv, _stream(stream)))
 
@@ -795,6 +830,9 @@ class SMetricKV:
     outputs there; the caller orders the two streams, as for its inputs.
     """
 
+    _flags = 0
+    _append_call, _attention_call = "smetric_kv_append", "smetric_paged_attention"
+
     def __init__(self, head_dim: int, num_q_heads: int, num_kv_heads: int, page_size: int, num_pages: int,
                  max_batch_requests: int, max_batch_tokens: int, dtype=None):
         import torch
@@ -802,7 +840,7 @@ class SMetricKV:
         code = {torch.bfloat16: SMETRIC_BF16, torch.float16: SMETRIC_F16}.get(self.dtype)
         if code is None:
             raise ValueError("dtype must be torch.bfloat16 or torch.float16")
-        self.cfg = smetric_kv_config(head_dim, num_q_heads, num_kv_heads, page_size, code, 0, num_pages,
+        self.cfg = smetric_kv_config(head_dim, num_q_heads, num_kv_heads, page_size, code, self._flags, num_pages,
                                      max_batch_requests, max_batch_tokens)
         self.handle = smetric_kv_create(self.cfg)
         self._n_tokens = None
@@ -844,6 +882,9 @@ class SMetricKV:
             raise ValueError(f"{name}: the elements of a head must be contiguous")
         # (the stride of a dimension of one is arbitrary)
         return smetric_heads(x.data_ptr(), token if n_tokens > 1 else 0, head if heads > 1 else 0)
+
+    def _caches(self, k_cache, v_cache):
+        return (self._cache(k_cache, v_cache),)
 
     def _cache(self, k_cache, v_cache) -> smetric_kv_cache:
         shape = self._cache_shape
@@ -985,7 +1026,7 @@ class SMetricKV:
         q_out (a new tensor by default) and returns it."""
         t, c = self._planned(), self.cfg
         hk, hq = c.num_kv_heads, c.num_q_heads
-        caches, kh, vh, qh = (self._cache(k_cache, v_cache), self._heads(k, hk, t, "k"), self._heads(v, hk, t, "v"),
+        caches, kh, vh, qh = (self._caches(k_cache, v_cache), self._heads(k, hk, t, "k"), self._heads(v, hk, t, "v"),
                               self._heads(q, hq, t, "q"))
         raw, other = self._stream(stream)
         if q is None:
@@ -994,9 +1035,9 @@ class SMetricKV:
             q_out, oh = self._new_heads(q, hq, t, other)
         else:
             oh = self._heads(q_out, hq, t, "q_out")
-        _check(self._lib.smetric_kv_append(self.handle, caches, kh, vh, qh, oh,
-                                           self._transform(cos_sin, interleaved, q_norm, k_norm, eps), raw),
-               "smetric_kv_append")
+        _check(getattr(self._lib, self._append_call)(self.handle, *caches, kh, vh, qh, oh,
+                                                     self._transform(cos_sin, interleaved, q_norm, k_norm, eps), raw),
+               self._append_call)
         return q_out
 
     def qk_norm_rope(self, q, k, positions, cos_sin=None, interleaved=False, q_norm=None, k_norm=None, eps=1e-6,
@@ -1031,17 +1072,17 @@ class SMetricKV:
         head_dim ** -0.5 by default. Returns out, or (out, lse) with want_lse
         (float32 [tokens, num_q_heads])."""
         t, hq = self._planned(), self.cfg.num_q_heads
-        caches, qh = self._cache(k_cache, v_cache), self._heads(q, hq, t, "q")
+        caches, qh = self._caches(k_cache, v_cache), self._heads(q, hq, t, "q")
         raw, other = self._stream(stream)
         if out is None:
             out, oh = self._new_heads(q, hq, t, other)
         else:
             oh = self._heads(out, hq, t, "out")
         lse = self._new(other, self._empty, (t, hq), dtype=self._f32, device=q.device) if want_lse else None
-        _check(self._lib.smetric_paged_attention(self.handle, caches, qh,
-                                                 self._dim ** -0.5 if scale is None else scale, oh,
-                                                 lse.data_ptr() if want_lse and t else None, raw),
-               "smetric_paged_attention")
+        _check(getattr(self._lib, self._attention_call)(self.handle, *caches, qh,
+                                                        self._dim ** -0.5 if scale is None else scale, oh,
+                                                        lse.data_ptr() if want_lse and t else None, raw),
+               self._attention_call)
         self._read(raw, other)
         return (out, lse) if want_lse else out
 
@@ -1052,3 +1093,108 @@ class SMetricKV:
         rc = self.status(stream)
         if rc != SMETRIC_OK:
             raise SmetricError(rc, "device")
+
+
+class Cache4(NamedTuple):
+    """Keys or values in 4 bits: codes uint8 [num_pages, page_size, num_kv_heads,
+    head_dim / 2] and scales torch.float8_e4m3fn [num_pages, page_size,
+    num_kv_heads, 4 (head_dim <= 64) or 8], views with any strides but the last;
+    what they hold is code * scale * 2 ** exp."""
+
+    codes: Any
+    scales: Any
+    exp: int = 0
+
+
+class SMetricKV4(SMetricKV):
+    """The paged KV$ operators with the caches in 4 bits (a scale of 8 bits for 16
+    elements): SMetricKV's calls with a Cache4 for each cache, and read().
+
+        kv = SMetricKV4(head_dim=128, num_q_heads=32, num_kv_heads=4, page_size=32, num_pages=16384,
+                        max_batch_requests=64, max_batch_tokens=8192)
+        cache = kv.new_cache()                                       # (keys, values)
+        kv.plan(offsets_i64, kv_lens_i32, pages_i32, n_tokens)       # once a step
+        kv.append(*cache, k, v, q=q, q_out=q, cos_sin=table, q_norm=wq, k_norm=wk)
+        out = kv.paged_attention(q, *cache)
+        k16, v16 = kv.read(*cache, rows_i64, pages_i32, n_rows)      # positions 0, 1, ... of every request
+        kv.check()
+
+    head_dim is a multiple of 32.
+    """
+
+    _flags = SMETRIC_KV_4BIT
+    _append_call, _attention_call = "smetric_kvq_append", "smetric_kvq_attention"
+
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        import torch
+        self._u8, self._e4m3, self._i64 = torch.uint8, torch.float8_e4m3fn, torch.int64
+        rows = self._cache_shape[:3]
+        self._codes_shape, self._scales_shape = rows + (self._dim // 2,), rows + (4 if self._dim <= 64 else 8,)
+
+    def new_cache(self, k_exp: int = 0, v_exp: int = 0):
+        """Caches for this handle: (keys, values), contiguous."""
+        import torch
+        make = lambda exp: Cache4(torch.zeros(self._codes_shape, dtype=self._u8, device=f"cuda:{self._device}"),  # noqa: E731
+                                  torch.zeros(self._scales_shape, dtype=self._e4m3, device=f"cuda:{self._device}"), exp)
+        return make(k_exp), make(v_exp)
+
+    def _caches(self, k_cache, v_cache):
+        return self._cache4(k_cache, "k_cache"), self._cache4(v_cache, "v_cache")
+
+    def _cache4(self, cache, name: str) -> smetric_kvq_cache:
+        codes, scales, exp = cache
+        here = self._device
+        if (codes.dtype != self._u8 or scales.dtype != self._e4m3 or codes.shape != self._codes_shape or
+                scales.shape != self._scales_shape or codes.get_device() != here or scales.get_device() != here):
+            raise ValueError(f"{name}: codes must be {self._u8} {list(self._codes_shape)} and scales {self._e4m3} "
+                             f"{list(self._scales_shape)}, on cuda:{here}")
+        if not -SMETRIC_KVQ_MAX_EXP <= exp <= SMETRIC_KVQ_MAX_EXP:
+            raise ValueError(f"{name}: exp must be within {SMETRIC_KVQ_MAX_EXP} of 0")
+        p, t, h, one = codes.stride()
+        sp, st, sh, sone = scales.stride()
+        if one != 1 or sone != 1:
+            raise ValueError(f"{name}: a head's codes and its scales must be contiguous")
+        if self._cache_shape[0] == 1:  # (the stride of a dimension of one is arbitrary)
+            p = sp = 0
+        if self._cache_shape[2] == 1:
+            h = sh = 0
+        return smetric_kvq_cache(codes.data_ptr(), scales.data_ptr(), p, t, h, sp, st, sh, exp, 0)
+
+    def read(self, k_cache, v_cache, offsets, pages, n_rows: int, first=None, k_out=None, v_out=None, stream=None):
+        """What the caches hold: rows offsets[r]:offsets[r + 1] of the outputs get
+        positions first[r], first[r] + 1, ... (0, 1, ... without first) of request
+        r, in the handle's dtype. offsets int64 [n+1], first int32 [n], pages int32
+        [n, max_pages] (row stride free). A cache may be None. Returns (k_out,
+        v_out), new tensors [n_rows, num_kv_heads, head_dim] unless given; rows of
+        no request are not written."""
+        hk = self.cfg.num_kv_heads
+        n = offsets.numel() - 1
+        if offsets.dim() != 1 or n < 0 or offsets.dtype != self._i64 or not offsets.is_contiguous():
+            raise ValueError("offsets must be torch.int64 [requests + 1], contiguous")
+        if pages.dtype != self._i32 or pages.dim() != 2 or pages.shape[0] != n or (pages.shape[1] > 1 and pages.stride(1) != 1):
+            raise ValueError("pages must be torch.int32 [requests, max_pages], a request's contiguous")
+        if first is not None and (first.dtype != self._i32 or first.shape != (n,) or not first.is_contiguous()):
+            raise ValueError("first must be torch.int32 [requests], contiguous")
+        if any(x is not None and x.get_device() != self._device for x in (offsets, pages, first)):
+            raise ValueError(f"offsets, pages and first must be on cuda:{self._device}")
+        raw, other = self._stream(stream)
+        none = smetric_kvq_cache()
+        outs, heads, caches = [], [], []
+        for cache, out, name in ((k_cache, k_out, "k"), (v_cache, v_out, "v")):
+            caches.append(none if cache is None else self._cache4(cache, name + "_cache"))
+            if cache is None:
+                out, described = None, _NO_HEADS
+            elif out is None:
+                out = self._new(other, self._empty, (n_rows, hk, self._dim), dtype=self.dtype, device=offsets.device)
+                described = smetric_heads(out.data_ptr(), hk * self._dim, self._dim)
+            else:
+                described = self._heads(out, hk, n_rows, name + "_out")
+            outs.append(out)
+            heads.append(described)
+        most = pages.shape[1]
+        _check(self._lib.smetric_kvq_read(self.handle, *caches, offsets.data_ptr(), n, n_rows,
+                                          first.data_ptr() if first is not None and n else None,
+                                          pages.data_ptr() if pages.numel() else None, most,
+                                          pages.stride(0) if n > 1 else most, *heads, raw), "smetric_kvq_read")
+        return tuple(outs)

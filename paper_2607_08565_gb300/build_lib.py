@@ -16,7 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libsmetric.so")
-SOURCES = ["index.cu", "route.cu", "imbalance.cu", "lru.cu", "kv.cu", "attention.cu"]
+SOURCES = ["index.cu", "route.cu", "imbalance.cu", "lru.cu", "kv.cu", "kv4.cu", "attention.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -195,7 +195,7 @@ __device__ void plan_units(const PlanArgs& a) {
     a.shares[c] = s;
   }
   __syncthreads();
-  if (threadIdx.x == 0) a.plan->n_split = n_split;
+  if (threadIdx.x == 0) a.plan->n_split = n_split, a.plan->n_units = U;
 }
 
 __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(const __grid_constant__ PlanArgs a) {
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(const __grid_constant_
       plan_units(a);
     } else {
       for (int i = threadIdx.x; i < a.ctas; i += kPlanThreads) a.shares[i].u0 = -1;
-      if (threadIdx.x == 0) a.plan->n_split = 0;
+      if (threadIdx.x == 0) a.plan->n_split = a.plan->n_units = 0;
     }
     return;
   }
@@ -282,6 +282,7 @@ struct HeadsArgs {
   smetric_heads q, k, v, q_out, k_out;  // absent: 0 heads
   int32_t hq, hk, hv;
   smetric_kv_cache cache;    // keys and values go here when tokens is not NULL
+  smetric_kvq_cache k4, v4;  // or here
   const KvToken* tokens;     // the plan's, or NULL: d_positions and k_out
   const KvPlan* plan;
   const int32_t* positions;
@@ -329,6 +330,47 @@ __device__ __forceinline__ void load_head(const Lane& l, const T* src, int h, in
   }
 }
 
+// A lane's norm and rotation, from its two pieces y to 16 elements f.
+template <typename T, bool kInterleaved>
+__device__ __forceinline__ void transform_lane(const Lane& l, const uint4 (&y)[2], bool on, const T* norm, float2 (&f)[8]) {
+#pragma unroll
+  for (int e = 0; e < 2; ++e) unpack<T>(y[e], &f[4 * e].x);
+  if (norm) {  // (the same for the warp: its lanes take part in the sum)
+    float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s2 = fma2(f[k], f[k], s2);
+    float ss = on ? s2.x + s2.y : 0.f;
+    for (int o = 1; o < 1 << l.lanes_shift; o <<= 1) ss += __shfl_xor_sync(kFull, ss, o);
+    if (on) {
+      const float inv = 1.0f / sqrtf(ss / (float)l.D + l.eps);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float2 g[4];
+        unpack<T>(*reinterpret_cast<const uint4*>(norm + (e ? l.e1 : l.e0)), &g[0].x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[4 * e + k] = mul2(mul2(f[4 * e + k], make_float2(inv, inv)), g[k]);
+      }
+    }
+  }
+  if (l.turned) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (kInterleaved) {  // pairs 2k and 2k + 1, as (a, b) each
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float c = i ? l.cs[k].y : l.cs[k].x, s = i ? l.sn[k].y : l.sn[k].x;
+          const float2 u = f[2 * k + i];
+          f[2 * k + i] = make_float2(u.x * c - u.y * s, u.y * c + u.x * s);
+        }
+      } else {
+        const float2 u = f[k], v = f[4 + k];
+        f[k] = fma2(u, l.cs[k], mul2(v, make_float2(-l.sn[k].x, -l.sn[k].y)));
+        f[4 + k] = fma2(v, l.cs[k], mul2(u, l.sn[k]));
+      }
+    }
+  }
+}
+
 // heads h, h + step, ... < heads of a token, from src to dst (both at head h);
 // x: the first of them. (A round's heads are loaded while the round before is
 // computed.)
@@ -348,45 +390,105 @@ __device__ __forceinline__ void transform_heads(const Lane& l, const T* src, int
       continue;
     }
     float2 f[8];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) unpack<T>(y[e], &f[4 * e].x);
-    if (norm) {  // (the same for the warp: its lanes take part in the sum)
-      float2 s2 = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) s2 = fma2(f[k], f[k], s2);
-      float ss = on ? s2.x + s2.y : 0.f;
-      for (int o = 1; o < 1 << l.lanes_shift; o <<= 1) ss += __shfl_xor_sync(kFull, ss, o);
-      if (on) {
-        const float inv = 1.0f / sqrtf(ss / (float)l.D + l.eps);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float2 g[4];
-          unpack<T>(*reinterpret_cast<const uint4*>(norm + (e ? l.e1 : l.e0)), &g[0].x);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) f[4 * e + k] = mul2(mul2(f[4 * e + k], make_float2(inv, inv)), g[k]);
-        }
-      }
-    }
-    if (l.turned) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (kInterleaved) {  // pairs 2k and 2k + 1, as (a, b) each
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float c = i ? l.cs[k].y : l.cs[k].x, s = i ? l.sn[k].y : l.sn[k].x;
-            const float2 u = f[2 * k + i];
-            f[2 * k + i] = make_float2(u.x * c - u.y * s, u.y * c + u.x * s);
-          }
-        } else {
-          const float2 u = f[k], v = f[4 + k];
-          f[k] = fma2(u, l.cs[k], mul2(v, make_float2(-l.sn[k].x, -l.sn[k].y)));
-          f[4 + k] = fma2(v, l.cs[k], mul2(u, l.sn[k]));
-        }
-      }
-    }
+    transform_lane<T, kInterleaved>(l, y, on, norm, f);
     if (on) {
       *reinterpret_cast<uint4*>(dst + l.e0) = pack<T>(&f[0].x);
       *reinterpret_cast<uint4*>(dst + l.e1) = pack<T>(&f[4].x);
+    }
+  }
+}
+
+// The larger magnitude; NaN if either is.
+__device__ __forceinline__ float max_nan(float x, float y) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(m) : "f"(x), "f"(y));
+  return m;
+}
+
+// A group's scale: its 8 bits, and 2^-exp / scale for its elements (0 where the
+// scale is 0 or NaN).
+__device__ __forceinline__ uint32_t scale_of(float top, float down, float& inv) {
+  uint32_t bits, half;
+  asm("{\n .reg .b16 b;\n cvt.rn.satfinite.e4m3x2.f32 b, %2, %2;\n cvt.u32.u16 %0, b;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
+      : "=r"(bits), "=r"(half) : "f"(__fdiv_rn(top * down, 6.f)));
+  const float s = __half2float(__ushort_as_half((unsigned short)half));
+  inv = s > 0.f ? __fdiv_rn(down, s) : 0.f;
+  return bits & 0xff;
+}
+
+// 8 codes. A product with the rounded reciprocal is within 2^-20 of the quotient
+// (of 6.4 at most), and quotients of 16-bit numbers that are not halfway between
+// two codes at least 2^-13 from there: adding and subtracting 24 leaves multiples
+// of 2^-19, so that what is halfway is seen so.
+__device__ __forceinline__ uint32_t codes_of(const float2* f, float inv) {
+  uint32_t r;
+  float2 y[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    y[k] = mul2(f[k], make_float2(inv, inv));
+    y[k] = make_float2(__fadd_rn(__fadd_rn(y[k].x, 24.f), -24.f), __fadd_rn(__fadd_rn(y[k].y, 24.f), -24.f));
+  }
+  asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}\n"
+      : "=r"(r) : "f"(y[0].x), "f"(y[0].y), "f"(y[1].x), "f"(y[1].y), "f"(y[2].x), "f"(y[2].y), "f"(y[3].x), "f"(y[3].y));
+  return r;
+}
+
+// Where quantised heads go, at the lane's first head.
+struct Codes {
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t step, scale_step;  // between its heads
+  float down;                // 2^-exp
+};
+
+// transform_heads into 4 bits. A group of 16 elements is two pieces of 8, which
+// a lane holds both unless a rotation by halves gave it pieces rot/2 elements
+// apart: then the lanes pass their pieces' largest magnitudes on. R: the lanes so
+// turned (lane p < R has pieces p and p + R, the others 2p and 2p + 1).
+template <typename T, bool kInterleaved>
+__device__ __forceinline__ void quantise_heads(const Lane& l, const T* src, int64_t src_step, Codes dst, int h, int step,
+                                               int heads, int rounds, const T* norm, int R, uint4 (&x)[2]) {
+  const int p[2] = {l.e0 >> 3, l.e1 >> 3};
+  const int base = threadIdx.x & 31 & ~((1 << l.lanes_shift) - 1);
+  int from[2], second[2];  // the lane that has the other piece of the group, and whether as its second
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int other = p[i] ^ 1;
+    from[i] = base + (other < R ? other : other < 2 * R ? other - R : other >> 1);
+    second[i] = other < R ? 0 : other < 2 * R ? 1 : other & 1;
+  }
+  for (int r = 0; r < rounds; ++r, h += step, dst.codes += dst.step, dst.scales += dst.scale_step) {
+    const bool on = l.held && h < heads;
+    const uint4 y[2] = {x[0], x[1]};
+    src += src_step;
+    load_head(l, src, h + step, heads, x);
+    float2 f[8];
+    transform_lane<T, kInterleaved>(l, y, on, norm, f);
+    float m[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      m[i] = max_nan(fabsf(f[4 * i].x), fabsf(f[4 * i].y));
+#pragma unroll
+      for (int k = 1; k < 4; ++k) m[i] = max_nan(m[i], max_nan(fabsf(f[4 * i + k].x), fabsf(f[4 * i + k].y)));
+    }
+    float top[2];
+    if (R > 0) {  // (the same for the warp)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float a = __shfl_sync(kFull, m[0], from[i]), b = __shfl_sync(kFull, m[1], from[i]);
+        top[i] = max_nan(m[i], second[i] ? b : a);
+      }
+    } else {
+      top[0] = top[1] = max_nan(m[0], m[1]);
+    }
+    if (!on) continue;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float inv;
+      const uint32_t scale = scale_of(top[i], dst.down, inv);
+      reinterpret_cast<uint32_t*>(dst.codes)[p[i]] = codes_of(f + 4 * i, inv);
+      if (!(p[i] & 1)) dst.scales[p[i] >> 1] = (uint8_t)scale;
     }
   }
 }
@@ -399,7 +501,7 @@ __device__ __forceinline__ void transform_heads(const Lane& l, const T* src, int
 // loaded once for all its heads. Bound by memory; the registers of 28 warps an
 // SM hold the bytes in flight: 72 a thread, with 44 to 60 bytes spilled (24 warps
 // of 80 took 101 us for 16,001 tokens of 64 + 4 heads, where these take 96).
-template <typename T, bool kInterleaved>
+template <typename T, bool kInterleaved, bool kFour>
 __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ HeadsArgs a) {
   pdl_enter();
   const int lane = threadIdx.x & 31;
@@ -428,7 +530,7 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   };
   // (the first loads run while the token's place is found)
   uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)}, y[2] = {x[0], x[1]};
-  if (v0 < rv) load_head(l, source(a.v, v0), v0 * per + first, a.hv, y);
+  if (!kFour && v0 < rv) load_head(l, source(a.v, v0), v0 * per + first, a.hv, y);
   if (k0 < rk) load_head(l, source(a.k, k0), k0 * per + first, a.hk, x);
   int64_t slot = 0;
   int32_t pos;
@@ -464,6 +566,33 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   };
   const int64_t at = (slot >> a.page_shift) * a.cache.page_stride +
                      (slot & ((1 << a.page_shift) - 1)) * a.cache.token_stride;
+  if constexpr (kFour) {
+    const auto quantise = [&](const Lane& ln, const smetric_heads& src, const smetric_kvq_cache& c4, int r, int rounds,
+                              int n_heads, const void* norm, int R, uint4(&z)[2]) {
+      if (r >= rounds) return;
+      const int64_t page = slot >> a.page_shift, in = slot & ((1 << a.page_shift) - 1);
+      Codes to;
+      to.codes = static_cast<uint8_t*>(c4.d_codes) + page * c4.page_stride + in * c4.token_stride +
+                 (r * per + first) * c4.head_stride;
+      to.scales = static_cast<uint8_t*>(c4.d_scales) + page * c4.scale_page_stride + in * c4.scale_token_stride +
+                  (r * per + first) * c4.scale_head_stride;
+      to.step = step * c4.head_stride;
+      to.scale_step = step * c4.scale_head_stride;
+      to.down = exp2f((float)-c4.exp);
+      quantise_heads<T, kInterleaved>(ln, source(src, r), step * src.head_stride, to, r * per + first, step, n_heads,
+                                      (rounds - r + a.splits - 1) / a.splits, static_cast<const T*>(norm), R, z);
+    };
+    Lane plain;  // a value's elements, in order
+    plain.held = l.held, plain.turned = false;
+    plain.e0 = 16 * c, plain.e1 = 16 * c + 8;
+    plain.lanes_shift = l.lanes_shift, plain.D = l.D, plain.eps = l.eps;
+    if (v0 < rv) load_head(plain, source(a.v, v0), v0 * per + first, a.hv, y);
+    quantise(plain, a.v, a.v4, v0, rv, a.hv, nullptr, 0, y);
+    if (q0 < rq) load_head(l, source(a.q, q0), q0 * per + first, a.hq, y);
+    quantise(l, a.k, a.k4, k0, rk, a.hk, a.k_norm, !kInterleaved && a.table ? a.rot / 16 : 0, x);
+    heads(a.q, static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride, a.q_out.head_stride, q0, rq, a.hq, a.q_norm, y);
+    return;
+  }
   l.turned = false;
   heads(a.v, static_cast<T*>(a.cache.d_v) + at, a.cache.head_stride, v0, rv, a.hv, nullptr, y);
   l.turned = turned;
@@ -475,12 +604,6 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   heads(a.q, static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride, a.q_out.head_stride, q0, rq, a.hq, a.q_norm, y);
 }
 
-// At a whole number of its elements, as loads need.
-template <typename E>
-bool aligned(const E* p) {
-  return reinterpret_cast<uintptr_t>(p) % sizeof(E) == 0;
-}
-
 bool transform_ok(const smetric_kv* kv, const smetric_kv_transform& t) {
   if (t.reserved || (t.flags & ~SMETRIC_KV_INTERLEAVED) || t.rot_dim < 0 || t.rot_dim > kv->cfg.head_dim ||
       t.rot_dim % 16 || t.table_rows < 0)
@@ -490,6 +613,7 @@ bool transform_ok(const smetric_kv* kv, const smetric_kv_transform& t) {
   return (!t.d_q_norm && !t.d_k_norm) || (std::isfinite(t.eps) && t.eps >= 0.f);
 }
 
+template <bool kFour>
 int launch_heads(smetric_kv* kv, HeadsArgs& a, const smetric_kv_transform& t, cudaStream_t s) {
   a.D = kv->cfg.head_dim;
   a.page_shift = __builtin_ctz((unsigned)kv->cfg.page_size);
@@ -510,8 +634,8 @@ int launch_heads(smetric_kv* kv, HeadsArgs& a, const smetric_kv_transform& t, cu
   const int64_t grid = (a.n_tokens * a.splits + 3) / 4;
   const bool il = t.flags & SMETRIC_KV_INTERLEAVED;
   const bool bf = kv->cfg.dtype == SMETRIC_BF16;
-  auto kern = bf ? (il ? k_kv_heads<__nv_bfloat16, true> : k_kv_heads<__nv_bfloat16, false>)
-                 : (il ? k_kv_heads<__half, true> : k_kv_heads<__half, false>);
+  auto kern = bf ? (il ? k_kv_heads<__nv_bfloat16, true, kFour> : k_kv_heads<__nv_bfloat16, false, kFour>)
+                 : (il ? k_kv_heads<__half, true, kFour> : k_kv_heads<__half, false, kFour>);
   kv->launches++;
   return launch_k(kern, dim3((unsigned)grid), dim3(128), 0, s, true, a);
 }
@@ -560,7 +684,8 @@ int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out) {
   if (c.head_dim < 16 || c.head_dim > SMETRIC_KV_MAX_HEAD_DIM || c.head_dim % 16 || c.num_kv_heads < 1 ||
       c.num_kv_heads > 4096 || c.num_q_heads < c.num_kv_heads || c.num_q_heads % c.num_kv_heads ||
       c.num_q_heads / c.num_kv_heads > SMETRIC_KV_MAX_GROUP || c.page_size < 16 || c.page_size > 256 ||
-      (c.page_size & (c.page_size - 1)) || (c.dtype != SMETRIC_BF16 && c.dtype != SMETRIC_F16) || c.flags ||
+      (c.page_size & (c.page_size - 1)) || (c.dtype != SMETRIC_BF16 && c.dtype != SMETRIC_F16) || (c.flags & ~SMETRIC_KV_4BIT) ||
+      ((c.flags & SMETRIC_KV_4BIT) && c.head_dim % 32) ||
       c.num_pages < 1 || c.num_pages > INT32_MAX || c.max_batch_requests < 0 ||
       c.max_batch_requests > SMETRIC_KV_MAX_REQUESTS || c.max_batch_tokens < 0 ||
       c.max_batch_tokens > SMETRIC_KV_MAX_TOKENS)
@@ -657,7 +782,7 @@ int smetric_kv_append(smetric_kv* kv, smetric_kv_cache cache, smetric_heads k, s
   CallRange range("smetric_kv_append");
   int rc = check_device(kv);
   if (rc) return rc;
-  if (!kv->planned || !transform_ok(kv, t) || !heads_ok(k, kv->n_tokens) || !heads_ok(v, kv->n_tokens) ||
+  if (four_bits(kv) || !kv->planned || !transform_ok(kv, t) || !heads_ok(k, kv->n_tokens) || !heads_ok(v, kv->n_tokens) ||
       (q.d_data && (!heads_ok(q, kv->n_tokens) || !heads_ok(q_out, kv->n_tokens))) || !cache_ok(cache))
     return SMETRIC_ERR_INVALID_ARG;
   if (kv->n_tokens == 0) return SMETRIC_OK;
@@ -672,7 +797,33 @@ int smetric_kv_append(smetric_kv* kv, smetric_kv_cache cache, smetric_heads k, s
   a.tokens = kv->tokens;
   a.plan = kv->plan;
   a.n_tokens = kv->n_tokens;
-  return launch_heads(kv, a, t, reinterpret_cast<cudaStream_t>(stream));
+  return launch_heads<false>(kv, a, t, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int smetric_kvq_append(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cache v_cache, smetric_heads k,
+                       smetric_heads v, smetric_heads q, smetric_heads q_out, smetric_kv_transform t,
+                       smetric_stream_t stream) {
+  CallRange range("smetric_kvq_append");
+  int rc = check_device(kv);
+  if (rc) return rc;
+  if (!four_bits(kv) || !kv->planned || !transform_ok(kv, t) || !heads_ok(k, kv->n_tokens) || !heads_ok(v, kv->n_tokens) ||
+      (q.d_data && (!heads_ok(q, kv->n_tokens) || !heads_ok(q_out, kv->n_tokens))) ||
+      !cache4_ok(k_cache, kv->cfg.head_dim) || !cache4_ok(v_cache, kv->cfg.head_dim))
+    return SMETRIC_ERR_INVALID_ARG;
+  if (kv->n_tokens == 0) return SMETRIC_OK;
+  HeadsArgs a = {};
+  a.k = k;
+  a.v = v;
+  a.q = q;
+  a.q_out = q_out;
+  a.hk = a.hv = kv->cfg.num_kv_heads;
+  a.hq = q.d_data ? kv->cfg.num_q_heads : 0;
+  a.k4 = k_cache;
+  a.v4 = v_cache;
+  a.tokens = kv->tokens;
+  a.plan = kv->plan;
+  a.n_tokens = kv->n_tokens;
+  return launch_heads<true>(kv, a, t, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int smetric_qk_norm_rope(smetric_kv* kv, smetric_heads q, smetric_heads k, const int32_t* d_positions,
@@ -696,7 +847,7 @@ int smetric_qk_norm_rope(smetric_kv* kv, smetric_heads q, smetric_heads k, const
   a.hq = q.d_data ? kv->cfg.num_q_heads : 0;
   a.positions = d_positions;
   a.n_tokens = n_tokens;
-  return launch_heads(kv, a, t, reinterpret_cast<cudaStream_t>(stream));
+  return launch_heads<false>(kv, a, t, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int smetric_kv_status(smetric_kv* kv, smetric_stream_t stream) {

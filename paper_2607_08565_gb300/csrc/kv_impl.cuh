@@ -21,7 +21,8 @@ struct KvPlan {
   int64_t first, last;  // tokens [first, last) belong to requests
   int32_t valid;        // 0: the batch's offsets or lengths were refused
   int32_t n_split;      // units that several CTAs share
-  int32_t reserved[2];
+  int32_t n_units;
+  int32_t reserved;
 };
 
 // Keys go through the attention in tiles of kTile, queries in tiles of kTile
@@ -94,4 +95,21 @@ inline bool cache_ok(const smetric_kv_cache& c) {
          c.page_stride >= 0 && c.token_stride >= 0 && c.head_stride >= 0 && c.page_stride % 8 == 0 &&
          c.token_stride % 8 == 0 && c.head_stride % 8 == 0;
 }
+// Bytes of a head's scales: head_dim / 16, to a whole load.
+__host__ __device__ constexpr int scale_bytes(int head_dim) { return head_dim <= 64 ? 4 : 8; }
+inline bool cache4_ok(const smetric_kvq_cache& c, int head_dim) {
+  const int s = scale_bytes(head_dim);
+  return c.d_codes && c.d_scales && !(reinterpret_cast<uintptr_t>(c.d_codes) & 15) &&
+         reinterpret_cast<uintptr_t>(c.d_scales) % s == 0 && c.page_stride >= 0 && c.token_stride >= 0 &&
+         c.head_stride >= 0 && c.scale_page_stride >= 0 && c.scale_token_stride >= 0 && c.scale_head_stride >= 0 &&
+         c.page_stride % 16 == 0 && c.token_stride % 16 == 0 && c.head_stride % 16 == 0 &&
+         c.scale_page_stride % s == 0 && c.scale_token_stride % s == 0 && c.scale_head_stride % s == 0 &&
+         c.exp >= -SMETRIC_KVQ_MAX_EXP && c.exp <= SMETRIC_KVQ_MAX_EXP && !c.reserved;
+}
+// At a whole number of its elements, as loads need.
+template <typename E>
+bool aligned(const E* p) {
+  return reinterpret_cast<uintptr_t>(p) % sizeof(E) == 0;
+}
+inline bool four_bits(const smetric_kv* kv) { return kv->cfg.flags & SMETRIC_KV_4BIT; }
 }  // namespace smetric
