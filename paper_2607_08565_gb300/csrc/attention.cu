@@ -62,11 +62,23 @@ constexpr int kThreads = 512;
 constexpr float kSlack = 8.f;     // log2 of how far scores may pass the reference
 constexpr uint32_t kHalf = 16384;  // bytes of 128 rows of 64 elements
 
-// Buffers of the ring: what 227 KB hold beside the two query tiles.
-__host__ __device__ constexpr int stages(int halves) { return halves == 2 ? 5 : 11; }
+// Buffers of the ring: what 227 KB hold beside the two query tiles (and, for
+// caches in 4 bits, their codes' way to the ring).
+__host__ __device__ constexpr int stages(int halves, bool four) {
+  return four ? (halves == 2 ? 4 : 9) : halves == 2 ? 5 : 11;
+}
+// Caches in 4 bits: each of 3 warps converts every third 16 rows of a tile, whose
+// codes and scales are copied two tiles ahead.
+constexpr int kConverters = 3;
+constexpr int kAhead = 3;  // buffers
+__host__ __device__ constexpr int group_bytes(int halves) { return 16 * (32 * halves + 4 * halves); }
+__host__ __device__ constexpr int staging_bytes(int halves, bool four) {
+  return four ? kConverters * kAhead * 3 * group_bytes(halves) : 0;
+}
 
 struct AttentionArgs {
   CUtensorMap q, k, v;
+  smetric_kvq_cache k4, v4;  // in place of k and v
   smetric_heads out;
   float* lse;
   const KvPlan* plan;
@@ -78,8 +90,9 @@ struct AttentionArgs {
   const int32_t* pages;
   int64_t pages_stride, n_tokens;
   int32_t num_pages, hq, kv_heads, group, tile_tokens, D, page_size, window;
-  float scale;
-  bool wide;  // outputs can be stored in pieces of 32 bytes
+  float scale, v_scale;
+  bool wide;    // outputs can be stored in pieces of 32 bytes
+  bool clears;  // zeros for tokens of no request are this kernel's
   int32_t* status;
 };
 
@@ -359,20 +372,37 @@ __device__ __forceinline__ uint32_t place_v(int j, int n) { return min(2 + 2 * j
 
 // ---- the warps ----
 
+// Query tile number nq of the CTA: tile t of the item's, when its buffer is free. The
+// whole warp calls.
+template <int HALVES>
+__device__ __forceinline__ void copy_queries(const AttentionArgs& a, Shared* sh, const Item& it, int t, uint32_t nq,
+                                             uint32_t q_smem) {
+  Barriers& b = sh->bar;
+  uint64_t* full = &b.q_full[nq & 1];
+  if (nq > 1) mbar_wait(&b.q_empty[nq & 1], (nq / 2 - 1) & 1, sh, a.status);
+  const bool stop = stopped(sh);
+  if ((threadIdx.x & 31) == 0 && !stop) {
+    mbar_expect(full, (uint32_t)a.tile_tokens * a.group * 128 * HALVES);
+#pragma unroll
+    for (int e = 0; e < HALVES; ++e)
+      tma_3d(q_smem + ((nq & 1) * HALVES + e) * kHalf, &a.q, 64 * e, it.h * a.group, it.unit.token + t * a.tile_tokens, full);
+  }
+  __syncwarp();
+}
+
 // One warp copies the query tiles and the keys, another the values (a tile of
 // 16-token pages is 16 copies, and one warp issues them no faster than memory
 // delivers half of them). A lane has a page and a half of the elements.
 template <int HALVES>
 __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, Walk w, uint32_t q_smem, uint32_t ring,
                                            const bool values) {
-  constexpr int S = stages(HALVES);
+  constexpr int S = stages(HALVES, false);
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31;
   const int rows = min(kTile, a.page_size), per = kTile / rows;  // of a copy, and pages of a tile
   const int page_shift = __ffs(a.page_size) - 1;
   const int mine = lane % per, half = lane / per;
   const bool copies = half < HALVES;
-  const uint32_t q_bytes = (uint32_t)a.tile_tokens * a.group * 128 * HALVES;
   const CUtensorMap* const map = values ? &a.v : &a.k;
   uint32_t base = 0, nq = 0;
   Item it;
@@ -406,19 +436,7 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
                a.page_size > kTile ? (it.tb + j) * kTile % a.page_size : 0, it.h, page, &b.full[s]);
       }
       if (j == 0 && !values) {
-        for (int t = 0; t < (it.pair ? 2 : 1); ++t, ++nq) {
-          uint64_t* full = &b.q_full[nq & 1];
-          if (nq > 1) mbar_wait(&b.q_empty[nq & 1], (nq / 2 - 1) & 1, sh, a.status);
-          const bool stop = stopped(sh);
-          if (lane == 0 && !stop) {
-            mbar_expect(full, q_bytes);
-#pragma unroll
-            for (int e = 0; e < HALVES; ++e)
-              tma_3d(q_smem + ((nq & 1) * HALVES + e) * kHalf, &a.q, 64 * e, it.h * a.group,
-                     it.unit.token + t * a.tile_tokens, full);
-          }
-          __syncwarp();
-        }
+        for (int t = 0; t < (it.pair ? 2 : 1); ++t, ++nq) copy_queries<HALVES>(a, sh, it, t, nq, q_smem);
       }
     }
     base += 2 * n;
@@ -426,12 +444,181 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
   }
 }
 
+// ---- caches in 4 bits ----
+
+template <int N>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool held) {
+  if constexpr (N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(held ? 16 : 0) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(held ? N : 0) : "memory");
+}
+
+// 8 elements of 16 bits: a word of codes times a scale, which stands twice in a word.
+// Codes have 2 bits and scales 4: the products are exact. In bf16 a code goes
+// through half precision, whose bits three places down are the bits of 2^-112 of
+// it in bf16; the scale brings the 2^112.
+template <typename T>
+struct Decode;
+template <>
+struct Decode<__half> {
+  static __device__ __forceinline__ uint32_t scale(uint32_t two, int which) {
+    return __byte_perm(two, 0, which ? 0x3232 : 0x1010);
+  }
+  static __device__ __forceinline__ uint32_t pair(uint32_t code, uint32_t scale) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(code), "r"(scale));
+    return r;
+  }
+};
+template <>
+struct Decode<__nv_bfloat16> {
+  static __device__ __forceinline__ uint32_t scale(uint32_t two, int which) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&two));
+    const float s = (which ? f.y : f.x) * 5192296858534827628530496329220096.f;  // 2^112
+    return Type<__nv_bfloat16>::pack(s, s);
+  }
+  static __device__ __forceinline__ uint32_t pair(uint32_t code, uint32_t scale) {
+    const uint32_t x = (code & 0x80008000u) | (code >> 3 & 0x0fff0fffu);
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;\n" : "=r"(r) : "r"(x), "r"(scale));
+    return r;
+  }
+};
+template <typename T>
+__device__ __forceinline__ uint4 decode8(uint32_t codes, uint32_t scale) {
+  uint32_t h[4];
+  asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+      " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}\n"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+  return make_uint4(Decode<T>::pair(h[0], scale), Decode<T>::pair(h[1], scale), Decode<T>::pair(h[2], scale),
+                    Decode<T>::pair(h[3], scale));
+}
+
+// What copy_tiles does, for caches in 4 bits: this warp's 16-row groups (number, +
+// 3, + 6) of every tile, copied as they are and written to the ring in 16 bits, in
+// the 128-byte swizzle. A tile's keys and values are laid out alike, so what is
+// converted needs no more than its place. Rows that nobody sees become zeros.
+template <typename T, int HALVES>
+__device__ __forceinline__ void convert_tiles(const AttentionArgs& a, Shared* sh, Walk w, uint32_t staging, uint32_t ring,
+                                              const int number) {
+  constexpr int S = stages(HALVES, true), SB = 4 * HALVES, G = group_bytes(HALVES), kCodes = 16 * 32 * HALVES;
+  Barriers& b = sh->bar;
+  const int lane = threadIdx.x & 31;
+  const int row = lane & 15;
+  const int pieces = a.D / 32;  // of 16 bytes, in a row; piece (lane >> 4) and, of longer heads, 2 more
+  const int page_shift = __ffs(a.page_size) - 1;
+  staging += number * kAhead * 3 * G;
+  // the next tile to copy
+  Item it;
+  bool more = w.next(a, it);
+  int place = 0, n = 0;
+  int32_t lo = 0, hi = 0, page = -1;  // the lane's 16-row group's page (lane & 7)
+  const auto tile_of = [&](bool& values) {
+    values = place == 2 * n - 1 || (place > 1 && !(place & 1));
+    return place == 2 * n - 1 ? n - 1 : place < 2 ? place : values ? (place - 2) / 2 : (place + 1) / 2;
+  };
+  const auto look_up = [&]() {
+    bool values;
+    const int64_t key = (int64_t)(it.tb + tile_of(values)) * kTile + 16 * (lane & 7);
+    page = key < hi && key + 16 > lo ? a.pages[it.unit.req * a.pages_stride + (key >> page_shift)] : INT32_MIN;
+  };
+  const auto enter = [&]() {
+    n = it.te - it.tb;
+    place = 0;
+    lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0;  // the keys that some query of the unit sees
+    hi = it.unit.pos + it.unit.tokens;
+    look_up();
+  };
+  if (more) enter();
+  uint32_t copied = 0;
+  const auto copy = [&]() {
+    if (more) {
+      bool values;
+      const int64_t key0 = (int64_t)(it.tb + tile_of(values)) * kTile;
+      const smetric_kvq_cache& c = values ? a.v4 : a.k4;
+      const uint8_t* codes = static_cast<const uint8_t*>(c.d_codes) + it.h * c.head_stride;
+      const uint8_t* scales = static_cast<const uint8_t*>(c.d_scales) + it.h * c.scale_head_stride;
+      if (page != INT32_MIN && (page < 0 || page >= a.num_pages)) {
+        latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
+        page = INT32_MIN;
+      }
+      const uint32_t to = staging + copied % kAhead * 3 * G;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int group = number + 3 * i;
+        const int32_t p = __shfl_sync(kFull, page, group & 7);
+        if (group >= kTile / 16) continue;
+        const int64_t key = key0 + 16 * group + row;
+        const bool held = p != INT32_MIN && key >= lo && key < hi;
+        const int64_t in = key & (a.page_size - 1), at = held ? p : 0;
+        const uint8_t* from = codes + at * c.page_stride + in * c.token_stride;
+#pragma unroll
+        for (int k = 0; k < HALVES; ++k) {
+          const int piece = 2 * k + (lane >> 4);
+          if (piece < pieces) copy_async<16>(to + i * G + (piece * 16 + row) * 16, from + 16 * piece, held);
+        }
+        if (lane < 16)
+          copy_async<SB>(to + i * G + kCodes + row * SB, scales + at * c.scale_page_stride + in * c.scale_token_stride, held);
+      }
+      ++copied;
+      if (++place == 2 * n) {
+        more = w.next(a, it);
+        if (more) enter();
+      } else {
+        look_up();
+      }
+    }
+    asm volatile("cp.async.commit_group;\n" ::: "memory");
+  };
+  for (int i = 0; i < kAhead - 1; ++i) copy();
+  for (uint32_t at = 0; at < copied; ++at) {
+    asm volatile("cp.async.wait_group %0;\n" ::"n"(kAhead - 2) : "memory");
+    __syncwarp();
+    copy();
+    const uint32_t s = at % S, from = staging + at % kAhead * 3 * G;
+    if (at >= S) mbar_wait(&b.empty[s], (at / S - 1) & 1, sh, a.status);
+    if (stopped(sh)) break;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const int group = number + 3 * i;
+      if (group >= kTile / 16) continue;
+      const int r = 16 * group + row;
+#pragma unroll
+      for (int k = 0; k < HALVES; ++k) {
+        const int piece = 2 * k + (lane >> 4);
+        if (piece >= pieces) continue;
+        uint4 x;
+        uint32_t two;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n"
+                     : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(from + i * G + (piece * 16 + row) * 16) : "memory");
+        asm volatile("{\n .reg .b16 x;\n ld.shared.b16 x, [%1];\n cvt.rn.f16x2.e4m3x2 %0, x;\n}\n"
+                     : "=r"(two) : "r"(from + i * G + kCodes + row * SB + 2 * piece) : "memory");
+        const uint32_t scale[2] = {Decode<T>::scale(two, 0), Decode<T>::scale(two, 1)};
+        const uint32_t word[4] = {x.x, x.y, x.z, x.w};
+        const uint32_t to = ring + (s * HALVES + (piece >> 1)) * kHalf + r * 128;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint4 y = decode8<T>(word[q], scale[q >> 1]);
+          const int chunk = (4 * piece + q) & 7;
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(to + ((chunk ^ (r & 7)) << 4)), "r"(y.x), "r"(y.y),
+                       "r"(y.z), "r"(y.w) : "memory");
+        }
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&b.full[s]);
+  }
+  asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+}
+
 // Issues the products, a step's (weights with values, then the half's next
 // scores) by one elected lane in one go: this warp is close to the limit, a wait
 // that is ready costs it 60 to 160 cycles. The two halves take turns.
-template <typename T, int HALVES>
+template <typename T, int HALVES, bool kFour>
 __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Walk w, uint32_t q_smem, uint32_t ring) {
-  constexpr int S = stages(HALVES);
+  constexpr int S = stages(HALVES, kFour);
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31;
   const uint32_t tmem = sh->tmem;
@@ -479,6 +666,7 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Wal
     // zero does not cancel what may lie there. (A row's 128 bytes are its own
     // under the swizzle.)
     const auto clear = [&](uint32_t place, int j) {
+      if (kFour) return;  // (they are zeros already)
       const int32_t key = (it.tb + j) * kTile;
       if (key >= lo && hi - key >= kTile) return;  // (key + kTile may pass 32 bits)
       const uint32_t at = ring + stage(place) * HALVES * kHalf;
@@ -710,15 +898,26 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
 
 // A unit's output: O / l, or its sums and statistics where other CTAs have
 // pieces of it.
-template <typename T>
-__device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Walk w) {
+// With caches in 4 bits its first warp also copies the query tiles, an item's
+// before the output of the item before: the converting warps, who could wait for a
+// query buffer only after the tiles that they have not converted yet, cannot.
+template <typename T, int HALVES, bool kFour>
+__device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Walk w, uint32_t q_smem) {
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
   const uint32_t o_all = sh->tmem + 2 * kTile + ((uint32_t)warp << 21);
   const int row_token = row / a.group, row_head = row - row_token * a.group;
-  uint32_t items = 0, no[2] = {0, 0};
+  uint32_t items = 0, no[2] = {0, 0}, nq = 0;
+  Walk ahead = w;
+  const auto queries = [&]() {
+    Item next;
+    if (ahead.next(a, next))
+      for (int t = 0; t < (next.pair ? 2 : 1); ++t, ++nq) copy_queries<HALVES>(a, sh, next, t, nq, q_smem);
+  };
+  if (kFour && warp == 0) queries();
   Item it;
   for (; w.next(a, it); ++items) {
+    if (kFour && warp == 0) queries();
     const bool two = !it.pair && it.te - it.tb > 1;  // sums of even and of odd key tiles
     for (int tile = 0; tile < (it.pair ? 2 : 1); ++tile) {
       const int n_rows = tile_rows(a, it, tile);
@@ -742,7 +941,8 @@ __device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Wa
         const bool mine = row < n_rows;
         const int64_t token = it.unit.token + tile_token(a, it, tile) + row_token;
         const int head = it.h * a.group + row_head;
-        const float inv = it.whole ? (st.y > 0.f ? 1.f / st.y : st.y) : 1.f;  // (NaN stays)
+        float inv = it.whole ? (st.y > 0.f ? 1.f / st.y : st.y) : 1.f;  // (NaN stays)
+        if (kFour && it.whole) inv *= a.v_scale;
         w1 *= inv, w2 *= inv;
         const uint32_t o_at = o_all + tile * kTile;
         T* out = static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride;
@@ -790,20 +990,20 @@ __device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Wa
   }
 }
 
-template <typename T, int HALVES>
+template <typename T, int HALVES, bool kFour>
 __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_constant__ AttentionArgs a) {
-  constexpr int S = stages(HALVES);
+  constexpr int S = stages(HALVES, kFour);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  Shared* sh = reinterpret_cast<Shared*>(smem_raw + (2 + S) * HALVES * kHalf);
+  Shared* sh = reinterpret_cast<Shared*>(smem_raw + (2 + S) * HALVES * kHalf + staging_bytes(HALVES, kFour));
   if (smem_u32(smem_raw) & 1023) {  // (the swizzle's groups of 8 rows)
     latch_error(a.status, SMETRIC_ERR_CUDA);
     return;
   }
-  const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + 2 * HALVES * kHalf;
+  const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + 2 * HALVES * kHalf, staging = ring + S * HALVES * kHalf;
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     Barriers& b = sh->bar;
-    for (int i = 0; i < S; ++i) mbar_init(&b.full[i], 1), mbar_init(&b.empty[i], 1);
+    for (int i = 0; i < S; ++i) mbar_init(&b.full[i], kFour ? kConverters : 1), mbar_init(&b.empty[i], 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(&b.q_full[t], 1);
       mbar_init(&b.q_empty[t], 1);
@@ -817,8 +1017,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     sh->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.q)) : "memory");
-    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.k)) : "memory");
-    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.v)) : "memory");
+    if (!kFour) {
+      asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.k)) : "memory");
+      asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.v)) : "memory");
+    }
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&sh->tmem))
@@ -838,31 +1040,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   // launched with, 16 of 128.
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
-    if (warp == 0) {
-      copy_tiles<HALVES>(a, sh, w, q_smem, ring, false);
-    } else if (warp == 1) {
-      multiply<T, HALVES>(a, sh, w, q_smem, ring);
-    } else if (warp == 2) {
-      copy_tiles<HALVES>(a, sh, w, q_smem, ring, true);
+    if (warp == 1) {
+      multiply<T, HALVES, kFour>(a, sh, w, q_smem, ring);
+    } else if (!kFour && warp != 3) {
+      copy_tiles<HALVES>(a, sh, w, q_smem, ring, warp == 2);
     } else {
-      // tokens of no request
-      const int64_t first = a.plan->first, last = a.plan->last, none = first + a.n_tokens - last;
-      const int64_t pieces = none * a.hq * (a.D / 8);
-      for (int64_t i = (int64_t)blockIdx.x * 32 + threadIdx.x - 96; i < pieces; i += (int64_t)gridDim.x * 32) {
-        const int64_t x = i / (a.D / 8), h = x % a.hq;
-        int64_t t = x / a.hq;
-        if (t >= first) t += last - first;
-        *reinterpret_cast<uint4*>(static_cast<T*>(a.out.d_data) + t * a.out.token_stride + h * a.out.head_stride +
-                                  i % (a.D / 8) * 8) = make_uint4(0, 0, 0, 0);
-        if (a.lse) a.lse[t * a.hq + h] = -INFINITY;
+      if (warp == 3 && (!kFour || a.clears)) {
+        // tokens of no request
+        const int64_t first = a.plan->first, last = a.plan->last, none = first + a.n_tokens - last;
+        const int64_t pieces = none * a.hq * (a.D / 8);
+        for (int64_t i = (int64_t)blockIdx.x * 32 + threadIdx.x - 96; i < pieces; i += (int64_t)gridDim.x * 32) {
+          const int64_t x = i / (a.D / 8), h = x % a.hq;
+          int64_t t = x / a.hq;
+          if (t >= first) t += last - first;
+          *reinterpret_cast<uint4*>(static_cast<T*>(a.out.d_data) + t * a.out.token_stride + h * a.out.head_stride +
+                                    i % (a.D / 8) * 8) = make_uint4(0, 0, 0, 0);
+          if (a.lse) a.lse[t * a.hq + h] = -INFINITY;
+        }
+        __syncwarp();
       }
+      if constexpr (kFour) convert_tiles<T, HALVES>(a, sh, w, staging, ring, warp == 0 ? 0 : warp - 1);
     }
   } else if (warp < 12) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 176;\n");
     softmax<T>(a, sh, w, (warp >> 2) - 1);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
-    write_out<T>(a, sh, w);
+    write_out<T, HALVES, kFour>(a, sh, w, q_smem);
   }
   __syncwarp();
   fence_before();
@@ -961,7 +1165,7 @@ __device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit,
       }
     }
     if (x >= n) continue;
-    const float inv = l > 0.f ? 1.f / l : l;  // (NaN stays)
+    const float inv = (l > 0.f ? 1.f / l : l) * a.v_scale;  // (NaN stays)
     const int64_t token = unit.token + r / a.group;
     const int head = h * a.group + r % a.group;
     T* out = static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride + 16 * column;
@@ -1009,8 +1213,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
     join<T, 32>(a, s.last, s.h1, c1, s.n_last, block, blocks);
 }
 
-constexpr size_t smem_bytes(int halves) { return (size_t)(2 + stages(halves)) * halves * kHalf + sizeof(Shared); }
-static_assert(smem_bytes(1) <= 232448 && smem_bytes(2) <= 232448, "227 KB");
+constexpr size_t smem_bytes(int halves, bool four) {
+  return (size_t)(2 + stages(halves, four)) * halves * kHalf + staging_bytes(halves, four) + sizeof(Shared);
+}
+static_assert(smem_bytes(1, false) <= 232448 && smem_bytes(2, false) <= 232448 && smem_bytes(1, true) <= 232448 &&
+                  smem_bytes(2, true) <= 232448, "227 KB");
 
 bool encode(CUtensorMap* m, int32_t dtype, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
             const cuuint32_t* box) {
@@ -1027,43 +1234,25 @@ cuuint64_t stride_of(int64_t elements, int64_t entries) { return entries > 1 ? (
 
 }  // namespace
 
-bool smetric::attention_limits() {
+namespace {
+template <typename T, bool kFour>
+bool limits() {
   const auto set = [](const void* f, int halves) {
-    return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(halves)) == cudaSuccess;
+    return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(halves, kFour)) == cudaSuccess;
   };
-  return set((const void*)k_paged_attention<__nv_bfloat16, 1>, 1) && set((const void*)k_paged_attention<__nv_bfloat16, 2>, 2) &&
-         set((const void*)k_paged_attention<__half, 1>, 1) && set((const void*)k_paged_attention<__half, 2>, 2);
+  return set((const void*)k_paged_attention<T, 1, kFour>, 1) && set((const void*)k_paged_attention<T, 2, kFour>, 2);
 }
 
-extern "C" {
-
-int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_heads q, float scale, smetric_heads out,
-                            float* d_lse, smetric_stream_t stream) {
-  CallRange range("smetric_paged_attention");
-  int rc = check_device(kv);
-  if (rc) return rc;
-  if (four_bits(kv) || !kv->planned || !std::isfinite(scale) || !(scale > 0.f) || !cache_ok(cache) || !heads_ok(q, kv->n_tokens) ||
-      !heads_ok(out, kv->n_tokens) || (reinterpret_cast<uintptr_t>(d_lse) & 3))
-    return SMETRIC_ERR_INVALID_ARG;
-  if (kv->n_tokens == 0) return SMETRIC_OK;
+// The attention and its join; `a` has the caches, the rest is set here.
+template <bool kFour>
+int launch_attention(smetric_kv* kv, AttentionArgs& a, const smetric_heads& q, float scale, const smetric_heads& out,
+                     float* d_lse, smetric_stream_t stream) {
   const smetric_kv_config& c = kv->cfg;
-  static thread_local AttentionArgs a;
   {
     const cuuint64_t dims[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.num_q_heads, (cuuint64_t)kv->n_tokens};
     const cuuint64_t strides[2] = {stride_of(q.head_stride, c.num_q_heads), stride_of(q.token_stride, kv->n_tokens)};
     const cuuint32_t box[3] = {64, (cuuint32_t)kv->group, (cuuint32_t)kv->tile_tokens};
     if (!encode(&a.q, c.dtype, 3, q.d_data, dims, strides, box)) return SMETRIC_ERR_INVALID_ARG;
-  }
-  {
-    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.num_kv_heads,
-                                (cuuint64_t)c.num_pages};
-    const cuuint64_t strides[3] = {stride_of(cache.token_stride, c.page_size),
-                                   stride_of(cache.head_stride, c.num_kv_heads),
-                                   stride_of(cache.page_stride, c.num_pages)};
-    const cuuint32_t box[4] = {64, (cuuint32_t)std::min(c.page_size, kTile), 1, 1};
-    if (!encode(&a.k, c.dtype, 4, cache.d_k, dims, strides, box) ||
-        !encode(&a.v, c.dtype, 4, cache.d_v, dims, strides, box))
-      return SMETRIC_ERR_INVALID_ARG;
   }
   a.out = out;
   a.lse = d_lse;
@@ -1089,15 +1278,61 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
   a.status = kv->status;
   const int halves = c.head_dim > 64 ? 2 : 1;
   auto kern = c.dtype == SMETRIC_BF16
-                  ? (halves == 2 ? k_paged_attention<__nv_bfloat16, 2> : k_paged_attention<__nv_bfloat16, 1>)
-                  : (halves == 2 ? k_paged_attention<__half, 2> : k_paged_attention<__half, 1>);
+                  ? (halves == 2 ? k_paged_attention<__nv_bfloat16, 2, kFour> : k_paged_attention<__nv_bfloat16, 1, kFour>)
+                  : (halves == 2 ? k_paged_attention<__half, 2, kFour> : k_paged_attention<__half, 1, kFour>);
   kv->launches += 2;
-  rc = launch_k(kern, dim3((unsigned)kv->num_sms), dim3(kThreads), smem_bytes(halves),
-                reinterpret_cast<cudaStream_t>(stream), true, a);
+  const int rc = launch_k(kern, dim3((unsigned)kv->num_sms), dim3(kThreads), smem_bytes(halves, kFour),
+                          reinterpret_cast<cudaStream_t>(stream), true, a);
   if (rc) return rc;
   auto join = c.dtype == SMETRIC_BF16 ? k_paged_join<__nv_bfloat16> : k_paged_join<__half>;
   return launch_k(join, dim3((unsigned)kv->num_sms * kJoinBlocks), dim3(kJoinThreads), 0,
                   reinterpret_cast<cudaStream_t>(stream), true, a);
+}
+}  // namespace
+
+bool smetric::attention_limits(bool four) {
+  return four ? limits<__nv_bfloat16, true>() && limits<__half, true>()
+              : limits<__nv_bfloat16, false>() && limits<__half, false>();
+}
+
+int smetric::attention_many_rows(smetric_kv* kv, const smetric_kvq_cache& k_cache, const smetric_kvq_cache& v_cache,
+                                 const smetric_heads& q, float scale, const smetric_heads& out, float* d_lse,
+                                 smetric_stream_t stream) {
+  static thread_local AttentionArgs a;
+  a.k4 = k_cache;
+  a.v4 = v_cache;
+  a.v_scale = std::ldexp(1.f, v_cache.exp);
+  a.clears = !kv->few.rows;
+  return launch_attention<true>(kv, a, q, std::ldexp(scale, k_cache.exp), out, d_lse, stream);
+}
+
+extern "C" {
+
+int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_heads q, float scale, smetric_heads out,
+                            float* d_lse, smetric_stream_t stream) {
+  CallRange range("smetric_paged_attention");
+  int rc = check_device(kv);
+  if (rc) return rc;
+  if (four_bits(kv) || !kv->planned || !std::isfinite(scale) || !(scale > 0.f) || !cache_ok(cache) || !heads_ok(q, kv->n_tokens) ||
+      !heads_ok(out, kv->n_tokens) || (reinterpret_cast<uintptr_t>(d_lse) & 3))
+    return SMETRIC_ERR_INVALID_ARG;
+  if (kv->n_tokens == 0) return SMETRIC_OK;
+  const smetric_kv_config& c = kv->cfg;
+  static thread_local AttentionArgs a;
+  {
+    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.num_kv_heads,
+                                (cuuint64_t)c.num_pages};
+    const cuuint64_t strides[3] = {stride_of(cache.token_stride, c.page_size),
+                                   stride_of(cache.head_stride, c.num_kv_heads),
+                                   stride_of(cache.page_stride, c.num_pages)};
+    const cuuint32_t box[4] = {64, (cuuint32_t)std::min(c.page_size, kTile), 1, 1};
+    if (!encode(&a.k, c.dtype, 4, cache.d_k, dims, strides, box) ||
+        !encode(&a.v, c.dtype, 4, cache.d_v, dims, strides, box))
+      return SMETRIC_ERR_INVALID_ARG;
+  }
+  a.v_scale = 1.f;
+  a.clears = true;
+  return launch_attention<false>(kv, a, q, scale, out, d_lse, stream);
 }
 
 }  // extern "C"

@@ -1,7 +1,8 @@
 // The paged KV$ operators around the attention: the handle, the plan of a
 // batch, and the norm + rotation + append pass.
 //
-//   k_kv_plan      block 0 checks the batch and shares its attention out;
+//   k_kv_plan      block 0 checks the batch and shares its attention out (with
+//                  caches in 4 bits block 1 does so for the requests of few rows);
 //                  the other blocks find each new token's request by bisection
 //                  of the offsets, its position and its slot in the cache.
 //                  Bound by latency: 5 to 8 us from one request to 86,000
@@ -37,13 +38,25 @@ constexpr unsigned kFull = 0xffffffffu;
 constexpr int kPlanThreads = 1024;
 constexpr int kMaxCtas = 1024;  // attention CTAs that a plan shares work out to
 
-// A unit's cost, in 1,000 cycles as measured with heads of 128 elements (shorter
-// ones, whose tiles cost less, have the same proportions by assumption): for each
-// key tile, where it has two query tiles or one, and for what it does once (its
-// queries' load, the first scores, its output). A CTA takes at least kMinCost, and a unit is cut
-// at least kMinTiles from its ends.
-__device__ __forceinline__ int tile_cost(const KvUnit& u, int tile_tokens) { return u.tokens > tile_tokens ? 3 : 2; }
-__device__ __forceinline__ int once_cost(const KvUnit& u, int tile_tokens) { return u.tokens > tile_tokens ? 6 : 4; }
+// What a kernel's units are and what they cost. For the attention of 16-bit
+// caches a unit's cost is in 1,000 cycles as measured with heads of 128 elements
+// (shorter ones, whose tiles cost less, have the same proportions by assumption):
+// for each key tile, where it has two query tiles or one, and for what it does
+// once (its queries' load, the first scores, its output). A CTA takes at least
+// min_cost, and a unit is cut at least min_tiles from its ends.
+struct PlanSet {
+  KvUnit* units;
+  int64_t* unit_cost;
+  int32_t* unit_base;
+  KvShare* shares;
+  int32_t* split;
+  int32_t* n_split;
+  int32_t over, up_to;   // its requests' new tokens: more than `over`, at most `up_to`
+  int32_t per, one;      // a unit's tokens at most, and those of one query tile
+  int32_t tile, heads;   // keys of a tile; heads (or blocks of them) a unit is done for, one at a time
+  int32_t tile_cost[2], once_cost[2];  // with one query tile, with two
+  int32_t min_cost, min_tiles;
+};
 constexpr int kMinCost = 8;
 constexpr int kMinTiles = 2;
 
@@ -55,14 +68,10 @@ struct PlanArgs {
   const int32_t* pages;
   int32_t max_pages, page_size;
   int64_t pages_stride, num_pages;
-  int32_t window, tile_tokens, kv_heads, ctas;
+  int32_t window, ctas, sets;
+  PlanSet set[2];
   KvPlan* plan;
   KvToken* tokens;
-  KvUnit* units;
-  int64_t* unit_cost;
-  int32_t* unit_base;
-  KvShare* shares;
-  int32_t* split;
   int32_t* status;
 };
 
@@ -109,18 +118,19 @@ __device__ int32_t last_at_most(const S* a, int32_t n, int64_t x, int64_t scale)
 // Shares the batch's attention out: the key tiles of all (unit, key head)
 // pairs in a row, cut into one stretch of equal cost for each CTA, so that one
 // long sequence and many short ones load the SMs alike.
-__device__ void plan_units(const PlanArgs& a) {
+__device__ void plan_units(const PlanArgs& a, const PlanSet& s) {
   __shared__ int64_t sums[32];
   __shared__ int32_t su[kMaxCtas + 1], sh[kMaxCtas + 1], st[kMaxCtas + 1];
   __shared__ int32_t n_split;
-  const int per = 2 * a.tile_tokens;
+  const int per = s.per;
   int64_t base = 0;
   for (int32_t r0 = 0; r0 < a.n; r0 += kPlanThreads) {
     const int32_t r = r0 + threadIdx.x;
-    const int64_t mine = r < a.n ? (a.off[r + 1] - a.off[r] + per - 1) / per : 0;
+    const int64_t lq = r < a.n ? a.off[r + 1] - a.off[r] : 0;
+    const int64_t mine = lq > s.over && lq <= s.up_to ? (lq + per - 1) / per : 0;
     int64_t total;
     const int64_t at = block_scan(mine, sums, total);
-    if (r < a.n) a.unit_base[r] = (int32_t)(base + at);
+    if (r < a.n) s.unit_base[r] = (int32_t)(base + at);
     base += total;
   }
   const int32_t U = (int32_t)base;
@@ -130,41 +140,41 @@ __device__ void plan_units(const PlanArgs& a) {
     const int32_t u = u0 + threadIdx.x;
     int64_t mine = 0;
     if (u < U) {
-      const int32_t r = last_at_most(a.unit_base, a.n, u, 1);
-      const int64_t first = (int64_t)(u - a.unit_base[r]) * per, lq = a.off[r + 1] - a.off[r];
+      const int32_t r = last_at_most(s.unit_base, a.n, u, 1);
+      const int64_t first = (int64_t)(u - s.unit_base[r]) * per, lq = a.off[r + 1] - a.off[r];
       KvUnit x = {};
       x.token = (int32_t)(a.off[r] + first);
       x.tokens = (int32_t)min((int64_t)per, lq - first);
       x.pos = (int32_t)(a.kv_lens[r] - lq + first);
       x.req = r;
-      x.tb = x.pos >= a.window ? (x.pos - a.window + 1) / kTile : 0;
-      x.te = (x.pos + x.tokens - 1) / kTile + 1;
-      a.units[u] = x;
-      mine = (x.te - x.tb) * tile_cost(x, a.tile_tokens) + once_cost(x, a.tile_tokens);
+      x.tb = x.pos >= a.window ? (x.pos - a.window + 1) / s.tile : 0;
+      x.te = (x.pos + x.tokens - 1) / s.tile + 1;
+      s.units[u] = x;
+      mine = (x.te - x.tb) * s.tile_cost[x.tokens > s.one] + s.once_cost[x.tokens > s.one];
     }
     int64_t total;
     const int64_t at = block_scan(mine, sums, total);
-    if (u < U) a.unit_cost[u] = cost + at;
+    if (u < U) s.unit_cost[u] = cost + at;
     cost += total;
   }
   __syncthreads();
-  cost *= a.kv_heads;
-  const int ctas = (int)max((int64_t)1, min((int64_t)a.ctas, cost / kMinCost));
+  cost *= s.heads;
+  const int ctas = (int)max((int64_t)1, min((int64_t)a.ctas, cost / s.min_cost));
   for (int c = threadIdx.x; c <= ctas; c += kPlanThreads) {
     int32_t u = U, h = 0, t = 0;
     if (c < ctas && U > 0) {
       const int64_t x = cost / ctas * c + cost % ctas * c / ctas;
-      u = last_at_most(a.unit_cost, U, x, a.kv_heads);
-      const KvUnit unit = a.units[u];
-      const int per_tile = tile_cost(unit, a.tile_tokens), once = once_cost(unit, a.tile_tokens);
-      const int64_t one = (int64_t)(unit.te - unit.tb) * per_tile + once, in = x - a.unit_cost[u] * a.kv_heads;
+      u = last_at_most(s.unit_cost, U, x, s.heads);
+      const KvUnit unit = s.units[u];
+      const int per_tile = s.tile_cost[unit.tokens > s.one], once = s.once_cost[unit.tokens > s.one];
+      const int64_t one = (int64_t)(unit.te - unit.tb) * per_tile + once, in = x - s.unit_cost[u] * s.heads;
       h = (int32_t)(in / one);
       t = unit.tb + (int32_t)(max((int64_t)0, in % one - once) / per_tile);
-      if (t - unit.tb < kMinTiles) {
+      if (t - unit.tb < s.min_tiles) {
         t = unit.tb;
-      } else if (unit.te - t < kMinTiles) {
-        if (++h == a.kv_heads) h = 0, ++u;
-        t = u < U ? a.units[u].tb : 0;
+      } else if (unit.te - t < s.min_tiles) {
+        if (++h == s.heads) h = 0, ++u;
+        t = u < U ? s.units[u].tb : 0;
       }
     }
     su[c] = u, sh[c] = h, st[c] = t;
@@ -172,56 +182,57 @@ __device__ void plan_units(const PlanArgs& a) {
   if (threadIdx.x == 0) n_split = 0;
   __syncthreads();
   for (int c = threadIdx.x; c < a.ctas; c += kPlanThreads) {
-    KvShare s = {};
-    s.u0 = -1;
+    KvShare x = {};
+    x.u0 = -1;
     if (c < ctas && (su[c] != su[c + 1] || sh[c] != sh[c + 1] || st[c] != st[c + 1])) {
-      s.u0 = su[c], s.h0 = sh[c], s.t0 = st[c];
-      s.first = a.units[s.u0];
-      s.u1 = su[c + 1], s.h1 = sh[c + 1], s.t1 = st[c + 1];
-      const bool cut = s.u1 < U && s.t1 > a.units[s.u1].tb;
+      x.u0 = su[c], x.h0 = sh[c], x.t0 = st[c];
+      x.first = s.units[x.u0];
+      x.u1 = su[c + 1], x.h1 = sh[c + 1], x.t1 = st[c + 1];
+      const bool cut = x.u1 < U && x.t1 > s.units[x.u1].tb;
       if (!cut) {
-        if (--s.h1 < 0) s.h1 = a.kv_heads - 1, --s.u1;
-        s.t1 = a.units[s.u1].te;
+        if (--x.h1 < 0) x.h1 = s.heads - 1, --x.u1;
+        x.t1 = s.units[x.u1].te;
       }
       const auto same = [&](int i, int32_t u, int32_t h) {
-        return i <= ctas && su[i] == u && sh[i] == h && u < U && st[i] > a.units[u].tb;
+        return i <= ctas && su[i] == u && sh[i] == h && u < U && st[i] > s.units[u].tb;
       };
-      s.last = a.units[s.u1];
-      s.n_last = 1;
-      while (same(c + s.n_last, s.u1, s.h1)) ++s.n_last;
+      x.last = s.units[x.u1];
+      x.n_last = 1;
+      while (same(c + x.n_last, x.u1, x.h1)) ++x.n_last;
       // (their order decides which blocks join them, not how)
-      if (s.n_last > 1 && !same(c, s.u1, s.h1)) a.split[atomicAdd(&n_split, 1)] = c;
+      if (x.n_last > 1 && !same(c, x.u1, x.h1)) s.split[atomicAdd(&n_split, 1)] = c;
     }
-    a.shares[c] = s;
+    s.shares[c] = x;
   }
   __syncthreads();
-  if (threadIdx.x == 0) a.plan->n_split = n_split, a.plan->n_units = U;
+  if (threadIdx.x == 0) *s.n_split = n_split;
 }
 
 __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(const __grid_constant__ PlanArgs a) {
   pdl_enter();
-  if (blockIdx.x == 0) {
+  if ((int)blockIdx.x < a.sets) {
+    const PlanSet& s = a.set[blockIdx.x];
     int bad = 0;
     for (int32_t r = threadIdx.x; r < a.n; r += blockDim.x) {
       const int64_t lo = a.off[r], hi = a.off[r + 1], kv = a.kv_lens[r];
       bad |= lo < 0 || hi < lo || hi > a.n_tokens || kv < hi - lo || kv > (int64_t)a.max_pages * a.page_size;
     }
     bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && blockIdx.x == 0) {
       if (bad) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
       a.plan->first = bad || a.n == 0 ? a.n_tokens : a.off[0];
       a.plan->last = bad || a.n == 0 ? a.n_tokens : a.off[a.n];
       a.plan->valid = !bad;
     }
     if (!bad) {
-      plan_units(a);
+      plan_units(a, s);
     } else {
-      for (int i = threadIdx.x; i < a.ctas; i += kPlanThreads) a.shares[i].u0 = -1;
-      if (threadIdx.x == 0) a.plan->n_split = a.plan->n_units = 0;
+      for (int i = threadIdx.x; i < a.ctas; i += kPlanThreads) s.shares[i].u0 = -1;
+      if (threadIdx.x == 0) *s.n_split = 0;
     }
     return;
   }
-  const int64_t t = (int64_t)(blockIdx.x - 1) * blockDim.x + threadIdx.x;
+  const int64_t t = (int64_t)(blockIdx.x - a.sets) * blockDim.x + threadIdx.x;
   if (t >= a.n_tokens) return;
   KvToken tok = {-1, -1, 0};
   if (a.n > 0) {
@@ -662,6 +673,17 @@ size_t lay_out(smetric_kv* kv, unsigned char* mem) {
   part(kv->split, kv->num_sms);
   part(kv->part, slots * kv->cfg.head_dim);
   part(kv->part_ml, slots);
+  KvFew& f = kv->few;
+  if (f.rows) {
+    const size_t rows = 2 * (size_t)kv->num_sms * f.heads * f.rows;
+    part(f.units, 2 * requests + 1);
+    part(f.unit_cost, 2 * requests + 2);
+    part(f.unit_base, requests + 1);
+    part(f.shares, kv->num_sms);
+    part(f.split, kv->num_sms);
+    part(f.part, rows * kv->cfg.head_dim);
+    part(f.part_ml, rows);
+  }
   return at;
 }
 
@@ -695,6 +717,13 @@ int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out) {
   kv->cfg = c;
   kv->group = c.num_q_heads / c.num_kv_heads;
   kv->tile_tokens = kTile / kv->group;
+  if (four_bits(kv) && kv->group <= 16) {
+    KvFew& f = kv->few;
+    f.rows = kv->group <= 8 ? 8 : 16;
+    f.tokens = f.rows / kv->group;
+    f.blocks = (c.num_kv_heads + few_heads(f.rows) - 1) / few_heads(f.rows);
+    f.heads = (c.num_kv_heads + f.blocks - 1) / f.blocks;
+  }
   unsigned char* mem = nullptr;
   bool ok = cudaGetDevice(&kv->device) == cudaSuccess &&
             cudaDeviceGetAttribute(&kv->num_sms, cudaDevAttrMultiProcessorCount, kv->device) == cudaSuccess;
@@ -704,7 +733,7 @@ int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out) {
   }
   if (ok) {
     lay_out(kv, mem);
-    ok = attention_limits() && cudaMemset(kv->status, 0, sizeof(int32_t)) == cudaSuccess &&
+    ok = attention_limits(four_bits(kv)) && (!kv->few.rows || few_limits()) && cudaMemset(kv->status, 0, sizeof(int32_t)) == cudaSuccess &&
          cudaDeviceSynchronize() == cudaSuccess;
   }
   if (!ok) {
@@ -754,22 +783,51 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
   a.pages_stride = pages_stride;
   a.num_pages = kv->cfg.num_pages;
   a.window = window > 0 ? window : INT32_MAX;
-  a.tile_tokens = kv->tile_tokens;
-  a.kv_heads = kv->cfg.num_kv_heads;
   a.ctas = kv->num_sms;
   a.plan = kv->plan;
   a.tokens = kv->tokens;
-  a.units = kv->units;
-  a.unit_cost = kv->unit_cost;
-  a.unit_base = kv->unit_base;
-  a.shares = kv->shares;
-  a.split = kv->split;
+  const KvFew& f = kv->few;
+  // A step of single tokens (or of requests with nothing new among them) goes to
+  // the few-row kernel whole, so that the other need not be launched.
+  const bool all_few = f.rows && n_tokens <= n_requests;
+  a.sets = f.rows ? 2 : 1;
+  PlanSet& s = a.set[0];
+  s.units = kv->units;
+  s.unit_cost = kv->unit_cost;
+  s.unit_base = kv->unit_base;
+  s.shares = kv->shares;
+  s.split = kv->split;
+  s.n_split = &kv->plan->n_split;
+  s.over = all_few ? INT32_MAX : f.rows ? f.tokens : 0;
+  s.up_to = INT32_MAX;
+  s.per = 2 * kv->tile_tokens, s.one = kv->tile_tokens;
+  s.tile = kTile, s.heads = kv->cfg.num_kv_heads;
+  s.tile_cost[0] = 2, s.tile_cost[1] = 3;
+  s.once_cost[0] = 4, s.once_cost[1] = 6;
+  s.min_cost = kMinCost, s.min_tiles = kMinTiles;
+  if (f.rows) {
+    PlanSet& w = a.set[1];
+    w.units = f.units;
+    w.unit_cost = f.unit_cost;
+    w.unit_base = f.unit_base;
+    w.shares = f.shares;
+    w.split = f.split;
+    w.n_split = &kv->plan->n_split_few;
+    w.over = 0;
+    w.up_to = all_few ? INT32_MAX : f.tokens;
+    w.per = w.one = f.tokens;
+    w.tile = kFewTile, w.heads = f.blocks;
+    w.tile_cost[0] = w.tile_cost[1] = f.heads;
+    w.once_cost[0] = w.once_cost[1] = 16;
+    w.min_cost = 16, w.min_tiles = 1;
+  }
   a.status = kv->status;
-  const unsigned grid = 1 + (unsigned)((n_tokens + kPlanThreads - 1) / kPlanThreads);
+  const unsigned grid = (unsigned)a.sets + (unsigned)((n_tokens + kPlanThreads - 1) / kPlanThreads);
   kv->launches++;
   rc = launch_k(k_kv_plan, dim3(grid), dim3(kPlanThreads), 0, reinterpret_cast<cudaStream_t>(stream), true, a);
   if (rc) return rc;
   kv->planned = true;
+  kv->all_few = all_few;
   kv->n_tokens = n_tokens;
   kv->pages = d_pages;
   kv->pages_stride = pages_stride;

@@ -141,88 +141,570 @@ __global__ void __launch_bounds__(kReadThreads) k_kv4_read(const __grid_constant
   }
 }
 
-// ---- attention ----
+// ---- attention of few rows ----
 
-struct Attention4Args {
+struct FewArgs {
   smetric_kvq_cache k, v;
   smetric_heads q, out;
   float* lse;
   const KvPlan* plan;
   const KvUnit* units;
+  const KvShare* shares;
+  const int32_t* split;
+  float* part;
+  float2* part_ml;
   const int32_t* pages;
   int64_t pages_stride, n_tokens;
-  int32_t num_pages, hq, kv_heads, group, D, page_shift, window;
-  float scale;
+  int32_t num_pages, hq, hk, group, heads, blocks, page_shift, window;
+  float scale;  // of scores in powers of 2
+  float v_scale;
+  bool bf16;
   int32_t* status;
 };
 
-template <typename T>
-__device__ __forceinline__ float to_float(T x);
-template <>
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <>
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+constexpr float kLift = 7.f;   // weights up to 2^(kLift + kSlack): half precision ends at 65,504
+constexpr float kSlack = 8.f;  // log2 of how far scores may pass the reference
 
-template <typename T>
-__global__ void __launch_bounds__(128) k_kv4_attention(const __grid_constant__ Attention4Args a) {
-  pdl_enter();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int E = a.D / 32;  // elements a lane
-  const float ks = exp2f((float)a.k.exp), vs = exp2f((float)a.v.exp);
-  for (int64_t x = blockIdx.x; x < (int64_t)a.plan->n_units * a.kv_heads; x += gridDim.x) {
-    const KvUnit u = a.units[x / a.kv_heads];
-    const int h = (int)(x % a.kv_heads);
-    const int32_t* pages = a.pages + u.req * a.pages_stride;
-    for (int row = warp; row < u.tokens * a.group; row += 4) {
-      const int64_t token = u.token + row / a.group;
-      const int head = h * a.group + row % a.group;
-      const int32_t pos = u.pos + row / a.group;
-      float q[4] = {}, o[4] = {};
-      for (int e = 0; e < E; ++e)
-        q[e] = to_float(static_cast<const T*>(a.q.d_data)[token * a.q.token_stride + head * a.q.head_stride + lane * E + e]);
-      float top = -INFINITY, l = 0.f;
-      for (int32_t j = pos >= a.window ? pos - a.window + 1 : 0; j <= pos; ++j) {
-        const int32_t page = pages[j >> a.page_shift];
-        const bool held = page >= 0 && page < a.num_pages;
-        if (!held) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
-        const int64_t in = j & ((1 << a.page_shift) - 1);
-        const auto element = [&](const smetric_kvq_cache& c, int d) {
-          if (!held) return 0.f;
-          const uint8_t b = static_cast<const uint8_t*>(c.d_codes)[page * c.page_stride + in * c.token_stride + h * c.head_stride + d / 2];
-          const uint8_t s = static_cast<const uint8_t*>(c.d_scales)[page * c.scale_page_stride + in * c.scale_token_stride +
-                                                                    h * c.scale_head_stride + d / 16];
-          const float2 f = floats(pair_of<0>(b));
-          return (d & 1 ? f.y : f.x) * floats(scales_of(s)).x;
-        };
-        float s = 0.f;
-        for (int e = 0; e < E; ++e) s += q[e] * element(a.k, lane * E + e);
-        for (int i = 16; i; i >>= 1) s += __shfl_xor_sync(kFull, s, i);
-        s *= a.scale * ks;
-        const float next = fmaxf(top, s);
-        const float f = expf(top - next), p = expf(s - next);
-        top = next;
-        l = l * f + p;
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f + p * element(a.v, lane * E + e);
+__host__ __device__ constexpr int stage_bytes(int D) { return 2 * kFewTile * (D / 2 + scale_bytes(D)); }
+__host__ __device__ constexpr int stages(int D, int rows) {
+  return 225 * 1024 / (few_heads(rows) * stage_bytes(D)) < 8 ? 225 * 1024 / (few_heads(rows) * stage_bytes(D)) : 8;
+}
+__host__ __device__ constexpr int ring_bytes(int D, int rows) { return few_heads(rows) * stages(D, rows) * stage_bytes(D); }
+// A row of a warp's sums in shared memory, in floats: 4 past a multiple of 32, so that
+// the rows of the lanes that store together lie in other banks.
+__host__ __device__ constexpr int sum_row(int D) { return D + 4; }
+__host__ __device__ constexpr int few_smem(int D, int rows) {
+  const int sums = few_heads(rows) * rows * (sum_row(D) + 2) * 4;
+  return ring_bytes(D, rows) > sums ? ring_bytes(D, rows) : sums;
+}
+static_assert(few_smem(128, 8) <= 232448 && few_smem(128, 16) <= 232448 && few_smem(32, 8) <= 232448, "227 KB");
+
+struct FewItem {
+  KvUnit unit;
+  int32_t hb, tb, te;  // block of key heads, its key tiles in this CTA
+  bool whole;          // nobody else has key tiles of it
+  int32_t slot;        // of its partial sums, where !whole
+};
+
+// The CTA's share, item by item.
+struct FewWalk {
+  KvUnit unit;
+  int32_t u, h, t0, u1, h1, t1;
+  bool first, done;
+  __device__ __forceinline__ void start(const FewArgs& a) {
+    const KvShare& s = a.shares[blockIdx.x];
+    unit = s.first;
+    u = s.u0, h = s.h0, t0 = s.t0, u1 = s.u1, h1 = s.h1, t1 = s.t1;
+    first = true;
+    done = u < 0;
+  }
+  __device__ __forceinline__ bool next(const FewArgs& a, FewItem& it) {
+    if (done) return false;
+    const bool last = u == u1 && h == h1;
+    it.unit = unit;
+    it.hb = h;
+    it.tb = first ? t0 : unit.tb;
+    it.te = last ? t1 : unit.te;
+    it.whole = it.tb == unit.tb && it.te == unit.te;
+    it.slot = 2 * (int32_t)blockIdx.x + (it.tb == unit.tb);
+    first = false;
+    done = last;
+    if (++h == a.blocks && !done) {
+      h = 0;
+      unit = a.units[++u];
+    }
+    return true;
+  }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// D (16 x 8, 32 bits) += A (16 x 16) B (16 x 8).
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
+  return r;
+}
+template <int N>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool held) {
+  if constexpr (N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(held ? 16 : 0) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(held ? N : 0) : "memory");
+}
+
+// A warp's two rows of queries as the products' B operand, and their powers of 2.
+// Lane (g, c) = (lane / 4, lane % 4) has row g's elements [c D/4, (c+1) D/4). A row
+// goes to half precision divided by the power of two of its largest element: 8 or 11
+// bits fit, and what is lost below 2^-24 of the largest is lost to 32-bit sums too.
+template <int D>
+__device__ __forceinline__ void load_rows(const FewArgs& a, const KvUnit& u, int head, int n0, uint32_t (&qf)[D / 16][2],
+                                          float& power) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3, n = n0 + g;
+  const bool mine = n < u.tokens * a.group;
+  float f[D / 4];
+#pragma unroll
+  for (int i = 0; i < D / 4; ++i) f[i] = 0.f;
+  if (mine) {
+    const int64_t at = (int64_t)(u.token + n / a.group) * a.q.token_stride + (int64_t)(head * a.group + n % a.group) * a.q.head_stride;
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q.d_data) + at + c * (D / 4));
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const uint4 x = p[i];
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 y = a.bf16 ? make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u)) : floats(w[k]);
+        f[8 * i + 2 * k] = y.x, f[8 * i + 2 * k + 1] = y.y;
       }
-      for (int e = 0; e < E; ++e) {
-        const uint32_t y = round2<T>(make_float2(o[e] / l * vs, 0.f));
-        reinterpret_cast<uint16_t*>(a.out.d_data)[token * a.out.token_stride + head * a.out.head_stride + lane * E + e] = (uint16_t)y;
-      }
-      if (a.lse && lane == 0) a.lse[token * a.hq + head] = top + logf(l);
     }
   }
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 4; ++i) top = fmaxf(top, fabsf(f[i]));
+  top = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
+  top = fmaxf(top, __shfl_xor_sync(kFull, top, 2));
+  // 2^(E - 127) <= top; infinities keep their row as it is
+  uint32_t E = __float_as_uint(top) >> 23;
+  E = E == 0 ? 1 : E >= 254 ? 127 : E;
+  const float down = __uint_as_float((254 - E) << 23);
+  power = __uint_as_float(E << 23);
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) qf[i][k] = round2<__half>(make_float2(f[4 * i + 2 * k] * down, f[4 * i + 2 * k + 1] * down));
+}
+
+// Attention of up to NB * 8 query rows (a token's heads of one key head, or a few
+// tokens') at a time. Every warp has a key head and every `streams`-th tile of 32
+// keys of the CTA's share, and joins its sums with the head's other warps' at the
+// item's end.
+//
+// Tokens are the long side of both products: S^T = K Q^T and O^T = V^T P^T, in
+// mma.sync of 16 x 8 x 16, so that a code goes from the cache to a register of the
+// operand with one conversion (two codes) and one product with its scale, both
+// exact in half precision (2 and 4 bits). P^T is S^T's registers after a transposition
+// of 8 x 8 blocks.
+template <int D, int NB>
+__global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __grid_constant__ FewArgs a) {
+  constexpr int kWarps = few_heads(8 * NB), kRows = 8 * NB, kStages = stages(D, kRows), kStage = stage_bytes(D);
+  constexpr int W = D / 32;               // words of codes a lane has of a key, and half words of a value
+  constexpr int kCodes = kFewTile * D / 2, kScales = kFewTile * scale_bytes(D), SB = scale_bytes(D);
+  extern __shared__ __align__(128) unsigned char smem[];
+  pdl_enter();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   // tokens of no request
-  const int64_t first = a.plan->first, last = a.plan->last, none = first + a.n_tokens - last;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < none * a.hq * a.D; i += (int64_t)gridDim.x * blockDim.x) {
-    const int64_t x = i / a.D, h = x % a.hq;
-    int64_t t = x / a.hq;
-    if (t >= first) t += last - first;
-    reinterpret_cast<uint16_t*>(a.out.d_data)[t * a.out.token_stride + h * a.out.head_stride + i % a.D] = 0;
-    if (a.lse) a.lse[t * a.hq + h] = -INFINITY;
+  {
+    const int64_t first = a.plan->first, last = a.plan->last, none = first + a.n_tokens - last, pieces = none * a.hq * (D / 8);
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * blockDim.x) {
+      const int64_t x = i / (D / 8), h = x % a.hq;
+      int64_t t = x / a.hq;
+      if (t >= first) t += last - first;
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out.d_data) + t * a.out.token_stride + h * a.out.head_stride + i % (D / 8) * 8) =
+          make_uint4(0, 0, 0, 0);
+      if (a.lse) a.lse[t * a.hq + h] = -INFINITY;
+    }
+  }
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * kStages * kStage;
+  const unsigned char* const ring_p = smem + warp * kStages * kStage;
+  const int page_size = 1 << a.page_shift;
+  // Row r of a tile's keys in shared memory (the product's row) is token 2 c -> c, 2 c + 1
+  // -> 4 + c of each 8: so lane (g, c)'s values, of the product's inner places 2 c, 2 c +
+  // 1, are tokens c and 4 + c, whose rows lie in other banks for other c.
+  const auto row_of = [](int token) { return (token & ~7) | (token & 3) << 1 | (token >> 2 & 1); };
+  const auto token_of = [](int row) { return (row & ~7) | (row & 1) << 2 | (row >> 1 & 3); };
+  FewWalk w;
+  w.start(a);
+  FewItem it;
+  while (w.next(a, it)) {
+    const int heads = min(a.heads, a.hk - it.hb * a.heads);
+    const int streams = kWarps / heads;
+    const int my_head = warp % heads, stream = warp / heads;
+    const bool busy = stream < streams;
+    const int head = it.hb * a.heads + my_head;
+    const KvUnit& u = it.unit;
+    const int32_t seen_lo = u.pos >= a.window ? u.pos - a.window + 1 : 0, seen_hi = u.pos + u.tokens;  // keys that some row sees
+    const int n = busy ? max(0, (it.te - it.tb - stream + streams - 1) / streams) : 0;
+    float o[D / 16][NB][4], ref[NB][2], lim[NB][2], l[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[m][b][i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) ref[b][i] = 0.f, lim[b][i] = -INFINITY, l[b][i] = 0.f;
+    }
+    if (n > 0) {
+      const int32_t* pages = a.pages + u.req * a.pages_stride;
+      const auto key_of = [&](int j) { return (int64_t)(it.tb + stream + (int64_t)j * streams) * kFewTile; };
+      // pages of a tile's two halves, -1 where nobody sees a key of it
+      const auto page_of = [&](int j, int half) {
+        const int64_t key = key_of(j) + 16 * half;
+        return j < n && key < seen_hi && key + 16 > seen_lo ? pages[key >> a.page_shift] : INT32_MIN;
+      };
+      int32_t next[2] = {page_of(0, 0), page_of(0, 1)};
+      const uint8_t* const kc = static_cast<const uint8_t*>(a.k.d_codes) + head * a.k.head_stride;
+      const uint8_t* const vc = static_cast<const uint8_t*>(a.v.d_codes) + head * a.v.head_stride;
+      const uint8_t* const ks = static_cast<const uint8_t*>(a.k.d_scales) + head * a.k.scale_head_stride;
+      const uint8_t* const vs = static_cast<const uint8_t*>(a.v.d_scales) + head * a.v.scale_head_stride;
+      const auto copy = [&](int j) {
+        const uint32_t at = ring + j % kStages * kStage;
+        int32_t page[2] = {next[0], next[1]};
+        next[0] = page_of(j + 1, 0), next[1] = page_of(j + 1, 1);
+        const int64_t key = key_of(j);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (page[h] != INT32_MIN && (page[h] < 0 || page[h] >= a.num_pages)) {
+            latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
+            page[h] = -1;
+          }
+        }
+        const int in = (int)(key & (page_size - 1));  // (of the second half: 16 more, or from its page's start)
+        const auto token_at = [&](int token, int64_t page_stride, int64_t token_stride) {
+          const int half = token >> 4;
+          const int64_t p = half ? page[1] : page[0];
+          return max(p, (int64_t)0) * page_stride + ((in + token) & (page_size - 1)) * token_stride;
+        };
+        const auto held = [&](int token) {
+          return (token >> 4 ? page[1] : page[0]) >= 0 && key + token >= seen_lo && key + token < seen_hi;
+        };
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const int x = i * 32 + lane, token = x / W, piece = x - token * W;
+          const bool in_cache = held(token);
+          copy_async<16>(at + row_of(token) * (D / 2) + 16 * piece, kc + token_at(token, a.k.page_stride, a.k.token_stride) + 16 * piece, in_cache);
+          // (128 elements: tokens 2, 3 of each 4 have their halves changed over, for the banks)
+          const int to = D == 128 ? piece ^ (token & 2) : piece;
+          copy_async<16>(at + kCodes + token * (D / 2) + 16 * to, vc + token_at(token, a.v.page_stride, a.v.token_stride) + 16 * piece, in_cache);
+        }
+        const bool in_cache = held(lane);
+        copy_async<SB>(at + 2 * kCodes + row_of(lane) * SB, ks + token_at(lane, a.k.scale_page_stride, a.k.scale_token_stride), in_cache);
+        copy_async<SB>(at + 2 * kCodes + kScales + lane * SB, vs + token_at(lane, a.v.scale_page_stride, a.v.scale_token_stride), in_cache);
+      };
+#pragma unroll
+      for (int j = 0; j < kStages - 1; ++j) {
+        if (j < n) copy(j);
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
+      }
+      uint32_t qf[NB][D / 16][2];
+      float cs[NB][2];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        float power;
+        load_rows<D>(a, u, head, 8 * b, qf[b], power);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) cs[b][i] = __shfl_sync(kFull, power, 4 * (2 * c + i)) * a.scale;
+      }
+      for (int j = 0; j < n; ++j) {
+        asm volatile("cp.async.wait_group %0;\n" ::"n"(kStages - 2) : "memory");
+        __syncwarp();
+        if (j + kStages - 1 < n) copy(j + kStages - 1);
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
+        const unsigned char* const at = ring_p + j % kStages * kStage;
+        // scores: S[half][block][...] of tokens token_of(g), token_of(g + 8) and rows 2c, 2c + 1
+        float s[2][NB][4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[t][b][i] = 0.f;
+          uint32_t codes[2][W], scales[2][W];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = 16 * t + 8 * i + g;
+            const unsigned char* p = at + row * (D / 2) + 4 * W * c;
+            if constexpr (W == 4) {
+              const uint4 x = *reinterpret_cast<const uint4*>(p);
+              codes[i][0] = x.x, codes[i][1] = x.y, codes[i][2] = x.z, codes[i][3] = x.w;
+            } else if constexpr (W == 2) {
+              const uint2 x = *reinterpret_cast<const uint2*>(p);
+              codes[i][0] = x.x, codes[i][1] = x.y;
+            } else {
+#pragma unroll
+              for (int k = 0; k < W; ++k) codes[i][k] = reinterpret_cast<const uint32_t*>(p)[k];
+            }
+            const uint32_t* sp = reinterpret_cast<const uint32_t*>(at + 2 * kCodes + row * SB);
+            const uint32_t lo = sp[0], hi = SB == 8 ? sp[1] : 0;
+#pragma unroll
+            for (int k = 0; k < W; ++k) scales[i][k] = scales_of(__byte_perm(lo, hi, (W * c + k) / 2 * 0x11));  // (its group's, twice)
+          }
+#pragma unroll
+          for (int k = 0; k < W; ++k) {
+            uint32_t f[2][2], h[2][2];  // the word's pairs: rows g, g + 8
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              f[i][0] = mul_h2(pair_of<0>(codes[i][k]), scales[i][k]);
+              f[i][1] = mul_h2(pair_of<1>(codes[i][k]), scales[i][k]);
+              h[i][0] = mul_h2(pair_of<2>(codes[i][k]), scales[i][k]);
+              h[i][1] = mul_h2(pair_of<3>(codes[i][k]), scales[i][k]);
+            }
+            const uint32_t x[4] = {f[0][0], f[1][0], f[0][1], f[1][1]}, y[4] = {h[0][0], h[1][0], h[0][1], h[1][1]};
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+              mma(s[t][b], x, qf[b][2 * k][0], qf[b][2 * k][1]);
+              mma(s[t][b], y, qf[b][2 * k + 1][0], qf[b][2 * k + 1][1]);
+            }
+          }
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[t][b][i] *= cs[b][i & 1];
+        }
+        const int64_t key = key_of(j);
+        if (key + kFewTile - 1 > u.pos || key < seen_hi - a.window) {  // some row does not see some key
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int64_t hi = u.pos + (8 * b + 2 * c + i) / a.group;
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const int64_t x = key + 16 * t + token_of(8 * k + g);
+                  if (x > hi || x <= hi - a.window) s[t][b][2 * k + i] = -INFINITY;
+                }
+            }
+        }
+        bool move = false;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            move |= fmaxf(fmaxf(s[0][b][i], s[0][b][i + 2]), fmaxf(s[1][b][i], s[1][b][i + 2])) > lim[b][i];
+        if (__any_sync(kFull, move)) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              float top = fmaxf(fmaxf(s[0][b][i], s[0][b][i + 2]), fmaxf(s[1][b][i], s[1][b][i + 2]));
+#pragma unroll
+              for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, x));
+              if (top > lim[b][i]) {
+                const float to = top - kLift, back = lim[b][i] == -INFINITY ? 0.f : ex2(ref[b][i] - to);
+                ref[b][i] = to, lim[b][i] = top + kSlack;
+                l[b][i] *= back;
+#pragma unroll
+                for (int m = 0; m < D / 16; ++m) o[m][b][i] *= back, o[m][b][i + 2] *= back;
+              }
+            }
+        }
+        uint32_t p[2][NB][2];  // weights, as the second product's operand
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float x = ex2(s[t][b][2 * k] - ref[b][0]), y = ex2(s[t][b][2 * k + 1] - ref[b][1]);
+              l[b][0] += x, l[b][1] += y;
+              p[t][b][k] = transposed(round2<__half>(make_float2(x, y)));
+            }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          // values of tokens c, 4 + c, 8 + c, 12 + c of the half, elements [g D/8, (g+1) D/8)
+          uint32_t even[2][(W + 1) / 2], odd[2][(W + 1) / 2], scales[2][2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            uint32_t x[2][(W + 1) / 2], sb[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int token = 16 * t + 8 * k + 4 * i + c;
+              const unsigned char* row = at + kCodes + token * (D / 2);
+              if constexpr (W == 4) {
+                const uint2 y = *reinterpret_cast<const uint2*>(row + 16 * ((g >> 1) ^ (token & 2)) + 8 * (g & 1));
+                x[i][0] = y.x, x[i][1] = y.y;
+              } else if constexpr (W == 2) {
+                x[i][0] = *reinterpret_cast<const uint32_t*>(row + 4 * g);
+              } else {
+                const uint16_t* y = reinterpret_cast<const uint16_t*>(row + 2 * W * g);
+                x[i][0] = y[0];
+                if constexpr (W == 3) x[i][0] |= (uint32_t)y[1] << 16, x[i][1] = y[2];
+              }
+              const unsigned char* sp = at + 2 * kCodes + kScales + token * SB;
+              sb[i][0] = sp[W * g / 4];
+              sb[i][1] = W == 3 ? sp[min((W * g / 4) + 1, D / 16 - 1)] : 0;
+            }
+#pragma unroll
+            for (int q = 0; q < (W + 1) / 2; ++q) {
+              const uint32_t y = x[0][q], z = x[1][q];
+              even[k][q] = (y & 0x0f0f0f0fu) | (z << 4 & 0xf0f0f0f0u);
+              odd[k][q] = (y >> 4 & 0x0f0f0f0fu) | (z & 0xf0f0f0f0u);
+            }
+            scales[k][0] = scales_of(sb[0][0] | sb[1][0] << 8);
+            scales[k][1] = W == 3 ? scales_of(sb[0][1] | sb[1][1] << 8) : 0;
+          }
+#pragma unroll
+          for (int m = 0; m < D / 16; ++m) {
+            const auto byte = [&](uint32_t x) {
+              return m % 4 == 0 ? pair_of<0>(x) : m % 4 == 1 ? pair_of<1>(x) : m % 4 == 2 ? pair_of<2>(x) : pair_of<3>(x);
+            };
+            // (heads of 96: a lane's 12 elements lie in two groups)
+            const bool second = W == 3 && (12 * g + 2 * m) / 16 > 12 * g / 16;
+            const uint32_t s0 = second ? scales[0][1] : scales[0][0], s1 = second ? scales[1][1] : scales[1][0];
+            const uint32_t x[4] = {mul_h2(byte(even[0][m / 4]), s0), mul_h2(byte(odd[0][m / 4]), s0),
+                                   mul_h2(byte(even[1][m / 4]), s1), mul_h2(byte(odd[1][m / 4]), s1)};
+#pragma unroll
+            for (int b = 0; b < NB; ++b) mma(o[m][b], x, p[t][b][0], p[t][b][1]);
+          }
+        }
+      }
+      asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+    }
+    // the item's sums: warps of a head side by side in shared memory
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[b][i] += __shfl_xor_sync(kFull, l[b][i], x);
+      }
+    __syncthreads();  // (the rings are done with)
+    float* const sums = reinterpret_cast<float*>(smem);
+    float2* const stats = reinterpret_cast<float2*>(sums + kWarps * kRows * sum_row(D));
+    if (busy) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = warp * kRows + 8 * b + 2 * c + i;
+#pragma unroll
+          for (int m = 0; m < D / 16; ++m)  // (elements g D/8 + 2m, + 1)
+            *reinterpret_cast<float2*>(sums + row * sum_row(D) + 16 * m + 2 * g) = make_float2(o[m][b][i], o[m][b][i + 2]);
+          if (g == 0) stats[row] = make_float2(lim[b][i] == -INFINITY && l[b][i] == 0.f ? -INFINITY : ref[b][i], l[b][i]);
+        }
+    }
+    __syncthreads();
+    const int rows = u.tokens * a.group;
+    for (int x = threadIdx.x; x < heads * rows * (D / 4); x += kWarps * 32) {
+      const int d = x % (D / 4) * 4, y = x / (D / 4), row = y % rows, h = y / rows;
+      float top = -INFINITY;
+      for (int k = 0; k < streams; ++k) top = fmaxf(top, stats[(k * heads + h) * kRows + row].x);
+      float sum = 0.f;
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < streams; ++k) {
+        const int at = (k * heads + h) * kRows + row;
+        const float2 st = stats[at];
+        if (st.x == -INFINITY) continue;
+        const float e = ex2(st.x - top);
+        const int q = d / (D / 8), m = d % (D / 8) / 2;
+        const float2 p0 = *reinterpret_cast<const float2*>(sums + at * sum_row(D) + 16 * m + 2 * q);
+        const float2 p1 = *reinterpret_cast<const float2*>(sums + at * sum_row(D) + 16 * (m + 1) + 2 * q);
+        sum += st.y * e;
+        f.x += p0.x * e, f.y += p0.y * e, f.z += p1.x * e, f.w += p1.y * e;
+      }
+      if (it.whole) {
+        const int64_t token = u.token + row / a.group;
+        const int qh = (it.hb * a.heads + h) * a.group + row % a.group;
+        const float inv = (sum > 0.f ? 1.f / sum : sum) * a.v_scale;  // (NaN stays)
+        uint16_t* to = static_cast<uint16_t*>(a.out.d_data) + token * a.out.token_stride + qh * a.out.head_stride + d;
+        const float2 e = make_float2(f.x * inv, f.y * inv), q = make_float2(f.z * inv, f.w * inv);
+        *reinterpret_cast<uint2*>(to) = a.bf16 ? make_uint2(round2<__nv_bfloat16>(e), round2<__nv_bfloat16>(q))
+                                               : make_uint2(round2<__half>(e), round2<__half>(q));
+        if (a.lse && d == 0) a.lse[token * a.hq + qh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+      } else {
+        const int64_t at = ((int64_t)it.slot * a.heads + h) * kRows + row;
+        *reinterpret_cast<float4*>(a.part + at * D + d) = f;
+        if (d == 0) a.part_ml[at] = make_float2(top, sum);
+      }
+    }
+    __syncthreads();  // (the sums' memory is the rings')
   }
 }
 
+// out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i over a unit's pieces.
+// A block has a row of a shared unit at a time, its 8 warps every 8th piece.
+constexpr int kFewJoin = 256;
+template <int D, int NB>
+__global__ void __launch_bounds__(kFewJoin) k_kv4_few_join(const __grid_constant__ FewArgs a) {
+  constexpr int kRows = 8 * NB;
+  __shared__ float4 sums[8][D / 4];
+  __shared__ float2 stats[8];
+  pdl_enter();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int per = a.heads * kRows;
+  for (int x = blockIdx.x; x < a.plan->n_split_few * per; x += gridDim.x) {
+    const int c1 = a.split[x / per], row = x % kRows, h = x % per / kRows;
+    const KvShare& s = a.shares[c1];
+    const KvUnit& u = s.last;
+    if (row >= u.tokens * a.group || s.h1 * a.heads + h >= a.hk) continue;  // (the same for the block)
+    const auto at = [&](int i) { return ((int64_t)(2 * (c1 + i) + (i == 0)) * a.heads + h) * kRows + row; };
+    float top = -INFINITY, l = 0.f;
+    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = warp; i < s.n_last; i += 8) {
+      const float2 ml = a.part_ml[at(i)];
+      float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (lane < D / 4) p = *reinterpret_cast<const float4*>(a.part + at(i) * D + 4 * lane);
+      const float to = fmaxf(top, ml.x);
+      if (to == -INFINITY) continue;
+      const float e = ex2(top - to), q = ex2(ml.x - to);
+      top = to;
+      l = l * e + ml.y * q;
+      f.x = f.x * e + p.x * q, f.y = f.y * e + p.y * q, f.z = f.z * e + p.z * q, f.w = f.w * e + p.w * q;
+    }
+    if (lane < D / 4) sums[warp][lane] = f;
+    if (lane == 0) stats[warp] = make_float2(top, l);
+    __syncthreads();
+    if (warp == 0 && lane < D / 4) {
+      top = -INFINITY, l = 0.f;
+      f = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top = fmaxf(top, stats[k].x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (stats[k].x == -INFINITY) continue;
+        const float e = ex2(stats[k].x - top);
+        const float4 p = sums[k][lane];
+        l += stats[k].y * e;
+        f.x += p.x * e, f.y += p.y * e, f.z += p.z * e, f.w += p.w * e;
+      }
+      const int64_t token = u.token + row / a.group;
+      const int qh = (s.h1 * a.heads + h) * a.group + row % a.group;
+      const float inv = (l > 0.f ? 1.f / l : l) * a.v_scale;
+      uint16_t* to = static_cast<uint16_t*>(a.out.d_data) + token * a.out.token_stride + qh * a.out.head_stride + 4 * lane;
+      const float2 e = make_float2(f.x * inv, f.y * inv), q = make_float2(f.z * inv, f.w * inv);
+      *reinterpret_cast<uint2*>(to) = a.bf16 ? make_uint2(round2<__nv_bfloat16>(e), round2<__nv_bfloat16>(q))
+                                             : make_uint2(round2<__half>(e), round2<__half>(q));
+      if (a.lse && lane == 0) a.lse[token * a.hq + qh] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+    }
+    __syncthreads();
+  }
+}
+
+template <int D, int NB>
+bool few_limit() {
+  return cudaFuncSetAttribute((const void*)k_kv4_few<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(D, 8 * NB)) ==
+         cudaSuccess;
+}
+template <int D, int NB>
+int launch_few(smetric_kv* kv, const FewArgs& a, cudaStream_t s) {
+  int rc = launch_k(k_kv4_few<D, NB>, dim3((unsigned)kv->num_sms), dim3(few_heads(8 * NB) * 32), (size_t)few_smem(D, 8 * NB), s, true, a);
+  if (rc) return rc;
+  kv->launches += 2;
+  return launch_k(k_kv4_few_join<D, NB>, dim3((unsigned)kv->num_sms * 4), dim3(kFewJoin), 0, s, true, a);
+}
+
 }  // namespace
+
+bool smetric::few_limits() {
+  return few_limit<32, 1>() && few_limit<32, 2>() && few_limit<64, 1>() && few_limit<64, 2>() && few_limit<96, 1>() &&
+         few_limit<96, 2>() && few_limit<128, 1>() && few_limit<128, 2>();
+}
 
 extern "C" {
 
@@ -274,29 +756,45 @@ int smetric_kvq_attention(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq
       !heads_ok(q, kv->n_tokens) || !heads_ok(out, kv->n_tokens) || (reinterpret_cast<uintptr_t>(d_lse) & 3))
     return SMETRIC_ERR_INVALID_ARG;
   if (kv->n_tokens == 0) return SMETRIC_OK;
-  Attention4Args a = {};
+  if (!kv->all_few) {
+    rc = attention_many_rows(kv, k_cache, v_cache, q, scale, out, d_lse, stream);
+    if (rc || !kv->few.rows) return rc;
+  }
+  FewArgs a = {};
   a.k = k_cache;
   a.v = v_cache;
   a.q = q;
   a.out = out;
   a.lse = d_lse;
   a.plan = kv->plan;
-  a.units = kv->units;
+  a.units = kv->few.units;
+  a.shares = kv->few.shares;
+  a.split = kv->few.split;
+  a.part = kv->few.part;
+  a.part_ml = kv->few.part_ml;
   a.pages = kv->pages;
   a.pages_stride = kv->pages_stride;
   a.n_tokens = kv->n_tokens;
   a.num_pages = (int32_t)c.num_pages;
   a.hq = c.num_q_heads;
-  a.kv_heads = c.num_kv_heads;
+  a.hk = c.num_kv_heads;
   a.group = kv->group;
-  a.D = c.head_dim;
+  a.heads = kv->few.heads;
+  a.blocks = kv->few.blocks;
   a.page_shift = __builtin_ctz((unsigned)c.page_size);
   a.window = kv->window;
-  a.scale = scale;
+  a.scale = std::ldexp(scale, k_cache.exp) * 1.4426950408889634f;
+  a.v_scale = std::ldexp(1.f, v_cache.exp);
+  a.bf16 = c.dtype == SMETRIC_BF16;
   a.status = kv->status;
-  kv->launches++;
-  return launch_k(c.dtype == SMETRIC_BF16 ? k_kv4_attention<__nv_bfloat16> : k_kv4_attention<__half>,
-                  dim3((unsigned)kv->num_sms * 8), dim3(128), 0, reinterpret_cast<cudaStream_t>(stream), true, a);
+  const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const bool one = kv->few.rows == 8;
+  switch (c.head_dim) {
+    case 32: return one ? launch_few<32, 1>(kv, a, s) : launch_few<32, 2>(kv, a, s);
+    case 64: return one ? launch_few<64, 1>(kv, a, s) : launch_few<64, 2>(kv, a, s);
+    case 96: return one ? launch_few<96, 1>(kv, a, s) : launch_few<96, 2>(kv, a, s);
+    default: return one ? launch_few<128, 1>(kv, a, s) : launch_few<128, 2>(kv, a, s);
+  }
 }
 
 }  // extern "C"

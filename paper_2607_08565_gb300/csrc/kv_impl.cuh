@@ -21,7 +21,7 @@ struct KvPlan {
   int64_t first, last;  // tokens [first, last) belong to requests
   int32_t valid;        // 0: the batch's offsets or lengths were refused
   int32_t n_split;      // units that several CTAs share
-  int32_t n_units;
+  int32_t n_split_few;  // the same of the units of few rows
   int32_t reserved;
 };
 
@@ -52,6 +52,26 @@ struct __align__(16) KvShare {
   KvUnit first, last;  // units u0 and u1
 };
 
+// Caches in 4 bits: requests whose new tokens have at most `rows` query rows for
+// a key head are the share of a kernel of their own (kv4.cu), in units of their
+// tokens and one of `blocks` blocks of `heads` key heads each, and in tiles of
+// kFewTile keys.
+constexpr int kFewTile = 32;
+// Its warps, and so the key heads of a block at most.
+__host__ __device__ constexpr int few_heads(int rows) { return rows == 8 ? 16 : 12; }
+struct KvFew {
+  int rows;    // 8, 16, or 0: no such kernel (more than 16 query heads per key head)
+  int tokens;  // rows / group
+  int heads, blocks;
+  KvUnit* units;       // 2 * max_batch_requests
+  int64_t* unit_cost;  // as many + 1
+  int32_t* unit_base;  // max_batch_requests + 1
+  KvShare* shares;     // num_sms
+  int32_t* split;      // num_sms
+  float* part;         // 2 * num_sms slots of heads * rows * head_dim partial sums
+  float2* part_ml;     // and their rows' (reference exponent, sum of weights)
+};
+
 }  // namespace smetric
 
 struct smetric_kv {
@@ -70,8 +90,10 @@ struct smetric_kv {
   int32_t* split;            // num_sms: the CTAs that start a unit which others go on with
   float* part;               // 2 * num_sms slots of partial sums: a CTA's first unit's, its last's
   float2* part_ml;           // and their rows' (reference exponent, sum of weights)
+  smetric::KvFew few;
   // of the last plan
   bool planned;
+  bool all_few;  // every unit is the few-row kernel's
   int64_t n_tokens;
   const int32_t* pages;
   int64_t pages_stride;
@@ -83,7 +105,12 @@ namespace smetric {
 // Returns SMETRIC_OK if the handle is usable from the current device.
 int check_device(const smetric_kv* kv);
 // Sets the attention kernels' shared-memory limits; false on a CUDA error.
-bool attention_limits();
+bool attention_limits(bool four);
+bool few_limits();
+// Attention over caches in 4 bits of the plan's requests of more rows than few.rows.
+int attention_many_rows(smetric_kv* kv, const smetric_kvq_cache& k_cache, const smetric_kvq_cache& v_cache,
+                        const smetric_heads& q, float scale, const smetric_heads& out, float* d_lse,
+                        smetric_stream_t stream);
 // A row of heads that a kernel can address: 16-byte aligned, strides of whole
 // 16-byte pieces.
 inline bool heads_ok(const smetric_heads& h, int64_t n_tokens) {
