@@ -621,7 +621,7 @@ typedef struct {
  * head_dim / 2 bytes of codes and of 4 (head_dim <= 64) or 8 bytes of scales,
  * of which the first head_dim / 16 are used. Strides in bytes, any but that
  * d_codes and its strides are multiples of 16 and d_scales and its strides
- * of 4 (head_dim <= 64) or 8. */
+ * of 4 (head_dim <= 64) or 8, and that the pages' and tokens' are below 2^32. */
 typedef struct {
   void* d_codes;
   void* d_scales;

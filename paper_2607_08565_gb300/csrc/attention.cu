@@ -44,6 +44,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "call_range.cuh"
 #include "kv_impl.cuh"
@@ -63,22 +64,23 @@ constexpr float kSlack = 8.f;     // log2 of how far scores may pass the referen
 constexpr uint32_t kHalf = 16384;  // bytes of 128 rows of 64 elements
 
 // Buffers of the ring: what 227 KB hold beside the two query tiles (and, for
-// caches in 4 bits, their codes' way to the ring).
+// caches in 4 bits, the codes' way to the ring).
 __host__ __device__ constexpr int stages(int halves, bool four) {
-  return four ? (halves == 2 ? 4 : 9) : halves == 2 ? 5 : 11;
+  return four ? (halves == 2 ? 4 : 10) : halves == 2 ? 5 : 11;
 }
-// Caches in 4 bits: each of 3 warps converts every third 16 rows of a tile, whose
-// codes and scales are copied two tiles ahead.
+// Caches in 4 bits: each of 3 warps converts every third 16 rows of a tile, of which
+// codes and scales were copied to one of its 3 buffers two tiles before.
 constexpr int kConverters = 3;
-constexpr int kAhead = 3;  // buffers
-__host__ __device__ constexpr int group_bytes(int halves) { return 16 * (32 * halves + 4 * halves); }
+constexpr int kAhead = 3;
+__host__ __device__ constexpr int codes_bytes(int halves) { return 16 * 32 * halves; }  // of 16 rows
+__host__ __device__ constexpr int buffer_bytes(int halves) { return 3 * codes_bytes(halves); }
 __host__ __device__ constexpr int staging_bytes(int halves, bool four) {
-  return four ? kConverters * kAhead * 3 * group_bytes(halves) : 0;
+  return four ? kConverters * kAhead * (buffer_bytes(halves) + 3 * 16 * 4 * halves) : 0;
 }
 
 struct AttentionArgs {
   CUtensorMap q, k, v;
-  smetric_kvq_cache k4, v4;  // in place of k and v
+  smetric_kvq_cache k4, v4;  // (in 4 bits; k and v are of the codes)
   smetric_heads out;
   float* lse;
   const KvPlan* plan;
@@ -94,6 +96,63 @@ struct AttentionArgs {
   bool wide;    // outputs can be stored in pieces of 32 bytes
   bool clears;  // zeros for tokens of no request are this kernel's
   int32_t* status;
+};
+
+// ---- a CTA's share ----
+
+struct Item {
+  KvUnit unit;
+  int32_t h, tb, te;  // key head, its key tiles in this CTA
+  bool whole;         // nobody else has key tiles of it
+  bool pair;          // two query tiles (else the even and the odd key tiles)
+  int32_t slot;       // of its partial sums, where !whole
+};
+
+struct Walk {
+  KvUnit unit;  // the next item's
+  int32_t u, h, t0, u1, h1, t1;
+  bool first, done;
+  __device__ __forceinline__ void load(const KvUnit* p) {
+    const int4 x = reinterpret_cast<const int4*>(p)[0];
+    const int2 y = reinterpret_cast<const int2*>(p)[2];
+    unit.token = x.x, unit.tokens = x.y, unit.pos = x.z, unit.req = x.w, unit.tb = y.x, unit.te = y.y;
+  }
+  __device__ __forceinline__ void start(const AttentionArgs& a) {
+    const KvShare* s = a.shares + blockIdx.x;
+    const int4 x = reinterpret_cast<const int4*>(s)[0];
+    const int2 y = reinterpret_cast<const int2*>(s)[2];
+    load(&s->first);
+    u = x.x, h = x.y, t0 = x.z, u1 = x.w, h1 = y.x, t1 = y.y;
+    first = true;
+    done = u < 0;
+  }
+  // Its state in 13 words.
+  __device__ __forceinline__ void put(volatile int32_t* p) const {
+    p[0] = unit.token, p[1] = unit.tokens, p[2] = unit.pos, p[3] = unit.req, p[4] = unit.tb, p[5] = unit.te;
+    p[6] = u, p[7] = h, p[8] = t0, p[9] = u1, p[10] = h1, p[11] = t1, p[12] = first | done << 1;
+  }
+  __device__ __forceinline__ void get(const volatile int32_t* p) {
+    unit.token = p[0], unit.tokens = p[1], unit.pos = p[2], unit.req = p[3], unit.tb = p[4], unit.te = p[5];
+    u = p[6], h = p[7], t0 = p[8], u1 = p[9], h1 = p[10], t1 = p[11], first = p[12] & 1, done = p[12] >> 1;
+  }
+  __device__ __forceinline__ bool next(const AttentionArgs& a, Item& it) {
+    if (done) return false;
+    const bool last = u == u1 && h == h1;
+    it.unit = unit;
+    it.h = h;
+    it.tb = first ? t0 : unit.tb;
+    it.te = last ? t1 : unit.te;
+    it.pair = unit.tokens > a.tile_tokens;
+    it.whole = it.tb == unit.tb && it.te == unit.te;
+    it.slot = 2 * (int32_t)blockIdx.x + (it.tb == unit.tb);
+    first = false;
+    done = last;
+    if (++h == a.kv_heads && !done) {
+      h = 0;
+      load(a.units + ++u);  // (ahead of its use)
+    }
+    return true;
+  }
 };
 
 // ---- shared memory, TMA, tensor cores ----
@@ -116,6 +175,13 @@ struct Shared {
   float2 stat[2][kTile];  // a unit's (reference exponent, sum of weights), rows of the two tiles
   uint32_t tmem;
   int32_t abort;          // a wait ran out: everybody stops waiting
+};
+// What caches in 4 bits need besides.
+struct SharedFour : Shared {
+  uint64_t staged[kConverters][kAhead];  // codes copied
+  uint64_t q_raw[2];                     // query tiles that are yet to be converted
+  int32_t walk[kConverters][13];         // the converting warps' Walks
+  uint8_t power[4][kTile];               // exponents of the rows of the last query tiles, where they were converted
 };
 
 __device__ __forceinline__ void mbar_init(uint64_t* b, uint32_t count) {
@@ -311,54 +377,6 @@ struct Type<__half> {
   }
 };
 
-// ---- a CTA's share ----
-
-struct Item {
-  KvUnit unit;
-  int32_t h, tb, te;  // key head, its key tiles in this CTA
-  bool whole;         // nobody else has key tiles of it
-  bool pair;          // two query tiles (else the even and the odd key tiles)
-  int32_t slot;       // of its partial sums, where !whole
-};
-
-struct Walk {
-  KvUnit unit;  // the next item's
-  int32_t u, h, t0, u1, h1, t1;
-  bool first, done;
-  __device__ __forceinline__ void load(const KvUnit* p) {
-    const int4 x = reinterpret_cast<const int4*>(p)[0];
-    const int2 y = reinterpret_cast<const int2*>(p)[2];
-    unit.token = x.x, unit.tokens = x.y, unit.pos = x.z, unit.req = x.w, unit.tb = y.x, unit.te = y.y;
-  }
-  __device__ __forceinline__ void start(const AttentionArgs& a) {
-    const KvShare* s = a.shares + blockIdx.x;
-    const int4 x = reinterpret_cast<const int4*>(s)[0];
-    const int2 y = reinterpret_cast<const int2*>(s)[2];
-    load(&s->first);
-    u = x.x, h = x.y, t0 = x.z, u1 = x.w, h1 = y.x, t1 = y.y;
-    first = true;
-    done = u < 0;
-  }
-  __device__ __forceinline__ bool next(const AttentionArgs& a, Item& it) {
-    if (done) return false;
-    const bool last = u == u1 && h == h1;
-    it.unit = unit;
-    it.h = h;
-    it.tb = first ? t0 : unit.tb;
-    it.te = last ? t1 : unit.te;
-    it.pair = unit.tokens > a.tile_tokens;
-    it.whole = it.tb == unit.tb && it.te == unit.te;
-    it.slot = 2 * (int32_t)blockIdx.x + (it.tb == unit.tb);
-    first = false;
-    done = last;
-    if (++h == a.kv_heads && !done) {
-      h = 0;
-      load(a.units + ++u);  // (ahead of its use)
-    }
-    return true;
-  }
-};
-
 // Partial sums: a slot's two query tiles, each D/4 columns of kTile rows of four
 // sums, so that the threads of a warp (a row each) store in whole lines. The
 // place of a column's first row, in units of four sums.
@@ -376,9 +394,8 @@ __device__ __forceinline__ uint32_t place_v(int j, int n) { return min(2 + 2 * j
 // whole warp calls.
 template <int HALVES>
 __device__ __forceinline__ void copy_queries(const AttentionArgs& a, Shared* sh, const Item& it, int t, uint32_t nq,
-                                             uint32_t q_smem) {
+                                             uint32_t q_smem, uint64_t* full) {
   Barriers& b = sh->bar;
-  uint64_t* full = &b.q_full[nq & 1];
   if (nq > 1) mbar_wait(&b.q_empty[nq & 1], (nq / 2 - 1) & 1, sh, a.status);
   const bool stop = stopped(sh);
   if ((threadIdx.x & 31) == 0 && !stop) {
@@ -436,7 +453,7 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
                a.page_size > kTile ? (it.tb + j) * kTile % a.page_size : 0, it.h, page, &b.full[s]);
       }
       if (j == 0 && !values) {
-        for (int t = 0; t < (it.pair ? 2 : 1); ++t, ++nq) copy_queries<HALVES>(a, sh, it, t, nq, q_smem);
+        for (int t = 0; t < (it.pair ? 2 : 1); ++t, ++nq) copy_queries<HALVES>(a, sh, it, t, nq, q_smem, &b.q_full[nq & 1]);
       }
     }
     base += 2 * n;
@@ -446,163 +463,135 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
 
 // ---- caches in 4 bits ----
 
+// 8 bytes to shared memory, or zeros (4 for heads of at most 64 elements).
 template <int N>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool held) {
-  if constexpr (N == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(held ? 16 : 0) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(held ? N : 0) : "memory");
-}
-
-// 8 elements of 16 bits: a word of codes times a scale, which stands twice in a word.
-// Codes have 2 bits and scales 4: the products are exact. In bf16 a code goes
-// through half precision, whose bits three places down are the bits of 2^-112 of
-// it in bf16; the scale brings the 2^112.
-template <typename T>
-struct Decode;
-template <>
-struct Decode<__half> {
-  static __device__ __forceinline__ uint32_t scale(uint32_t two, int which) {
-    return __byte_perm(two, 0, which ? 0x3232 : 0x1010);
-  }
-  static __device__ __forceinline__ uint32_t pair(uint32_t code, uint32_t scale) {
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(code), "r"(scale));
-    return r;
-  }
-};
-template <>
-struct Decode<__nv_bfloat16> {
-  static __device__ __forceinline__ uint32_t scale(uint32_t two, int which) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&two));
-    const float s = (which ? f.y : f.x) * 5192296858534827628530496329220096.f;  // 2^112
-    return Type<__nv_bfloat16>::pack(s, s);
-  }
-  static __device__ __forceinline__ uint32_t pair(uint32_t code, uint32_t scale) {
-    const uint32_t x = (code & 0x80008000u) | (code >> 3 & 0x0fff0fffu);
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;\n" : "=r"(r) : "r"(x), "r"(scale));
-    return r;
-  }
-};
-template <typename T>
-__device__ __forceinline__ uint4 decode8(uint32_t codes, uint32_t scale) {
-  uint32_t h[4];
-  asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
-      " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}\n"
-      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
-  return make_uint4(Decode<T>::pair(h[0], scale), Decode<T>::pair(h[1], scale), Decode<T>::pair(h[2], scale),
-                    Decode<T>::pair(h[3], scale));
+__device__ __forceinline__ void copy_scales(uint32_t dst, const void* src, bool held) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(held ? N : 0) : "memory");
 }
 
 // What copy_tiles does, for caches in 4 bits: this warp's 16-row groups (number, +
-// 3, + 6) of every tile, copied as they are and written to the ring in 16 bits, in
-// the 128-byte swizzle. A tile's keys and values are laid out alike, so what is
-// converted needs no more than its place. Rows that nobody sees become zeros.
-template <typename T, int HALVES>
-__device__ __forceinline__ void convert_tiles(const AttentionArgs& a, Shared* sh, Walk w, uint32_t staging, uint32_t ring,
-                                              const int number) {
-  constexpr int S = stages(HALVES, true), SB = 4 * HALVES, G = group_bytes(HALVES), kCodes = 16 * 32 * HALVES;
+// 3, + 6) of every tile go as they are to a buffer of the warp's, and from there to the
+// ring in half precision, in the 128-byte swizzle: a conversion for two codes and a
+// product with their scale, both exact (2 and 4 bits). Rows that nobody sees have
+// scales of zero.
+template <int HALVES>
+__device__ __forceinline__ void convert_tiles(const AttentionArgs& a, SharedFour* sh, uint32_t ring, uint32_t staging, const int number) {
+  constexpr int S = stages(HALVES, true), SB = 4 * HALVES;
   Barriers& b = sh->bar;
-  const int lane = threadIdx.x & 31;
-  const int row = lane & 15;
-  const int pieces = a.D / 32;  // of 16 bytes, in a row; piece (lane >> 4) and, of longer heads, 2 more
-  const int page_shift = __ffs(a.page_size) - 1;
-  staging += number * kAhead * 3 * G;
-  // the next tile to copy
-  Item it;
-  bool more = w.next(a, it);
-  int place = 0, n = 0;
-  int32_t lo = 0, hi = 0, page = -1;  // the lane's 16-row group's page (lane & 7)
-  const auto tile_of = [&](bool& values) {
-    values = place == 2 * n - 1 || (place > 1 && !(place & 1));
-    return place == 2 * n - 1 ? n - 1 : place < 2 ? place : values ? (place - 2) / 2 : (place + 1) / 2;
-  };
+  const int lane = threadIdx.x & 31, row = lane & 15, odd = lane >> 4;
+  const int pieces = a.D / 32;  // of 16 bytes, in a row: a lane has piece `odd` and, of longer heads, 2 + odd
+  const int row_bytes = a.D / 2, page_shift = __ffs(a.page_size) - 1;
+  const uint32_t staged = staging + number * kAhead * buffer_bytes(HALVES);
+  const uint32_t staged_scales = staging + kConverters * kAhead * buffer_bytes(HALVES) + number * kAhead * 3 * 16 * SB;
+  // the item whose tiles are copied, what was copied of it, and the page of the lane's
+  // 16 rows (lane & 7) of its next tile
+  int32_t h = 0, tb = 0, n = 0, jk = 0, jv = 0, lo = 0, hi = 0, page = INT32_MIN;
+  const int32_t* row_pages = nullptr;
+  const auto is_values = [&]() { return jk == n || (jk > 1 && jv < jk - 1); };  // K0 K1 V0 K2 V1 K3 ...
   const auto look_up = [&]() {
-    bool values;
-    const int64_t key = (int64_t)(it.tb + tile_of(values)) * kTile + 16 * (lane & 7);
-    page = key < hi && key + 16 > lo ? a.pages[it.unit.req * a.pages_stride + (key >> page_shift)] : INT32_MIN;
+    const int64_t key = (int64_t)(tb + (is_values() ? jv : jk)) * kTile + 16 * (lane & 7);
+    page = key < hi && key + 16 > lo ? row_pages[key >> page_shift] : INT32_MIN;
   };
-  const auto enter = [&]() {
-    n = it.te - it.tb;
-    place = 0;
+  const auto next_item = [&]() {
+    Walk w;
+    w.get(sh->walk[number]);  // (not kept in registers: the loop has use for them)
+    Item it;
+    n = 0;
+    if (!w.next(a, it)) return;
+    __syncwarp();
+    if (lane == 0) w.put(sh->walk[number]);
+    __syncwarp();
+    h = it.h, tb = it.tb, n = it.te - it.tb, jk = jv = 0;
     lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0;  // the keys that some query of the unit sees
     hi = it.unit.pos + it.unit.tokens;
+    row_pages = a.pages + it.unit.req * a.pages_stride;
     look_up();
   };
-  if (more) enter();
+  next_item();
   uint32_t copied = 0;
   const auto copy = [&]() {
-    if (more) {
-      bool values;
-      const int64_t key0 = (int64_t)(it.tb + tile_of(values)) * kTile;
-      const smetric_kvq_cache& c = values ? a.v4 : a.k4;
-      const uint8_t* codes = static_cast<const uint8_t*>(c.d_codes) + it.h * c.head_stride;
-      const uint8_t* scales = static_cast<const uint8_t*>(c.d_scales) + it.h * c.scale_head_stride;
-      if (page != INT32_MIN && (page < 0 || page >= a.num_pages)) {
+    if (n > 0) {
+      const bool values = is_values();
+      const int64_t key = (int64_t)(tb + (values ? jv : jk)) * kTile;
+      const uint32_t in_page = (uint32_t)key & (a.page_size - 1);
+      if (page != INT32_MIN && (uint32_t)page >= (uint32_t)a.num_pages) {
         latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
         page = INT32_MIN;
       }
-      const uint32_t to = staging + copied % kAhead * 3 * G;
+      const uint32_t buffer = copied % kAhead;
+      uint64_t* const full = &sh->staged[number][buffer];
+      const int mine = number + 3 * lane;  // lanes 0 to 2: a group each
+      const int32_t p = __shfl_sync(kFull, page, mine & 7);
+      const bool copies = lane < 3 && mine < kTile / 16 && p != INT32_MIN;
+      const unsigned who = __ballot_sync(kFull, copies);
+      if (lane == 0) mbar_expect(full, __popc(who) * 16 * row_bytes);
+      __syncwarp();
+      if (copies)
+        tma_4d(staged + buffer * buffer_bytes(HALVES) + lane * codes_bytes(HALVES), values ? &a.v : &a.k, 0,
+               (in_page + 16 * mine) & (a.page_size - 1), h, p, full);
+      const smetric_kvq_cache& c = values ? a.v4 : a.k4;
+      const uint8_t* scales = static_cast<const uint8_t*>(c.d_scales) + h * c.scale_head_stride;
 #pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        const int group = number + 3 * i;
-        const int32_t p = __shfl_sync(kFull, page, group & 7);
-        if (group >= kTile / 16) continue;
-        const int64_t key = key0 + 16 * group + row;
-        const bool held = p != INT32_MIN && key >= lo && key < hi;
-        const int64_t in = key & (a.page_size - 1), at = held ? p : 0;
-        const uint8_t* from = codes + at * c.page_stride + in * c.token_stride;
-#pragma unroll
-        for (int k = 0; k < HALVES; ++k) {
-          const int piece = 2 * k + (lane >> 4);
-          if (piece < pieces) copy_async<16>(to + i * G + (piece * 16 + row) * 16, from + 16 * piece, held);
-        }
-        if (lane < 16)
-          copy_async<SB>(to + i * G + kCodes + row * SB, scales + at * c.scale_page_stride + in * c.scale_token_stride, held);
+      for (int i = 0; i < 2; ++i) {
+        const int g = odd + 2 * i, group = number + 3 * g;  // the lane's row of it
+        const int32_t q = __shfl_sync(kFull, page, group & 7);
+        const int64_t x = key + 16 * group + row;
+        const bool held = q != INT32_MIN && x >= lo && x < hi;
+        const uint32_t in = (in_page + 16 * group + row) & (a.page_size - 1);
+        // (strides below 2^32)
+        if (g < 3 && group < kTile / 16)
+          copy_scales<SB>(staged_scales + (buffer * 48 + 16 * g + row) * SB,
+                          scales + (uint64_t)(held ? (uint32_t)q : 0u) * (uint32_t)c.scale_page_stride +
+                              (uint64_t)in * (uint32_t)c.scale_token_stride, held);
       }
       ++copied;
-      if (++place == 2 * n) {
-        more = w.next(a, it);
-        if (more) enter();
-      } else {
+      if (values)
+        ++jv;
+      else
+        ++jk;
+      if (jv == n)
+        next_item();
+      else
         look_up();
-      }
     }
     asm volatile("cp.async.commit_group;\n" ::: "memory");
   };
   for (int i = 0; i < kAhead - 1; ++i) copy();
   for (uint32_t at = 0; at < copied; ++at) {
-    asm volatile("cp.async.wait_group %0;\n" ::"n"(kAhead - 2) : "memory");
-    __syncwarp();
     copy();
-    const uint32_t s = at % S, from = staging + at % kAhead * 3 * G;
+    const uint32_t s = at % S, buffer = at % kAhead;
+    asm volatile("cp.async.wait_group %0;\n" ::"n"(kAhead - 1) : "memory");
+    mbar_wait(&sh->staged[number][buffer], at / kAhead & 1, sh, a.status);
     if (at >= S) mbar_wait(&b.empty[s], (at / S - 1) & 1, sh, a.status);
     if (stopped(sh)) break;
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       const int group = number + 3 * i;
       if (group >= kTile / 16) continue;
-      const int r = 16 * group + row;
 #pragma unroll
-      for (int k = 0; k < HALVES; ++k) {
-        const int piece = 2 * k + (lane >> 4);
+      for (int e = 0; e < HALVES; ++e) {
+        const int piece = 2 * e + odd;
         if (piece >= pieces) continue;
-        uint4 x;
-        uint32_t two;
+        // (rows of 64 and of 32 bytes are swizzled, for the banks)
+        const int at_piece = row_bytes == 64 ? piece ^ (row >> 1 & 3) : row_bytes == 32 ? piece ^ (row >> 2 & 1) : piece;
+        uint32_t word[4], h2;
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n"
-                     : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(from + i * G + (piece * 16 + row) * 16) : "memory");
+                     : "=r"(word[0]), "=r"(word[1]), "=r"(word[2]), "=r"(word[3])
+                     : "r"(staged + buffer * buffer_bytes(HALVES) + i * codes_bytes(HALVES) + row * row_bytes + 16 * at_piece)
+                     : "memory");
         asm volatile("{\n .reg .b16 x;\n ld.shared.b16 x, [%1];\n cvt.rn.f16x2.e4m3x2 %0, x;\n}\n"
-                     : "=r"(two) : "r"(from + i * G + kCodes + row * SB + 2 * piece) : "memory");
-        const uint32_t scale[2] = {Decode<T>::scale(two, 0), Decode<T>::scale(two, 1)};
-        const uint32_t word[4] = {x.x, x.y, x.z, x.w};
-        const uint32_t to = ring + (s * HALVES + (piece >> 1)) * kHalf + r * 128;
+                     : "=r"(h2) : "r"(staged_scales + (buffer * 48 + 16 * i + row) * SB + 2 * piece) : "memory");
+        const uint32_t scale[2] = {__byte_perm(h2, 0, 0x1010), __byte_perm(h2, 0, 0x3232)};
+        const uint32_t dst = ring + (s * HALVES + e) * kHalf + (16 * group + row) * 128;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const uint4 y = decode8<T>(word[q], scale[q >> 1]);
-          const int chunk = (4 * piece + q) & 7;
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(to + ((chunk ^ (r & 7)) << 4)), "r"(y.x), "r"(y.y),
-                       "r"(y.z), "r"(y.w) : "memory");
+          uint32_t y[4];
+          asm("{\n .reg .b8 a, b, c, d;\n .reg .b32 e, f, g, h;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 e, a;\n"
+              " cvt.rn.f16x2.e2m1x2 f, b;\n cvt.rn.f16x2.e2m1x2 g, c;\n cvt.rn.f16x2.e2m1x2 h, d;\n mul.rn.f16x2 %0, e, %5;\n"
+              " mul.rn.f16x2 %1, f, %5;\n mul.rn.f16x2 %2, g, %5;\n mul.rn.f16x2 %3, h, %5;\n}\n"
+              : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(word[q]), "r"(scale[q >> 1]));
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(dst + (((4 * odd + q) ^ (row & 7)) << 4)), "r"(y[0]),
+                       "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
         }
       }
     }
@@ -611,6 +600,36 @@ __device__ __forceinline__ void convert_tiles(const AttentionArgs& a, Shared* sh
     if (lane == 0) mbar_arrive(&b.full[s]);
   }
   asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+}
+
+// A row (the thread's) of query tile number nq from bf16 to half precision, in its
+// place: divided by the power of two of its largest element, so that its 8 bits fit;
+// what is lost below 2^-24 of the largest is lost to 32-bit sums too.
+template <int HALVES>
+__device__ __forceinline__ void convert_row(SharedFour* sh, uint32_t nq, uint32_t q_smem, int row) {
+  const uint32_t at = q_smem + (nq & 1) * HALVES * kHalf + row * 128;
+  const auto chunk = [&](int j) { return at + (j >> 3) * kHalf + (((j & 7) ^ (row & 7)) << 4); };
+  uint32_t top = 0;  // magnitudes' bits order as they do
+#pragma unroll 4
+  for (int j = 0; j < 8 * HALVES; ++j) {
+    uint32_t x[4];
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(chunk(j)) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __vmaxu2(top, x[i] & 0x7fff7fffu);
+  }
+  const uint32_t most = max(top >> 16, top & 0xffff) >> 7;
+  const uint32_t E = most == 0 ? 1 : most >= 254 ? 127 : most;  // (infinities keep their row as it is)
+  const float down = __uint_as_float((254 - E) << 23);
+  sh->power[nq & 3][row] = (uint8_t)E;
+#pragma unroll 4
+  for (int j = 0; j < 8 * HALVES; ++j) {
+    uint32_t x[4];
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(chunk(j)) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      x[i] = Type<__half>::pack(__uint_as_float(x[i] << 16) * down, __uint_as_float(x[i] & 0xffff0000u) * down);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(chunk(j)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+  }
 }
 
 // Issues the products, a step's (weights with values, then the half's next
@@ -791,15 +810,16 @@ __device__ __forceinline__ int tile_rows(const AttentionArgs& a, const Item& it,
 __device__ __forceinline__ uint32_t below(int32_t n) { return n <= 0 ? 0 : n >= 32 ? kFull : (1u << n) - 1; }
 
 // (One code for both tiles: two copies miss the instruction cache.)
-template <typename T>
+// kPowers: the scores are of rows divided by a power of two.
+template <typename T, bool kPowers>
 __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk w, const int tile) {
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)warp << 21;  // the warp's TMEM lanes
   const uint32_t s_at = sh->tmem + tile * kTile + lanes, o_at = sh->tmem + 2 * kTile + tile * kTile + lanes;
   const int row_token = row / a.group;
-  const float c = a.scale * 1.4426950408889634f;
-  uint32_t ns = 0, items = 0;
+  float c = a.scale * 1.4426950408889634f;
+  uint32_t ns = 0, items = 0, nq = 0;
   Item it;
   for (; w.next(a, it); ++items) {
     const int n = it.te - it.tb;
@@ -815,6 +835,9 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
     float l = 0.f;
     for (int j = it.pair ? 0 : tile; j < n; j += it.pair ? 1 : 2) {
       mbar_wait(&b.s_full[tile], ns++ & 1, sh, a.status);
+      if (kPowers && j <= tile)
+        c = a.scale * 1.4426950408889634f *
+            __uint_as_float((uint32_t) * (volatile uint8_t*)&static_cast<SharedFour*>(sh)->power[(nq + (it.pair ? tile : 0)) & 3][row] << 23);
       if (!busy) {
         __syncwarp();
         if (lane == 0) mbar_arrive(&b.p_full[tile]);
@@ -887,6 +910,7 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
       const float2 all = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
       l += all.x + all.y;
     }
+    nq += it.pair ? 2 : 1;
     if (items) mbar_wait(&b.o_free[tile], (items - 1) & 1, sh, a.status);
     // (scores that are all NaN leave top where it was, but not l: the row is not
     // one without keys, and what joins its pieces must not pass over it)
@@ -898,9 +922,9 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
 
 // A unit's output: O / l, or its sums and statistics where other CTAs have
 // pieces of it.
-// With caches in 4 bits its first warp also copies the query tiles, an item's
-// before the output of the item before: the converting warps, who could wait for a
-// query buffer only after the tiles that they have not converted yet, cannot.
+// With caches in 4 bits these warps also have the query tiles, an item's before the
+// output of the item before (its converting warps could wait for a query buffer only
+// after the tiles that they have not converted yet): copied, and in bf16 converted.
 template <typename T, int HALVES, bool kFour>
 __device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Walk w, uint32_t q_smem) {
   Barriers& b = sh->bar;
@@ -908,16 +932,30 @@ __device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Wa
   const uint32_t o_all = sh->tmem + 2 * kTile + ((uint32_t)warp << 21);
   const int row_token = row / a.group, row_head = row - row_token * a.group;
   uint32_t items = 0, no[2] = {0, 0}, nq = 0;
+  constexpr bool kConvert = kFour && std::is_same<T, __nv_bfloat16>::value;
   Walk ahead = w;
   const auto queries = [&]() {
     Item next;
-    if (ahead.next(a, next))
-      for (int t = 0; t < (next.pair ? 2 : 1); ++t, ++nq) copy_queries<HALVES>(a, sh, next, t, nq, q_smem);
+    if (!ahead.next(a, next)) return;
+    const int tiles = next.pair ? 2 : 1;
+    if (warp == 0)
+      for (int t = 0; t < tiles; ++t)
+        copy_queries<HALVES>(a, sh, next, t, nq + t, q_smem, (kConvert ? static_cast<SharedFour*>(sh)->q_raw : b.q_full) + (nq + t & 1));
+    if (kConvert) {
+      for (int t = 0; t < tiles; ++t) {
+        mbar_wait(&static_cast<SharedFour*>(sh)->q_raw[nq + t & 1], (nq + t) / 2 & 1, sh, a.status);
+        convert_row<HALVES>(static_cast<SharedFour*>(sh), nq + t, q_smem, row);
+        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b.q_full[nq + t & 1]);
+      }
+    }
+    nq += tiles;
   };
-  if (kFour && warp == 0) queries();
+  if (kFour) queries();
   Item it;
   for (; w.next(a, it); ++items) {
-    if (kFour && warp == 0) queries();
+    if (kFour) queries();
     const bool two = !it.pair && it.te - it.tb > 1;  // sums of even and of odd key tiles
     for (int tile = 0; tile < (it.pair ? 2 : 1); ++tile) {
       const int n_rows = tile_rows(a, it, tile);
@@ -993,8 +1031,10 @@ __device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Wa
 template <typename T, int HALVES, bool kFour>
 __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_constant__ AttentionArgs a) {
   constexpr int S = stages(HALVES, kFour);
+  using M = std::conditional_t<kFour, __half, T>;  // what the matrix products take
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  Shared* sh = reinterpret_cast<Shared*>(smem_raw + (2 + S) * HALVES * kHalf + staging_bytes(HALVES, kFour));
+  using Sh = std::conditional_t<kFour, SharedFour, Shared>;
+  Sh* sh = reinterpret_cast<Sh*>(smem_raw + (2 + S) * HALVES * kHalf + staging_bytes(HALVES, kFour));
   if (smem_u32(smem_raw) & 1023) {  // (the swizzle's groups of 8 rows)
     latch_error(a.status, SMETRIC_ERR_CUDA);
     return;
@@ -1005,7 +1045,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     Barriers& b = sh->bar;
     for (int i = 0; i < S; ++i) mbar_init(&b.full[i], kFour ? kConverters : 1), mbar_init(&b.empty[i], 1);
     for (int t = 0; t < 2; ++t) {
-      mbar_init(&b.q_full[t], 1);
+      mbar_init(&b.q_full[t], kFour && std::is_same<T, __nv_bfloat16>::value ? 4 : 1);
       mbar_init(&b.q_empty[t], 1);
       mbar_init(&b.s_full[t], 1);
       mbar_init(&b.p_full[t], 4);  // (a lane of each warp)
@@ -1013,14 +1053,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
       mbar_init(&b.o_free[t], 4);
       mbar_init(&b.stat_full[t], 4);
     }
+    if constexpr (kFour) {
+      for (int i = 0; i < kConverters * kAhead; ++i) mbar_init(&sh->staged[i / kAhead][i % kAhead], 1);
+      mbar_init(&sh->q_raw[0], 1), mbar_init(&sh->q_raw[1], 1);
+    }
     mbar_init(&b.drain, 1);
     sh->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.q)) : "memory");
-    if (!kFour) {
-      asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.k)) : "memory");
-      asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.v)) : "memory");
-    }
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.k)) : "memory");
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&a.v)) : "memory");
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&sh->tmem))
@@ -1033,6 +1075,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   Walk w;
   w.start(a);  // (its loads run while the CTA is set up)
+  if constexpr (kFour) {
+    if (threadIdx.x < kConverters) w.put(sh->walk[threadIdx.x]);
+  }
   fence_before();
   __syncthreads();
   fence_after();
@@ -1041,7 +1086,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
     if (warp == 1) {
-      multiply<T, HALVES, kFour>(a, sh, w, q_smem, ring);
+      multiply<M, HALVES, kFour>(a, sh, w, q_smem, ring);
     } else if (!kFour && warp != 3) {
       copy_tiles<HALVES>(a, sh, w, q_smem, ring, warp == 2);
     } else {
@@ -1059,11 +1104,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         }
         __syncwarp();
       }
-      if constexpr (kFour) convert_tiles<T, HALVES>(a, sh, w, staging, ring, warp == 0 ? 0 : warp - 1);
+      if constexpr (kFour) convert_tiles<HALVES>(a, sh, ring, staging, warp == 0 ? 0 : warp - 1);
     }
   } else if (warp < 12) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 176;\n");
-    softmax<T>(a, sh, w, (warp >> 2) - 1);
+    softmax<M, !std::is_same<M, T>::value>(a, sh, w, (warp >> 2) - 1);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
     write_out<T, HALVES, kFour>(a, sh, w, q_smem);
@@ -1214,7 +1259,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
 }
 
 constexpr size_t smem_bytes(int halves, bool four) {
-  return (size_t)(2 + stages(halves, four)) * halves * kHalf + staging_bytes(halves, four) + sizeof(Shared);
+  return (size_t)(2 + stages(halves, four)) * halves * kHalf + staging_bytes(halves, four) +
+         (four ? sizeof(SharedFour) : sizeof(Shared));
 }
 static_assert(smem_bytes(1, false) <= 232448 && smem_bytes(2, false) <= 232448 && smem_bytes(1, true) <= 232448 &&
                   smem_bytes(2, true) <= 232448, "227 KB");
@@ -1227,6 +1273,22 @@ bool encode(CUtensorMap* m, int32_t dtype, int rank, const void* base, const cuu
                     const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// 16 rows of a head's codes.
+bool encode_codes(CUtensorMap* m, const smetric_kv_config& c, const smetric_kvq_cache& cache) {
+  EncodeTiledFn enc = tensor_map_encoder();
+  const cuuint32_t one[4] = {1, 1, 1, 1}, box[4] = {(cuuint32_t)c.head_dim / 2, 16, 1, 1};
+  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim / 2, (cuuint64_t)c.page_size, (cuuint64_t)c.num_kv_heads,
+                              (cuuint64_t)c.num_pages};
+  // (a dimension of one entry may have any stride)
+  const cuuint64_t strides[3] = {(cuuint64_t)cache.token_stride, c.num_kv_heads > 1 ? (cuuint64_t)cache.head_stride : 256,
+                                 c.num_pages > 1 ? (cuuint64_t)cache.page_stride : 256};
+  return enc && enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, cache.d_codes, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    c.head_dim == 128  ? CU_TENSOR_MAP_SWIZZLE_64B
+                    : c.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_32B
+                                       : CU_TENSOR_MAP_SWIZZLE_NONE,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_64B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Bytes of a stride; a dimension of one entry may have any.
@@ -1299,6 +1361,7 @@ int smetric::attention_many_rows(smetric_kv* kv, const smetric_kvq_cache& k_cach
                                  const smetric_heads& q, float scale, const smetric_heads& out, float* d_lse,
                                  smetric_stream_t stream) {
   static thread_local AttentionArgs a;
+  if (!encode_codes(&a.k, kv->cfg, k_cache) || !encode_codes(&a.v, kv->cfg, v_cache)) return SMETRIC_ERR_INVALID_ARG;
   a.k4 = k_cache;
   a.v4 = v_cache;
   a.v_scale = std::ldexp(1.f, v_cache.exp);

@@ -238,12 +238,13 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
   return r;
 }
+// N bytes, of which the first `full` are read and the others zeros.
 template <int N>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool held) {
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int full) {
   if constexpr (N == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(held ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(full) : "memory");
   else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(held ? N : 0) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(full) : "memory");
 }
 
 // A warp's two rows of queries as the products' B operand, and their powers of 2.
@@ -350,50 +351,70 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
     }
     if (n > 0) {
       const int32_t* pages = a.pages + u.req * a.pages_stride;
-      const auto key_of = [&](int j) { return (int64_t)(it.tb + stream + (int64_t)j * streams) * kFewTile; };
-      // pages of a tile's two halves, -1 where nobody sees a key of it
-      const auto page_of = [&](int j, int half) {
-        const int64_t key = key_of(j) + 16 * half;
-        return j < n && key < seen_hi && key + 16 > seen_lo ? pages[key >> a.page_shift] : INT32_MIN;
+      const uint32_t key0 = (uint32_t)(it.tb + stream) * kFewTile, key_step = (uint32_t)streams * kFewTile;
+      // pages of a tile's two halves, INT32_MIN where nobody sees a key of one
+      const auto page_of = [&](int j, uint32_t key) {
+        return j < n && key < (uint32_t)seen_hi && key + 16 > (uint32_t)seen_lo ? pages[key >> a.page_shift] : INT32_MIN;
       };
-      int32_t next[2] = {page_of(0, 0), page_of(0, 1)};
-      const uint8_t* const kc = static_cast<const uint8_t*>(a.k.d_codes) + head * a.k.head_stride;
-      const uint8_t* const vc = static_cast<const uint8_t*>(a.v.d_codes) + head * a.v.head_stride;
+      int32_t next[2] = {page_of(0, key0), page_of(0, key0 + 16)};
+      uint32_t copy_key = key0, copy_to = ring;
+      // A lane copies pieces (lane & 1) and 2 + (lane & 1) of token lane / 2 of each half,
+      // the last piece of heads of 32 or 96 of token `lane`, and that token's scales.
+      const uint8_t* const kp = static_cast<const uint8_t*>(a.k.d_codes) + head * a.k.head_stride + 16 * (lane & 1);
+      const uint8_t* const vp = static_cast<const uint8_t*>(a.v.d_codes) + head * a.v.head_stride + 16 * (lane & 1);
       const uint8_t* const ks = static_cast<const uint8_t*>(a.k.d_scales) + head * a.k.scale_head_stride;
       const uint8_t* const vs = static_cast<const uint8_t*>(a.v.d_scales) + head * a.v.scale_head_stride;
+      const auto place = [](const uint8_t* base, int32_t page, int64_t page_stride, uint32_t in, int64_t token_stride) {
+        return base + (uint64_t)(uint32_t)page * (uint32_t)page_stride + (uint64_t)in * (uint32_t)token_stride;  // (both below 2^32)
+      };
       const auto copy = [&](int j) {
-        const uint32_t at = ring + j % kStages * kStage;
         int32_t page[2] = {next[0], next[1]};
-        next[0] = page_of(j + 1, 0), next[1] = page_of(j + 1, 1);
-        const int64_t key = key_of(j);
+        const uint32_t key = copy_key, at = copy_to;
+        copy_key += key_step;
+        next[0] = page_of(j + 1, copy_key), next[1] = page_of(j + 1, copy_key + 16);
+        copy_to = copy_to + kStage == ring + kStages * kStage ? ring : copy_to + kStage;
+        int full[2] = {16, 16}, full_lane = 16, full_scale = SB;  // bytes that are read, the others become zeros
+        if ((uint32_t)page[0] >= (uint32_t)a.num_pages || (uint32_t)page[1] >= (uint32_t)a.num_pages || key < (uint32_t)seen_lo ||
+            key + kFewTile > (uint32_t)seen_hi) {
+          bool held[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (page[h] != INT32_MIN && (page[h] < 0 || page[h] >= a.num_pages)) {
-            latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
-            page[h] = -1;
+          for (int h = 0; h < 2; ++h) {
+            held[h] = (uint32_t)page[h] < (uint32_t)a.num_pages;
+            if (!held[h] && page[h] != INT32_MIN) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
+            if (!held[h]) page[h] = 0;
+            const uint32_t x = key + 16 * h + (lane >> 1);
+            full[h] = held[h] && x >= (uint32_t)seen_lo && x < (uint32_t)seen_hi ? 16 : 0;
+          }
+          const uint32_t x = key + lane;
+          if (!(lane < 16 ? held[0] : held[1]) || x < (uint32_t)seen_lo || x >= (uint32_t)seen_hi) full_lane = full_scale = 0;
+        }
+        const uint32_t in_page = page_size - 1, in = key & in_page;
+        if constexpr (W >= 2) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t token = 16 * h + (lane >> 1), x = in + token & in_page;
+            const uint8_t* k = place(kp, page[h], a.k.page_stride, x, a.k.token_stride);
+            const uint8_t* v = place(vp, page[h], a.v.page_stride, x, a.v.token_stride);
+            const uint32_t k_to = at + row_of(token) * (D / 2) + 16 * (lane & 1);
+            // (128 elements: tokens 2, 3 of each 4 have their halves changed over, for the banks)
+            const uint32_t v_to = at + kCodes + token * (D / 2) + 16 * (lane & 1) + (D == 128 ? (token & 2) << 4 : 0);
+            copy_async<16>(k_to, k, full[h]);
+            copy_async<16>(v_to, v, full[h]);
+            if constexpr (W == 4) {
+              copy_async<16>(k_to + 32, k + 32, full[h]);
+              copy_async<16>(v_to ^ 32, v + 32, full[h]);
+            }
           }
         }
-        const int in = (int)(key & (page_size - 1));  // (of the second half: 16 more, or from its page's start)
-        const auto token_at = [&](int token, int64_t page_stride, int64_t token_stride) {
-          const int half = token >> 4;
-          const int64_t p = half ? page[1] : page[0];
-          return max(p, (int64_t)0) * page_stride + ((in + token) & (page_size - 1)) * token_stride;
-        };
-        const auto held = [&](int token) {
-          return (token >> 4 ? page[1] : page[0]) >= 0 && key + token >= seen_lo && key + token < seen_hi;
-        };
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const int x = i * 32 + lane, token = x / W, piece = x - token * W;
-          const bool in_cache = held(token);
-          copy_async<16>(at + row_of(token) * (D / 2) + 16 * piece, kc + token_at(token, a.k.page_stride, a.k.token_stride) + 16 * piece, in_cache);
-          // (128 elements: tokens 2, 3 of each 4 have their halves changed over, for the banks)
-          const int to = D == 128 ? piece ^ (token & 2) : piece;
-          copy_async<16>(at + kCodes + token * (D / 2) + 16 * to, vc + token_at(token, a.v.page_stride, a.v.token_stride) + 16 * piece, in_cache);
+        const int32_t own = lane < 16 ? page[0] : page[1];
+        const uint32_t x = in + lane & in_page;
+        if constexpr (W & 1) {
+          const int last = 16 * (W - 1) - 16 * (lane & 1);
+          copy_async<16>(at + row_of(lane) * (D / 2) + 16 * (W - 1), place(kp, own, a.k.page_stride, x, a.k.token_stride) + last, full_lane);
+          copy_async<16>(at + kCodes + lane * (D / 2) + 16 * (W - 1), place(vp, own, a.v.page_stride, x, a.v.token_stride) + last, full_lane);
         }
-        const bool in_cache = held(lane);
-        copy_async<SB>(at + 2 * kCodes + row_of(lane) * SB, ks + token_at(lane, a.k.scale_page_stride, a.k.scale_token_stride), in_cache);
-        copy_async<SB>(at + 2 * kCodes + kScales + lane * SB, vs + token_at(lane, a.v.scale_page_stride, a.v.scale_token_stride), in_cache);
+        copy_async<SB>(at + 2 * kCodes + row_of(lane) * SB, place(ks, own, a.k.scale_page_stride, x, a.k.scale_token_stride), full_scale);
+        copy_async<SB>(at + 2 * kCodes + kScales + lane * SB, place(vs, own, a.v.scale_page_stride, x, a.v.scale_token_stride), full_scale);
       };
 #pragma unroll
       for (int j = 0; j < kStages - 1; ++j) {
@@ -409,12 +430,13 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 #pragma unroll
         for (int i = 0; i < 2; ++i) cs[b][i] = __shfl_sync(kFull, power, 4 * (2 * c + i)) * a.scale;
       }
+      const unsigned char* at = ring_p;
+      uint32_t key = key0;
       for (int j = 0; j < n; ++j) {
         asm volatile("cp.async.wait_group %0;\n" ::"n"(kStages - 2) : "memory");
         __syncwarp();
         if (j + kStages - 1 < n) copy(j + kStages - 1);
         asm volatile("cp.async.commit_group;\n" ::: "memory");
-        const unsigned char* const at = ring_p + j % kStages * kStage;
         // scores: S[half][block][...] of tokens token_of(g), token_of(g + 8) and rows 2c, 2c + 1
         float s[2][NB][4];
 #pragma unroll
@@ -438,10 +460,21 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 #pragma unroll
               for (int k = 0; k < W; ++k) codes[i][k] = reinterpret_cast<const uint32_t*>(p)[k];
             }
-            const uint32_t* sp = reinterpret_cast<const uint32_t*>(at + 2 * kCodes + row * SB);
-            const uint32_t lo = sp[0], hi = SB == 8 ? sp[1] : 0;
+            // each word's group's scale, twice
+            const unsigned char* sp = at + 2 * kCodes + row * SB;
+            if constexpr (W == 4) {
+              const uint32_t two = scales_of(reinterpret_cast<const uint16_t*>(sp)[c]);
+              scales[i][0] = scales[i][1] = __byte_perm(two, 0, 0x1010);
+              scales[i][2] = scales[i][3] = __byte_perm(two, 0, 0x3232);
+            } else if constexpr (W == 3) {  // (12 words of 6 groups: the middle word goes with the first or the last)
+              const uint32_t x = sp[3 * c / 2], y = sp[3 * c / 2 + 1];
+              scales[i][0] = scales_of(x * 0x101), scales[i][2] = scales_of(y * 0x101);
+              scales[i][1] = c & 1 ? scales[i][2] : scales[i][0];
+            } else {
+              const uint32_t x = sp[W * c / 2];
 #pragma unroll
-            for (int k = 0; k < W; ++k) scales[i][k] = scales_of(__byte_perm(lo, hi, (W * c + k) / 2 * 0x11));  // (its group's, twice)
+              for (int k = 0; k < W; ++k) scales[i][k] = scales_of(x * 0x101);
+            }
           }
 #pragma unroll
           for (int k = 0; k < W; ++k) {
@@ -460,13 +493,8 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
               mma(s[t][b], y, qf[b][2 * k + 1][0], qf[b][2 * k + 1][1]);
             }
           }
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[t][b][i] *= cs[b][i & 1];
         }
-        const int64_t key = key_of(j);
-        if (key + kFewTile - 1 > u.pos || key < seen_hi - a.window) {  // some row does not see some key
+        if (key + kFewTile - 1 > (uint32_t)u.pos || (int64_t)key < seen_hi - a.window) {  // some row does not see some key
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -476,7 +504,7 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
               for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                  const int64_t x = key + 16 * t + token_of(8 * k + g);
+                  const int64_t x = (int64_t)key + 16 * t + token_of(8 * k + g);
                   if (x > hi || x <= hi - a.window) s[t][b][2 * k + i] = -INFINITY;
                 }
             }
@@ -496,8 +524,8 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 #pragma unroll
               for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, x));
               if (top > lim[b][i]) {
-                const float to = top - kLift, back = lim[b][i] == -INFINITY ? 0.f : ex2(ref[b][i] - to);
-                ref[b][i] = to, lim[b][i] = top + kSlack;
+                const float to = top * cs[b][i] - kLift, back = lim[b][i] == -INFINITY ? 0.f : ex2(ref[b][i] - to);
+                ref[b][i] = to, lim[b][i] = top + kSlack / cs[b][i];
                 l[b][i] *= back;
 #pragma unroll
                 for (int m = 0; m < D / 16; ++m) o[m][b][i] *= back, o[m][b][i + 2] *= back;
@@ -511,7 +539,7 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
           for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const float x = ex2(s[t][b][2 * k] - ref[b][0]), y = ex2(s[t][b][2 * k + 1] - ref[b][1]);
+              const float x = ex2(fmaf(s[t][b][2 * k], cs[b][0], -ref[b][0])), y = ex2(fmaf(s[t][b][2 * k + 1], cs[b][1], -ref[b][1]));
               l[b][0] += x, l[b][1] += y;
               p[t][b][k] = transposed(round2<__half>(make_float2(x, y)));
             }
@@ -563,6 +591,8 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
             for (int b = 0; b < NB; ++b) mma(o[m][b], x, p[t][b][0], p[t][b][1]);
           }
         }
+        at = at + kStage == ring_p + kStages * kStage ? ring_p : at + kStage;
+        key += key_step;
       }
       asm volatile("cp.async.wait_group 0;\n" ::: "memory");
     }

@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "smetric_impl.cuh"
 
 namespace smetric {
@@ -131,6 +133,7 @@ inline bool cache4_ok(const smetric_kvq_cache& c, int head_dim) {
          c.head_stride >= 0 && c.scale_page_stride >= 0 && c.scale_token_stride >= 0 && c.scale_head_stride >= 0 &&
          c.page_stride % 16 == 0 && c.token_stride % 16 == 0 && c.head_stride % 16 == 0 &&
          c.scale_page_stride % s == 0 && c.scale_token_stride % s == 0 && c.scale_head_stride % s == 0 &&
+         std::max({c.page_stride, c.token_stride, c.scale_page_stride, c.scale_token_stride}) <= UINT32_MAX &&
          c.exp >= -SMETRIC_KVQ_MAX_EXP && c.exp <= SMETRIC_KVQ_MAX_EXP && !c.reserved;
 }
 // At a whole number of its elements, as loads need.

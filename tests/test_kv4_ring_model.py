@@ -39,7 +39,7 @@ def run(seed, stages, units):
     """units: (two query tiles?, key tiles) of a CTA's share, in order."""
     rng = random.Random(seed)
     new = lambda k, count=1: [Barrier(count) for _ in range(k)]  # noqa: E731
-    full, empty, q_full, q_empty = new(stages, CONVERTERS), new(stages), new(2), new(2)
+    full, empty, q_raw, q_full, q_empty = new(stages, CONVERTERS), new(stages), new(2), new(2), new(2)
     s_full, p_full, o_full, o_free, stat_full = new(2), new(2), new(2), new(2), new(2)
     # a tile of the ring: how often each third of it was written, and what with
     thirds = [[None] * CONVERTERS for _ in range(stages)]
@@ -162,9 +162,13 @@ def run(seed, stages, units):
                 for t in range(2 if units[u][0] else 1):
                     if nq > 1:
                         yield from wait(q_empty[nq & 1], nq // 2 - 1 & 1)
-                    q_tiles[nq & 1] = (u, t)
-                    copies.append(q_full[nq & 1].arrive)
+                    copies.append(q_raw[nq & 1].arrive)
                     nq += 1
+                    yield
+                for t in range(nq - (2 if units[u][0] else 1), nq):
+                    yield from wait(q_raw[t & 1], t // 2 & 1)
+                    q_tiles[t & 1] = (u, t - nq + (2 if units[u][0] else 1))
+                    q_full[t & 1].arrive()  # (converted)
                     yield
 
         yield from queries(0)
@@ -207,7 +211,7 @@ def run(seed, stages, units):
     raise AssertionError(f"no end: {sorted(warps)} of {units}")
 
 
-@pytest.mark.parametrize("stages", [4, 9])
+@pytest.mark.parametrize("stages", [4, 10])
 def test_random_shares(stages):
     for seed in range(150):
         rng = random.Random(seed)
@@ -215,7 +219,7 @@ def test_random_shares(stages):
         run(seed, stages, units)
 
 
-@pytest.mark.parametrize("stages", [4, 9])
+@pytest.mark.parametrize("stages", [4, 10])
 def test_short_units_after_long_ones(stages):
     for seed in range(40):
         run(seed, stages, [(True, 1), (True, 3), (False, 1), (False, 2), (False, 1), (False, 1), (True, 2), (False, 7), (False, 1)])
