@@ -68,14 +68,11 @@ constexpr uint32_t kHalf = 16384;  // bytes of 128 rows of 64 elements
 __host__ __device__ constexpr int stages(int halves, bool four) {
   return four ? (halves == 2 ? 4 : 10) : halves == 2 ? 5 : 11;
 }
-// Caches in 4 bits: each of 3 warps converts every third 16 rows of a tile, of which
-// codes and scales were copied to one of its 3 buffers two tiles before.
-constexpr int kConverters = 3;
-constexpr int kAhead = 3;
-__host__ __device__ constexpr int codes_bytes(int halves) { return 16 * 32 * halves; }  // of 16 rows
-__host__ __device__ constexpr int buffer_bytes(int halves) { return 3 * codes_bytes(halves); }
+// Caches in 4 bits: tiles of codes and scales as they are, on their way to the ring.
+constexpr int kStaged = 3;
+__host__ __device__ constexpr int codes_bytes(int halves) { return kTile * 32 * halves; }
 __host__ __device__ constexpr int staging_bytes(int halves, bool four) {
-  return four ? kConverters * kAhead * (buffer_bytes(halves) + 3 * 16 * 4 * halves) : 0;
+  return four ? kStaged * (codes_bytes(halves) + kTile * 4 * halves) : 0;
 }
 
 struct AttentionArgs {
@@ -126,15 +123,6 @@ struct Walk {
     first = true;
     done = u < 0;
   }
-  // Its state in 13 words.
-  __device__ __forceinline__ void put(volatile int32_t* p) const {
-    p[0] = unit.token, p[1] = unit.tokens, p[2] = unit.pos, p[3] = unit.req, p[4] = unit.tb, p[5] = unit.te;
-    p[6] = u, p[7] = h, p[8] = t0, p[9] = u1, p[10] = h1, p[11] = t1, p[12] = first | done << 1;
-  }
-  __device__ __forceinline__ void get(const volatile int32_t* p) {
-    unit.token = p[0], unit.tokens = p[1], unit.pos = p[2], unit.req = p[3], unit.tb = p[4], unit.te = p[5];
-    u = p[6], h = p[7], t0 = p[8], u1 = p[9], h1 = p[10], t1 = p[11], first = p[12] & 1, done = p[12] >> 1;
-  }
   __device__ __forceinline__ bool next(const AttentionArgs& a, Item& it) {
     if (done) return false;
     const bool last = u == u1 && h == h1;
@@ -178,10 +166,9 @@ struct Shared {
 };
 // What caches in 4 bits need besides.
 struct SharedFour : Shared {
-  uint64_t staged[kConverters][kAhead];  // codes copied
-  uint64_t q_raw[2];                     // query tiles that are yet to be converted
-  int32_t walk[kConverters][13];         // the converting warps' Walks
-  uint8_t power[4][kTile];               // exponents of the rows of the last query tiles, where they were converted
+  uint64_t staged_full[kStaged], staged_empty[kStaged];
+  uint64_t q_raw[2];        // query tiles that are yet to be converted
+  uint8_t power[4][kTile];  // exponents of the rows of the last query tiles, where they were converted
 };
 
 __device__ __forceinline__ void mbar_init(uint64_t* b, uint32_t count) {
@@ -463,143 +450,106 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
 
 // ---- caches in 4 bits ----
 
+// The tile at a place of an item's order, of n key tiles: K0 K1 V0 K2 V1 K3 ...
+__device__ __forceinline__ int tile_at(int place, int n, bool& values) {
+  values = place == 2 * n - 1 || (place > 1 && !(place & 1));
+  return place == 2 * n - 1 ? n - 1 : place < 2 ? place : values ? place / 2 - 1 : (place + 1) / 2;
+}
+
+// One warp copies the tiles' codes as they are, a lane a page.
+template <int HALVES>
+__device__ __forceinline__ void copy_codes(const AttentionArgs& a, SharedFour* sh, Walk w, uint32_t staging) {
+  const int lane = threadIdx.x & 31;
+  const int rows = min(kTile, a.page_size), per = kTile / rows;  // of a copy, and pages of a tile
+  const int page_shift = __ffs(a.page_size) - 1, row_bytes = a.D / 2;
+  uint32_t at = 0;
+  Item it;
+  while (w.next(a, it)) {
+    const int n = it.te - it.tb;
+    const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
+    const int32_t* pages = a.pages + it.unit.req * a.pages_stride;
+    // the lane's page of a tile, INT32_MIN where nobody sees a key of it
+    const auto page_of = [&](int place) {
+      bool values;
+      const int64_t key = (int64_t)(it.tb + tile_at(place, n, values)) * kTile + lane * rows;
+      return lane < per && place < 2 * n && key < hi && key + rows > lo ? pages[key >> page_shift] : INT32_MIN;
+    };
+    int32_t next = page_of(0);
+    for (int place = 0; place < 2 * n; ++place, ++at) {
+      int32_t page = next;
+      next = page_of(place + 1);
+      bool values;
+      const int j = tile_at(place, n, values);
+      const uint32_t s = at % kStaged;
+      if (at >= kStaged) mbar_wait(&sh->staged_empty[s], (at / kStaged - 1) & 1, sh, a.status);
+      if (stopped(sh)) break;
+      if (page != INT32_MIN && (uint32_t)page >= (uint32_t)a.num_pages) {
+        latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
+        page = INT32_MIN;  // (its scales become zeros)
+      }
+      const bool held = page != INT32_MIN;
+      const unsigned who = __ballot_sync(kFull, held);
+      if (lane == 0) mbar_expect(&sh->staged_full[s], __popc(who) * rows * row_bytes);
+      __syncwarp();
+      if (held)
+        tma_4d(staging + s * codes_bytes(HALVES) + lane * rows * row_bytes, values ? &a.v : &a.k, 0,
+               a.page_size > kTile ? (it.tb + j) * kTile % a.page_size : 0, it.h, page, &sh->staged_full[s]);
+    }
+    if (stopped(sh)) break;
+  }
+}
+
 // 8 bytes to shared memory, or zeros (4 for heads of at most 64 elements).
 template <int N>
-__device__ __forceinline__ void copy_scales(uint32_t dst, const void* src, bool held) {
+__device__ __forceinline__ void copy_row_scales(uint32_t dst, const void* src, bool held) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(held ? N : 0) : "memory");
 }
 
-// What copy_tiles does, for caches in 4 bits: this warp's 16-row groups (number, +
-// 3, + 6) of every tile go as they are to a buffer of the warp's, and from there to the
-// ring in half precision, in the 128-byte swizzle: a conversion for two codes and a
-// product with their scale, both exact (2 and 4 bits). Rows that nobody sees have
+// Another warp copies their scales, a lane every 32nd row. Rows that nobody sees have
 // scales of zero.
 template <int HALVES>
-__device__ __forceinline__ void convert_tiles(const AttentionArgs& a, SharedFour* sh, uint32_t ring, uint32_t staging, const int number) {
-  constexpr int S = stages(HALVES, true), SB = 4 * HALVES;
-  Barriers& b = sh->bar;
-  const int lane = threadIdx.x & 31, row = lane & 15, odd = lane >> 4;
-  const int pieces = a.D / 32;  // of 16 bytes, in a row: a lane has piece `odd` and, of longer heads, 2 + odd
-  const int row_bytes = a.D / 2, page_shift = __ffs(a.page_size) - 1;
-  const uint32_t staged = staging + number * kAhead * buffer_bytes(HALVES);
-  const uint32_t staged_scales = staging + kConverters * kAhead * buffer_bytes(HALVES) + number * kAhead * 3 * 16 * SB;
-  // the item whose tiles are copied, what was copied of it, and the page of the lane's
-  // 16 rows (lane & 7) of its next tile
-  int32_t h = 0, tb = 0, n = 0, jk = 0, jv = 0, lo = 0, hi = 0, page = INT32_MIN;
-  const int32_t* row_pages = nullptr;
-  const auto is_values = [&]() { return jk == n || (jk > 1 && jv < jk - 1); };  // K0 K1 V0 K2 V1 K3 ...
-  const auto look_up = [&]() {
-    const int64_t key = (int64_t)(tb + (is_values() ? jv : jk)) * kTile + 16 * (lane & 7);
-    page = key < hi && key + 16 > lo ? row_pages[key >> page_shift] : INT32_MIN;
-  };
-  const auto next_item = [&]() {
-    Walk w;
-    w.get(sh->walk[number]);  // (not kept in registers: the loop has use for them)
-    Item it;
-    n = 0;
-    if (!w.next(a, it)) return;
-    __syncwarp();
-    if (lane == 0) w.put(sh->walk[number]);
-    __syncwarp();
-    h = it.h, tb = it.tb, n = it.te - it.tb, jk = jv = 0;
-    lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0;  // the keys that some query of the unit sees
-    hi = it.unit.pos + it.unit.tokens;
-    row_pages = a.pages + it.unit.req * a.pages_stride;
-    look_up();
-  };
-  next_item();
-  uint32_t copied = 0;
-  const auto copy = [&]() {
-    if (n > 0) {
-      const bool values = is_values();
-      const int64_t key = (int64_t)(tb + (values ? jv : jk)) * kTile;
-      const uint32_t in_page = (uint32_t)key & (a.page_size - 1);
-      if (page != INT32_MIN && (uint32_t)page >= (uint32_t)a.num_pages) {
-        latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
-        page = INT32_MIN;
-      }
-      const uint32_t buffer = copied % kAhead;
-      uint64_t* const full = &sh->staged[number][buffer];
-      const int mine = number + 3 * lane;  // lanes 0 to 2: a group each
-      const int32_t p = __shfl_sync(kFull, page, mine & 7);
-      const bool copies = lane < 3 && mine < kTile / 16 && p != INT32_MIN;
-      const unsigned who = __ballot_sync(kFull, copies);
-      if (lane == 0) mbar_expect(full, __popc(who) * 16 * row_bytes);
-      __syncwarp();
-      if (copies)
-        tma_4d(staged + buffer * buffer_bytes(HALVES) + lane * codes_bytes(HALVES), values ? &a.v : &a.k, 0,
-               (in_page + 16 * mine) & (a.page_size - 1), h, p, full);
+__device__ __forceinline__ void copy_scales(const AttentionArgs& a, SharedFour* sh, Walk w, uint32_t staging) {
+  constexpr int SB = 4 * HALVES;
+  const int lane = threadIdx.x & 31, page_shift = __ffs(a.page_size) - 1;
+  staging += kStaged * codes_bytes(HALVES);
+  uint32_t at = 0;
+  Item it;
+  while (w.next(a, it)) {
+    const int n = it.te - it.tb;
+    const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
+    const int32_t* pages = a.pages + it.unit.req * a.pages_stride;
+    // the page of 16 rows (lane & 7) of a tile
+    const auto page_of = [&](int place) {
+      bool values;
+      const int64_t key = (int64_t)(it.tb + tile_at(place, n, values)) * kTile + 16 * (lane & 7);
+      return place < 2 * n && key < hi && key + 16 > lo ? pages[key >> page_shift] : -1;
+    };
+    int32_t next = page_of(0);
+    for (int place = 0; place < 2 * n; ++place, ++at) {
+      const int32_t page = next;
+      next = page_of(place + 1);
+      bool values;
+      const int64_t key = (int64_t)(it.tb + tile_at(place, n, values)) * kTile + lane;
       const smetric_kvq_cache& c = values ? a.v4 : a.k4;
-      const uint8_t* scales = static_cast<const uint8_t*>(c.d_scales) + h * c.scale_head_stride;
+      const uint8_t* scales = static_cast<const uint8_t*>(c.d_scales) + it.h * c.scale_head_stride;
+      const uint32_t page_stride = (uint32_t)c.scale_page_stride, token_stride = (uint32_t)c.scale_token_stride;  // (below 2^32)
+      const uint32_t s = at % kStaged;
+      if (at >= kStaged) mbar_wait(&sh->staged_empty[s], (at / kStaged - 1) & 1, sh, a.status);
+      if (stopped(sh)) break;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int g = odd + 2 * i, group = number + 3 * g;  // the lane's row of it
-        const int32_t q = __shfl_sync(kFull, page, group & 7);
-        const int64_t x = key + 16 * group + row;
-        const bool held = q != INT32_MIN && x >= lo && x < hi;
-        const uint32_t in = (in_page + 16 * group + row) & (a.page_size - 1);
-        // (strides below 2^32)
-        if (g < 3 && group < kTile / 16)
-          copy_scales<SB>(staged_scales + (buffer * 48 + 16 * g + row) * SB,
-                          scales + (uint64_t)(held ? (uint32_t)q : 0u) * (uint32_t)c.scale_page_stride +
-                              (uint64_t)in * (uint32_t)c.scale_token_stride, held);
+      for (int i = 0; i < 4; ++i) {
+        const int64_t x = key + 32 * i;
+        const int32_t p = __shfl_sync(kFull, page, 2 * i + (lane >> 4));
+        const bool held = (uint32_t)p < (uint32_t)a.num_pages && x >= lo && x < hi;
+        const uint32_t in = (uint32_t)x & (a.page_size - 1);
+        copy_row_scales<SB>(staging + (s * kTile + 32 * i + lane) * SB,
+                            scales + (uint64_t)(held ? (uint32_t)p : 0u) * page_stride + (uint64_t)in * token_stride, held);
       }
-      ++copied;
-      if (values)
-        ++jv;
-      else
-        ++jk;
-      if (jv == n)
-        next_item();
-      else
-        look_up();
+      asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];\n" ::"r"(smem_u32(&sh->staged_full[s])) : "memory");
     }
-    asm volatile("cp.async.commit_group;\n" ::: "memory");
-  };
-  for (int i = 0; i < kAhead - 1; ++i) copy();
-  for (uint32_t at = 0; at < copied; ++at) {
-    copy();
-    const uint32_t s = at % S, buffer = at % kAhead;
-    asm volatile("cp.async.wait_group %0;\n" ::"n"(kAhead - 1) : "memory");
-    mbar_wait(&sh->staged[number][buffer], at / kAhead & 1, sh, a.status);
-    if (at >= S) mbar_wait(&b.empty[s], (at / S - 1) & 1, sh, a.status);
     if (stopped(sh)) break;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const int group = number + 3 * i;
-      if (group >= kTile / 16) continue;
-#pragma unroll
-      for (int e = 0; e < HALVES; ++e) {
-        const int piece = 2 * e + odd;
-        if (piece >= pieces) continue;
-        // (rows of 64 and of 32 bytes are swizzled, for the banks)
-        const int at_piece = row_bytes == 64 ? piece ^ (row >> 1 & 3) : row_bytes == 32 ? piece ^ (row >> 2 & 1) : piece;
-        uint32_t word[4], h2;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n"
-                     : "=r"(word[0]), "=r"(word[1]), "=r"(word[2]), "=r"(word[3])
-                     : "r"(staged + buffer * buffer_bytes(HALVES) + i * codes_bytes(HALVES) + row * row_bytes + 16 * at_piece)
-                     : "memory");
-        asm volatile("{\n .reg .b16 x;\n ld.shared.b16 x, [%1];\n cvt.rn.f16x2.e4m3x2 %0, x;\n}\n"
-                     : "=r"(h2) : "r"(staged_scales + (buffer * 48 + 16 * i + row) * SB + 2 * piece) : "memory");
-        const uint32_t scale[2] = {__byte_perm(h2, 0, 0x1010), __byte_perm(h2, 0, 0x3232)};
-        const uint32_t dst = ring + (s * HALVES + e) * kHalf + (16 * group + row) * 128;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t y[4];
-          asm("{\n .reg .b8 a, b, c, d;\n .reg .b32 e, f, g, h;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 e, a;\n"
-              " cvt.rn.f16x2.e2m1x2 f, b;\n cvt.rn.f16x2.e2m1x2 g, c;\n cvt.rn.f16x2.e2m1x2 h, d;\n mul.rn.f16x2 %0, e, %5;\n"
-              " mul.rn.f16x2 %1, f, %5;\n mul.rn.f16x2 %2, g, %5;\n mul.rn.f16x2 %3, h, %5;\n}\n"
-              : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(word[q]), "r"(scale[q >> 1]));
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(dst + (((4 * odd + q) ^ (row & 7)) << 4)), "r"(y[0]),
-                       "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
-        }
-      }
-    }
-    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&b.full[s]);
   }
-  asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+  asm volatile("cp.async.wait_all;\n" ::: "memory");
 }
 
 // A row (the thread's) of query tile number nq from bf16 to half precision, in its
@@ -629,6 +579,102 @@ __device__ __forceinline__ void convert_row(SharedFour* sh, uint32_t nq, uint32_
     for (int i = 0; i < 4; ++i)
       x[i] = Type<__half>::pack(__uint_as_float(x[i] << 16) * down, __uint_as_float(x[i] & 0xffff0000u) * down);
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(chunk(j)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+  }
+}
+
+// Four warps turn tiles of codes into tiles of the ring in half precision, in the
+// 128-byte swizzle, 32 rows each: a conversion for two codes and a product with their
+// scale, both exact (2 and 4 bits). A tile's keys and values are laid out alike. They
+// also convert an item's query tiles (kQueries), after its first two tiles: those, and
+// all before, are used up without the queries that this warp would wait with.
+template <int HALVES, bool kQueries>
+__device__ __forceinline__ void convert_tiles(const AttentionArgs& a, SharedFour* sh, Walk w, uint32_t q_smem, uint32_t ring,
+                                              uint32_t staging) {
+  constexpr int S = stages(HALVES, true), SB = 4 * HALVES;
+  Barriers& b = sh->bar;
+  const int lane = threadIdx.x & 31, odd = lane >> 4, row = (threadIdx.x >> 5 & 3) * 32 + (lane & 15);
+  const int pieces = a.D / 32;  // of 16 bytes, in a row: a lane has piece `odd` and, of longer heads, 2 + odd
+  const int row_bytes = a.D / 2;
+  // (rows of 64 and of 32 bytes are swizzled, for the banks; 16 rows on, alike)
+  const int swizzle = row_bytes == 64 ? row >> 1 & 3 : row_bytes == 32 ? row >> 2 & 1 : 0;
+  uint32_t at = 0, nq = 0;
+  Item it;
+  while (w.next(a, it)) {
+    const int n = it.te - it.tb;
+    for (int place = 0; place < 2 * n; ++place, ++at) {
+      const uint32_t s = at % S, from = at % kStaged;
+      mbar_wait(&sh->staged_full[from], at / kStaged & 1, sh, a.status);
+      if (stopped(sh)) break;
+      uint32_t word[2][HALVES][4], two[2][HALVES];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int e = 0; e < HALVES; ++e) {
+          const int piece = 2 * e + odd;
+          if (piece < pieces) {
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n"
+                         : "=r"(word[i][e][0]), "=r"(word[i][e][1]), "=r"(word[i][e][2]), "=r"(word[i][e][3])
+                         : "r"(staging + from * codes_bytes(HALVES) + (row + 16 * i) * row_bytes + 16 * (piece ^ swizzle)) : "memory");
+            asm volatile("{\n .reg .b16 x;\n ld.shared.b16 x, [%1];\n cvt.u32.u16 %0, x;\n}\n"
+                         : "=r"(two[i][e])
+                         : "r"(staging + kStaged * codes_bytes(HALVES) + (from * kTile + row + 16 * i) * SB + 2 * piece) : "memory");
+          }
+        }
+      }
+      if (at >= S) mbar_wait(&b.empty[s], (at / S - 1) & 1, sh, a.status);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int e = 0; e < HALVES; ++e) {
+          uint32_t h2;
+          asm("{\n .reg .b16 x, y;\n mov.b32 {x, y}, %1;\n cvt.rn.f16x2.e4m3x2 %0, x;\n}\n" : "=r"(h2) : "r"(two[i][e]));
+          const uint32_t scale[2] = {__byte_perm(h2, 0, 0x1010), __byte_perm(h2, 0, 0x3232)};
+          const uint32_t dst = ring + (s * HALVES + e) * kHalf + (row + 16 * i) * 128;
+          uint32_t y[4][4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            asm("{\n .reg .b8 a, b, c, d;\n .reg .b32 e, f, g, h;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 e, a;\n"
+                " cvt.rn.f16x2.e2m1x2 f, b;\n cvt.rn.f16x2.e2m1x2 g, c;\n cvt.rn.f16x2.e2m1x2 h, d;\n mul.rn.f16x2 %0, e, %5;\n"
+                " mul.rn.f16x2 %1, f, %5;\n mul.rn.f16x2 %2, g, %5;\n mul.rn.f16x2 %3, h, %5;\n}\n"
+                : "=r"(y[q][0]), "=r"(y[q][1]), "=r"(y[q][2]), "=r"(y[q][3]) : "r"(word[i][e][q]), "r"(scale[q >> 1]));
+          if (2 * e + odd < pieces) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(dst + (((4 * odd + q) ^ (row & 7)) << 4)),
+                           "r"(y[q][0]), "r"(y[q][1]), "r"(y[q][2]), "r"(y[q][3]) : "memory");
+          }
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&sh->staged_empty[from]);
+        mbar_arrive(&b.full[s]);
+      }
+      if (kQueries && place == 1) {
+        const int tiles = it.pair ? 2 : 1;
+        for (int t = 0; t < tiles; ++t, ++nq) {
+          mbar_wait(&sh->q_raw[nq & 1], nq / 2 & 1, sh, a.status);
+          convert_row<HALVES>(sh, nq, q_smem, threadIdx.x & 127);
+          asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&b.q_full[nq & 1]);
+        }
+      }
+    }
+    if (stopped(sh)) break;
+  }
+}
+
+// The query tiles of every item, in order.
+template <int HALVES, bool kQueries>
+__device__ __forceinline__ void copy_all_queries(const AttentionArgs& a, SharedFour* sh, Walk w, uint32_t q_smem) {
+  uint32_t nq = 0;
+  Item it;
+  while (w.next(a, it)) {
+    for (int t = 0; t < (it.pair ? 2 : 1); ++t, ++nq)
+      copy_queries<HALVES>(a, sh, it, t, nq, q_smem, (kQueries ? sh->q_raw : sh->bar.q_full) + (nq & 1));
+    if (stopped(sh)) break;
   }
 }
 
@@ -809,9 +855,97 @@ __device__ __forceinline__ int tile_rows(const AttentionArgs& a, const Item& it,
 // The lowest n bits, none or all where n is outside 0..32.
 __device__ __forceinline__ uint32_t below(int32_t n) { return n <= 0 ? 0 : n >= 32 ? kFull : (1u << n) - 1; }
 
+// An item's output (a query tile's of two): O / l, or its sums and statistics where
+// other CTAs have pieces of it. The four warps of a tile call, for the even and the odd
+// key tiles together where an item has one query tile. no: ends of products so far.
+template <typename T, bool kFour>
+__device__ __forceinline__ void write_tile(const AttentionArgs& a, Shared* sh, const Item& it, int tile, uint32_t items,
+                                           uint32_t (&no)[2]) {
+  Barriers& b = sh->bar;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
+  const uint32_t o_all = sh->tmem + 2 * kTile + ((uint32_t)warp << 21);
+  const int row_token = row / a.group, row_head = row - row_token * a.group;
+  const bool two = !it.pair && it.te - it.tb > 1;  // sums of even and of odd key tiles
+        const int n_rows = tile_rows(a, it, tile);
+        mbar_wait(&b.stat_full[tile], items & 1, sh, a.status);
+        float2 st = sh->stat[tile][row];
+        float w1 = 1.f, w2 = 0.f;  // the even and the odd tiles' shares
+        if (!it.pair) {
+          mbar_wait(&b.stat_full[1], items & 1, sh, a.status);
+          const float2 odd = sh->stat[1][row];
+          const float both = fmaxf(st.x, odd.x);
+          if (both > -INFINITY) {
+            w1 = ex2(st.x - both);
+            w2 = ex2(odd.x - both);
+            st = make_float2(both, st.y * w1 + odd.y * w2);
+          }
+          if (two) mbar_wait(&b.o_full[1], no[1]++ & 1, sh, a.status);
+        }
+        mbar_wait(&b.o_full[tile], no[tile]++ & 1, sh, a.status);
+        if (32 * warp < n_rows) {
+          fence_after();
+          const bool mine = row < n_rows;
+          const int64_t token = it.unit.token + tile_token(a, it, tile) + row_token;
+          const int head = it.h * a.group + row_head;
+          float inv = it.whole ? (st.y > 0.f ? 1.f / st.y : st.y) : 1.f;  // (NaN stays)
+          if (kFour && it.whole) inv *= a.v_scale;
+          w1 *= inv, w2 *= inv;
+          const uint32_t o_at = o_all + tile * kTile;
+          T* out = static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride;
+          for (int d = 0; d < a.D; d += 16) {
+            uint32_t o[16];
+            float f[16];
+            tmem_ld16(o_at + d, o);
+            wait_ld(o);
+  #pragma unroll
+            for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(o[i]) * w1;
+            if (two) {
+              tmem_ld16(o_at + kTile + d, o);
+              wait_ld(o);
+  #pragma unroll
+              for (int i = 0; i < 16; ++i) f[i] += __uint_as_float(o[i]) * w2;
+            }
+            if (mine) {
+              if (it.whole) {
+                uint32_t y[8];
+  #pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
+                store16(a, out + d, y);
+              } else {
+                float4* p = reinterpret_cast<float4*>(a.part) + part_at(a.D, it.slot, tile, d / 4) + row;
+  #pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  p[i * kTile] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+              }
+            }
+          }
+          fence_before();
+          if (mine) {
+            if (!it.whole)
+              a.part_ml[(int64_t)it.slot * 2 * kTile + tile * kTile + row] = st;
+            else if (a.lse)
+              a.lse[token * a.hq + head] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * 0.6931471805599453f;
+          }
+        }
+  __syncwarp();
+  if (lane == 0) {
+    mbar_arrive(&b.o_free[tile]);
+    if (!it.pair) mbar_arrive(&b.o_free[1]);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Walk w) {
+  uint32_t items = 0, no[2] = {0, 0};
+  Item it;
+  for (; w.next(a, it); ++items)
+    for (int tile = 0; tile < (it.pair ? 2 : 1); ++tile) write_tile<T, false>(a, sh, it, tile, items, no);
+}
+
 // (One code for both tiles: two copies miss the instruction cache.)
-// kPowers: the scores are of rows divided by a power of two.
-template <typename T, bool kPowers>
+// With caches in 4 bits the scores may be of rows divided by a power of two
+// (kPowers), and these warps write the output, as the ones that do else convert.
+template <typename T, typename Out, bool kFour>
 __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk w, const int tile) {
   Barriers& b = sh->bar;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
@@ -819,7 +953,8 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
   const uint32_t s_at = sh->tmem + tile * kTile + lanes, o_at = sh->tmem + 2 * kTile + tile * kTile + lanes;
   const int row_token = row / a.group;
   float c = a.scale * 1.4426950408889634f;
-  uint32_t ns = 0, items = 0, nq = 0;
+  constexpr bool kPowers = !std::is_same<T, Out>::value;
+  uint32_t ns = 0, items = 0, nq = 0, no[2] = {0, 0};
   Item it;
   for (; w.next(a, it); ++items) {
     const int n = it.te - it.tb;
@@ -917,113 +1052,10 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
     sh->stat[tile][row] = make_float2(top == -INFINITY && l == 0.f ? -INFINITY : ref, l);
     __syncwarp();
     if (lane == 0) mbar_arrive(&b.stat_full[tile]);
-  }
-}
-
-// A unit's output: O / l, or its sums and statistics where other CTAs have
-// pieces of it.
-// With caches in 4 bits these warps also have the query tiles, an item's before the
-// output of the item before (its converting warps could wait for a query buffer only
-// after the tiles that they have not converted yet): copied, and in bf16 converted.
-template <typename T, int HALVES, bool kFour>
-__device__ __forceinline__ void write_out(const AttentionArgs& a, Shared* sh, Walk w, uint32_t q_smem) {
-  Barriers& b = sh->bar;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, row = threadIdx.x & 127;
-  const uint32_t o_all = sh->tmem + 2 * kTile + ((uint32_t)warp << 21);
-  const int row_token = row / a.group, row_head = row - row_token * a.group;
-  uint32_t items = 0, no[2] = {0, 0}, nq = 0;
-  constexpr bool kConvert = kFour && std::is_same<T, __nv_bfloat16>::value;
-  Walk ahead = w;
-  const auto queries = [&]() {
-    Item next;
-    if (!ahead.next(a, next)) return;
-    const int tiles = next.pair ? 2 : 1;
-    if (warp == 0)
-      for (int t = 0; t < tiles; ++t)
-        copy_queries<HALVES>(a, sh, next, t, nq + t, q_smem, (kConvert ? static_cast<SharedFour*>(sh)->q_raw : b.q_full) + (nq + t & 1));
-    if (kConvert) {
-      for (int t = 0; t < tiles; ++t) {
-        mbar_wait(&static_cast<SharedFour*>(sh)->q_raw[nq + t & 1], (nq + t) / 2 & 1, sh, a.status);
-        convert_row<HALVES>(static_cast<SharedFour*>(sh), nq + t, q_smem, row);
-        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&b.q_full[nq + t & 1]);
-      }
-    }
-    nq += tiles;
-  };
-  if (kFour) queries();
-  Item it;
-  for (; w.next(a, it); ++items) {
-    if (kFour) queries();
-    const bool two = !it.pair && it.te - it.tb > 1;  // sums of even and of odd key tiles
-    for (int tile = 0; tile < (it.pair ? 2 : 1); ++tile) {
-      const int n_rows = tile_rows(a, it, tile);
-      mbar_wait(&b.stat_full[tile], items & 1, sh, a.status);
-      float2 st = sh->stat[tile][row];
-      float w1 = 1.f, w2 = 0.f;  // the even and the odd tiles' shares
-      if (!it.pair) {
-        mbar_wait(&b.stat_full[1], items & 1, sh, a.status);
-        const float2 odd = sh->stat[1][row];
-        const float both = fmaxf(st.x, odd.x);
-        if (both > -INFINITY) {
-          w1 = ex2(st.x - both);
-          w2 = ex2(odd.x - both);
-          st = make_float2(both, st.y * w1 + odd.y * w2);
-        }
-        if (two) mbar_wait(&b.o_full[1], no[1]++ & 1, sh, a.status);
-      }
-      mbar_wait(&b.o_full[tile], no[tile]++ & 1, sh, a.status);
-      if (32 * warp < n_rows) {
-        fence_after();
-        const bool mine = row < n_rows;
-        const int64_t token = it.unit.token + tile_token(a, it, tile) + row_token;
-        const int head = it.h * a.group + row_head;
-        float inv = it.whole ? (st.y > 0.f ? 1.f / st.y : st.y) : 1.f;  // (NaN stays)
-        if (kFour && it.whole) inv *= a.v_scale;
-        w1 *= inv, w2 *= inv;
-        const uint32_t o_at = o_all + tile * kTile;
-        T* out = static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride;
-        for (int d = 0; d < a.D; d += 16) {
-          uint32_t o[16];
-          float f[16];
-          tmem_ld16(o_at + d, o);
-          wait_ld(o);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(o[i]) * w1;
-          if (two) {
-            tmem_ld16(o_at + kTile + d, o);
-            wait_ld(o);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) f[i] += __uint_as_float(o[i]) * w2;
-          }
-          if (mine) {
-            if (it.whole) {
-              uint32_t y[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
-              store16(a, out + d, y);
-            } else {
-              float4* p = reinterpret_cast<float4*>(a.part) + part_at(a.D, it.slot, tile, d / 4) + row;
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                p[i * kTile] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-            }
-          }
-        }
-        fence_before();
-        if (mine) {
-          if (!it.whole)
-            a.part_ml[(int64_t)it.slot * 2 * kTile + tile * kTile + row] = st;
-          else if (a.lse)
-            a.lse[token * a.hq + head] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * 0.6931471805599453f;
-        }
-      }
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&b.o_free[tile]);
-        if (!it.pair) mbar_arrive(&b.o_free[1]);
-      }
+    if (kFour) {
+      if (it.pair || tile == 0) write_tile<Out, true>(a, sh, it, tile, items, no);
+      // (ends of the other tile's products)
+      if (tile == 0 ? it.pair : !it.pair && n > 1) ++no[1];
     }
   }
 }
@@ -1032,6 +1064,7 @@ template <typename T, int HALVES, bool kFour>
 __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_constant__ AttentionArgs a) {
   constexpr int S = stages(HALVES, kFour);
   using M = std::conditional_t<kFour, __half, T>;  // what the matrix products take
+  constexpr bool kQueries = !std::is_same<M, T>::value;  // queries are converted
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   using Sh = std::conditional_t<kFour, SharedFour, Shared>;
   Sh* sh = reinterpret_cast<Sh*>(smem_raw + (2 + S) * HALVES * kHalf + staging_bytes(HALVES, kFour));
@@ -1043,9 +1076,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     Barriers& b = sh->bar;
-    for (int i = 0; i < S; ++i) mbar_init(&b.full[i], kFour ? kConverters : 1), mbar_init(&b.empty[i], 1);
+    for (int i = 0; i < S; ++i) mbar_init(&b.full[i], kFour ? 4 : 1), mbar_init(&b.empty[i], 1);
     for (int t = 0; t < 2; ++t) {
-      mbar_init(&b.q_full[t], kFour && std::is_same<T, __nv_bfloat16>::value ? 4 : 1);
+      mbar_init(&b.q_full[t], kQueries ? 4 : 1);
       mbar_init(&b.q_empty[t], 1);
       mbar_init(&b.s_full[t], 1);
       mbar_init(&b.p_full[t], 4);  // (a lane of each warp)
@@ -1054,7 +1087,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
       mbar_init(&b.stat_full[t], 4);
     }
     if constexpr (kFour) {
-      for (int i = 0; i < kConverters * kAhead; ++i) mbar_init(&sh->staged[i / kAhead][i % kAhead], 1);
+      // (the codes' copy and 32 lanes' of scales; four warps)
+      for (int i = 0; i < kStaged; ++i) mbar_init(&sh->staged_full[i], 33), mbar_init(&sh->staged_empty[i], 4);
       mbar_init(&sh->q_raw[0], 1), mbar_init(&sh->q_raw[1], 1);
     }
     mbar_init(&b.drain, 1);
@@ -1075,9 +1109,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   Walk w;
   w.start(a);  // (its loads run while the CTA is set up)
-  if constexpr (kFour) {
-    if (threadIdx.x < kConverters) w.put(sh->walk[threadIdx.x]);
-  }
   fence_before();
   __syncthreads();
   fence_after();
@@ -1087,10 +1118,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
     if (warp == 1) {
       multiply<M, HALVES, kFour>(a, sh, w, q_smem, ring);
-    } else if (!kFour && warp != 3) {
-      copy_tiles<HALVES>(a, sh, w, q_smem, ring, warp == 2);
+    } else if (warp != 3) {
+      if constexpr (kFour) {
+        if (warp == 0)
+          copy_codes<HALVES>(a, sh, w, staging);
+        else
+          copy_scales<HALVES>(a, sh, w, staging);
+      } else {
+        copy_tiles<HALVES>(a, sh, w, q_smem, ring, warp == 2);
+      }
     } else {
-      if (warp == 3 && (!kFour || a.clears)) {
+      if (!kFour || a.clears) {
         // tokens of no request
         const int64_t first = a.plan->first, last = a.plan->last, none = first + a.n_tokens - last;
         const int64_t pieces = none * a.hq * (a.D / 8);
@@ -1104,14 +1142,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         }
         __syncwarp();
       }
-      if constexpr (kFour) convert_tiles<HALVES>(a, sh, ring, staging, warp == 0 ? 0 : warp - 1);
+      if constexpr (kFour) copy_all_queries<HALVES, kQueries>(a, sh, w, q_smem);
     }
   } else if (warp < 12) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 176;\n");
-    softmax<M, !std::is_same<M, T>::value>(a, sh, w, (warp >> 2) - 1);
+    softmax<M, T, kFour>(a, sh, w, (warp >> 2) - 1);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
-    write_out<T, HALVES, kFour>(a, sh, w, q_smem);
+    if constexpr (kFour)
+      convert_tiles<HALVES, kQueries>(a, sh, w, q_smem, ring, staging);
+    else
+      write_out<T>(a, sh, w);
   }
   __syncwarp();
   fence_before();
@@ -1275,10 +1316,10 @@ bool encode(CUtensorMap* m, int32_t dtype, int rank, const void* base, const cuu
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// 16 rows of a head's codes.
+// A page's rows of a head's codes, up to 128.
 bool encode_codes(CUtensorMap* m, const smetric_kv_config& c, const smetric_kvq_cache& cache) {
   EncodeTiledFn enc = tensor_map_encoder();
-  const cuuint32_t one[4] = {1, 1, 1, 1}, box[4] = {(cuuint32_t)c.head_dim / 2, 16, 1, 1};
+  const cuuint32_t one[4] = {1, 1, 1, 1}, box[4] = {(cuuint32_t)c.head_dim / 2, (cuuint32_t)std::min(c.page_size, kTile), 1, 1};
   const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim / 2, (cuuint64_t)c.page_size, (cuuint64_t)c.num_kv_heads,
                               (cuuint64_t)c.num_pages};
   // (a dimension of one entry may have any stride)

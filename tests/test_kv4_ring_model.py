@@ -1,17 +1,17 @@
 """The barriers of the paged attention over caches in 4 bits, in a model run in
-random order on the CPU: three warps that each convert a third of every key and
-value tile, one that issues the matrix products, the two halves' softmax, and the
-warps that write a unit's output and, before that, load the next unit's query
-tiles. A barrier is waited for by its phase's parity alone, as on the device, so a
-phase that a warp misses, or asks for two phases early, shows as a wrong tile, an
-overwritten one or a run that does not end."""
+random order on the CPU: warps that copy codes, scales and query tiles, four that
+convert (a quarter of every key and value tile, and of an item's query tiles after its
+first two tiles), one that issues the matrix products, and the two halves' softmax, who
+write the output. A barrier is waited for by its phase's parity alone, as on the
+device, so a phase that a warp misses, or asks for two phases early, shows as a wrong
+tile, an overwritten one or a run that does not end."""
 
 import random
 
 import pytest
 
 
-CONVERTERS = 3
+CONVERTERS, STAGED = 4, 3
 
 
 class Barrier:
@@ -39,16 +39,18 @@ def run(seed, stages, units):
     """units: (two query tiles?, key tiles) of a CTA's share, in order."""
     rng = random.Random(seed)
     new = lambda k, count=1: [Barrier(count) for _ in range(k)]  # noqa: E731
-    full, empty, q_raw, q_full, q_empty = new(stages, CONVERTERS), new(stages), new(2), new(2), new(2)
+    full, empty, q_raw, q_full, q_empty = new(stages, CONVERTERS), new(stages), new(2), new(2, CONVERTERS), new(2)
+    staged_full, staged_empty = new(STAGED, 2), new(STAGED, CONVERTERS)
     s_full, p_full, o_full, o_free, stat_full = new(2), new(2), new(2), new(2), new(2)
-    # a tile of the ring: how often each third of it was written, and what with
-    thirds = [[None] * CONVERTERS for _ in range(stages)]
+    # a tile of the ring: what each converting warp wrote to it last
+    parts = [[None] * CONVERTERS for _ in range(stages)]
     free, q_tiles = [[True] * CONVERTERS for _ in range(stages)], [None, None]
+    outputs = [0, 0]  # items written
     copies, products = [], []  # in flight: copies end in any order, products in theirs
 
     class Tiles:
         def __getitem__(self, s):
-            x = thirds[s]
+            x = parts[s]
             return x[0] if all(y == x[0] for y in x) else None
 
     tiles = Tiles()
@@ -57,21 +59,59 @@ def run(seed, stages, units):
         while not barrier.done(parity):
             yield
 
-    def converter(number):
-        base = 0
-        for u, (pair, n) in enumerate(units):
+    def places():
+        for u, (_, n) in enumerate(units):
             order = {place_k(j): ("k", j) for j in range(n)} | {place_v(j, n): ("v", j) for j in range(n)}
             assert sorted(order) == list(range(2 * n))
             for place in range(2 * n):
-                at = base + place
-                s = at % stages
-                if at >= stages:
-                    yield from wait(empty[s], at // stages - 1 & 1)
-                assert free[s][number], "a tile in use is overwritten"
-                free[s][number], thirds[s][number] = False, (u, *order[place])
+                yield u, place, (u, *order[place])
+
+    staged = [[None, None] for _ in range(STAGED)]
+    read = [[True] * CONVERTERS for _ in range(STAGED)]
+
+    def copier(what):  # codes or scales
+        for at, (_, _, tile) in enumerate(places()):
+            s = at % STAGED
+            if at >= STAGED:
+                yield from wait(staged_empty[s], at // STAGED - 1 & 1)
+            assert all(read[s]) or staged[s][1 - what] == tile, "codes in use are overwritten"
+            staged[s][what] = tile
+            read[s] = [False] * CONVERTERS
+            copies.append(staged_full[s].arrive)
+            yield
+
+    def queries():
+        nq = 0
+        for u, (pair, _) in enumerate(units):
+            for t in range(2 if pair else 1):
+                if nq > 1:
+                    yield from wait(q_empty[nq & 1], nq // 2 - 1 & 1)
+                q_tiles[nq & 1] = (u, t)
+                copies.append(q_raw[nq & 1].arrive)
+                nq += 1
                 yield
-                full[s].arrive()
-            base += 2 * n
+
+    def converter(number):
+        nq = 0
+        for at, (u, place, tile) in enumerate(places()):
+            s, f = at % stages, at % STAGED
+            yield from wait(staged_full[f], at // STAGED & 1)
+            assert staged[f] == [tile, tile]
+            if at >= stages:
+                yield from wait(empty[s], at // stages - 1 & 1)
+            assert free[s][number], "a tile in use is overwritten"
+            free[s][number], parts[s][number] = False, tile
+            read[f][number] = True
+            yield
+            staged_empty[f].arrive()
+            full[s].arrive()
+            if place == 1:
+                for t in range(2 if units[u][0] else 1):
+                    yield from wait(q_raw[nq & 1], nq // 2 & 1)
+                    assert q_tiles[nq & 1] == (u, t)
+                    q_full[nq & 1].arrive()  # (converted)
+                    nq += 1
+                    yield
 
     def issuer():
         base = nq = 0
@@ -141,6 +181,7 @@ def run(seed, stages, units):
 
     def softmax(t):
         ns = 0
+        ends = [0, 0]
         for u, (pair, n) in enumerate(units):
             for _ in range(0 if pair else t, n, 1 if pair else 2):
                 yield from wait(s_full[t], ns & 1)
@@ -151,42 +192,26 @@ def run(seed, stages, units):
                 yield from wait(o_free[t], u - 1 & 1)
             stat_full[t].arrive()
             yield
-
-    def writer():
-        ends = [0, 0]
-        nq = 0
-
-        def queries(u):
-            nonlocal nq
-            if u < len(units):
-                for t in range(2 if units[u][0] else 1):
-                    if nq > 1:
-                        yield from wait(q_empty[nq & 1], nq // 2 - 1 & 1)
-                    copies.append(q_raw[nq & 1].arrive)
-                    nq += 1
-                    yield
-                for t in range(nq - (2 if units[u][0] else 1), nq):
-                    yield from wait(q_raw[t & 1], t // 2 & 1)
-                    q_tiles[t & 1] = (u, t - nq + (2 if units[u][0] else 1))
-                    q_full[t & 1].arrive()  # (converted)
-                    yield
-
-        yield from queries(0)
-        for u, (pair, n) in enumerate(units):
-            yield from queries(u + 1)
-            for tile in range(2 if pair else 1):
-                yield from wait(stat_full[tile], u & 1)
+            if pair or t == 0:  # the output
+                yield from wait(stat_full[t], u & 1)
                 if not pair:
                     yield from wait(stat_full[1], u & 1)
                     if n > 1:
                         yield from wait(o_full[1], ends[1] & 1)
                         ends[1] += 1
-                yield from wait(o_full[tile], ends[tile] & 1)
-                ends[tile] += 1
+                yield from wait(o_full[t], ends[t] & 1)
+                ends[t] += 1
+                assert outputs[t] == u
+                outputs[t] += 1
+                if not pair:
+                    assert outputs[1] == u
+                    outputs[1] += 1
                 yield
-                o_free[tile].arrive()
+                o_free[t].arrive()
                 if not pair:
                     o_free[1].arrive()
+            if pair if t == 0 else not pair and n > 1:
+                ends[1] += 1
 
     def hardware(queue, pick):
         while True:
@@ -194,7 +219,8 @@ def run(seed, stages, units):
                 queue.pop(pick(len(queue)))()
             yield
 
-    warps = {**{f"c{i}": converter(i) for i in range(CONVERTERS)}, "mma": issuer(), "s0": softmax(0), "s1": softmax(1), "out": writer()}
+    warps = {"codes": copier(0), "scales": copier(1), "queries": queries(), **{f"c{i}": converter(i) for i in range(CONVERTERS)},
+             "mma": issuer(), "s0": softmax(0), "s1": softmax(1)}
     rest = {"tensor": hardware(products, lambda n: 0), "memory": hardware(copies, rng.randrange)}
     pace = {}
     for step in range(300_000):
