@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "call_range.cuh"
 #include "kv_impl.cuh"
@@ -233,18 +234,49 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// D = A B.
+__device__ __forceinline__ void mma_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+// The low four bits of each byte of x, the high four of y.
+__device__ __forceinline__ uint32_t low_nibbles(uint32_t x, uint32_t y) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, 0x0f0f0f0f, 0xe4;\n" : "=r"(r) : "r"(x), "r"(y));
+  return r;
+}
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  float2 r;
+  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+      " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y), "f"(z.x), "f"(z.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 r;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 d, a, b;\n"
+      " mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+  return r;
+}
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
   return r;
 }
-// N bytes, of which the first `full` are read and the others zeros.
-template <int N>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int full) {
-  if constexpr (N == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(full) : "memory");
+// N bytes; zeros where !held.
+template <int N, bool kWhole>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool held) {
+  if constexpr (kWhole && N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+  else if constexpr (kWhole)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;\n" ::"r"(dst), "l"(src), "n"(N) : "memory");
+  else if constexpr (N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(held ? 16 : 0) : "memory");
   else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(full) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(held ? N : 0) : "memory");
 }
 
 // A warp's two rows of queries as the products' B operand, and their powers of 2.
@@ -306,6 +338,7 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
   constexpr int kCodes = kFewTile * D / 2, kScales = kFewTile * scale_bytes(D), SB = scale_bytes(D);
   extern __shared__ __align__(128) unsigned char smem[];
   pdl_enter();
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");  // (the join's blocks, which wait for this kernel's end)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   // tokens of no request
   {
@@ -320,7 +353,6 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
     }
   }
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * kStages * kStage;
-  const unsigned char* const ring_p = smem + warp * kStages * kStage;
   const int page_size = 1 << a.page_shift;
   // Row r of a tile's keys in shared memory (the product's row) is token 2 c -> c, 2 c + 1
   // -> 4 + c of each 8: so lane (g, c)'s values, of the product's inner places 2 c, 2 c +
@@ -352,69 +384,107 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
     if (n > 0) {
       const int32_t* pages = a.pages + u.req * a.pages_stride;
       const uint32_t key0 = (uint32_t)(it.tb + stream) * kFewTile, key_step = (uint32_t)streams * kFewTile;
-      // pages of a tile's two halves, INT32_MIN where nobody sees a key of one
-      const auto page_of = [&](int j, uint32_t key) {
-        return j < n && key < (uint32_t)seen_hi && key + 16 > (uint32_t)seen_lo ? pages[key >> a.page_shift] : INT32_MIN;
+      // Pages of 16 tiles' halves, a lane each: of the tiles now copied, and of the next
+      // 16. Bits of the halves that are in the cache, and of those without a key that nobody sees.
+      uint32_t pages_now = 0, in_cache = 0, in_whole = 0;
+      int32_t pages_next;
+      const auto look_up = [&](int j) {  // of tiles j..
+        const int x = j + (lane >> 1);
+        const uint32_t key = key0 + (uint32_t)x * key_step + 16 * (lane & 1);
+        pages_next = x < n && key < (uint32_t)seen_hi && key + 16 > (uint32_t)seen_lo ? pages[key >> a.page_shift] : INT32_MIN;
       };
-      int32_t next[2] = {page_of(0, key0), page_of(0, key0 + 16)};
+      const auto turn = [&](int j) {  // to tiles j..
+        const bool held = (uint32_t)pages_next < (uint32_t)a.num_pages;
+        if (!held && pages_next != INT32_MIN) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
+        pages_now = held ? pages_next : 0;
+        const uint32_t key = key0 + (uint32_t)(j + (lane >> 1)) * key_step + 16 * (lane & 1);
+        in_cache = __ballot_sync(kFull, held);
+        in_whole = __ballot_sync(kFull, held && key >= (uint32_t)seen_lo && key + 16 <= (uint32_t)seen_hi);
+        if (j + 16 < n) look_up(j + 16);
+      };
+      look_up(0);
       uint32_t copy_key = key0, copy_to = ring;
       // A lane copies pieces (lane & 1) and 2 + (lane & 1) of token lane / 2 of each half,
       // the last piece of heads of 32 or 96 of token `lane`, and that token's scales.
-      const uint8_t* const kp = static_cast<const uint8_t*>(a.k.d_codes) + head * a.k.head_stride + 16 * (lane & 1);
-      const uint8_t* const vp = static_cast<const uint8_t*>(a.v.d_codes) + head * a.v.head_stride + 16 * (lane & 1);
-      const uint8_t* const ks = static_cast<const uint8_t*>(a.k.d_scales) + head * a.k.scale_head_stride;
-      const uint8_t* const vs = static_cast<const uint8_t*>(a.v.d_scales) + head * a.v.scale_head_stride;
-      const auto place = [](const uint8_t* base, int32_t page, int64_t page_stride, uint32_t in, int64_t token_stride) {
-        return base + (uint64_t)(uint32_t)page * (uint32_t)page_stride + (uint64_t)in * (uint32_t)token_stride;  // (both below 2^32)
-      };
-      const auto copy = [&](int j) {
-        int32_t page[2] = {next[0], next[1]};
-        const uint32_t key = copy_key, at = copy_to;
-        copy_key += key_step;
-        next[0] = page_of(j + 1, copy_key), next[1] = page_of(j + 1, copy_key + 16);
-        copy_to = copy_to + kStage == ring + kStages * kStage ? ring : copy_to + kStage;
-        int full[2] = {16, 16}, full_lane = 16, full_scale = SB;  // bytes that are read, the others become zeros
-        if ((uint32_t)page[0] >= (uint32_t)a.num_pages || (uint32_t)page[1] >= (uint32_t)a.num_pages || key < (uint32_t)seen_lo ||
-            key + kFewTile > (uint32_t)seen_hi) {
-          bool held[2];
+      // Places in pages of 16 tokens are the lane's own, in larger ones the tile's are added.
+      const bool small = page_size == 16;
+      const uint32_t half_token = lane >> 1, own_token = small ? lane & 15 : lane, own_to = row_of(lane);
+      const uint32_t k_page = (uint32_t)a.k.page_stride, k_token = (uint32_t)a.k.token_stride;  // (all below 2^32)
+      const uint32_t v_page = (uint32_t)a.v.page_stride, v_token = (uint32_t)a.v.token_stride;
+      const uint32_t ks_page = (uint32_t)a.k.scale_page_stride, ks_token = (uint32_t)a.k.scale_token_stride;
+      const uint32_t vs_page = (uint32_t)a.v.scale_page_stride, vs_token = (uint32_t)a.v.scale_token_stride;
+      const auto times = [](uint32_t x, uint32_t y) { return (uint64_t)x * y; };
+      const uint8_t* const kh = static_cast<const uint8_t*>(a.k.d_codes) + head * a.k.head_stride;
+      const uint8_t* const vh = static_cast<const uint8_t*>(a.v.d_codes) + head * a.v.head_stride;
+      const uint8_t* const kp = kh + 16 * (lane & 1) + times(half_token, k_token);
+      const uint8_t* const vp = vh + 16 * (lane & 1) + times(half_token, v_token);
+      const uint8_t* const kl = kh + 16 * (W - 1) + times(own_token, k_token);
+      const uint8_t* const vl = vh + 16 * (W - 1) + times(own_token, v_token);
+      const uint8_t* const ks = static_cast<const uint8_t*>(a.k.d_scales) + head * a.k.scale_head_stride + times(own_token, ks_token);
+      const uint8_t* const vs = static_cast<const uint8_t*>(a.v.d_scales) + head * a.v.scale_head_stride + times(own_token, vs_token);
+      const uint32_t k_to = row_of(half_token) * (D / 2) + 16 * (lane & 1);
+      // (128 elements: tokens 2, 3 of each 4 have their halves changed over, for the banks)
+      const uint32_t v_to = kCodes + half_token * (D / 2) + 16 * (lane & 1) + (D == 128 ? (half_token & 2) << 4 : 0);
+      // the tile's copies; kWhole: all of it is in the cache and seen
+      const auto copy_tile = [&](auto whole, int shift, uint32_t key, uint32_t at) {
+        constexpr bool kWhole = decltype(whole)::value;
+        bool held[2] = {true, true}, held_own = true;
+        if (!kWhole) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            held[h] = (uint32_t)page[h] < (uint32_t)a.num_pages;
-            if (!held[h] && page[h] != INT32_MIN) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
-            if (!held[h]) page[h] = 0;
-            const uint32_t x = key + 16 * h + (lane >> 1);
-            full[h] = held[h] && x >= (uint32_t)seen_lo && x < (uint32_t)seen_hi ? 16 : 0;
+            const uint32_t x = key + 16 * h + half_token;
+            held[h] = (in_cache >> (shift + h) & 1) && x >= (uint32_t)seen_lo && x < (uint32_t)seen_hi;
           }
           const uint32_t x = key + lane;
-          if (!(lane < 16 ? held[0] : held[1]) || x < (uint32_t)seen_lo || x >= (uint32_t)seen_hi) full_lane = full_scale = 0;
+          held_own = (in_cache >> (shift + (lane >> 4)) & 1) && x >= (uint32_t)seen_lo && x < (uint32_t)seen_hi;
         }
-        const uint32_t in_page = page_size - 1, in = key & in_page;
-        if constexpr (W >= 2) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t token = 16 * h + (lane >> 1), x = in + token & in_page;
-            const uint8_t* k = place(kp, page[h], a.k.page_stride, x, a.k.token_stride);
-            const uint8_t* v = place(vp, page[h], a.v.page_stride, x, a.v.token_stride);
-            const uint32_t k_to = at + row_of(token) * (D / 2) + 16 * (lane & 1);
-            // (128 elements: tokens 2, 3 of each 4 have their halves changed over, for the banks)
-            const uint32_t v_to = at + kCodes + token * (D / 2) + 16 * (lane & 1) + (D == 128 ? (token & 2) << 4 : 0);
-            copy_async<16>(k_to, k, full[h]);
-            copy_async<16>(v_to, v, full[h]);
-            if constexpr (W == 4) {
-              copy_async<16>(k_to + 32, k + 32, full[h]);
-              copy_async<16>(v_to ^ 32, v + 32, full[h]);
-            }
+        const auto codes = [&](const uint8_t* k, const uint8_t* v, int h) {
+          copy_async<16, kWhole>(at + k_to + 16 * h * (D / 2), k, held[h]);
+          copy_async<16, kWhole>(at + v_to + 16 * h * (D / 2), v, held[h]);
+          if constexpr (W == 4) {
+            copy_async<16, kWhole>(at + k_to + 16 * h * (D / 2) + 32, k + 32, held[h]);
+            copy_async<16, kWhole>(at + (v_to ^ 32) + 16 * h * (D / 2), v + 32, held[h]);
           }
+        };
+        const auto rest = [&](const uint8_t* k, const uint8_t* v, const uint8_t* k_scale, const uint8_t* v_scale) {
+          if constexpr (W & 1) {
+            copy_async<16, kWhole>(at + own_to * (D / 2) + 16 * (W - 1), k, held_own);
+            copy_async<16, kWhole>(at + kCodes + lane * (D / 2) + 16 * (W - 1), v, held_own);
+          }
+          copy_async<SB, kWhole>(at + 2 * kCodes + own_to * SB, k_scale, held_own);
+          copy_async<SB, kWhole>(at + 2 * kCodes + kScales + lane * SB, v_scale, held_own);
+        };
+        if (small) {
+          const uint32_t page0 = __shfl_sync(kFull, pages_now, shift), page1 = __shfl_sync(kFull, pages_now, shift + 1);
+          const uint32_t own = lane < 16 ? page0 : page1;
+          if constexpr (W >= 2) {
+            codes(kp + times(page0, k_page), vp + times(page0, v_page), 0);
+            codes(kp + times(page1, k_page), vp + times(page1, v_page), 1);
+          }
+          rest(kl + times(own, k_page), vl + times(own, v_page), ks + times(own, ks_page), vs + times(own, vs_page));
+        } else {
+          // (one page; where only the second half is in the cache, it is the second's)
+          const uint32_t page = __shfl_sync(kFull, pages_now, kWhole || (in_cache >> shift & 1) ? shift : shift + 1);
+          const uint32_t in = key & (page_size - 1);
+          const uint8_t* k = kp + times(page, k_page) + times(in, k_token);
+          const uint8_t* v = vp + times(page, v_page) + times(in, v_token);
+          if constexpr (W >= 2) {
+            codes(k, v, 0);
+            codes(k + times(16, k_token), v + times(16, v_token), 1);
+          }
+          rest(kl + times(page, k_page) + times(in, k_token), vl + times(page, v_page) + times(in, v_token),
+               ks + times(page, ks_page) + times(in, ks_token), vs + times(page, vs_page) + times(in, vs_token));
         }
-        const int32_t own = lane < 16 ? page[0] : page[1];
-        const uint32_t x = in + lane & in_page;
-        if constexpr (W & 1) {
-          const int last = 16 * (W - 1) - 16 * (lane & 1);
-          copy_async<16>(at + row_of(lane) * (D / 2) + 16 * (W - 1), place(kp, own, a.k.page_stride, x, a.k.token_stride) + last, full_lane);
-          copy_async<16>(at + kCodes + lane * (D / 2) + 16 * (W - 1), place(vp, own, a.v.page_stride, x, a.v.token_stride) + last, full_lane);
-        }
-        copy_async<SB>(at + 2 * kCodes + row_of(lane) * SB, place(ks, own, a.k.scale_page_stride, x, a.k.scale_token_stride), full_scale);
-        copy_async<SB>(at + 2 * kCodes + kScales + lane * SB, place(vs, own, a.v.scale_page_stride, x, a.v.scale_token_stride), full_scale);
+      };
+      const auto copy = [&](int j) {
+        if ((j & 15) == 0) turn(j);
+        const int shift = 2 * (j & 15);
+        if ((in_whole >> shift & 3) == 3)
+          copy_tile(std::true_type(), shift, copy_key, copy_to);
+        else
+          copy_tile(std::false_type(), shift, copy_key, copy_to);
+        copy_key += key_step;
+        copy_to = copy_to + kStage == ring + kStages * kStage ? ring : copy_to + kStage;
       };
 #pragma unroll
       for (int j = 0; j < kStages - 1; ++j) {
@@ -430,8 +500,11 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 #pragma unroll
         for (int i = 0; i < 2; ++i) cs[b][i] = __shfl_sync(kFull, power, 4 * (2 * c + i)) * a.scale;
       }
-      const unsigned char* at = ring_p;
+      uint32_t at = warp * kStages * kStage;  // in smem
       uint32_t key = key0;
+      // tiles that every row sees whole begin within
+      const uint32_t whole_lo = (uint32_t)max((int64_t)seen_hi - a.window, (int64_t)0);
+      const int32_t whole_hi = u.pos - (kFewTile - 1);
       for (int j = 0; j < n; ++j) {
         asm volatile("cp.async.wait_group %0;\n" ::"n"(kStages - 2) : "memory");
         __syncwarp();
@@ -441,15 +514,11 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
         float s[2][NB][4];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[t][b][i] = 0.f;
           uint32_t codes[2][W], scales[2][W];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int row = 16 * t + 8 * i + g;
-            const unsigned char* p = at + row * (D / 2) + 4 * W * c;
+            const unsigned char* p = smem + (at + row * (D / 2) + 4 * W * c);
             if constexpr (W == 4) {
               const uint4 x = *reinterpret_cast<const uint4*>(p);
               codes[i][0] = x.x, codes[i][1] = x.y, codes[i][2] = x.z, codes[i][3] = x.w;
@@ -461,7 +530,7 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
               for (int k = 0; k < W; ++k) codes[i][k] = reinterpret_cast<const uint32_t*>(p)[k];
             }
             // each word's group's scale, twice
-            const unsigned char* sp = at + 2 * kCodes + row * SB;
+            const unsigned char* sp = smem + (at + 2 * kCodes + row * SB);
             if constexpr (W == 4) {
               const uint32_t two = scales_of(reinterpret_cast<const uint16_t*>(sp)[c]);
               scales[i][0] = scales[i][1] = __byte_perm(two, 0, 0x1010);
@@ -489,12 +558,15 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
             const uint32_t x[4] = {f[0][0], f[1][0], f[0][1], f[1][1]}, y[4] = {h[0][0], h[1][0], h[0][1], h[1][1]};
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-              mma(s[t][b], x, qf[b][2 * k][0], qf[b][2 * k][1]);
+              if (k == 0)
+                mma_first(s[t][b], x, qf[b][0][0], qf[b][0][1]);
+              else
+                mma(s[t][b], x, qf[b][2 * k][0], qf[b][2 * k][1]);
               mma(s[t][b], y, qf[b][2 * k + 1][0], qf[b][2 * k + 1][1]);
             }
           }
         }
-        if (key + kFewTile - 1 > (uint32_t)u.pos || (int64_t)key < seen_hi - a.window) {  // some row does not see some key
+        if ((int32_t)key > whole_hi || key < whole_lo) {  // some row does not see some key
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -539,9 +611,12 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
           for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const float x = ex2(fmaf(s[t][b][2 * k], cs[b][0], -ref[b][0])), y = ex2(fmaf(s[t][b][2 * k + 1], cs[b][1], -ref[b][1]));
-              l[b][0] += x, l[b][1] += y;
-              p[t][b][k] = transposed(round2<__half>(make_float2(x, y)));
+              float2 x = fma2(make_float2(s[t][b][2 * k], s[t][b][2 * k + 1]), make_float2(cs[b][0], cs[b][1]),
+                              make_float2(-ref[b][0], -ref[b][1]));
+              x = make_float2(ex2(x.x), ex2(x.y));
+              const float2 sum = add2(make_float2(l[b][0], l[b][1]), x);
+              l[b][0] = sum.x, l[b][1] = sum.y;
+              p[t][b][k] = transposed(round2<__half>(x));
             }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -553,9 +628,9 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               const int token = 16 * t + 8 * k + 4 * i + c;
-              const unsigned char* row = at + kCodes + token * (D / 2);
+              const unsigned char* row = smem + (at + kCodes + token * (D / 2));
               if constexpr (W == 4) {
-                const uint2 y = *reinterpret_cast<const uint2*>(row + 16 * ((g >> 1) ^ (token & 2)) + 8 * (g & 1));
+                const uint2 y = *reinterpret_cast<const uint2*>(row + 16 * ((g >> 1) ^ (c & 2)) + 8 * (g & 1));
                 x[i][0] = y.x, x[i][1] = y.y;
               } else if constexpr (W == 2) {
                 x[i][0] = *reinterpret_cast<const uint32_t*>(row + 4 * g);
@@ -564,15 +639,15 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
                 x[i][0] = y[0];
                 if constexpr (W == 3) x[i][0] |= (uint32_t)y[1] << 16, x[i][1] = y[2];
               }
-              const unsigned char* sp = at + 2 * kCodes + kScales + token * SB;
+              const unsigned char* sp = smem + (at + 2 * kCodes + kScales + token * SB);
               sb[i][0] = sp[W * g / 4];
               sb[i][1] = W == 3 ? sp[min((W * g / 4) + 1, D / 16 - 1)] : 0;
             }
 #pragma unroll
             for (int q = 0; q < (W + 1) / 2; ++q) {
               const uint32_t y = x[0][q], z = x[1][q];
-              even[k][q] = (y & 0x0f0f0f0fu) | (z << 4 & 0xf0f0f0f0u);
-              odd[k][q] = (y >> 4 & 0x0f0f0f0fu) | (z & 0xf0f0f0f0u);
+              even[k][q] = low_nibbles(y, z << 4);
+              odd[k][q] = low_nibbles(y >> 4, z);
             }
             scales[k][0] = scales_of(sb[0][0] | sb[1][0] << 8);
             scales[k][1] = W == 3 ? scales_of(sb[0][1] | sb[1][1] << 8) : 0;
@@ -591,7 +666,7 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
             for (int b = 0; b < NB; ++b) mma(o[m][b], x, p[t][b][0], p[t][b][1]);
           }
         }
-        at = at + kStage == ring_p + kStages * kStage ? ring_p : at + kStage;
+        at = at + kStage == (warp + 1) * kStages * kStage ? warp * kStages * kStage : at + kStage;
         key += key_step;
       }
       asm volatile("cp.async.wait_group 0;\n" ::: "memory");
@@ -657,60 +732,129 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
   }
 }
 
-// out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i over a unit's pieces.
-// A block has a row of a shared unit at a time, its 8 warps every 8th piece.
+// out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i over a unit's pieces, the
+// pieces in an order that depends on their number alone. The blocks in turn for the
+// units that are shared. A row of few pieces has a warp, one of many (a long sequence
+// alone) a block.
 constexpr int kFewJoin = 256;
+constexpr int kFewPieces = 8;
+
+// Elements 4 lane .. 4 lane + 3 of a row.
+template <int D>
+__device__ __forceinline__ void write_row(const FewArgs& a, const KvUnit& u, int head, int row, float4 f, float top, float l) {
+  const int lane = threadIdx.x & 31;
+  const int64_t token = u.token + row / a.group;
+  const int qh = head * a.group + row % a.group;
+  const float inv = (l > 0.f ? 1.f / l : l) * a.v_scale;  // (NaN stays)
+  if (lane < D / 4) {
+    uint16_t* to = static_cast<uint16_t*>(a.out.d_data) + token * a.out.token_stride + qh * a.out.head_stride + 4 * lane;
+    const float2 e = make_float2(f.x * inv, f.y * inv), q = make_float2(f.z * inv, f.w * inv);
+    *reinterpret_cast<uint2*>(to) = a.bf16 ? make_uint2(round2<__nv_bfloat16>(e), round2<__nv_bfloat16>(q))
+                                           : make_uint2(round2<__half>(e), round2<__half>(q));
+  }
+  if (a.lse && lane == 0) a.lse[token * a.hq + qh] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+}
+
 template <int D, int NB>
 __global__ void __launch_bounds__(kFewJoin) k_kv4_few_join(const __grid_constant__ FewArgs a) {
-  constexpr int kRows = 8 * NB;
-  __shared__ float4 sums[8][D / 4];
-  __shared__ float2 stats[8];
-  pdl_enter();
+  constexpr int kRows = 8 * NB, kWarps = kFewJoin / 32, kMany = 1024;
+  __shared__ float4 sums[kWarps][D / 4];
+  __shared__ float2 stats[kWarps];
+  __shared__ float weights[kMany];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int per = a.heads * kRows;
-  for (int x = blockIdx.x; x < a.plan->n_split_few * per; x += gridDim.x) {
-    const int c1 = a.split[x / per], row = x % kRows, h = x % per / kRows;
-    const KvShare& s = a.shares[c1];
-    const KvUnit& u = s.last;
-    if (row >= u.tokens * a.group || s.h1 * a.heads + h >= a.hk) continue;  // (the same for the block)
-    const auto at = [&](int i) { return ((int64_t)(2 * (c1 + i) + (i == 0)) * a.heads + h) * kRows + row; };
-    float top = -INFINITY, l = 0.f;
-    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = warp; i < s.n_last; i += 8) {
-      const float2 ml = a.part_ml[at(i)];
-      float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (lane < D / 4) p = *reinterpret_cast<const float4*>(a.part + at(i) * D + 4 * lane);
-      const float to = fmaxf(top, ml.x);
-      if (to == -INFINITY) continue;
-      const float e = ex2(top - to), q = ex2(ml.x - to);
-      top = to;
-      l = l * e + ml.y * q;
-      f.x = f.x * e + p.x * q, f.y = f.y * e + p.y * q, f.z = f.z * e + p.z * q, f.w = f.w * e + p.w * q;
+  // (the plan was done before the kernel that this one waits for)
+  const int units = a.plan->n_split_few, blocks = units ? gridDim.x / units : 0, block = units ? blockIdx.x / units : 0;
+  KvShare s = {};
+  int c1 = 0;
+  if (block < blocks) {
+    c1 = a.split[blockIdx.x % units];
+    s = a.shares[c1];
+  }
+  pdl_enter();
+  if (block >= blocks) return;
+  const KvUnit& u = s.last;
+  const int unit_rows = u.tokens * a.group, rows = min(a.heads, a.hk - s.h1 * a.heads) * unit_rows, n = s.n_last;
+  const bool holds = lane < D / 4;
+  if (n <= kFewPieces) {
+    for (int x = block * kWarps + warp; x < rows; x += blocks * kWarps) {
+      const int h = x / unit_rows, row = x - h * unit_rows;
+      const auto at = [&](int i) { return ((int64_t)(2 * (c1 + i) + (i == 0)) * a.heads + h) * kRows + row; };
+      float2 ml[kFewPieces];
+      float4 p[kFewPieces];
+#pragma unroll
+      for (int i = 0; i < kFewPieces; ++i) {
+        ml[i] = make_float2(-INFINITY, 0.f);
+        p[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < n) {
+          ml[i] = a.part_ml[at(i)];
+          if (holds) p[i] = *reinterpret_cast<const float4*>(a.part + at(i) * D + 4 * lane);
+        }
+      }
+      float top = -INFINITY, l = 0.f;
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kFewPieces; ++i) top = fmaxf(top, ml[i].x);
+#pragma unroll
+      for (int i = 0; i < kFewPieces; ++i) {
+        const float e = ml[i].x == -INFINITY ? 0.f : ex2(ml[i].x - top);  // (no key of it is seen)
+        l += ml[i].y * e;
+        f.x += p[i].x * e, f.y += p[i].y * e, f.z += p[i].z * e, f.w += p[i].w * e;
+      }
+      write_row<D>(a, u, s.h1 * a.heads + h, row, f, top, l);
     }
-    if (lane < D / 4) sums[warp][lane] = f;
-    if (lane == 0) stats[warp] = make_float2(top, l);
+    return;
+  }
+  for (int x = block; x < rows; x += blocks) {
+    const int h = x / unit_rows, row = x - h * unit_rows;
+    const auto at = [&](int i) { return ((int64_t)(2 * (c1 + i) + (i == 0)) * a.heads + h) * kRows + row; };
+    float2 ml[kMany / kFewJoin];
+    float top = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < kMany / kFewJoin; ++k) {
+      const int i = k * kFewJoin + threadIdx.x;
+      ml[k] = i < n ? a.part_ml[at(i)] : make_float2(-INFINITY, 0.f);
+      top = fmaxf(top, ml[k].x);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+    if (lane == 0) stats[warp].x = top;
     __syncthreads();
-    if (warp == 0 && lane < D / 4) {
-      top = -INFINITY, l = 0.f;
-      f = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) top = fmaxf(top, stats[k].x);
+    for (int k = 0; k < kWarps; ++k) top = fmaxf(top, stats[k].x);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if (stats[k].x == -INFINITY) continue;
-        const float e = ex2(stats[k].x - top);
-        const float4 p = sums[k][lane];
-        l += stats[k].y * e;
+    for (int k = 0; k < kMany / kFewJoin; ++k) {
+      const int i = k * kFewJoin + threadIdx.x;
+      const float e = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - top);
+      if (i < n) weights[i] = e;
+      l += ml[k].y * e;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(kFull, l, o);
+    if (lane == 0) stats[warp].y = l;
+    __syncthreads();
+    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (holds) {
+#pragma unroll 8
+      for (int i = warp; i < n; i += kWarps) {
+        const float4 p = *reinterpret_cast<const float4*>(a.part + at(i) * D + 4 * lane);
+        const float e = weights[i];
         f.x += p.x * e, f.y += p.y * e, f.z += p.z * e, f.w += p.w * e;
       }
-      const int64_t token = u.token + row / a.group;
-      const int qh = (s.h1 * a.heads + h) * a.group + row % a.group;
-      const float inv = (l > 0.f ? 1.f / l : l) * a.v_scale;
-      uint16_t* to = static_cast<uint16_t*>(a.out.d_data) + token * a.out.token_stride + qh * a.out.head_stride + 4 * lane;
-      const float2 e = make_float2(f.x * inv, f.y * inv), q = make_float2(f.z * inv, f.w * inv);
-      *reinterpret_cast<uint2*>(to) = a.bf16 ? make_uint2(round2<__nv_bfloat16>(e), round2<__nv_bfloat16>(q))
-                                             : make_uint2(round2<__half>(e), round2<__half>(q));
-      if (a.lse && lane == 0) a.lse[token * a.hq + qh] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+      sums[warp][lane] = f;
+    }
+    __syncthreads();
+    if (warp == 0) {
+      l = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) l += stats[k].y;
+      if (holds) {
+#pragma unroll
+        for (int k = 1; k < kWarps; ++k) {
+          const float4 p = sums[k][lane];
+          f.x += p.x, f.y += p.y, f.z += p.z, f.w += p.w;
+        }
+      }
+      write_row<D>(a, u, s.h1 * a.heads + h, row, f, top, l);
     }
     __syncthreads();
   }

@@ -60,7 +60,7 @@ struct __align__(16) KvShare {
 // kFewTile keys.
 constexpr int kFewTile = 32;
 // Its warps, and so the key heads of a block at most.
-__host__ __device__ constexpr int few_heads(int rows) { return rows == 8 ? 16 : 12; }
+__host__ __device__ constexpr int few_heads(int rows) { return rows == 8 ? 12 : 12; }
 struct KvFew {
   int rows;    // 8, 16, or 0: no such kernel (more than 16 query heads per key head)
   int tokens;  // rows / group
