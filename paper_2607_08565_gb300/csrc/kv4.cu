@@ -230,13 +230,13 @@ __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
 }
 // D (16 x 8, 32 bits) += A (16 x 16) B (16 x 8).
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // D = A B.
 __device__ __forceinline__ void mma_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
                : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
@@ -279,30 +279,31 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool h
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(N), "r"(held ? N : 0) : "memory");
 }
 
-// A warp's two rows of queries as the products' B operand, and their powers of 2.
-// Lane (g, c) = (lane / 4, lane % 4) has row g's elements [c D/4, (c+1) D/4). A row
+// Query rows n0 .. n0 + 7 of a key head as the products' B operand, and their powers of
+// 2. Lane (g, c) = (lane / 4, lane % 4) has row g's elements [c D/4, (c+1) D/4). A row
 // goes to half precision divided by the power of two of its largest element: 8 or 11
 // bits fit, and what is lost below 2^-24 of the largest is lost to 32-bit sums too.
 template <int D>
-__device__ __forceinline__ void load_rows(const FewArgs& a, const KvUnit& u, int head, int n0, uint32_t (&qf)[D / 16][2],
-                                          float& power) {
-  const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3, n = n0 + g;
-  const bool mine = n < u.tokens * a.group;
+__device__ __forceinline__ void load_rows(const FewArgs& a, const KvUnit& u, int head, int n0, uint4 (&x)[D / 32]) {
+  const int lane = threadIdx.x & 31, n = n0 + (lane >> 2);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) x[i] = make_uint4(0, 0, 0, 0);
+  if (n >= u.tokens * a.group) return;
+  const int64_t at = (int64_t)(u.token + n / a.group) * a.q.token_stride + (int64_t)(head * a.group + n % a.group) * a.q.head_stride;
+  const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q.d_data) + at + (lane & 3) * (D / 4));
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) x[i] = p[i];
+}
+template <int D>
+__device__ __forceinline__ void convert_rows(const uint4 (&x)[D / 32], bool bf16, uint32_t (&qf)[D / 16][2], float& power) {
   float f[D / 4];
 #pragma unroll
-  for (int i = 0; i < D / 4; ++i) f[i] = 0.f;
-  if (mine) {
-    const int64_t at = (int64_t)(u.token + n / a.group) * a.q.token_stride + (int64_t)(head * a.group + n % a.group) * a.q.head_stride;
-    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q.d_data) + at + c * (D / 4));
+  for (int i = 0; i < D / 32; ++i) {
+    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      const uint4 x = p[i];
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 y = a.bf16 ? make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u)) : floats(w[k]);
-        f[8 * i + 2 * k] = y.x, f[8 * i + 2 * k + 1] = y.y;
-      }
+    for (int k = 0; k < 4; ++k) {
+      const float2 y = bf16 ? make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u)) : floats(w[k]);
+      f[8 * i + 2 * k] = y.x, f[8 * i + 2 * k + 1] = y.y;
     }
   }
   float top = 0.f;
@@ -319,6 +320,22 @@ __device__ __forceinline__ void load_rows(const FewArgs& a, const KvUnit& u, int
   for (int i = 0; i < D / 16; ++i)
 #pragma unroll
     for (int k = 0; k < 2; ++k) qf[i][k] = round2<__half>(make_float2(f[4 * i + 2 * k] * down, f[4 * i + 2 * k + 1] * down));
+}
+
+// Elements 4 lane .. 4 lane + 3 of a row.
+template <int D>
+__device__ __forceinline__ void write_row(const FewArgs& a, const KvUnit& u, int head, int row, float4 f, float top, float l) {
+  const int lane = threadIdx.x & 31;
+  const int64_t token = u.token + row / a.group;
+  const int qh = head * a.group + row % a.group;
+  const float inv = (l > 0.f ? 1.f / l : l) * a.v_scale;  // (NaN stays)
+  if (lane < D / 4) {
+    uint16_t* to = static_cast<uint16_t*>(a.out.d_data) + token * a.out.token_stride + qh * a.out.head_stride + 4 * lane;
+    const float2 e = make_float2(f.x * inv, f.y * inv), q = make_float2(f.z * inv, f.w * inv);
+    *reinterpret_cast<uint2*>(to) = a.bf16 ? make_uint2(round2<__nv_bfloat16>(e), round2<__nv_bfloat16>(q))
+                                           : make_uint2(round2<__half>(e), round2<__half>(q));
+  }
+  if (a.lse && lane == 0) a.lse[token * a.hq + qh] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
 }
 
 // Attention of up to NB * 8 query rows (a token's heads of one key head, or a few
@@ -403,6 +420,10 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
         if (j + 16 < n) look_up(j + 16);
       };
       look_up(0);
+      // (on their way with the pages)
+      uint4 queries[NB][D / 32];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) load_rows<D>(a, u, head, 8 * b, queries[b]);
       uint32_t copy_key = key0, copy_to = ring;
       // A lane copies pieces (lane & 1) and 2 + (lane & 1) of token lane / 2 of each half,
       // the last piece of heads of 32 or 96 of token `lane`, and that token's scales.
@@ -496,7 +517,7 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         float power;
-        load_rows<D>(a, u, head, 8 * b, qf[b], power);
+        convert_rows<D>(queries[b], a.bf16, qf[b], power);
 #pragma unroll
         for (int i = 0; i < 2; ++i) cs[b][i] = __shfl_sync(kFull, power, 4 * (2 * c + i)) * a.scale;
       }
@@ -512,50 +533,55 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
         asm volatile("cp.async.commit_group;\n" ::: "memory");
         // scores: S[half][block][...] of tokens token_of(g), token_of(g + 8) and rows 2c, 2c + 1
         float s[2][NB][4];
+        uint32_t codes[2][2][W], k_scales[2][2][W];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          uint32_t codes[2][W], scales[2][W];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int row = 16 * t + 8 * i + g;
             const unsigned char* p = smem + (at + row * (D / 2) + 4 * W * c);
+            uint32_t(&x)[W] = codes[t][i];
+            uint32_t(&scale)[W] = k_scales[t][i];
             if constexpr (W == 4) {
-              const uint4 x = *reinterpret_cast<const uint4*>(p);
-              codes[i][0] = x.x, codes[i][1] = x.y, codes[i][2] = x.z, codes[i][3] = x.w;
+              const uint4 y = *reinterpret_cast<const uint4*>(p);
+              x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
             } else if constexpr (W == 2) {
-              const uint2 x = *reinterpret_cast<const uint2*>(p);
-              codes[i][0] = x.x, codes[i][1] = x.y;
+              const uint2 y = *reinterpret_cast<const uint2*>(p);
+              x[0] = y.x, x[1] = y.y;
             } else {
 #pragma unroll
-              for (int k = 0; k < W; ++k) codes[i][k] = reinterpret_cast<const uint32_t*>(p)[k];
+              for (int k = 0; k < W; ++k) x[k] = reinterpret_cast<const uint32_t*>(p)[k];
             }
             // each word's group's scale, twice
             const unsigned char* sp = smem + (at + 2 * kCodes + row * SB);
             if constexpr (W == 4) {
               const uint32_t two = scales_of(reinterpret_cast<const uint16_t*>(sp)[c]);
-              scales[i][0] = scales[i][1] = __byte_perm(two, 0, 0x1010);
-              scales[i][2] = scales[i][3] = __byte_perm(two, 0, 0x3232);
+              scale[0] = scale[1] = __byte_perm(two, 0, 0x1010);
+              scale[2] = scale[3] = __byte_perm(two, 0, 0x3232);
             } else if constexpr (W == 3) {  // (12 words of 6 groups: the middle word goes with the first or the last)
-              const uint32_t x = sp[3 * c / 2], y = sp[3 * c / 2 + 1];
-              scales[i][0] = scales_of(x * 0x101), scales[i][2] = scales_of(y * 0x101);
-              scales[i][1] = c & 1 ? scales[i][2] : scales[i][0];
+              const uint32_t y = sp[3 * c / 2], z = sp[3 * c / 2 + 1];
+              scale[0] = scales_of(y * 0x101), scale[2] = scales_of(z * 0x101);
+              scale[1] = c & 1 ? scale[2] : scale[0];
             } else {
-              const uint32_t x = sp[W * c / 2];
+              const uint32_t y = sp[W * c / 2];
 #pragma unroll
-              for (int k = 0; k < W; ++k) scales[i][k] = scales_of(x * 0x101);
+              for (int k = 0; k < W; ++k) scale[k] = scales_of(y * 0x101);
             }
           }
+        }
+        // (the halves in turn: a product takes longer than the conversions for the next)
 #pragma unroll
-          for (int k = 0; k < W; ++k) {
-            uint32_t f[2][2], h[2][2];  // the word's pairs: rows g, g + 8
+        for (int k = 0; k < W; ++k) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            uint32_t x[4], y[4];  // the word's pairs: rows g, g + 8
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              f[i][0] = mul_h2(pair_of<0>(codes[i][k]), scales[i][k]);
-              f[i][1] = mul_h2(pair_of<1>(codes[i][k]), scales[i][k]);
-              h[i][0] = mul_h2(pair_of<2>(codes[i][k]), scales[i][k]);
-              h[i][1] = mul_h2(pair_of<3>(codes[i][k]), scales[i][k]);
+              x[i] = mul_h2(pair_of<0>(codes[t][i][k]), k_scales[t][i][k]);
+              x[2 + i] = mul_h2(pair_of<1>(codes[t][i][k]), k_scales[t][i][k]);
+              y[i] = mul_h2(pair_of<2>(codes[t][i][k]), k_scales[t][i][k]);
+              y[2 + i] = mul_h2(pair_of<3>(codes[t][i][k]), k_scales[t][i][k]);
             }
-            const uint32_t x[4] = {f[0][0], f[1][0], f[0][1], f[1][1]}, y[4] = {h[0][0], h[1][0], h[0][1], h[1][1]};
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
               if (k == 0)
@@ -696,8 +722,8 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
     }
     __syncthreads();
     const int rows = u.tokens * a.group;
-    for (int x = threadIdx.x; x < heads * rows * (D / 4); x += kWarps * 32) {
-      const int d = x % (D / 4) * 4, y = x / (D / 4), row = y % rows, h = y / rows;
+    for (int y = warp; y < heads * rows; y += kWarps) {  // a row a warp
+      const int h = y / rows, row = y - h * rows, d = 4 * lane, q = d / (D / 8), m = d % (D / 8) / 2;
       float top = -INFINITY;
       for (int k = 0; k < streams; ++k) top = fmaxf(top, stats[(k * heads + h) * kRows + row].x);
       float sum = 0.f;
@@ -705,27 +731,20 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
       for (int k = 0; k < streams; ++k) {
         const int at = (k * heads + h) * kRows + row;
         const float2 st = stats[at];
-        if (st.x == -INFINITY) continue;
-        const float e = ex2(st.x - top);
-        const int q = d / (D / 8), m = d % (D / 8) / 2;
-        const float2 p0 = *reinterpret_cast<const float2*>(sums + at * sum_row(D) + 16 * m + 2 * q);
-        const float2 p1 = *reinterpret_cast<const float2*>(sums + at * sum_row(D) + 16 * (m + 1) + 2 * q);
+        const float e = st.x == -INFINITY ? 0.f : ex2(st.x - top);
         sum += st.y * e;
-        f.x += p0.x * e, f.y += p0.y * e, f.z += p1.x * e, f.w += p1.y * e;
+        if (D == 128 || d < D) {
+          const float2 p0 = *reinterpret_cast<const float2*>(sums + at * sum_row(D) + 16 * m + 2 * q);
+          const float2 p1 = *reinterpret_cast<const float2*>(sums + at * sum_row(D) + 16 * (m + 1) + 2 * q);
+          f.x += p0.x * e, f.y += p0.y * e, f.z += p1.x * e, f.w += p1.y * e;
+        }
       }
       if (it.whole) {
-        const int64_t token = u.token + row / a.group;
-        const int qh = (it.hb * a.heads + h) * a.group + row % a.group;
-        const float inv = (sum > 0.f ? 1.f / sum : sum) * a.v_scale;  // (NaN stays)
-        uint16_t* to = static_cast<uint16_t*>(a.out.d_data) + token * a.out.token_stride + qh * a.out.head_stride + d;
-        const float2 e = make_float2(f.x * inv, f.y * inv), q = make_float2(f.z * inv, f.w * inv);
-        *reinterpret_cast<uint2*>(to) = a.bf16 ? make_uint2(round2<__nv_bfloat16>(e), round2<__nv_bfloat16>(q))
-                                               : make_uint2(round2<__half>(e), round2<__half>(q));
-        if (a.lse && d == 0) a.lse[token * a.hq + qh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+        write_row<D>(a, u, it.hb * a.heads + h, row, f, top, sum);
       } else {
         const int64_t at = ((int64_t)it.slot * a.heads + h) * kRows + row;
-        *reinterpret_cast<float4*>(a.part + at * D + d) = f;
-        if (d == 0) a.part_ml[at] = make_float2(top, sum);
+        if (D == 128 || d < D) *reinterpret_cast<float4*>(a.part + at * D + d) = f;
+        if (lane == 0) a.part_ml[at] = make_float2(top, sum);
       }
     }
     __syncthreads();  // (the sums' memory is the rings')
@@ -736,31 +755,14 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 // pieces in an order that depends on their number alone. The blocks in turn for the
 // units that are shared. A row of few pieces has a warp, one of many (a long sequence
 // alone) a block.
-constexpr int kFewJoin = 256;
+constexpr int kFewJoin = 512;
 constexpr int kFewPieces = 8;
-
-// Elements 4 lane .. 4 lane + 3 of a row.
-template <int D>
-__device__ __forceinline__ void write_row(const FewArgs& a, const KvUnit& u, int head, int row, float4 f, float top, float l) {
-  const int lane = threadIdx.x & 31;
-  const int64_t token = u.token + row / a.group;
-  const int qh = head * a.group + row % a.group;
-  const float inv = (l > 0.f ? 1.f / l : l) * a.v_scale;  // (NaN stays)
-  if (lane < D / 4) {
-    uint16_t* to = static_cast<uint16_t*>(a.out.d_data) + token * a.out.token_stride + qh * a.out.head_stride + 4 * lane;
-    const float2 e = make_float2(f.x * inv, f.y * inv), q = make_float2(f.z * inv, f.w * inv);
-    *reinterpret_cast<uint2*>(to) = a.bf16 ? make_uint2(round2<__nv_bfloat16>(e), round2<__nv_bfloat16>(q))
-                                           : make_uint2(round2<__half>(e), round2<__half>(q));
-  }
-  if (a.lse && lane == 0) a.lse[token * a.hq + qh] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
-}
 
 template <int D, int NB>
 __global__ void __launch_bounds__(kFewJoin) k_kv4_few_join(const __grid_constant__ FewArgs a) {
-  constexpr int kRows = 8 * NB, kWarps = kFewJoin / 32, kMany = 1024;
+  constexpr int kRows = 8 * NB, kWarps = kFewJoin / 32;
   __shared__ float4 sums[kWarps][D / 4];
   __shared__ float2 stats[kWarps];
-  __shared__ float weights[kMany];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // (the plan was done before the kernel that this one waits for)
   const int units = a.plan->n_split_few, blocks = units ? gridDim.x / units : 0, block = units ? blockIdx.x / units : 0;
@@ -807,54 +809,55 @@ __global__ void __launch_bounds__(kFewJoin) k_kv4_few_join(const __grid_constant
   for (int x = block; x < rows; x += blocks) {
     const int h = x / unit_rows, row = x - h * unit_rows;
     const auto at = [&](int i) { return ((int64_t)(2 * (c1 + i) + (i == 0)) * a.heads + h) * kRows + row; };
-    float2 ml[kMany / kFewJoin];
+    constexpr int P = 5;  // pieces a warp has on their way
     float top = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int k = 0; k < kMany / kFewJoin; ++k) {
-      const int i = k * kFewJoin + threadIdx.x;
-      ml[k] = i < n ? a.part_ml[at(i)] : make_float2(-INFINITY, 0.f);
-      top = fmaxf(top, ml[k].x);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-    if (lane == 0) stats[warp].x = top;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kWarps; ++k) top = fmaxf(top, stats[k].x);
-#pragma unroll
-    for (int k = 0; k < kMany / kFewJoin; ++k) {
-      const int i = k * kFewJoin + threadIdx.x;
-      const float e = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - top);
-      if (i < n) weights[i] = e;
-      l += ml[k].y * e;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(kFull, l, o);
-    if (lane == 0) stats[warp].y = l;
-    __syncthreads();
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (holds) {
-#pragma unroll 8
-      for (int i = warp; i < n; i += kWarps) {
-        const float4 p = *reinterpret_cast<const float4*>(a.part + at(i) * D + 4 * lane);
-        const float e = weights[i];
-        f.x += p.x * e, f.y += p.y * e, f.z += p.z * e, f.w += p.w * e;
-      }
-      sums[warp][lane] = f;
-    }
-    __syncthreads();
-    if (warp == 0) {
-      l = 0.f;
+    for (int i0 = warp; i0 < n; i0 += P * kWarps) {
+      float2 ml[P];
+      float4 p[P];
 #pragma unroll
-      for (int k = 0; k < kWarps; ++k) l += stats[k].y;
-      if (holds) {
-#pragma unroll
-        for (int k = 1; k < kWarps; ++k) {
-          const float4 p = sums[k][lane];
-          f.x += p.x, f.y += p.y, f.z += p.z, f.w += p.w;
+      for (int k = 0; k < P; ++k) {
+        const int i = i0 + k * kWarps;
+        ml[k] = make_float2(-INFINITY, 0.f);
+        p[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < n) {
+          ml[k] = a.part_ml[at(i)];
+          if (holds) p[k] = *reinterpret_cast<const float4*>(a.part + at(i) * D + 4 * lane);
         }
       }
-      write_row<D>(a, u, s.h1 * a.heads + h, row, f, top, l);
+      float to = top;
+#pragma unroll
+      for (int k = 0; k < P; ++k) to = fmaxf(to, ml[k].x);
+      const float back = top == -INFINITY ? 0.f : ex2(top - to);
+      top = to;
+      l *= back;
+      f.x *= back, f.y *= back, f.z *= back, f.w *= back;
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        const float e = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - to);
+        l += ml[k].y * e;
+        f.x += p[k].x * e, f.y += p[k].y * e, f.z += p[k].z * e, f.w += p[k].w * e;
+      }
+    }
+    if (holds) sums[warp][lane] = f;
+    if (lane == 0) stats[warp] = make_float2(top, l);
+    __syncthreads();
+    if (warp == 0) {
+      float all = -INFINITY;
+      l = 0.f;
+      f = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) all = fmaxf(all, stats[k].x);
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) {
+        const float e = stats[k].x == -INFINITY ? 0.f : ex2(stats[k].x - all);
+        l += stats[k].y * e;
+        if (holds) {
+          const float4 p = sums[k][lane];
+          f.x += p.x * e, f.y += p.y * e, f.z += p.z * e, f.w += p.w * e;
+        }
+      }
+      write_row<D>(a, u, s.h1 * a.heads + h, row, f, all, l);
     }
     __syncthreads();
   }
@@ -870,7 +873,7 @@ int launch_few(smetric_kv* kv, const FewArgs& a, cudaStream_t s) {
   int rc = launch_k(k_kv4_few<D, NB>, dim3((unsigned)kv->num_sms), dim3(few_heads(8 * NB) * 32), (size_t)few_smem(D, 8 * NB), s, true, a);
   if (rc) return rc;
   kv->launches += 2;
-  return launch_k(k_kv4_few_join<D, NB>, dim3((unsigned)kv->num_sms * 4), dim3(kFewJoin), 0, s, true, a);
+  return launch_k(k_kv4_few_join<D, NB>, dim3((unsigned)kv->num_sms * 2), dim3(kFewJoin), 0, s, true, a);
 }
 
 }  // namespace
