@@ -289,21 +289,29 @@ __device__ __forceinline__ uint4 pack(const float* f) {
                     Pair<T>::put(f[6], f[7]));
 }
 
+// Rounds of heads; of a share, `each`, and one more of the first `rest` shares.
+struct Rounds {
+  int32_t all, each, rest;
+};
+
 struct HeadsArgs {
   smetric_heads q, k, v, q_out, k_out;  // absent: 0 heads
   int32_t hq, hk, hv;
   smetric_kv_cache cache;    // keys and values go here when tokens is not NULL
   smetric_kvq_cache k4, v4;  // or here
+  float k_down, v_down;      // 2^-exp
   const KvToken* tokens;     // the plan's, or NULL: d_positions and k_out
   const KvPlan* plan;
   const int32_t* positions;
   int64_t n_tokens;
   int32_t D, page_shift, rot, lanes_shift, splits;
+  Rounds rounds_k, rounds_v, rounds_q;
+  int32_t before_v, before_q;  // rounds before the values' and the queries', by the shares
   uint32_t rows;  // positions below it are taken: the table's rows, all that are not negative without one
   const float* table;
   const void* q_norm;
   const void* k_norm;
-  float eps;
+  float eps, one_of_D;
   int32_t* status;
 };
 
@@ -328,7 +336,7 @@ struct Lane {
   bool held, turned;  // it has elements of a head; they are rotated
   int e0, e1;         // the pieces' first elements
   int lanes_shift, D;
-  float eps;
+  float eps, one_of_D;
   float2 cs[4], sn[4];  // of its 8 pairs
 };
 
@@ -342,7 +350,7 @@ __device__ __forceinline__ void load_head(const Lane& l, const T* src, int h, in
 }
 
 // A lane's norm and rotation, from its two pieces y to 16 elements f.
-template <typename T, bool kInterleaved>
+template <typename T, bool kInterleaved, bool kFour>
 __device__ __forceinline__ void transform_lane(const Lane& l, const uint4 (&y)[2], bool on, const T* norm, float2 (&f)[8]) {
 #pragma unroll
   for (int e = 0; e < 2; ++e) unpack<T>(y[e], &f[4 * e].x);
@@ -353,7 +361,8 @@ __device__ __forceinline__ void transform_lane(const Lane& l, const uint4 (&y)[2
     float ss = on ? s2.x + s2.y : 0.f;
     for (int o = 1; o < 1 << l.lanes_shift; o <<= 1) ss += __shfl_xor_sync(kFull, ss, o);
     if (on) {
-      const float inv = 1.0f / sqrtf(ss / (float)l.D + l.eps);
+      // (in 4 bits, where instructions count: 2^-22 of it off at most)
+      const float inv = kFour ? rsqrtf(ss * l.one_of_D + l.eps) : 1.0f / sqrtf(ss / (float)l.D + l.eps);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         float2 g[4];
@@ -385,7 +394,7 @@ __device__ __forceinline__ void transform_lane(const Lane& l, const uint4 (&y)[2
 // heads h, h + step, ... < heads of a token, from src to dst (both at head h);
 // x: the first of them. (A round's heads are loaded while the round before is
 // computed.)
-template <typename T, bool kInterleaved>
+template <typename T, bool kInterleaved, bool kFour>
 __device__ __forceinline__ void transform_heads(const Lane& l, const T* src, int64_t src_step, T* dst, int64_t dst_step,
                                                 int h, int step, int heads, int rounds, const T* norm, uint4 (&x)[2]) {
   for (int r = 0; r < rounds; ++r, h += step, dst += dst_step) {
@@ -401,7 +410,7 @@ __device__ __forceinline__ void transform_heads(const Lane& l, const T* src, int
       continue;
     }
     float2 f[8];
-    transform_lane<T, kInterleaved>(l, y, on, norm, f);
+    transform_lane<T, kInterleaved, kFour>(l, y, on, norm, f);
     if (on) {
       *reinterpret_cast<uint4*>(dst + l.e0) = pack<T>(&f[0].x);
       *reinterpret_cast<uint4*>(dst + l.e1) = pack<T>(&f[4].x);
@@ -409,36 +418,47 @@ __device__ __forceinline__ void transform_heads(const Lane& l, const T* src, int
   }
 }
 
-// The larger magnitude; NaN if either is.
-__device__ __forceinline__ float max_nan(float x, float y) {
+// The largest magnitude; NaN if one is.
+__device__ __forceinline__ float max_nan(float x, float y, float z) {
   float m;
-  asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(m) : "f"(x), "f"(y));
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;\n" : "=f"(m) : "f"(x), "f"(y), "f"(z));
   return m;
 }
 
 // A group's scale: its 8 bits, and 2^-exp / scale for its elements (0 where the
-// scale is 0 or NaN).
+// scale is 0 or NaN). The sixth is a product, at most 1.25 units in the last place off:
+// rounded to multiples of 4 of them it is the quotient where that is halfway between
+// two scales (5 bits), and no other quotient of a 16-bit number comes that near.
 __device__ __forceinline__ uint32_t scale_of(float top, float down, float& inv) {
+  // (a NaN of all ones would become -0)
+  const float sixth = __uint_as_float((min(__float_as_uint(top * down * 0.16666667f), 0x7fc00000u) + 2) & ~3u);
   uint32_t bits, half;
   asm("{\n .reg .b16 b;\n cvt.rn.satfinite.e4m3x2.f32 b, %2, %2;\n cvt.u32.u16 %0, b;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
-      : "=r"(bits), "=r"(half) : "f"(__fdiv_rn(top * down, 6.f)));
+      : "=r"(bits), "=r"(half) : "f"(sixth));
   const float s = __half2float(__ushort_as_half((unsigned short)half));
-  inv = s > 0.f ? __fdiv_rn(down, s) : 0.f;
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(s));
+  inv = s > 0.f ? down * r : 0.f;
   return bits & 0xff;
 }
 
-// 8 codes. A product with the rounded reciprocal is within 2^-20 of the quotient
-// (of 6.4 at most), and quotients of 16-bit numbers that are not halfway between
-// two codes at least 2^-13 from there: adding and subtracting 24 leaves multiples
-// of 2^-19, so that what is halfway is seen so.
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 r;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 d, a, b;\n"
+      " mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+  return r;
+}
+
+// 8 codes. The reciprocal is within 2^-23 of itself, so that a product of 5 (the last
+// number halfway between two codes) at most is less than 2^-20 from the quotient, and
+// quotients of 16-bit numbers that are not halfway are at least 2^-13 from there: adding
+// and subtracting 24 leaves multiples of 2^-19, so that what is halfway is seen so.
 __device__ __forceinline__ uint32_t codes_of(const float2* f, float inv) {
   uint32_t r;
   float2 y[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    y[k] = mul2(f[k], make_float2(inv, inv));
-    y[k] = make_float2(__fadd_rn(__fadd_rn(y[k].x, 24.f), -24.f), __fadd_rn(__fadd_rn(y[k].y, 24.f), -24.f));
-  }
+  for (int k = 0; k < 4; ++k) y[k] = add2(add2(mul2(f[k], make_float2(inv, inv)), make_float2(24.f, 24.f)), make_float2(-24.f, -24.f));
   asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
       " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}\n"
       : "=r"(r) : "f"(y[0].x), "f"(y[0].y), "f"(y[1].x), "f"(y[1].y), "f"(y[2].x), "f"(y[2].y), "f"(y[3].x), "f"(y[3].y));
@@ -475,31 +495,35 @@ __device__ __forceinline__ void quantise_heads(const Lane& l, const T* src, int6
     src += src_step;
     load_head(l, src, h + step, heads, x);
     float2 f[8];
-    transform_lane<T, kInterleaved>(l, y, on, norm, f);
+    transform_lane<T, kInterleaved, true>(l, y, on, norm, f);
     float m[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      m[i] = max_nan(fabsf(f[4 * i].x), fabsf(f[4 * i].y));
-#pragma unroll
-      for (int k = 1; k < 4; ++k) m[i] = max_nan(m[i], max_nan(fabsf(f[4 * i + k].x), fabsf(f[4 * i + k].y)));
+      m[i] = max_nan(f[4 * i].x, f[4 * i].y, f[4 * i + 1].x);
+      m[i] = max_nan(m[i], f[4 * i + 1].y, f[4 * i + 2].x);
+      m[i] = max_nan(m[i], f[4 * i + 2].y, f[4 * i + 3].x);
+      m[i] = max_nan(m[i], f[4 * i + 3].y, 0.f);
     }
-    float top[2];
     if (R > 0) {  // (the same for the warp)
+      float top[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const float a = __shfl_sync(kFull, m[0], from[i]), b = __shfl_sync(kFull, m[1], from[i]);
-        top[i] = max_nan(m[i], second[i] ? b : a);
+        top[i] = max_nan(m[i], second[i] ? b : a, 0.f);
       }
-    } else {
-      top[0] = top[1] = max_nan(m[0], m[1]);
-    }
-    if (!on) continue;
+      if (!on) continue;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < 2; ++i) {
+        float inv;
+        const uint32_t scale = scale_of(top[i], dst.down, inv);
+        reinterpret_cast<uint32_t*>(dst.codes)[p[i]] = codes_of(f + 4 * i, inv);
+        if (!(p[i] & 1)) dst.scales[p[i] >> 1] = (uint8_t)scale;
+      }
+    } else if (on) {
       float inv;
-      const uint32_t scale = scale_of(top[i], dst.down, inv);
-      reinterpret_cast<uint32_t*>(dst.codes)[p[i]] = codes_of(f + 4 * i, inv);
-      if (!(p[i] & 1)) dst.scales[p[i] >> 1] = (uint8_t)scale;
+      const uint32_t scale = scale_of(max_nan(m[0], m[1], 0.f), dst.down, inv);
+      *reinterpret_cast<uint2*>(dst.codes + 4 * p[0]) = make_uint2(codes_of(f, inv), codes_of(f + 4, inv));
+      dst.scales[p[0] >> 1] = (uint8_t)scale;
     }
   }
 }
@@ -517,7 +541,8 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   pdl_enter();
   const int lane = threadIdx.x & 31;
   const int64_t w = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const int64_t t = w / a.splits;
+  // (few tokens have several warps each: 32 bits hold their number)
+  const int64_t t = a.splits == 1 ? w : (uint32_t)w / (uint32_t)a.splits;
   const int share = (int)(w - t * a.splits);
   if (t >= a.n_tokens) return;
   Lane l;
@@ -528,20 +553,25 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   l.e1 = l.turned && !kInterleaved ? 8 * c + a.rot / 2 : 16 * c + 8;
   l.lanes_shift = a.lanes_shift;
   l.D = a.D;
+  l.one_of_D = a.one_of_D;
   l.eps = a.eps;
   const int per = 32 >> a.lanes_shift;  // heads a warp takes at a time
   const int step = per * a.splits, first = lane >> a.lanes_shift;
   // rounds of heads: the keys', then the values', then the queries'; the share
   // has every splits-th, from rounds k0, v0, q0 of each
-  const int rk = (a.hk + per - 1) / per, rv = (a.hv + per - 1) / per, rq = (a.hq + per - 1) / per;
-  const auto start = [&](int before) { return (share - before % a.splits + a.splits) % a.splits; };
-  const int k0 = share, v0 = start(rk), q0 = start(rk + rv);
+  const int k0 = share, v0 = share - a.before_v + (share < a.before_v ? a.splits : 0),
+            q0 = share - a.before_q + (share < a.before_q ? a.splits : 0);
+  const int rk = a.rounds_k.all, rv = a.rounds_v.all, rq = a.rounds_q.all;
   const auto source = [&](const smetric_heads& src, int r) {
     return static_cast<const T*>(src.d_data) + t * src.token_stride + (r * per + first) * src.head_stride;
   };
   // (the first loads run while the token's place is found)
   uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)}, y[2] = {x[0], x[1]};
-  if (!kFour && v0 < rv) load_head(l, source(a.v, v0), v0 * per + first, a.hv, y);
+  Lane plain;  // (in 4 bits) a value's elements, in order
+  plain.held = l.held, plain.turned = false;
+  plain.e0 = 16 * c, plain.e1 = 16 * c + 8;
+  plain.lanes_shift = l.lanes_shift, plain.D = l.D, plain.eps = l.eps, plain.one_of_D = l.one_of_D;
+  if (v0 < rv) load_head(kFour ? plain : l, source(a.v, v0), v0 * per + first, a.hv, y);
   if (k0 < rk) load_head(l, source(a.k, k0), k0 * per + first, a.hk, x);
   int64_t slot = 0;
   int32_t pos;
@@ -568,51 +598,48 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
       l.sn[2 * i] = make_float2(v.x, v.y), l.sn[2 * i + 1] = make_float2(v.z, v.w);
     }
   }
-  const auto heads = [&](const smetric_heads& src, T* dst, int64_t head_stride, int r, int rounds, int n_heads,
+  const auto heads = [&](const smetric_heads& src, T* dst, int64_t head_stride, int r, const Rounds& rounds, int n_heads,
                          const void* norm, uint4(&z)[2]) {
-    if (r < rounds)
-      transform_heads<T, kInterleaved>(l, source(src, r), step * src.head_stride,
+    if (r < rounds.all)
+      transform_heads<T, kInterleaved, kFour>(l, source(src, r), step * src.head_stride,
                                        dst + (r * per + first) * head_stride, step * head_stride, r * per + first, step,
-                                       n_heads, (rounds - r + a.splits - 1) / a.splits, static_cast<const T*>(norm), z);
+                                       n_heads, rounds.each + (r < rounds.rest), static_cast<const T*>(norm), z);
   };
-  const int64_t at = (slot >> a.page_shift) * a.cache.page_stride +
-                     (slot & ((1 << a.page_shift) - 1)) * a.cache.token_stride;
   if constexpr (kFour) {
-    const auto quantise = [&](const Lane& ln, const smetric_heads& src, const smetric_kvq_cache& c4, int r, int rounds,
-                              int n_heads, const void* norm, int R, uint4(&z)[2]) {
-      if (r >= rounds) return;
-      const int64_t page = slot >> a.page_shift, in = slot & ((1 << a.page_shift) - 1);
+    const uint32_t page = (uint32_t)(slot >> a.page_shift), in = (uint32_t)slot & ((1 << a.page_shift) - 1);
+    const auto quantise = [&](const Lane& ln, const smetric_heads& src, const smetric_kvq_cache& c4, float down, int r,
+                              const Rounds& rounds, int n_heads, const void* norm, int R, uint4(&z)[2]) {
+      if (r >= rounds.all) return;
+      // (page and token strides are below 2^32)
+      const auto times = [](uint32_t x, int64_t stride) { return (uint64_t)x * (uint32_t)stride; };
+      const int head = r * per + first;
       Codes to;
-      to.codes = static_cast<uint8_t*>(c4.d_codes) + page * c4.page_stride + in * c4.token_stride +
-                 (r * per + first) * c4.head_stride;
-      to.scales = static_cast<uint8_t*>(c4.d_scales) + page * c4.scale_page_stride + in * c4.scale_token_stride +
-                  (r * per + first) * c4.scale_head_stride;
+      to.codes = static_cast<uint8_t*>(c4.d_codes) + times(page, c4.page_stride) + times(in, c4.token_stride) + head * c4.head_stride;
+      to.scales = static_cast<uint8_t*>(c4.d_scales) + times(page, c4.scale_page_stride) + times(in, c4.scale_token_stride) +
+                  head * c4.scale_head_stride;
       to.step = step * c4.head_stride;
       to.scale_step = step * c4.scale_head_stride;
-      to.down = exp2f((float)-c4.exp);
-      quantise_heads<T, kInterleaved>(ln, source(src, r), step * src.head_stride, to, r * per + first, step, n_heads,
-                                      (rounds - r + a.splits - 1) / a.splits, static_cast<const T*>(norm), R, z);
+      to.down = down;
+      quantise_heads<T, kInterleaved>(ln, source(src, r), step * src.head_stride, to, head, step, n_heads,
+                                      rounds.each + (r < rounds.rest), static_cast<const T*>(norm), R, z);
     };
-    Lane plain;  // a value's elements, in order
-    plain.held = l.held, plain.turned = false;
-    plain.e0 = 16 * c, plain.e1 = 16 * c + 8;
-    plain.lanes_shift = l.lanes_shift, plain.D = l.D, plain.eps = l.eps;
-    if (v0 < rv) load_head(plain, source(a.v, v0), v0 * per + first, a.hv, y);
-    quantise(plain, a.v, a.v4, v0, rv, a.hv, nullptr, 0, y);
+    quantise(plain, a.v, a.v4, a.v_down, v0, a.rounds_v, a.hv, nullptr, 0, y);
     if (q0 < rq) load_head(l, source(a.q, q0), q0 * per + first, a.hq, y);
-    quantise(l, a.k, a.k4, k0, rk, a.hk, a.k_norm, !kInterleaved && a.table ? a.rot / 16 : 0, x);
-    heads(a.q, static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride, a.q_out.head_stride, q0, rq, a.hq, a.q_norm, y);
+    quantise(l, a.k, a.k4, a.k_down, k0, a.rounds_k, a.hk, a.k_norm, !kInterleaved && a.table ? a.rot / 16 : 0, x);
+    heads(a.q, static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride, a.q_out.head_stride, q0, a.rounds_q, a.hq, a.q_norm, y);
     return;
   }
+  const int64_t at = (slot >> a.page_shift) * a.cache.page_stride +
+                     (slot & ((1 << a.page_shift) - 1)) * a.cache.token_stride;
   l.turned = false;
-  heads(a.v, static_cast<T*>(a.cache.d_v) + at, a.cache.head_stride, v0, rv, a.hv, nullptr, y);
+  heads(a.v, static_cast<T*>(a.cache.d_v) + at, a.cache.head_stride, v0, a.rounds_v, a.hv, nullptr, y);
   l.turned = turned;
   if (q0 < rq) load_head(l, source(a.q, q0), q0 * per + first, a.hq, y);
   if (a.tokens)
-    heads(a.k, static_cast<T*>(a.cache.d_k) + at, a.cache.head_stride, k0, rk, a.hk, a.k_norm, x);
+    heads(a.k, static_cast<T*>(a.cache.d_k) + at, a.cache.head_stride, k0, a.rounds_k, a.hk, a.k_norm, x);
   else
-    heads(a.k, static_cast<T*>(a.k_out.d_data) + t * a.k_out.token_stride, a.k_out.head_stride, k0, rk, a.hk, a.k_norm, x);
-  heads(a.q, static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride, a.q_out.head_stride, q0, rq, a.hq, a.q_norm, y);
+    heads(a.k, static_cast<T*>(a.k_out.d_data) + t * a.k_out.token_stride, a.k_out.head_stride, k0, a.rounds_k, a.hk, a.k_norm, x);
+  heads(a.q, static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride, a.q_out.head_stride, q0, a.rounds_q, a.hq, a.q_norm, y);
 }
 
 bool transform_ok(const smetric_kv* kv, const smetric_kv_transform& t) {
@@ -634,6 +661,7 @@ int launch_heads(smetric_kv* kv, HeadsArgs& a, const smetric_kv_transform& t, cu
   a.q_norm = a.hq ? t.d_q_norm : nullptr;
   a.k_norm = a.hk ? t.d_k_norm : nullptr;
   a.eps = t.eps;
+  a.one_of_D = 1.f / (float)a.D;
   a.status = kv->status;
   a.lanes_shift = 0;
   while (16 << a.lanes_shift < a.D) a.lanes_shift++;
@@ -642,6 +670,14 @@ int launch_heads(smetric_kv* kv, HeadsArgs& a, const smetric_kv_transform& t, cu
   const int rounds = (a.hq + a.hk + a.hv + (32 >> a.lanes_shift) - 1) / (32 >> a.lanes_shift);
   const int64_t room = (int64_t)kv->num_sms * 28 / std::max<int64_t>(1, a.n_tokens);
   a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, room));
+  const int per = 32 >> a.lanes_shift;
+  const auto count = [&](int heads) {
+    const int all = (heads + per - 1) / per;
+    return Rounds{all, all / a.splits, all % a.splits};
+  };
+  a.rounds_k = count(a.hk), a.rounds_v = count(a.hv), a.rounds_q = count(a.hq);
+  a.before_v = a.rounds_k.all % a.splits;
+  a.before_q = (a.rounds_k.all + a.rounds_v.all) % a.splits;
   const int64_t grid = (a.n_tokens * a.splits + 3) / 4;
   const bool il = t.flags & SMETRIC_KV_INTERLEAVED;
   const bool bf = kv->cfg.dtype == SMETRIC_BF16;
@@ -878,6 +914,8 @@ int smetric_kvq_append(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_ca
   a.hq = q.d_data ? kv->cfg.num_q_heads : 0;
   a.k4 = k_cache;
   a.v4 = v_cache;
+  a.k_down = std::ldexp(1.f, -k_cache.exp);
+  a.v_down = std::ldexp(1.f, -v_cache.exp);
   a.tokens = kv->tokens;
   a.plan = kv->plan;
   a.n_tokens = kv->n_tokens;

@@ -60,6 +60,15 @@ __device__ __forceinline__ uint32_t round2<__half>(float2 x) {
   return *reinterpret_cast<const uint32_t*>(&p);
 }
 
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+  float2 r;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 d, a, b;\n"
+      " mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+  return r;
+}
+
 // ---- reading back ----
 
 struct ReadArgs {
@@ -70,16 +79,20 @@ struct ReadArgs {
   const int32_t* pages;
   int64_t pages_stride, n_rows, num_pages;
   int32_t n, max_pages, page_shift, D, hk, rows;  // rows of a block
+  bool wide[2];  // outputs can be stored in pieces of 32 bytes
   int32_t* status;
 };
 
 constexpr int kReadThreads = 128;
+constexpr int kReadRows = 32;  // of a block, at most
 
-// A block takes `rows` rows: a thread each finds their slots, then all copy, 16
-// elements (a group, whole sectors of the output) a thread at a time.
+// A block takes some rows: a thread each finds where they are, then all copy, 16
+// elements (a group, whole sectors of the output) a thread at a time; a thread has the
+// same group of the same head for every row that it takes. Bound by memory: the output
+// is 3.6 times the input.
 template <typename T>
 __global__ void __launch_bounds__(kReadThreads) k_kv4_read(const __grid_constant__ ReadArgs a) {
-  __shared__ int64_t slots[kReadThreads];  // -1: left as it is, -2: zeros
+  __shared__ int64_t codes_at[kReadRows][2], scales_at[kReadRows][2];  // -1: left as it is, -2: zeros
   pdl_enter();
   const int64_t row0 = (int64_t)blockIdx.x * a.rows;
   const int rows = (int)min((int64_t)a.rows, a.n_rows - row0);
@@ -96,49 +109,74 @@ __global__ void __launch_bounds__(kReadThreads) k_kv4_read(const __grid_constant
         hi = mid;
     }
     const int64_t begin = a.off[lo], end = a.off[lo + 1];
-    int64_t slot = -1;
+    int32_t page = -1, in = -1;
     if (begin < 0 || end < begin || end > a.n_rows) {
       latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
     } else if (begin <= i && i < end) {
       const int64_t pos = (a.first ? a.first[lo] : 0) + (i - begin), at = pos >> a.page_shift;
-      const int32_t page = pos >= 0 && at < a.max_pages ? a.pages[lo * a.pages_stride + at] : -1;
-      slot = page >= 0 && page < a.num_pages ? ((int64_t)page << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : -2;
-      if (slot < 0) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
+      page = pos >= 0 && at < a.max_pages ? a.pages[lo * a.pages_stride + at] : -1;
+      in = page >= 0 && page < a.num_pages ? (int32_t)(pos & ((1 << a.page_shift) - 1)) : -2;
+      if (in < 0) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
     }
-    slots[threadIdx.x] = slot;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      codes_at[threadIdx.x][w] = in < 0 ? in : page * a.c[w].page_stride + in * a.c[w].token_stride;
+      scales_at[threadIdx.x][w] = page * a.c[w].scale_page_stride + in * a.c[w].scale_token_stride;
+    }
   }
   __syncthreads();
-  const int groups = a.D / 16, per = a.hk * groups;  // of a row, for keys or values
-  for (int x = threadIdx.x; x < rows * 2 * per; x += kReadThreads) {
-    const int row = x / (2 * per), y = x - row * 2 * per, which = y >= per;
-    const int z = y - which * per, h = z / groups, g = z - h * groups;
-    const int64_t slot = slots[row];
+  // columns: a group of a head's keys or values each; `width` of them at a time
+  const int groups = a.D / 16, per = a.hk * groups, width = min(2 * per, kReadThreads);
+  const int stride = kReadThreads / width, first = threadIdx.x / width;
+  if (first >= stride) return;
+  for (int column = threadIdx.x - first * width; column < 2 * per; column += width) {
+    const int which = column >= per, z = column - which * per, h = z / groups, g = z - h * groups;
     const smetric_heads& out = a.out[which];
-    if (slot == -1 || !out.d_data) continue;
-    uint2 w = make_uint2(0, 0);
-    uint32_t scale = 0;
+    if (!out.d_data) continue;
     const smetric_kvq_cache& c = a.c[which];
-    if (slot >= 0) {
-      const int64_t page = slot >> a.page_shift, in = slot & ((1 << a.page_shift) - 1);
-      w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.d_codes) + page * c.page_stride +
-                                          in * c.token_stride + h * c.head_stride + 8 * g);
-      scale = static_cast<const uint8_t*>(c.d_scales)[page * c.scale_page_stride + in * c.scale_token_stride +
-                                                      h * c.scale_head_stride + g];
-    }
-    const float s = floats(scales_of(scale)).x * exp2f((float)c.exp);
-    uint32_t r[8];
-    const auto four = [&](uint32_t codes, uint32_t* to) {
-      const uint32_t p[4] = {pair_of<0>(codes), pair_of<1>(codes), pair_of<2>(codes), pair_of<3>(codes)};
+    const uint8_t* const codes = static_cast<const uint8_t*>(c.d_codes) + h * c.head_stride + 8 * g;
+    const uint8_t* const scales = static_cast<const uint8_t*>(c.d_scales) + h * c.scale_head_stride + g;
+    T* to = static_cast<T*>(out.d_data) + (row0 + first) * out.token_stride + h * out.head_stride + 16 * g;
+    const float unit = exp2f((float)c.exp);
+    constexpr int P = 4;  // rows on their way
+    for (int row0 = first; row0 < rows; row0 += P * stride) {
+      int64_t at[P];
+      uint2 w[P];
+      uint32_t scale[P];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 f = floats(p[k]);
-        to[k] = round2<T>(make_float2(f.x * s, f.y * s));
+      for (int k = 0; k < P; ++k) {
+        const int row = row0 + k * stride;
+        at[k] = row < rows ? codes_at[row][which] : -1;
+        w[k] = make_uint2(0, 0);
+        scale[k] = 0;
+        if (at[k] >= 0) {
+          w[k] = *reinterpret_cast<const uint2*>(codes + at[k]);
+          scale[k] = scales[scales_at[row][which]];
+        }
       }
-    };
-    four(w.x, r), four(w.y, r + 4);
-    uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(out.d_data) + (row0 + row) * out.token_stride + h * out.head_stride + 16 * g);
-    to[0] = make_uint4(r[0], r[1], r[2], r[3]);
-    to[1] = make_uint4(r[4], r[5], r[6], r[7]);
+#pragma unroll
+      for (int k = 0; k < P; ++k, to += stride * out.token_stride) {
+        if (at[k] == -1) continue;
+        const float s = floats(scales_of(scale[k])).x * unit;
+        uint32_t r[8];
+        const auto four = [&](uint32_t x, uint32_t* y) {
+          const uint32_t p[4] = {pair_of<0>(x), pair_of<1>(x), pair_of<2>(x), pair_of<3>(x)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = round2<T>(mul2(floats(p[i]), make_float2(s, s)));
+        };
+        four(w[k].x, r), four(w[k].y, r + 4);
+        // (a whole sector in one store: two halves took 97 us for 148,000 rows of 2 x 4 heads
+        // of 128, as every sector went to the L2 cache twice)
+        if (a.wide[which]) {
+          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                       "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+        } else {
+          uint4* q = reinterpret_cast<uint4*>(to);
+          q[0] = make_uint4(r[0], r[1], r[2], r[3]);
+          q[1] = make_uint4(r[4], r[5], r[6], r[7]);
+        }
+      }
+    }
   }
 }
 
@@ -914,7 +952,10 @@ int smetric_kvq_read(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cach
   a.page_shift = __builtin_ctz((unsigned)c.page_size);
   a.D = c.head_dim;
   a.hk = c.num_kv_heads;
-  a.rows = 8;
+  // (few rows: enough blocks for the SMs first)
+  a.rows = (int32_t)std::min<int64_t>(kReadRows, std::max<int64_t>(1, n_rows / (8 * kv->num_sms)));
+  for (int w = 0; w < 2; ++w)
+    a.wide[w] = !(reinterpret_cast<uintptr_t>(a.out[w].d_data) & 31) && a.out[w].token_stride % 16 == 0 && a.out[w].head_stride % 16 == 0;
   a.status = kv->status;
   const int64_t grid = (n_rows + a.rows - 1) / a.rows;
   kv->launches++;
