@@ -3,9 +3,9 @@ to the instance whose KV$ blocks make it cheapest, and that instance prefills
 only what its cache does not hold. One attention layer of random weights
 stands in for the model.
 
-    python examples/serve_turns.py
+    python examples/serve_turns.py [4]
 
-Every turn's output is compared with the same prompt prefilled from nothing."""
+With 4 the caches are held in 4 bits. Every turn's output is compared with the same prompt prefilled from nothing."""
 
 from __future__ import annotations
 
@@ -45,10 +45,12 @@ class Layer:
 class Instance:
     """A serving instance: a paged cache whose full blocks are found by their chain hash."""
 
-    def __init__(self, pages: int, requests: int, tokens: int):
-        self.cache = [torch.empty(pages, BLOCK, HK, D, dtype=torch.bfloat16, device=dev) for _ in range(2)]
-        self.kv = pkg.SMetricKV(head_dim=D, num_q_heads=HQ, num_kv_heads=HK, page_size=BLOCK, num_pages=pages,
-                                max_batch_requests=requests, max_batch_tokens=tokens)
+    def __init__(self, pages: int, requests: int, tokens: int, bits: int = 16):
+        kind = pkg.SMetricKV4 if bits == 4 else pkg.SMetricKV
+        self.kv = kind(head_dim=D, num_q_heads=HQ, num_kv_heads=HK, page_size=BLOCK, num_pages=pages,
+                       max_batch_requests=requests, max_batch_tokens=tokens)
+        self.cache = (self.kv.new_cache() if bits == 4 else
+                      [torch.empty(pages, BLOCK, HK, D, dtype=torch.bfloat16, device=dev) for _ in range(2)])
         self.free, self.held = list(range(pages)), {}
 
     def prefill(self, layer, prompts, hits, hashes):
@@ -77,7 +79,7 @@ class Instance:
         return out, new
 
 
-def serve(sessions=12, turns=4, instances=3, seed=0, say=print):
+def serve(sessions=12, turns=4, instances=3, seed=0, say=print, bits=16):
     """Returns (tokens prefilled, tokens of all prompts, largest difference from prefilling from nothing)."""
     g = torch.Generator().manual_seed(seed)
     text = lambda n: torch.randint(0, VOCAB, (n,), generator=g).tolist()  # noqa: E731
@@ -86,7 +88,7 @@ def serve(sessions=12, turns=4, instances=3, seed=0, say=print):
     most = sessions * (len(system) + 300 * (turns + 1) + 17 * sessions)
     layer = Layer(most)
     ix = pkg.SMetricIndex(instances, BLOCK, 1, capacity_slots=1 << 16, max_batch_requests=sessions, max_batch_tokens=most)
-    nodes = [Instance(8192, sessions, most) for _ in range(instances)]
+    nodes = [Instance(8192, sessions, most, bits) for _ in range(instances)]
     load = torch.zeros(instances, dtype=torch.int64, device=dev)
     done = total = 0
     worst = 0.0
@@ -106,7 +108,7 @@ def serve(sessions=12, turns=4, instances=3, seed=0, say=print):
                 continue
             ps, hs = [prompts[r] for r in mine], [hashes[at[r]:at[r + 1]] for r in mine]
             got, new = node.prefill(layer, ps, [hit[r] for r in mine], hs)
-            whole, all_new = Instance(8192, sessions, most).prefill(layer, ps, [0] * len(mine), [[]] * len(mine))
+            whole, all_new = Instance(8192, sessions, most, bits).prefill(layer, ps, [0] * len(mine), [[]] * len(mine))
             a = b = 0
             for n, m in zip(new, all_new):
                 worst = max(worst, (got[a:a + n].float() - whole[b + m - n:b + m].float()).abs().max().item())
@@ -118,4 +120,4 @@ def serve(sessions=12, turns=4, instances=3, seed=0, say=print):
 
 
 if __name__ == "__main__":
-    serve()
+    serve(bits=int(sys.argv[1]) if len(sys.argv) > 1 else 16)

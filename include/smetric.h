@@ -735,10 +735,13 @@ int smetric_kvq_read(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cach
                      int32_t max_pages, int64_t pages_stride, smetric_heads k, smetric_heads v,
                      smetric_stream_t stream);
 
-/* smetric_paged_attention over caches in 4 bits. Codes times scales are exact
- * in 16 bits, and so are scores of the values that the caches stand for, up to
- * the sums' 32 bits. scale * 2^exp of the keys is finite and > 0. Masked
- * positions of a request's own length may hold anything too. */
+/* smetric_paged_attention over caches in 4 bits, as the numbers that they stand
+ * for. Codes times scales are exact in half precision, which the products take
+ * whatever the handle's dtype: queries are divided by a power of two for each row,
+ * and the softmax's weights are rounded to half precision (to within 2^-32 of the
+ * row's largest where they are below 2^-21 of it). scale * 2^exp of the keys is finite
+ * and > 0. Scales at masked positions of a request's own length must not be
+ * NaN; what lies past its length or before its window may be anything. */
 int smetric_kvq_attention(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cache v_cache, smetric_heads q,
                           float scale, smetric_heads out, float* d_lse, smetric_stream_t stream);
 

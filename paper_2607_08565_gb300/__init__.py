@@ -1095,6 +1095,9 @@ class SMetricKV:
             raise SmetricError(rc, "device")
 
 
+_NO_CACHE4 = smetric_kvq_cache()
+
+
 class Cache4(NamedTuple):
     """Keys or values in 4 bits: codes uint8 [num_pages, page_size, num_kv_heads,
     head_dim / 2] and scales torch.float8_e4m3fn [num_pages, page_size,
@@ -1143,6 +1146,8 @@ class SMetricKV4(SMetricKV):
         return self._cache4(k_cache, "k_cache"), self._cache4(v_cache, "v_cache")
 
     def _cache4(self, cache, name: str) -> smetric_kvq_cache:
+        if not isinstance(cache, Cache4):
+            raise ValueError(f"{name} must be a Cache4")
         codes, scales, exp = cache
         here = self._device
         if (codes.dtype != self._u8 or scales.dtype != self._e4m3 or codes.shape != self._codes_shape or
@@ -1168,33 +1173,38 @@ class SMetricKV4(SMetricKV):
         [n, max_pages] (row stride free). A cache may be None. Returns (k_out,
         v_out), new tensors [n_rows, num_kv_heads, head_dim] unless given; rows of
         no request are not written."""
-        hk = self.cfg.num_kv_heads
+        hk, here, dim = self.cfg.num_kv_heads, self._device, self._dim
         n = offsets.numel() - 1
-        if offsets.dim() != 1 or n < 0 or offsets.dtype != self._i64 or not offsets.is_contiguous():
+        if offsets.dtype != self._i64 or offsets.dim() != 1 or n < 0 or not offsets.is_contiguous():
             raise ValueError("offsets must be torch.int64 [requests + 1], contiguous")
-        if pages.dtype != self._i32 or pages.dim() != 2 or pages.shape[0] != n or (pages.shape[1] > 1 and pages.stride(1) != 1):
+        if pages.dtype != self._i32 or pages.dim() != 2:
+            raise ValueError("pages must be torch.int32 [requests, max_pages]")
+        (rows, most), (row_stride, one) = pages.shape, pages.stride()
+        if rows != n or (most > 1 and one != 1):
             raise ValueError("pages must be torch.int32 [requests, max_pages], a request's contiguous")
-        if first is not None and (first.dtype != self._i32 or first.shape != (n,) or not first.is_contiguous()):
-            raise ValueError("first must be torch.int32 [requests], contiguous")
-        if any(x is not None and x.get_device() != self._device for x in (offsets, pages, first)):
-            raise ValueError(f"offsets, pages and first must be on cuda:{self._device}")
+        if first is not None and (first.dtype != self._i32 or first.shape != (n,) or not first.is_contiguous() or
+                                  first.get_device() != here):
+            raise ValueError(f"first must be torch.int32 [requests], contiguous, on cuda:{here}")
+        if offsets.get_device() != here or pages.get_device() != here:
+            raise ValueError(f"offsets and pages must be on cuda:{here}")
         raw, other = self._stream(stream)
-        none = smetric_kvq_cache()
-        outs, heads, caches = [], [], []
-        for cache, out, name in ((k_cache, k_out, "k"), (v_cache, v_out, "v")):
-            caches.append(none if cache is None else self._cache4(cache, name + "_cache"))
+
+        def out_of(cache, out, name):
+            """A cache's description, its output and that one's description."""
             if cache is None:
-                out, described = None, _NO_HEADS
-            elif out is None:
-                out = self._new(other, self._empty, (n_rows, hk, self._dim), dtype=self.dtype, device=offsets.device)
-                described = smetric_heads(out.data_ptr(), hk * self._dim, self._dim)
-            else:
-                described = self._heads(out, hk, n_rows, name + "_out")
-            outs.append(out)
-            heads.append(described)
-        most = pages.shape[1]
-        _check(self._lib.smetric_kvq_read(self.handle, *caches, offsets.data_ptr(), n, n_rows,
+                return _NO_CACHE4, None, _NO_HEADS
+            described = self._cache4(cache, name)
+            if out is not None:
+                return described, out, self._heads(out, hk, n_rows, name)
+            shape = (n_rows, hk, dim)
+            out = (self._empty(shape, dtype=self.dtype, device=offsets.device) if other is None else
+                   self._new(other, self._empty, shape, dtype=self.dtype, device=offsets.device))
+            return described, out, smetric_heads(out.data_ptr(), hk * dim, dim)
+
+        kc, k_out, kh = out_of(k_cache, k_out, "k")
+        vc, v_out, vh = out_of(v_cache, v_out, "v")
+        _check(self._lib.smetric_kvq_read(self.handle, kc, vc, offsets.data_ptr(), n, n_rows,
                                           first.data_ptr() if first is not None and n else None,
-                                          pages.data_ptr() if pages.numel() else None, most,
-                                          pages.stride(0) if n > 1 else most, *heads, raw), "smetric_kvq_read")
-        return tuple(outs)
+                                          pages.data_ptr() if n and most else None, most, row_stride if n > 1 else most,
+                                          kh, vh, raw), "smetric_kvq_read")
+        return k_out, v_out
