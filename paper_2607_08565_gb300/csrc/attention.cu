@@ -450,11 +450,31 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
 
 // ---- caches in 4 bits ----
 
-// The tile at a place of an item's order, of n key tiles: K0 K1 V0 K2 V1 K3 ...
-__device__ __forceinline__ int tile_at(int place, int n, bool& values) {
-  values = place == 2 * n - 1 || (place > 1 && !(place & 1));
-  return place == 2 * n - 1 ? n - 1 : place < 2 ? place : values ? place / 2 - 1 : (place + 1) / 2;
-}
+// An item's tiles in their order, K0 K1 V0 K2 V1 K3 ..., and the lane's page of each: a
+// tile's values have the pages of its keys, two places on.
+struct Order {
+  int32_t n, jk, jv;         // key tiles; keys' and values' so far
+  int32_t ahead, last, before;  // pages of the next keys, of the last ones, of those before
+  template <typename F>
+  __device__ __forceinline__ void start(int32_t tiles, F page_of) {
+    n = tiles, jk = jv = 0;
+    last = before = INT32_MIN;
+    ahead = page_of(0);
+  }
+  // The next tile, its page and whether it is of values; page_of(j) is the page of tile j.
+  template <typename F>
+  __device__ __forceinline__ int32_t next(F page_of, bool& values, int32_t& page) {
+    values = jk == n || (jk > 1 && jv < jk - 1);
+    if (values) {
+      page = jv == jk - 1 ? last : before;
+      return jv++;
+    }
+    page = ahead;
+    before = last, last = ahead;
+    ahead = jk + 1 < n ? page_of(jk + 1) : INT32_MIN;
+    return jk++;
+  }
+};
 
 // One warp copies the tiles' codes as they are, a lane a page.
 template <int HALVES>
@@ -463,23 +483,21 @@ __device__ __forceinline__ void copy_codes(const AttentionArgs& a, SharedFour* s
   const int rows = min(kTile, a.page_size), per = kTile / rows;  // of a copy, and pages of a tile
   const int page_shift = __ffs(a.page_size) - 1, row_bytes = a.D / 2;
   uint32_t at = 0;
+  Order order;
   Item it;
   while (w.next(a, it)) {
-    const int n = it.te - it.tb;
     const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
     const int32_t* pages = a.pages + it.unit.req * a.pages_stride;
-    // the lane's page of a tile, INT32_MIN where nobody sees a key of it
-    const auto page_of = [&](int place) {
-      bool values;
-      const int64_t key = (int64_t)(it.tb + tile_at(place, n, values)) * kTile + lane * rows;
-      return lane < per && place < 2 * n && key < hi && key + rows > lo ? pages[key >> page_shift] : INT32_MIN;
+    // INT32_MIN where nobody sees a key of it
+    const auto page_of = [&](int j) {
+      const int64_t key = (int64_t)(it.tb + j) * kTile + lane * rows;
+      return lane < per && key < hi && key + rows > lo ? pages[key >> page_shift] : INT32_MIN;
     };
-    int32_t next = page_of(0);
-    for (int place = 0; place < 2 * n; ++place, ++at) {
-      int32_t page = next;
-      next = page_of(place + 1);
+    order.start(it.te - it.tb, page_of);
+    for (int place = 0; place < 2 * order.n; ++place, ++at) {
       bool values;
-      const int j = tile_at(place, n, values);
+      int32_t page;
+      const int j = order.next(page_of, values, page);
       const uint32_t s = at % kStaged;
       if (at >= kStaged) mbar_wait(&sh->staged_empty[s], (at / kStaged - 1) & 1, sh, a.status);
       if (stopped(sh)) break;
@@ -513,23 +531,21 @@ __device__ __forceinline__ void copy_scales(const AttentionArgs& a, SharedFour* 
   const int lane = threadIdx.x & 31, page_shift = __ffs(a.page_size) - 1;
   staging += kStaged * codes_bytes(HALVES);
   uint32_t at = 0;
+  Order order;
   Item it;
   while (w.next(a, it)) {
-    const int n = it.te - it.tb;
     const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
     const int32_t* pages = a.pages + it.unit.req * a.pages_stride;
     // the page of 16 rows (lane & 7) of a tile
-    const auto page_of = [&](int place) {
-      bool values;
-      const int64_t key = (int64_t)(it.tb + tile_at(place, n, values)) * kTile + 16 * (lane & 7);
-      return place < 2 * n && key < hi && key + 16 > lo ? pages[key >> page_shift] : -1;
+    const auto page_of = [&](int j) {
+      const int64_t key = (int64_t)(it.tb + j) * kTile + 16 * (lane & 7);
+      return key < hi && key + 16 > lo ? pages[key >> page_shift] : INT32_MIN;
     };
-    int32_t next = page_of(0);
-    for (int place = 0; place < 2 * n; ++place, ++at) {
-      const int32_t page = next;
-      next = page_of(place + 1);
+    order.start(it.te - it.tb, page_of);
+    for (int place = 0; place < 2 * order.n; ++place, ++at) {
       bool values;
-      const int64_t key = (int64_t)(it.tb + tile_at(place, n, values)) * kTile + lane;
+      int32_t page;
+      const int64_t key = (int64_t)(it.tb + order.next(page_of, values, page)) * kTile + lane;
       const smetric_kvq_cache& c = values ? a.v4 : a.k4;
       const uint8_t* scales = static_cast<const uint8_t*>(c.d_scales) + it.h * c.scale_head_stride;
       const uint32_t page_stride = (uint32_t)c.scale_page_stride, token_stride = (uint32_t)c.scale_token_stride;  // (below 2^32)
@@ -585,8 +601,9 @@ __device__ __forceinline__ void convert_row(SharedFour* sh, uint32_t nq, uint32_
 // Four warps turn tiles of codes into tiles of the ring in half precision, in the
 // 128-byte swizzle, 32 rows each: a conversion for two codes and a product with their
 // scale, both exact (2 and 4 bits). A tile's keys and values are laid out alike. They
-// also convert an item's query tiles (kQueries), after its first two tiles: those, and
-// all before, are used up without the queries that this warp would wait with.
+// also convert an item's query tiles (kQueries), when they find them there between two
+// of its tiles, and after its fourth (or last) at the latest: the ring takes so many, and
+// all before are used up without the queries.
 template <int HALVES, bool kQueries>
 __device__ __forceinline__ void convert_tiles(const AttentionArgs& a, SharedFour* sh, Walk w, uint32_t q_smem, uint32_t ring,
                                               uint32_t staging) {
@@ -601,6 +618,7 @@ __device__ __forceinline__ void convert_tiles(const AttentionArgs& a, SharedFour
   Item it;
   while (w.next(a, it)) {
     const int n = it.te - it.tb;
+    int queries = it.pair ? 2 : 1;  // tiles left to convert
     for (int place = 0; place < 2 * n; ++place, ++at) {
       const uint32_t s = at % S, from = at % kStaged;
       mbar_wait(&sh->staged_full[from], at / kStaged & 1, sh, a.status);
@@ -651,14 +669,16 @@ __device__ __forceinline__ void convert_tiles(const AttentionArgs& a, SharedFour
         mbar_arrive(&sh->staged_empty[from]);
         mbar_arrive(&b.full[s]);
       }
-      if (kQueries && place == 1) {
-        const int tiles = it.pair ? 2 : 1;
-        for (int t = 0; t < tiles; ++t, ++nq) {
-          mbar_wait(&sh->q_raw[nq & 1], nq / 2 & 1, sh, a.status);
+      if (kQueries) {
+        while (queries > 0) {
+          uint64_t* const raw = &sh->q_raw[nq & 1];
+          if (place < min(S, 2 * n) - 1 && !__any_sync(kFull, mbar_test(raw, nq / 2 & 1))) break;
+          mbar_wait(raw, nq / 2 & 1, sh, a.status);
           convert_row<HALVES>(sh, nq, q_smem, threadIdx.x & 127);
           asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(&b.q_full[nq & 1]);
+          ++nq, --queries;
         }
       }
     }

@@ -1,7 +1,7 @@
 """The barriers of the paged attention over caches in 4 bits, in a model run in
 random order on the CPU: warps that copy codes, scales and query tiles, four that
-convert (a quarter of every key and value tile, and of an item's query tiles after its
-first two tiles), one that issues the matrix products, and the two halves' softmax, who
+convert (a quarter of every key and value tile, and of an item's query tiles, when they
+are there, after its first tiles at the latest), one that issues the matrix products, and the two halves' softmax, who
 write the output. A barrier is waited for by its phase's parity alone, as on the
 device, so a phase that a warp misses, or asks for two phases early, shows as a wrong
 tile, an overwritten one or a run that does not end."""
@@ -92,7 +92,7 @@ def run(seed, stages, units):
                 yield
 
     def converter(number):
-        nq = 0
+        nq = left = 0
         for at, (u, place, tile) in enumerate(places()):
             s, f = at % stages, at % STAGED
             yield from wait(staged_full[f], at // STAGED & 1)
@@ -105,13 +105,19 @@ def run(seed, stages, units):
             yield
             staged_empty[f].arrive()
             full[s].arrive()
-            if place == 1:
-                for t in range(2 if units[u][0] else 1):
-                    yield from wait(q_raw[nq & 1], nq // 2 & 1)
-                    assert q_tiles[nq & 1] == (u, t)
-                    q_full[nq & 1].arrive()  # (converted)
-                    nq += 1
-                    yield
+            left = (2 if units[u][0] else 1) if place == 0 else left
+            while left:
+                last = place == min(stages, 2 * units[u][1]) - 1
+                if not last and not q_raw[nq & 1].done(nq // 2 & 1):
+                    break
+                yield from wait(q_raw[nq & 1], nq // 2 & 1)
+                assert q_tiles[nq & 1] == (u, nq - first_tile(u))
+                q_full[nq & 1].arrive()  # (converted)
+                nq, left = nq + 1, left - 1
+                yield
+
+    def first_tile(u):
+        return sum(2 if pair else 1 for pair, _ in units[:u])
 
     def issuer():
         base = nq = 0
