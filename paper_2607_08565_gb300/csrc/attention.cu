@@ -886,67 +886,68 @@ __device__ __forceinline__ void write_tile(const AttentionArgs& a, Shared* sh, c
   const uint32_t o_all = sh->tmem + 2 * kTile + ((uint32_t)warp << 21);
   const int row_token = row / a.group, row_head = row - row_token * a.group;
   const bool two = !it.pair && it.te - it.tb > 1;  // sums of even and of odd key tiles
-        const int n_rows = tile_rows(a, it, tile);
-        mbar_wait(&b.stat_full[tile], items & 1, sh, a.status);
-        float2 st = sh->stat[tile][row];
-        float w1 = 1.f, w2 = 0.f;  // the even and the odd tiles' shares
-        if (!it.pair) {
-          mbar_wait(&b.stat_full[1], items & 1, sh, a.status);
-          const float2 odd = sh->stat[1][row];
-          const float both = fmaxf(st.x, odd.x);
-          if (both > -INFINITY) {
-            w1 = ex2(st.x - both);
-            w2 = ex2(odd.x - both);
-            st = make_float2(both, st.y * w1 + odd.y * w2);
-          }
-          if (two) mbar_wait(&b.o_full[1], no[1]++ & 1, sh, a.status);
-        }
-        mbar_wait(&b.o_full[tile], no[tile]++ & 1, sh, a.status);
-        if (32 * warp < n_rows) {
-          fence_after();
-          const bool mine = row < n_rows;
-          const int64_t token = it.unit.token + tile_token(a, it, tile) + row_token;
-          const int head = it.h * a.group + row_head;
-          float inv = it.whole ? (st.y > 0.f ? 1.f / st.y : st.y) : 1.f;  // (NaN stays)
-          if (kFour && it.whole) inv *= a.v_scale;
-          w1 *= inv, w2 *= inv;
-          const uint32_t o_at = o_all + tile * kTile;
-          T* out = static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride;
-          for (int d = 0; d < a.D; d += 16) {
-            uint32_t o[16];
-            float f[16];
-            tmem_ld16(o_at + d, o);
-            wait_ld(o);
-  #pragma unroll
-            for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(o[i]) * w1;
-            if (two) {
-              tmem_ld16(o_at + kTile + d, o);
-              wait_ld(o);
-  #pragma unroll
-              for (int i = 0; i < 16; ++i) f[i] += __uint_as_float(o[i]) * w2;
-            }
-            if (mine) {
-              if (it.whole) {
-                uint32_t y[8];
-  #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
-                store16(a, out + d, y);
-              } else {
-                float4* p = reinterpret_cast<float4*>(a.part) + part_at(a.D, it.slot, tile, d / 4) + row;
-  #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  p[i * kTile] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-              }
-            }
-          }
-          fence_before();
-          if (mine) {
-            if (!it.whole)
-              a.part_ml[(int64_t)it.slot * 2 * kTile + tile * kTile + row] = st;
-            else if (a.lse)
-              a.lse[token * a.hq + head] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * 0.6931471805599453f;
-          }
-        }
+  const int n_rows = tile_rows(a, it, tile);
+  mbar_wait(&b.stat_full[tile], items & 1, sh, a.status);
+  float2 st = sh->stat[tile][row];
+  float w1 = 1.f, w2 = 0.f;  // the even and the odd tiles' shares
+  if (!it.pair) {
+    mbar_wait(&b.stat_full[1], items & 1, sh, a.status);
+    const float2 odd = sh->stat[1][row];
+    const float both = fmaxf(st.x, odd.x);
+    if (both > -INFINITY) {
+      w1 = ex2(st.x - both);
+      w2 = ex2(odd.x - both);
+      st = make_float2(both, st.y * w1 + odd.y * w2);
+    }
+    if (two) mbar_wait(&b.o_full[1], no[1]++ & 1, sh, a.status);
+  }
+  mbar_wait(&b.o_full[tile], no[tile]++ & 1, sh, a.status);
+  if (32 * warp < n_rows) {
+    fence_after();
+    const bool mine = row < n_rows;
+    const int64_t token = it.unit.token + tile_token(a, it, tile) + row_token;
+    const int head = it.h * a.group + row_head;
+    float inv = it.whole ? (st.y > 0.f ? 1.f / st.y : st.y) : 1.f;  // (NaN stays)
+    if (kFour && it.whole) inv *= a.v_scale;
+    w1 *= inv, w2 *= inv;
+    const uint32_t o_at = o_all + tile * kTile;
+    T* out = static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride;
+    const auto store = [&](int d, const float (&f)[16]) {
+      if (!mine) return;
+      if (it.whole) {
+        uint32_t y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
+        store16(a, out + d, y);
+      } else {
+        float4* p = reinterpret_cast<float4*>(a.part) + part_at(a.D, it.slot, tile, d / 4) + row;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i * kTile] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+      }
+    };
+    for (int d = 0; d < a.D; d += 16) {
+      uint32_t o[16];
+      float f[16];
+      tmem_ld16(o_at + d, o);
+      wait_ld(o);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(o[i]) * w1;
+      if (two) {
+        tmem_ld16(o_at + kTile + d, o);
+        wait_ld(o);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f[i] += __uint_as_float(o[i]) * w2;
+      }
+      store(d, f);
+    }
+    fence_before();
+    if (mine) {
+      if (!it.whole)
+        a.part_ml[(int64_t)it.slot * 2 * kTile + tile * kTile + row] = st;
+      else if (a.lse)
+        a.lse[token * a.hq + head] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * 0.6931471805599453f;
+    }
+  }
   __syncwarp();
   if (lane == 0) {
     mbar_arrive(&b.o_free[tile]);

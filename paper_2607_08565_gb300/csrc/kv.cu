@@ -838,9 +838,20 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
   s.up_to = INT32_MAX;
   s.per = 2 * kv->tile_tokens, s.one = kv->tile_tokens;
   s.tile = kTile, s.heads = kv->cfg.num_kv_heads;
-  s.tile_cost[0] = 2, s.tile_cost[1] = 3;
-  s.once_cost[0] = 4, s.once_cost[1] = 6;
-  s.min_cost = kMinCost, s.min_tiles = kMinTiles;
+  if (!four_bits(kv)) {
+    s.tile_cost[0] = 2, s.tile_cost[1] = 3;
+    s.once_cost[0] = 4, s.once_cost[1] = 6;
+    s.min_cost = kMinCost, s.min_tiles = kMinTiles;
+  } else {
+    // In 500 cycles: a key tile takes 2,400 and 3,400, and a unit's ends, where its
+    // queries are converted and the softmax's warps write its output, 10,000 to 20,000.
+    // (With the costs of 16-bit caches chunks of 128 to 1,024 tokens on prefixes of 2k
+    // to 24k took 494 us instead of 434, two prompts of 7,600 tokens 788 instead of 700,
+    // chunks of up to 700 in a window 215 instead of 222.)
+    s.tile_cost[0] = 5, s.tile_cost[1] = 7;
+    s.once_cost[0] = 40, s.once_cost[1] = 34;
+    s.min_cost = 20, s.min_tiles = kMinTiles;
+  }
   if (f.rows) {
     PlanSet& w = a.set[1];
     w.units = f.units;
@@ -853,8 +864,11 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
     w.up_to = all_few ? INT32_MAX : f.tokens;
     w.per = w.one = f.tokens;
     w.tile = kFewTile, w.heads = f.blocks;
+    // In tiles of one key head: a unit's ends (pages and queries on their way, the joined
+    // sums) take as long as 48. (64 single tokens over 2k to 48k keys: 175 us with 16, 172
+    // with 32, 170 with 48 to 96; 19 over up to 900: 11.7, 10.4, 11.2 to 12.1.)
     w.tile_cost[0] = w.tile_cost[1] = f.heads;
-    w.once_cost[0] = w.once_cost[1] = 16;
+    w.once_cost[0] = w.once_cost[1] = 48;
     w.min_cost = 16, w.min_tiles = 1;
   }
   a.status = kv->status;
