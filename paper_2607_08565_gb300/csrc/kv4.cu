@@ -301,7 +301,7 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
   return r;
 }
 // N bytes; zeros where !held.
