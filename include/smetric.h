@@ -654,8 +654,9 @@ typedef struct {
 /* Create a handle and its device memory on the current device: the plan (16
  * bytes a token, and 40 for every 2 * (128 / group) of them, group =
  * num_q_heads / num_kv_heads; 44 bytes a request) and the partial results of
- * sequences that several SMs share (4 * 128 * (head_dim + 2) floats an SM).
- * Errors as smetric_index_create. */
+ * sequences that several SMs share (4 * 128 * (head_dim + 2) floats an SM; with
+ * caches in 4 bits another 2 * 12 * 16 * (head_dim + 2) at most, and 84 bytes a
+ * request). Errors as smetric_index_create. */
 int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out);
 
 /* Free the handle and its device memory. Waits for the device first.
@@ -717,7 +718,9 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
  * 448), and a code the e2m1 number nearest to y / s (at most 6 in magnitude;
  * where s is 0 the codes are), halves to even in both. So elements up to 2,688 *
  * 2^exp are held to within a sixth of their group's largest. A NaN makes its 16
- * elements NaN; an infinite one is held as 2,688 * 2^exp. */
+ * elements NaN; an infinite one is held as 2,688 * 2^exp. (A 32-bit value within 2^-20
+ * of its size of the border between two numbers may go to either.) Two tokens with one
+ * slot may leave a mixture of both. */
 int smetric_kvq_append(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cache v_cache, smetric_heads k,
                        smetric_heads v, smetric_heads q, smetric_heads q_out, smetric_kv_transform t,
                        smetric_stream_t stream);

@@ -10,10 +10,14 @@
 //   k_kv_heads     one pass over the new tokens' heads: queries and keys are
 //                  normed and rotated in registers, keys and values go to
 //                  their slots (or, for the transform alone, to rows). Bound by
-//                  memory: 35,862 tokens of 32 + 2 x 4 heads of 128 (753 MB) 127
-//                  us, 87 % of a copy; 16,001 of 64 + 4 (565 MB) 95 us; 86,444 of
-//                  2 x 8 of 64 (366 MB) 70 us, 77 %, as a warp has 2 KB to copy
+//                  memory: 35,862 tokens of 32 + 2 x 4 heads of 128 (753 MB) 122
+//                  us, 92 % of a copy; 16,001 of 64 + 4 (565 MB) 93 us; 86,444 of
+//                  2 x 8 of 64 (366 MB) 63 us, 87 %, as a warp has 2 KB to copy
 //                  and two dependent reads to make first. Few tokens: 2 us.
+//                  Into 4 bits: the same tokens (680 MB with the queries, 240 MB) 119
+//                  and 71 us, bound by issue slots (60 %) as much as by memory: a group's
+//                  largest, its scale and its codes are some 120 instructions for 16
+//                  elements of a lane.
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

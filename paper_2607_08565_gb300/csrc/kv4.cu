@@ -1,7 +1,15 @@
-// The paged KV$ operators over caches in 4 bits: reading back, and attention.
+// The paged KV$ operators over caches in 4 bits: reading back, and the attention of
+// requests with few query rows (single tokens; others are attention.cu's). Appending
+// is kv.cu's.
 //
-//   k_kv4_read       rows of positions in 16 bits.
-//   k_kv4_attention  a warp for each query row.
+//   k_kv4_read      rows of positions in 16 bits.
+//   k_kv4_few       one CTA an SM, each with the share of the batch that the plan gave
+//                   it.
+//   k_kv4_few_join  joins the pieces of the units that several CTAs share.
+//
+// An element is code * scale * 2^exp: 4 bits (e2m1) and, for 16 of them, 8 (e4m3). Code
+// times scale has 6 bits and lies within 2^-10 .. 2,688: exact in half precision, in
+// which the products are. The exponents go into the scores' factor and the output's.
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -88,8 +96,10 @@ constexpr int kReadRows = 32;  // of a block, at most
 
 // A block takes some rows: a thread each finds where they are, then all copy, 16
 // elements (a group, whole sectors of the output) a thread at a time; a thread has the
-// same group of the same head for every row that it takes. Bound by memory: the output
-// is 3.6 times the input.
+// same group of the same head for every row that it takes, four rows on their way.
+// Bound by memory (the output is 3.6 times the input): 148,000 rows of 2 x 4 heads of 128,
+// 474 MB, take 77 us, 92 % of a copy. With a row and a column found by divisions for every
+// 16 elements 87 us, at 268 instructions for each; blocks of 16 and 64 rows 79 and 80 us.
 template <typename T>
 __global__ void __launch_bounds__(kReadThreads) k_kv4_read(const __grid_constant__ ReadArgs a) {
   __shared__ int64_t codes_at[kReadRows][2], scales_at[kReadRows][2];  // -1: left as it is, -2: zeros
@@ -201,6 +211,7 @@ struct FewArgs {
   int32_t* status;
 };
 
+// (as the attention of 16-bit caches has them in half precision)
 constexpr float kLift = 7.f;   // weights up to 2^(kLift + kSlack): half precision ends at 65,504
 constexpr float kSlack = 8.f;  // log2 of how far scores may pass the reference
 
@@ -378,14 +389,30 @@ __device__ __forceinline__ void write_row(const FewArgs& a, const KvUnit& u, int
 
 // Attention of up to NB * 8 query rows (a token's heads of one key head, or a few
 // tokens') at a time. Every warp has a key head and every `streams`-th tile of 32
-// keys of the CTA's share, and joins its sums with the head's other warps' at the
-// item's end.
+// keys of the CTA's share, copies it for itself into a ring of its own (no barriers
+// between warps), and joins its sums with the head's other warps' at the item's end.
+// All key heads of a tile are read by one CTA at about the same time: a token's scales
+// are 8 bytes a head, a quarter of what memory delivers.
 //
 // Tokens are the long side of both products: S^T = K Q^T and O^T = V^T P^T, in
-// mma.sync of 16 x 8 x 16, so that a code goes from the cache to a register of the
-// operand with one conversion (two codes) and one product with its scale, both
-// exact in half precision (2 and 4 bits). P^T is S^T's registers after a transposition
-// of 8 x 8 blocks.
+// mma.sync of 16 x 8 x 16, so that a code goes from shared memory to a register of the
+// operand with one conversion (two codes) and one product with its scale. P^T is S^T's
+// registers after a transposition of 8 x 8 blocks. (tcgen05 takes its operands from
+// shared memory or TMEM: the same conversions, and a way there and back. At 8 rows the
+// products need a third of mma.sync's rate, 1,012 multiply-adds a cycle and SM.)
+//
+// What bounds it: 32 keys of a head are 4.6 KB, 200 cycles of an SM's share of memory,
+// and 555 instructions, 139 cycles of issue slots; conversions and their products take
+// half of theirs (64 lanes a cycle each). Both together come to 234 cycles, at 56 % of
+// the issue slots: 64 single tokens over 2k to 48k keys (4 key heads of 128, 896 MB) take
+// 170 us, 5.3 TB/s, 79 % of a copy's rate, where the copies alone take 148 and the
+// arithmetic alone 137, and 12 of them are the start, the item's end and the join. 37
+// tokens of 16 rows (347 MB) take 98 us, with twice the products. One token over 24,577
+// keys takes 12.4 us on the device: share, pages and first tile 3.5, tiles 2, the
+// item's end 2, the join 3, launches.
+//
+// 12 warps of 168 registers: 16 of 128 took 178 us for the 64 tokens, 20 of 96 239, 8 of
+// 255 205. The next tile's scores computed beside this tile's weights took 186.
 template <int D, int NB>
 __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __grid_constant__ FewArgs a) {
   constexpr int kWarps = few_heads(8 * NB), kRows = 8 * NB, kStages = stages(D, kRows), kStage = stage_bytes(D);
@@ -792,7 +819,7 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 // out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i over a unit's pieces, the
 // pieces in an order that depends on their number alone. The blocks in turn for the
 // units that are shared. A row of few pieces has a warp, one of many (a long sequence
-// alone) a block.
+// alone) a block. Bound by latency: 3 to 5 us.
 constexpr int kFewJoin = 512;
 constexpr int kFewPieces = 8;
 
