@@ -15,7 +15,7 @@
 //                  2 x 8 of 64 (366 MB) 63 us, 87 %, as a warp has 2 KB to copy
 //                  and two dependent reads to make first. Few tokens: 2 us.
 //                  Into 4 bits: the same tokens (680 MB with the queries, 240 MB) 119
-//                  and 71 us, bound by issue slots (60 %) as much as by memory: a group's
+//                  and 68 us, bound by issue slots (60 %) as much as by memory: a group's
 //                  largest, its scale and its codes are some 120 instructions for 16
 //                  elements of a lane.
 
@@ -293,6 +293,11 @@ __device__ __forceinline__ uint4 pack(const float* f) {
                     Pair<T>::put(f[6], f[7]));
 }
 
+// 2^-exp, and a sixth of it.
+struct Exponent {
+  float down, sixth;
+};
+
 // Rounds of heads; of a share, `each`, and one more of the first `rest` shares.
 struct Rounds {
   int32_t all, each, rest;
@@ -303,7 +308,7 @@ struct HeadsArgs {
   int32_t hq, hk, hv;
   smetric_kv_cache cache;    // keys and values go here when tokens is not NULL
   smetric_kvq_cache k4, v4;  // or here
-  float k_down, v_down;      // 2^-exp
+  Exponent k_exponent, v_exponent;
   const KvToken* tokens;     // the plan's, or NULL: d_positions and k_out
   const KvPlan* plan;
   const int32_t* positions;
@@ -433,16 +438,16 @@ __device__ __forceinline__ float max_nan(float x, float y, float z) {
 // scale is 0 or NaN). The sixth is a product, at most 1.25 units in the last place off:
 // rounded to multiples of 4 of them it is the quotient where that is halfway between
 // two scales (5 bits), and no other quotient of a 16-bit number comes that near.
-__device__ __forceinline__ uint32_t scale_of(float top, float down, float& inv) {
+__device__ __forceinline__ uint32_t scale_of(float top, const Exponent& e, float& inv) {
   // (a NaN of all ones would become -0)
-  const float sixth = __uint_as_float((min(__float_as_uint(top * down * 0.16666667f), 0x7fc00000u) + 2) & ~3u);
+  const float sixth = __uint_as_float((min(__float_as_uint(top * e.sixth), 0x7fc00000u) + 2) & ~3u);
   uint32_t bits, half;
   asm("{\n .reg .b16 b;\n cvt.rn.satfinite.e4m3x2.f32 b, %2, %2;\n cvt.u32.u16 %0, b;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
       : "=r"(bits), "=r"(half) : "f"(sixth));
   const float s = __half2float(__ushort_as_half((unsigned short)half));
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(s));
-  inv = s > 0.f ? down * r : 0.f;
+  inv = s > 0.f ? e.down * r : 0.f;
   return bits & 0xff;
 }
 
@@ -457,12 +462,13 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
 // 8 codes. The reciprocal is within 2^-23 of itself, so that a product of 5 (the last
 // number halfway between two codes) at most is less than 2^-20 from the quotient, and
 // quotients of 16-bit numbers that are not halfway are at least 2^-13 from there: adding
-// and subtracting 24 leaves multiples of 2^-19, so that what is halfway is seen so.
+// 24 (with the product, in one rounding) and subtracting it leaves multiples of 2^-19, so
+// that what is halfway is seen so.
 __device__ __forceinline__ uint32_t codes_of(const float2* f, float inv) {
   uint32_t r;
   float2 y[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) y[k] = add2(add2(mul2(f[k], make_float2(inv, inv)), make_float2(24.f, 24.f)), make_float2(-24.f, -24.f));
+  for (int k = 0; k < 4; ++k) y[k] = add2(fma2(f[k], make_float2(inv, inv), make_float2(24.f, 24.f)), make_float2(-24.f, -24.f));
   asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
       " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}\n"
       : "=r"(r) : "f"(y[0].x), "f"(y[0].y), "f"(y[1].x), "f"(y[1].y), "f"(y[2].x), "f"(y[2].y), "f"(y[3].x), "f"(y[3].y));
@@ -474,7 +480,7 @@ struct Codes {
   uint8_t* codes;
   uint8_t* scales;
   int64_t step, scale_step;  // between its heads
-  float down;                // 2^-exp
+  Exponent exponent;
 };
 
 // transform_heads into 4 bits. A group of 16 elements is two pieces of 8, which
@@ -496,8 +502,10 @@ __device__ __forceinline__ void quantise_heads(const Lane& l, const T* src, int6
   for (int r = 0; r < rounds; ++r, h += step, dst.codes += dst.step, dst.scales += dst.scale_step) {
     const bool on = l.held && h < heads;
     const uint4 y[2] = {x[0], x[1]};
-    src += src_step;
-    load_head(l, src, h + step, heads, x);
+    if (r + 1 < rounds) {  // (often there is one round)
+      src += src_step;
+      load_head(l, src, h + step, heads, x);
+    }
     float2 f[8];
     transform_lane<T, kInterleaved, true>(l, y, on, norm, f);
     float m[2];
@@ -519,13 +527,13 @@ __device__ __forceinline__ void quantise_heads(const Lane& l, const T* src, int6
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         float inv;
-        const uint32_t scale = scale_of(top[i], dst.down, inv);
+        const uint32_t scale = scale_of(top[i], dst.exponent, inv);
         reinterpret_cast<uint32_t*>(dst.codes)[p[i]] = codes_of(f + 4 * i, inv);
         if (!(p[i] & 1)) dst.scales[p[i] >> 1] = (uint8_t)scale;
       }
     } else if (on) {
       float inv;
-      const uint32_t scale = scale_of(max_nan(m[0], m[1], 0.f), dst.down, inv);
+      const uint32_t scale = scale_of(max_nan(m[0], m[1], 0.f), dst.exponent, inv);
       *reinterpret_cast<uint2*>(dst.codes + 4 * p[0]) = make_uint2(codes_of(f, inv), codes_of(f + 4, inv));
       dst.scales[p[0] >> 1] = (uint8_t)scale;
     }
@@ -538,7 +546,7 @@ __device__ __forceinline__ void quantise_heads(const Lane& l, const T* src, int6
 // pairs, or 16 elements past rot. So a rotation never leaves the lane, a norm
 // is a sum over the group's lanes, and the token's cosines and sines are
 // loaded once for all its heads. Bound by memory; the registers of 28 warps an
-// SM hold the bytes in flight: 72 a thread, with 44 to 60 bytes spilled (24 warps
+// SM hold the bytes in flight: 72 a thread, with 28 to 40 bytes spilled (24 warps
 // of 80 took 101 us for 16,001 tokens of 64 + 4 heads, where these take 96).
 template <typename T, bool kInterleaved, bool kFour>
 __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ HeadsArgs a) {
@@ -611,7 +619,7 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   };
   if constexpr (kFour) {
     const uint32_t page = (uint32_t)(slot >> a.page_shift), in = (uint32_t)slot & ((1 << a.page_shift) - 1);
-    const auto quantise = [&](const Lane& ln, const smetric_heads& src, const smetric_kvq_cache& c4, float down, int r,
+    const auto quantise = [&](const Lane& ln, const smetric_heads& src, const smetric_kvq_cache& c4, const Exponent& exponent, int r,
                               const Rounds& rounds, int n_heads, const void* norm, int R, uint4(&z)[2]) {
       if (r >= rounds.all) return;
       // (page and token strides are below 2^32)
@@ -623,13 +631,13 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
                   head * c4.scale_head_stride;
       to.step = step * c4.head_stride;
       to.scale_step = step * c4.scale_head_stride;
-      to.down = down;
+      to.exponent = exponent;
       quantise_heads<T, kInterleaved>(ln, source(src, r), step * src.head_stride, to, head, step, n_heads,
                                       rounds.each + (r < rounds.rest), static_cast<const T*>(norm), R, z);
     };
-    quantise(plain, a.v, a.v4, a.v_down, v0, a.rounds_v, a.hv, nullptr, 0, y);
+    quantise(plain, a.v, a.v4, a.v_exponent, v0, a.rounds_v, a.hv, nullptr, 0, y);
     if (q0 < rq) load_head(l, source(a.q, q0), q0 * per + first, a.hq, y);
-    quantise(l, a.k, a.k4, a.k_down, k0, a.rounds_k, a.hk, a.k_norm, !kInterleaved && a.table ? a.rot / 16 : 0, x);
+    quantise(l, a.k, a.k4, a.k_exponent, k0, a.rounds_k, a.hk, a.k_norm, !kInterleaved && a.table ? a.rot / 16 : 0, x);
     heads(a.q, static_cast<T*>(a.q_out.d_data) + t * a.q_out.token_stride, a.q_out.head_stride, q0, a.rounds_q, a.hq, a.q_norm, y);
     return;
   }
@@ -932,8 +940,9 @@ int smetric_kvq_append(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_ca
   a.hq = q.d_data ? kv->cfg.num_q_heads : 0;
   a.k4 = k_cache;
   a.v4 = v_cache;
-  a.k_down = std::ldexp(1.f, -k_cache.exp);
-  a.v_down = std::ldexp(1.f, -v_cache.exp);
+  const auto exponent = [](int32_t e) { return Exponent{std::ldexp(1.f, -e), std::ldexp(0.16666667f, -e)}; };
+  a.k_exponent = exponent(k_cache.exp);
+  a.v_exponent = exponent(v_cache.exp);
   a.tokens = kv->tokens;
   a.plan = kv->plan;
   a.n_tokens = kv->n_tokens;
