@@ -598,7 +598,7 @@ __device__ __forceinline__ void convert_row(SharedFour* sh, uint32_t nq, uint32_
     for (int i = 0; i < 4; ++i) top = __vmaxu2(top, x[i] & 0x7fff7fffu);
   }
   const uint32_t most = max(top >> 16, top & 0xffff) >> 7;
-  const uint32_t E = most == 0 ? 1 : most >= 254 ? 127 : most;  // (infinities keep their row as it is)
+  const uint32_t E = most == 0 ? 1 : most == 255 ? 127 : min(most, 253);  // (infinities keep their row as it is)
   const float down = __uint_as_float((254 - E) << 23);
   sh->power[nq & 3][row] = (uint8_t)E;
 #pragma unroll 4

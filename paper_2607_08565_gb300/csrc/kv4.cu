@@ -360,9 +360,9 @@ __device__ __forceinline__ void convert_rows(const uint4 (&x)[D / 32], bool bf16
   for (int i = 0; i < D / 4; ++i) top = fmaxf(top, fabsf(f[i]));
   top = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
   top = fmaxf(top, __shfl_xor_sync(kFull, top, 2));
-  // 2^(E - 127) <= top; infinities keep their row as it is
+  // 2^(E - 127) <= top, its reciprocal a number; infinities keep their row as it is
   uint32_t E = __float_as_uint(top) >> 23;
-  E = E == 0 ? 1 : E >= 254 ? 127 : E;
+  E = E == 255 ? 127 : min(max(E, 1u), 253u);
   const float down = __uint_as_float((254 - E) << 23);
   power = __uint_as_float(E << 23);
 #pragma unroll

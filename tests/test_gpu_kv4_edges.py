@@ -72,6 +72,30 @@ def test_queries_of_any_size(new, lens, power):
     check(b)
 
 
+@pytest.mark.parametrize("new,lens", [([1, 1], [3000, 70]), ([200, 3], [900, 70])])
+def test_queries_up_to_the_largest(new, lens):
+    """Rows whose largest elements are in the type's last power of two. (None so small that half precision
+    would round it: the same outputs, bit for bit, as of the rows divided by 2^126.)"""
+    b = Batch4(new, lens, 16, 2, 128, 32).fill()
+    b.q = b.q.clamp(-3.5, 3.5) * (b.q.abs() > 2.0 ** -8)
+    b.q[:, :, 5] = 3.0
+    kv = b.handle()
+    good, good_lse = kv.paged_attention(b.q, *b.caches, scale=1.0, want_lse=True)
+    kv.check()
+    # Scores of up to 40: their errors of (d + 2) 2^-24 each are within 2^-11 of a weight; weights below 2^-21 of the
+    # largest are off by up to 2^-32 of it (half precision's smallest step), each with its value.
+    want, want_lse, mag = b.attend64(1.0)
+    values = torch.stack([b.values[r].abs().sum(0) for r in range(b.n) for _ in range(b.new[r])]).repeat_interleave(8, 1)
+    off = (good.double() - want).abs() - (2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -11) * mag + 2.0 ** -32 * values)
+    assert bool((off <= 0).all()) and bool(((good_lse.double() - want_lse).abs() <= 2.0 ** -11).all())
+    big = b.q * 2.0 ** 126
+    assert bool((big.abs().amax(-1) >= 2.0 ** 127).all()) and bool(big.isfinite().all())
+    out, lse = kv.paged_attention(big, *b.caches, scale=2.0 ** -126, want_lse=True)
+    kv.check()
+    kv.close()
+    assert torch.equal(out, good) and torch.equal(lse, good_lse)
+
+
 @pytest.mark.parametrize("window", [100, 400])
 @pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("new", [1, 3, 40])
