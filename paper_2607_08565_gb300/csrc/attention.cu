@@ -1006,8 +1006,9 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
     for (int j = it.pair ? 0 : tile; j < n; j += it.pair ? 1 : 2) {
       mbar_wait(&b.s_full[tile], ns++ & 1, sh, a.status);
       if (kPowers && j <= tile)
-        c = a.scale * 1.4426950408889634f *
-            __uint_as_float((uint32_t) * (volatile uint8_t*)&static_cast<SharedFour*>(sh)->power[(nq + (it.pair ? tile : 0)) & 3][row] << 23);
+        c = score_factor(
+            a.scale * 1.4426950408889634f *
+            __uint_as_float((uint32_t) * (volatile uint8_t*)&static_cast<SharedFour*>(sh)->power[(nq + (it.pair ? tile : 0)) & 3][row] << 23));
       if (!busy) {
         __syncwarp();
         if (lane == 0) mbar_arrive(&b.p_full[tile]);

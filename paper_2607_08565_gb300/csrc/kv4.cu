@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
         float power;
         convert_rows<D>(queries[b], a.bf16, qf[b], power);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) cs[b][i] = __shfl_sync(kFull, power, 4 * (2 * c + i)) * a.scale;
+        for (int i = 0; i < 2; ++i) cs[b][i] = score_factor(__shfl_sync(kFull, power, 4 * (2 * c + i)) * a.scale);
       }
       uint32_t at = warp * kStages * kStage;  // in smem
       uint32_t key = key0;

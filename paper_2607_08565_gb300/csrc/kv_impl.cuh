@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cfloat>
 
 #include "smetric_impl.cuh"
 
@@ -124,6 +125,11 @@ inline bool cache_ok(const smetric_kv_cache& c) {
          c.page_stride >= 0 && c.token_stride >= 0 && c.head_stride >= 0 && c.page_stride % 8 == 0 &&
          c.token_stride % 8 == 0 && c.head_stride % 8 == 0;
 }
+// What scores are multiplied by, of a row that was divided by a power of two: a normal
+// number, as 0 times the -inf of a key that is not seen is NaN, and infinity times the
+// score 0 is. (A row of zeros has the power 2^-126. Scores are below 2^23 before, so that
+// those below 2^-103 after it may be any so small.)
+__device__ __forceinline__ float score_factor(float c) { return fminf(fmaxf(c, FLT_MIN), FLT_MAX); }
 // Bytes of a head's scales: head_dim / 16, to a whole load.
 __host__ __device__ constexpr int scale_bytes(int head_dim) { return head_dim <= 64 ? 4 : 8; }
 inline bool cache4_ok(const smetric_kvq_cache& c, int head_dim) {
