@@ -65,7 +65,7 @@ enum {
   SMETRIC_ERR_OOM = -2,         /* device allocation failed at create */
   SMETRIC_ERR_TABLE_FULL = -3,  /* an insert found no free slot */
   SMETRIC_ERR_CUDA = -4,        /* a CUDA runtime call failed */
-  SMETRIC_ERR_OVERFLOW = -5,    /* a load or prompt length outside the exact int64 range */
+  SMETRIC_ERR_OVERFLOW = -5,    /* a load or prompt length outside the exact int64 range, a position or a score out of range */
   SMETRIC_ERR_TOO_LARGE = -6    /* batch larger than smetric_block_hashes_noalloc's fixed scratch */
 };
 
@@ -708,7 +708,8 @@ int smetric_qk_norm_rope(smetric_kv* kv, smetric_heads q, smetric_heads k, const
  * lse = -inf. scale is finite and > 0. d_lse: NULL or float [n_tokens,
  * num_q_heads]. out must not overlap q. Values at masked positions of a
  * request's own length must be finite; what lies past its length or before
- * its window may be anything. */
+ * its window may be anything. A row whose largest score is 2^27 or more in
+ * magnitude (2^29 in bf16) may latch OVERFLOW; its output is not defined then. */
 int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_heads q, float scale, smetric_heads out,
                             float* d_lse, smetric_stream_t stream);
 
@@ -743,8 +744,9 @@ int smetric_kvq_read(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cach
  * whatever the handle's dtype: queries are divided by a power of two for each row,
  * and the softmax's weights are rounded to half precision (to within 2^-32 of the
  * row's largest where they are below 2^-21 of it). scale * 2^exp of the keys is finite
- * and > 0. Scales at masked positions of a request's own length must not be
- * NaN; what lies past its length or before its window may be anything. */
+ * and > 0; scores of 2^27 and more may latch OVERFLOW. Scales at masked positions
+ * of a request's own length must not be NaN; what lies past its length or before its
+ * window may be anything. */
 int smetric_kvq_attention(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cache v_cache, smetric_heads q,
                           float scale, smetric_heads out, float* d_lse, smetric_stream_t stream);
 

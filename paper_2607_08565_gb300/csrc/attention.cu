@@ -9,7 +9,9 @@
 // cores (tcgen05, sums in TMEM), P = exp2(c S - ref) in between, c = scale *
 // log2(e). ref is the row's reference exponent: its largest c S when it was
 // last moved. It moves only when a score exceeds it by 2^kSlack, since a common
-// factor of P and its sum l cancels in O / l: so O is seldom rescaled.
+// factor of P and its sum l cancels in O / l: so O is seldom rescaled. (Of scores past 2^27,
+// 2^29 where P is in bf16, ref's rounding alone takes P out of its type's range: the
+// error is latched.)
 //
 // Two query tiles are in flight, so that one's softmax runs while the tensor
 // cores work on the other: a unit of more than 128 rows has its two halves
@@ -1043,7 +1045,7 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
       if (__any_sync(kFull, move)) {
         float back = 1.f;
         if (move) {
-          const float next = most * c - Type<T>::kLift;
+          const float next = reference(most, c, Type<T>::kLift);
           back = top == -INFINITY ? 0.f : ex2(ref - next);
           top = most;
           ref = next;
@@ -1081,6 +1083,7 @@ __device__ __forceinline__ void softmax(const AttentionArgs& a, Shared* sh, Walk
       const float2 all = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
       l += all.x + all.y;
     }
+    if (mine && too_far(ref, Type<T>::kLift)) latch_error(a.status, SMETRIC_ERR_OVERFLOW);
     nq += it.pair ? 2 : 1;
     if (items) mbar_wait(&b.o_free[tile], (items - 1) & 1, sh, a.status);
     // (scores that are all NaN leave top where it was, but not l: the row is not

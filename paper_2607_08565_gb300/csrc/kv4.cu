@@ -687,8 +687,8 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 #pragma unroll
               for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, x));
               if (top > lim[b][i]) {
-                const float to = top * cs[b][i] - kLift, back = lim[b][i] == -INFINITY ? 0.f : ex2(ref[b][i] - to);
-                ref[b][i] = to, lim[b][i] = top + kSlack / cs[b][i];
+                const float to = reference(top, cs[b][i], kLift), back = lim[b][i] == -INFINITY ? 0.f : ex2(ref[b][i] - to);
+                ref[b][i] = to, lim[b][i] = __fadd_rd(top, kSlack / cs[b][i]);
                 l[b][i] *= back;
 #pragma unroll
                 for (int m = 0; m < D / 16; ++m) o[m][b][i] *= back, o[m][b][i + 2] *= back;
@@ -782,6 +782,7 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
 #pragma unroll
           for (int m = 0; m < D / 16; ++m)  // (elements g D/8 + 2m, + 1)
             *reinterpret_cast<float2*>(sums + row * sum_row(D) + 16 * m + 2 * g) = make_float2(o[m][b][i], o[m][b][i + 2]);
+          if (g == 0 && 8 * b + 2 * c + i < u.tokens * a.group && too_far(ref[b][i], kLift)) latch_error(a.status, SMETRIC_ERR_OVERFLOW);
           if (g == 0) stats[row] = make_float2(lim[b][i] == -INFINITY && l[b][i] == 0.f ? -INFINITY : ref[b][i], l[b][i]);
         }
     }

@@ -130,6 +130,14 @@ inline bool cache_ok(const smetric_kv_cache& c) {
 // score 0 is. (A row of zeros has the power 2^-126. Scores are below 2^23 before, so that
 // those below 2^-103 after it may be any so small.)
 __device__ __forceinline__ float score_factor(float c) { return fminf(fmaxf(c, FLT_MIN), FLT_MAX); }
+// A reference exponent, score * factor - lift rounded up, so that no weight passes
+// 2^(lift + slack): weights are of exactly this reference, and the largest one's is
+// 2^lift / 2^ulp(reference) or more. That is a number above 0 of the weights' type while
+// the reference is below 2^28 (half precision, a lift of 7) or 2^30 (bf16, none).
+__device__ __forceinline__ float reference(float score, float factor, float lift) { return __fmaf_ru(score, factor, -lift); }
+__device__ __forceinline__ bool too_far(float reference, float lift) {
+  return fabsf(reference) >= (lift > 0.f ? 0x1p28f : 0x1p30f) && fabsf(reference) < INFINITY;
+}
 // Bytes of a head's scales: head_dim / 16, to a whole load.
 __host__ __device__ constexpr int scale_bytes(int head_dim) { return head_dim <= 64 ? 4 : 8; }
 inline bool cache4_ok(const smetric_kvq_cache& c, int head_dim) {
