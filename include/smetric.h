@@ -741,12 +741,14 @@ int smetric_kvq_read(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cach
 
 /* smetric_paged_attention over caches in 4 bits, as the numbers that they stand
  * for. Codes times scales are exact in half precision, which the products take
- * whatever the handle's dtype: queries are divided by a power of two for each row,
- * and the softmax's weights are rounded to half precision (to within 2^-32 of the
- * row's largest where they are below 2^-21 of it). scale * 2^exp of the keys is finite
- * and > 0; scores of 2^27 and more may latch OVERFLOW. Scales at masked positions
- * of a request's own length must not be NaN; what lies past its length or before its
- * window may be anything. */
+ * whatever the handle's dtype: queries in bf16 are divided by a power of two for each
+ * row, which is exact for elements of 2^-17 of the row's largest and more (smaller
+ * ones are rounded to multiples of up to 2^-24 of it), and the softmax's weights are
+ * rounded to half precision (to within 2^-32 of the row's largest where they are
+ * below 2^-21 of it). scale * 2^exp of the keys is finite and > 0; scores of
+ * 2^27 and more may latch OVERFLOW. Scales at masked positions of a request's own
+ * length must not be NaN; what lies past its length or before its window may be
+ * anything. */
 int smetric_kvq_attention(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cache v_cache, smetric_heads q,
                           float scale, smetric_heads out, float* d_lse, smetric_stream_t stream);
 

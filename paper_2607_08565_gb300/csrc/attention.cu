@@ -585,8 +585,8 @@ __device__ __forceinline__ void copy_scales(const AttentionArgs& a, SharedFour* 
 }
 
 // A row (the thread's) of query tile number nq from bf16 to half precision, in its
-// place: divided by the power of two of its largest element, so that its 8 bits fit;
-// what is lost below 2^-24 of the largest is lost to 32-bit sums too.
+// place: divided by the power of two of its largest element, so that 8 bits of elements
+// of 2^-17 of it and more fit; smaller ones are rounded to multiples of 2^-24 of it.
 template <int HALVES>
 __device__ __forceinline__ void convert_row(SharedFour* sh, uint32_t nq, uint32_t q_smem, int row) {
   const uint32_t at = q_smem + (nq & 1) * HALVES * kHalf + row * 128;

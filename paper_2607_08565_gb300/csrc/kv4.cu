@@ -329,9 +329,10 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool h
 }
 
 // Query rows n0 .. n0 + 7 of a key head as the products' B operand, and their powers of
-// 2. Lane (g, c) = (lane / 4, lane % 4) has row g's elements [c D/4, (c+1) D/4). A row
-// goes to half precision divided by the power of two of its largest element: 8 or 11
-// bits fit, and what is lost below 2^-24 of the largest is lost to 32-bit sums too.
+// 2. Lane (g, c) = (lane / 4, lane % 4) has row g's elements [c D/4, (c+1) D/4). A row in
+// bf16 goes to half precision divided by the power of two of its largest element: its 8
+// bits fit where an element is 2^-17 of the largest or more, and smaller ones are rounded
+// to multiples of 2^-24 of it. (Where the largest meets codes of 0 they can count.)
 template <int D>
 __device__ __forceinline__ void load_rows(const FewArgs& a, const KvUnit& u, int head, int n0, uint4 (&x)[D / 32]) {
   const int lane = threadIdx.x & 31, n = n0 + (lane >> 2);
@@ -360,9 +361,9 @@ __device__ __forceinline__ void convert_rows(const uint4 (&x)[D / 32], bool bf16
   for (int i = 0; i < D / 4; ++i) top = fmaxf(top, fabsf(f[i]));
   top = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
   top = fmaxf(top, __shfl_xor_sync(kFull, top, 2));
-  // 2^(E - 127) <= top, its reciprocal a number; infinities keep their row as it is
+  // 2^(E - 127) <= top, its reciprocal a number; infinities keep their row as it is, and half precision is it
   uint32_t E = __float_as_uint(top) >> 23;
-  E = E == 255 ? 127 : min(max(E, 1u), 253u);
+  E = !bf16 || E == 255 ? 127 : min(max(E, 1u), 253u);
   const float down = __uint_as_float((254 - E) << 23);
   power = __uint_as_float(E << 23);
 #pragma unroll

@@ -1,5 +1,6 @@
 """Query rows at the ends of their range over the 4-bit paged cache: zeros and the
-smallest numbers, with scales and exponents that leave next to nothing of a score."""
+smallest numbers, with scales and exponents that leave next to nothing of a score; and
+small elements beside a large one."""
 
 import pytest
 import torch
@@ -51,3 +52,17 @@ def test_rows_of_zeros_and_of_the_smallest_numbers(new, lens, hq, hk, d, dtype, 
     b.q = (b.q.double() * torch.tensor(sizes, dtype=torch.float64, device=DEV)[pick][..., None]).to(dtype)
     assert bool((b.q == 0).all(-1).any()) and bool(b.q.isfinite().all())
     check(b, scale)
+
+
+@pytest.mark.parametrize("new,lens,hq,hk,d", SHAPES)
+@pytest.mark.parametrize("lift", [12, 24])
+def test_small_elements_beside_a_large_one(new, lens, hq, hk, d, lift):
+    """Half-precision queries whose largest element meets zeros alone: the others make the scores, with all their bits."""
+    b = Batch4(new, lens, hq, hk, d, 16, HF)
+    for r in range(b.n):
+        b.held[0][r][0][..., 5] = 0
+        b.keys[r] = values64(*b.held[0][r])
+    b.fill()
+    b.q = (b.q.double() * 2.0 ** -lift * 2.0 ** 8).to(HF)
+    b.q[..., 5] = 2.0 ** 15
+    check(b, d ** -0.5 * 2.0 ** (lift - 8))
