@@ -1172,7 +1172,9 @@ class SMetricKV4(SMetricKV):
         r, in the handle's dtype. offsets int64 [n+1], first int32 [n], pages int32
         [n, max_pages] (row stride free). A cache may be None. Returns (k_out,
         v_out), new tensors [n_rows, num_kv_heads, head_dim] unless given; rows of
-        no request are not written."""
+        no request are not written. offsets, pages and first may be dropped after
+        the call, on another stream too; those that a captured call reads are the
+        graph's owner's to keep."""
         hk, here, dim = self.cfg.num_kv_heads, self._device, self._dim
         n = offsets.numel() - 1
         if offsets.dtype != self._i64 or offsets.dim() != 1 or n < 0 or not offsets.is_contiguous():
@@ -1207,4 +1209,7 @@ class SMetricKV4(SMetricKV):
                                           first.data_ptr() if first is not None and n else None,
                                           pages.data_ptr() if n and most else None, most, row_stride if n > 1 else most,
                                           kh, vh, raw), "smetric_kvq_read")
+        if other is not None:  # (torch may hand their memory out again only when that stream is done with them)
+            for x in (offsets, pages) if first is None else (offsets, pages, first):
+                x.record_stream(other)
         return k_out, v_out
