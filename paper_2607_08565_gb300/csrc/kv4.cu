@@ -92,7 +92,7 @@ struct ReadArgs {
 };
 
 constexpr int kReadThreads = 128;
-constexpr int kReadRows = 32;  // of a block, at most
+constexpr int kReadRows = 32;  // of a block, at most: a warp's lanes
 
 // A block takes some rows: a thread each finds where they are, then all copy, 16
 // elements (a group, whole sectors of the output) a thread at a time; a thread has the
@@ -132,6 +132,12 @@ __global__ void __launch_bounds__(kReadThreads) k_kv4_read(const __grid_constant
     for (int w = 0; w < 2; ++w) {
       codes_at[threadIdx.x][w] = in < 0 ? in : page * a.c[w].page_stride + in * a.c[w].token_stride;
       scales_at[threadIdx.x][w] = page * a.c[w].scale_page_stride + in * a.c[w].scale_token_stride;
+    }
+  } else if (threadIdx.x >= 32) {  // meanwhile: offsets that no row leads to
+    constexpr int kRest = kReadThreads - 32;
+    for (int64_t r = (int64_t)blockIdx.x * kRest + threadIdx.x - 32; r < a.n; r += (int64_t)gridDim.x * kRest) {
+      const int64_t begin = a.off[r], end = a.off[r + 1];
+      if (begin < 0 || end < begin || end > a.n_rows) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
     }
   }
   __syncthreads();
