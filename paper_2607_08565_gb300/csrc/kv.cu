@@ -358,8 +358,9 @@ __device__ __forceinline__ void load_head(const Lane& l, const T* src, int h, in
   }
 }
 
-// A lane's norm and rotation, from its two pieces y to 16 elements f.
-template <typename T, bool kInterleaved, bool kFour>
+// A lane's norm and rotation, from its two pieces y to 16 elements f, which become codes
+// (kCodes) or are rounded to T.
+template <typename T, bool kInterleaved, bool kCodes>
 __device__ __forceinline__ void transform_lane(const Lane& l, const uint4 (&y)[2], bool on, const T* norm, float2 (&f)[8]) {
 #pragma unroll
   for (int e = 0; e < 2; ++e) unpack<T>(y[e], &f[4 * e].x);
@@ -370,8 +371,8 @@ __device__ __forceinline__ void transform_lane(const Lane& l, const uint4 (&y)[2
     float ss = on ? s2.x + s2.y : 0.f;
     for (int o = 1; o < 1 << l.lanes_shift; o <<= 1) ss += __shfl_xor_sync(kFull, ss, o);
     if (on) {
-      // (in 4 bits, where instructions count: 2^-22 of it off at most)
-      const float inv = kFour ? rsqrtf(ss * l.one_of_D + l.eps) : 1.0f / sqrtf(ss / (float)l.D + l.eps);
+      // (of codes, which have 2 bits, where instructions count: 2^-22 of it off at most)
+      const float inv = kCodes ? rsqrtf(ss * l.one_of_D + l.eps) : 1.0f / sqrtf(ss / (float)l.D + l.eps);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         float2 g[4];
@@ -403,7 +404,7 @@ __device__ __forceinline__ void transform_lane(const Lane& l, const uint4 (&y)[2
 // heads h, h + step, ... < heads of a token, from src to dst (both at head h);
 // x: the first of them. (A round's heads are loaded while the round before is
 // computed.)
-template <typename T, bool kInterleaved, bool kFour>
+template <typename T, bool kInterleaved>
 __device__ __forceinline__ void transform_heads(const Lane& l, const T* src, int64_t src_step, T* dst, int64_t dst_step,
                                                 int h, int step, int heads, int rounds, const T* norm, uint4 (&x)[2]) {
   for (int r = 0; r < rounds; ++r, h += step, dst += dst_step) {
@@ -419,7 +420,7 @@ __device__ __forceinline__ void transform_heads(const Lane& l, const T* src, int
       continue;
     }
     float2 f[8];
-    transform_lane<T, kInterleaved, kFour>(l, y, on, norm, f);
+    transform_lane<T, kInterleaved, false>(l, y, on, norm, f);
     if (on) {
       *reinterpret_cast<uint4*>(dst + l.e0) = pack<T>(&f[0].x);
       *reinterpret_cast<uint4*>(dst + l.e1) = pack<T>(&f[4].x);
@@ -613,7 +614,7 @@ __global__ void __launch_bounds__(128, 7) k_kv_heads(const __grid_constant__ Hea
   const auto heads = [&](const smetric_heads& src, T* dst, int64_t head_stride, int r, const Rounds& rounds, int n_heads,
                          const void* norm, uint4(&z)[2]) {
     if (r < rounds.all)
-      transform_heads<T, kInterleaved, kFour>(l, source(src, r), step * src.head_stride,
+      transform_heads<T, kInterleaved>(l, source(src, r), step * src.head_stride,
                                        dst + (r * per + first) * head_stride, step * head_stride, r * per + first, step,
                                        n_heads, rounds.each + (r < rounds.rest), static_cast<const T*>(norm), z);
   };
