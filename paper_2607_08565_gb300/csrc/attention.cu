@@ -76,6 +76,7 @@ constexpr unsigned kFull = 0xffffffffu;
 constexpr long long kWaitCycles = 1ll << 32;  // bounded mbarrier waits: about 2 s
 constexpr uint32_t kNap = 20000;  // ns that a waiting warp sleeps between looks at most
 constexpr int kThreads = 512;
+static_assert(kTile == 1 << 7, "shifts");
 constexpr float kSlack = 8.f;     // log2 of how far scores may pass the reference
 constexpr uint32_t kHalf = 16384;  // bytes of 128 rows of 64 elements
 
@@ -393,6 +394,20 @@ __device__ __forceinline__ uint32_t place_v(int j, int n) { return min(2 + 2 * j
 
 // ---- the warps ----
 
+// The tiles of an item, from its first, of which some query sees a key among `rows` ones
+// from row `at`: a lane's page. (A page number says nothing of that: it may be any.)
+struct Tiles {
+  int32_t begin, end;
+  uint32_t key0;
+  __device__ __forceinline__ Tiles(const Item& it, int32_t lo, int32_t hi, int at, int rows, bool any) {
+    begin = ((lo - rows - at) >> 7) + 1 - it.tb;  // (kTile is 2^7)
+    end = any ? min(((hi - at - 1) >> 7) + 1, it.te) - it.tb : INT32_MIN;
+    key0 = (uint32_t)it.tb * kTile + at;
+  }
+  __device__ __forceinline__ bool operator()(int j) const { return j >= begin && j < end; }
+  __device__ __forceinline__ uint32_t key(int j) const { return key0 + (uint32_t)j * kTile; }
+};
+
 // Query tile number nq of the CTA: tile t of the item's, when its buffer is free. The
 // whole warp calls.
 template <int HALVES>
@@ -431,11 +446,8 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
     // the keys that some query of the unit sees
     const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
     const int32_t* pages = a.pages + it.unit.req * a.pages_stride;
-    // the lane's page of a tile, INT32_MIN where nobody sees a key of it
-    const auto page_of = [&](int j) {
-      const int64_t key = (int64_t)(it.tb + j) * kTile + mine * rows;
-      return copies && j < n && key < hi && key + rows > lo ? pages[key >> page_shift] : INT32_MIN;
-    };
+    const Tiles seen(it, lo, hi, mine * rows, rows, copies);
+    const auto page_of = [&](int j) { return seen(j) ? pages[seen.key(j) >> page_shift] : -1; };
     int32_t next = page_of(0);
     for (int j = 0; j < n; ++j) {
       int32_t page = next;
@@ -443,7 +455,7 @@ __device__ __forceinline__ void copy_tiles(const AttentionArgs& a, Shared* sh, W
       const uint32_t at = base + (values ? place_v(j, n) : place_k(j)), s = at % S;
       if (at >= S) mbar_wait(&b.empty[s], (at / S - 1) & 1, sh, a.status);
       if (stopped(sh)) break;
-      const bool held = page != INT32_MIN;
+      const bool held = seen(j);
       const unsigned who = __ballot_sync(kFull, held);
       if (lane == 0) mbar_expect(&b.full[s], __popc(who) * rows * 128);
       __syncwarp();
@@ -474,7 +486,7 @@ struct Order {
   template <typename F>
   __device__ __forceinline__ void start(int32_t tiles, F page_of) {
     n = tiles, jk = jv = 0;
-    last = before = INT32_MIN;
+    last = before = -1;
     ahead = page_of(0);
   }
   // The next tile, its page and whether it is of values; page_of(j) is the page of tile j.
@@ -487,7 +499,7 @@ struct Order {
     }
     page = ahead;
     before = last, last = ahead;
-    ahead = jk + 1 < n ? page_of(jk + 1) : INT32_MIN;
+    ahead = jk + 1 < n ? page_of(jk + 1) : -1;
     return jk++;
   }
 };
@@ -504,11 +516,8 @@ __device__ __forceinline__ void copy_codes(const AttentionArgs& a, SharedFour* s
   while (w.next(a, it)) {
     const int32_t lo = it.unit.pos >= a.window ? it.unit.pos - a.window + 1 : 0, hi = it.unit.pos + it.unit.tokens;
     const int32_t* pages = a.pages + it.unit.req * a.pages_stride;
-    // INT32_MIN where nobody sees a key of it
-    const auto page_of = [&](int j) {
-      const int64_t key = (int64_t)(it.tb + j) * kTile + lane * rows;
-      return lane < per && key < hi && key + rows > lo ? pages[key >> page_shift] : INT32_MIN;
-    };
+    const Tiles seen(it, lo, hi, lane * rows, rows, lane < per);
+    const auto page_of = [&](int j) { return seen(j) ? pages[seen.key(j) >> page_shift] : -1; };
     order.start(it.te - it.tb, page_of);
     for (int place = 0; place < 2 * order.n; ++place, ++at) {
       bool values;
@@ -517,11 +526,8 @@ __device__ __forceinline__ void copy_codes(const AttentionArgs& a, SharedFour* s
       const uint32_t s = at % kStaged;
       if (at >= kStaged) mbar_wait(&sh->staged_empty[s], (at / kStaged - 1) & 1, sh, a.status);
       if (stopped(sh)) break;
-      if (page != INT32_MIN && (uint32_t)page >= (uint32_t)a.num_pages) {
-        latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
-        page = INT32_MIN;  // (its scales become zeros)
-      }
-      const bool held = page != INT32_MIN;
+      const bool held = (uint32_t)page < (uint32_t)a.num_pages;
+      if (!held && seen(j)) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);  // (its scales become zeros)
       const unsigned who = __ballot_sync(kFull, held);
       if (lane == 0) mbar_expect(&sh->staged_full[s], __popc(who) * rows * row_bytes);
       __syncwarp();
@@ -555,7 +561,7 @@ __device__ __forceinline__ void copy_scales(const AttentionArgs& a, SharedFour* 
     // the page of 16 rows (lane & 7) of a tile
     const auto page_of = [&](int j) {
       const int64_t key = (int64_t)(it.tb + j) * kTile + 16 * (lane & 7);
-      return key < hi && key + 16 > lo ? pages[key >> page_shift] : INT32_MIN;
+      return key < hi && key + 16 > lo ? pages[key >> page_shift] : -1;
     };
     order.start(it.te - it.tb, page_of);
     for (int place = 0; place < 2 * order.n; ++place, ++at) {

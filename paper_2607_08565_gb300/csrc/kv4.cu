@@ -480,13 +480,14 @@ __global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __g
       const auto look_up = [&](int j) {  // of tiles j..
         const int x = j + (lane >> 1);
         const uint32_t key = key0 + (uint32_t)x * key_step + 16 * (lane & 1);
-        pages_next = x < n && key < (uint32_t)seen_hi && key + 16 > (uint32_t)seen_lo ? pages[key >> a.page_shift] : INT32_MIN;
+        pages_next = x < n && key < (uint32_t)seen_hi && key + 16 > (uint32_t)seen_lo ? pages[key >> a.page_shift] : -1;
       };
       const auto turn = [&](int j) {  // to tiles j..
         const bool held = (uint32_t)pages_next < (uint32_t)a.num_pages;
-        if (!held && pages_next != INT32_MIN) latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
         pages_now = held ? pages_next : 0;
         const uint32_t key = key0 + (uint32_t)(j + (lane >> 1)) * key_step + 16 * (lane & 1);
+        if (!held && j + (lane >> 1) < n && key < (uint32_t)seen_hi && key + 16 > (uint32_t)seen_lo)
+          latch_error(a.status, SMETRIC_ERR_INVALID_ARG);
         in_cache = __ballot_sync(kFull, held);
         in_whole = __ballot_sync(kFull, held && key >= (uint32_t)seen_lo && key + 16 <= (uint32_t)seen_hi);
         if (j + 16 < n) look_up(j + 16);
