@@ -684,6 +684,14 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
                     const int32_t* d_kv_lens, const int32_t* d_pages, int32_t max_pages, int64_t pages_stride,
                     int32_t window, smetric_stream_t stream);
 
+/* smetric_kv_plan of requests that have at most max_new new tokens each (a request
+ * with more counts as bad offsets). What is known of them saves a launch: with
+ * caches in 4 bits and up to 16 query heads a key head, single tokens (or 8 / group
+ * tokens a request) need no kernel for chunks. */
+int smetric_kv_plan_up_to(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests, int64_t n_tokens,
+                          const int32_t* d_kv_lens, const int32_t* d_pages, int32_t max_pages, int64_t pages_stride,
+                          int32_t window, int64_t max_new, smetric_stream_t stream);
+
 /* Append the planned batch's keys and values to the cache, the keys (and the
  * queries, when q.d_data is not NULL, into q_out) transformed on the way.
  * Two tokens with one slot are the caller's error (either may win). q_out may

@@ -69,7 +69,7 @@ EXPORTED = (
     "smetric_route_batches", "smetric_index_set_lru", "smetric_index_lru_sizes", "smetric_route_commit_batch",
     "smetric_kv_create", "smetric_kv_destroy", "smetric_kv_plan", "smetric_kv_append", "smetric_qk_norm_rope",
     "smetric_paged_attention", "smetric_kv_status", "smetric_kv_launch_count",
-    "smetric_kvq_append", "smetric_kvq_read", "smetric_kvq_attention",
+    "smetric_kvq_append", "smetric_kvq_read", "smetric_kvq_attention", "smetric_kv_plan_up_to",
 )
 
 
@@ -189,6 +189,7 @@ def lib():
             "smetric_kv_create": (C.c_int, [C.POINTER(smetric_kv_config), C.POINTER(P)]),
             "smetric_kv_destroy": (C.c_int, [P]),
             "smetric_kv_plan": (C.c_int, [P, P, I32, I64, P, P, I32, I64, I32, P]),
+            "smetric_kv_plan_up_to": (C.c_int, [P, P, I32, I64, P, P, I32, I64, I32, I64, P]),
             "smetric_kv_append": (C.c_int, [P, smetric_kv_cache, smetric_heads, smetric_heads, smetric_heads,
                                             smetric_heads, smetric_kv_transform, P]),
             "smetric_qk_norm_rope": (C.c_int, [P, smetric_heads, smetric_heads, P, I64, smetric_kv_transform,
@@ -490,6 +491,12 @@ def smetric_kv_plan(kv: int, d_offsets, n_requests: int, n_tokens: int, d_kv_len
                     pages_stride: int, window: int = 0, stream=None) -> None:
     _check(lib().smetric_kv_plan(kv, _ptr(d_offsets), n_requests, n_tokens, _ptr(d_kv_lens), _ptr(d_pages), max_pages,
                                  pages_stride, window, _stream(stream)), "smetric_kv_plan")
+
+
+def smetric_kv_plan_up_to(kv: int, d_offsets, n_requests: int, n_tokens: int, d_kv_lens, d_pages, max_pages: int,
+                          pages_stride: int, window: int, max_new: int, stream=None) -> None:
+    _check(lib().smetric_kv_plan_up_to(kv, _ptr(d_offsets), n_requests, n_tokens, _ptr(d_kv_lens), _ptr(d_pages), max_pages,
+                                       pages_stride, window, max_new, _stream(stream)), "smetric_kv_plan_up_to")
 
 
 def smetric_kv_append(kv: int, cache: smetric_kv_cache, k: smetric_heads, v: smetric_heads, q: smetric_heads,
@@ -989,10 +996,12 @@ class SMetricKV:
         return smetric_kv_transform(table, rows or 0, self._norm(q_norm), self._norm(k_norm), eps, rot or 0,
                                     SMETRIC_KV_INTERLEAVED if interleaved else 0, 0)
 
-    def plan(self, offsets, kv_lens, pages, n_tokens: int, window: int = 0, stream=None):
+    def plan(self, offsets, kv_lens, pages, n_tokens: int, window: int = 0, stream=None, max_new: Optional[int] = None):
         """Plans a batch: offsets int64 [n+1], kv_lens int32 [n], pages int32
         [n, max_pages] (row stride free). The window is the plan's: layers that
-        alternate need two plans or handles. The handle keeps the tensors until
+        alternate need two plans or handles. max_new: no request has more new
+        tokens (one that has is an error); steps of single tokens over caches in
+        4 bits are faster when it says so. The handle keeps the tensors until
         the next plan, and until what read them on another stream than torch's
         current one at this call is done; those that a captured call reads are
         the graph's owner's to keep."""
@@ -1008,8 +1017,12 @@ class SMetricKV:
             raise ValueError("a request's pages must be contiguous")
         most = pages.shape[1]
         raw, other = self._stream(stream)
-        smetric_kv_plan(self.handle, offsets, n, n_tokens, kv_lens, pages.data_ptr() if pages.numel() else None, most,
-                        pages.stride(0) if n > 1 else most, max(-1 << 31, min(window, (1 << 31) - 1)), raw)
+        args = (self.handle, offsets, n, n_tokens, kv_lens, pages.data_ptr() if pages.numel() else None, most,
+                pages.stride(0) if n > 1 else most, max(-1 << 31, min(window, (1 << 31) - 1)))
+        if max_new is None:
+            smetric_kv_plan(*args, raw)
+        else:
+            smetric_kv_plan_up_to(*args, max(-1, min(max_new, (1 << 63) - 1)), raw)
         self._n_tokens = n_tokens
         self._keep((offsets, kv_lens, pages))
         self._read(raw, other)

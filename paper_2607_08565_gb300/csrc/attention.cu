@@ -62,6 +62,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "attention_join.cuh"
 #include "call_range.cuh"
 #include "kv_impl.cuh"
 #include "launch.cuh"
@@ -331,12 +332,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
       "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
-  return y;
-}
-
 __device__ __forceinline__ float max3(float x, float y, float z) {
   float m;
   asm("max.f32 %0, %1, %2, %3;\n" : "=f"(m) : "f"(x), "f"(y), "f"(z));
@@ -356,36 +351,6 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
       " mov.b64 {%0, %1}, d;\n}\n"
       : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
   return r;
-}
-
-template <typename T>
-struct Type;
-template <>
-struct Type<__nv_bfloat16> {
-  static constexpr uint32_t kFormat = 1;  // of the tensor cores' operands
-  static constexpr float kLift = 0.f;
-  static __device__ __forceinline__ uint32_t pack(float a, float b) {
-    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&p);
-  }
-};
-template <>
-struct Type<__half> {
-  static constexpr uint32_t kFormat = 0;
-  // Weights up to 2^(kLift + kSlack) = 2^15: half precision's range ends at
-  // 65,504, and the small weights of long rows stay normal numbers longer.
-  static constexpr float kLift = 7.f;
-  static __device__ __forceinline__ uint32_t pack(float a, float b) {
-    const __half2 p = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&p);
-  }
-};
-
-// Partial sums: a slot's two query tiles, each D/4 columns of kTile rows of four
-// sums, so that the threads of a warp (a row each) store in whole lines. The
-// place of a column's first row, in units of four sums.
-__device__ __forceinline__ int64_t part_at(int D, int64_t slot, int tile, int column) {
-  return ((slot * 2 + tile) * (D / 4) + column) * kTile;
 }
 
 // Places of an item's tiles in the ring, of n key tiles: K0 K1 V0 K2 V1 K3 ...
@@ -875,17 +840,6 @@ __device__ __forceinline__ void multiply(const AttentionArgs& a, Shared* sh, Wal
   }
 }
 
-// 16 elements of an output.
-__device__ __forceinline__ void store16(const AttentionArgs& a, void* p, const uint32_t* r) {
-  if (a.wide) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
-                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
-  } else {
-    static_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
-    static_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
-  }
-}
-
 // A tile's first token in its unit, and its rows.
 __device__ __forceinline__ int tile_token(const AttentionArgs& a, const Item& it, int tile) {
   return it.pair ? tile * a.tile_tokens : 0;
@@ -940,7 +894,7 @@ __device__ __forceinline__ void write_tile(const AttentionArgs& a, Shared* sh, c
         uint32_t y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = Type<T>::pack(f[2 * i], f[2 * i + 1]);
-        store16(a, out + d, y);
+        store16(a.wide, out + d, y);
       } else {
         float4* p = reinterpret_cast<float4*>(a.part) + part_at(a.D, it.slot, tile, d / 4) + row;
 #pragma unroll
@@ -1119,6 +1073,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   }
   const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + 2 * HALVES * kHalf, staging = ring + S * HALVES * kHalf;
   const int warp = threadIdx.x >> 5;
+  if constexpr (kFour) {  // (steps of single tokens have no chunks)
+    pdl_enter();
+    if (a.shares[blockIdx.x].u0 < 0 && !a.clears) return;
+  }
   if (threadIdx.x == 0) {
     Barriers& b = sh->bar;
     for (int i = 0; i < S; ++i) mbar_init(&b.full[i], kFour ? 4 : 1), mbar_init(&b.empty[i], 1);
@@ -1216,112 +1174,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
   }
 }
 
-// The pieces of 16 elements of a row, so far.
-struct Joined {
-  float top = -INFINITY, l = 0.f;  // largest reference exponent; sum of weights, to it
-  float4 o[4] = {};
-  __device__ __forceinline__ void add(float ref, float weights, const float4 (&p)[4]) {
-    const float next = fmaxf(top, ref);
-    if (next == -INFINITY) return;  // no key so far
-    const float f = ex2(top - next), g = ex2(ref - next);
-    top = next;
-    l = l * f + weights * g;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      o[i].x = o[i].x * f + p[i].x * g, o[i].y = o[i].y * f + p[i].y * g;
-      o[i].z = o[i].z * f + p[i].z * g, o[i].w = o[i].w * f + p[i].w * g;
-    }
-  }
-};
-
-// out = sum_i 2^(ref_i - top) O_i / sum_i 2^(ref_i - top) l_i over a unit's
-// pieces. G threads share 16 elements of a row (a whole sector of the output),
-// thread g taking pieces g, g + G, ..., two of them in flight: the order of the
-// sums depends on the number of pieces alone.
-// CTA c1's share starts the unit; the block is one of `blocks` for it.
-constexpr int kJoinThreads = 128;
 constexpr int kJoinBlocks = 16;  // an SM
-template <typename T, int G>
-__device__ __forceinline__ void join(const AttentionArgs& a, const KvUnit& unit, int h, int c1, int pieces, int block,
-                                     int blocks) {
-  const int n_rows = unit.tokens * a.group, full_rows = a.tile_tokens * a.group;
-  constexpr int P = 2;
-  const int n = n_rows * (a.D / 16), g = threadIdx.x % G, step = blocks * (kJoinThreads / G);
-  for (int x = block * (kJoinThreads / G) + threadIdx.x / G; x - (int)(threadIdx.x % 32) / G < n; x += step) {
-    const int column = min(x, n - 1) / n_rows, r = min(x, n - 1) - column * n_rows;
-    const int tile = r >= full_rows, row = r - tile * full_rows;
-    Joined s;
-    for (int i0 = g; i0 < pieces; i0 += P * G) {
-      float2 ml[P];
-      float4 p[P][4];
-#pragma unroll
-      for (int k = 0; k < P; ++k) {
-        const int i = i0 + k * G;
-        if (i >= pieces) continue;
-        const int64_t slot = 2 * ((int64_t)c1 + i) + (i == 0);
-        ml[k] = a.part_ml[slot * 2 * kTile + tile * kTile + row];
-        const float4* from = reinterpret_cast<const float4*>(a.part) + part_at(a.D, slot, tile, 4 * column) + row;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) p[k][q] = from[q * kTile];
-      }
-#pragma unroll
-      for (int k = 0; k < P; ++k)
-        if (i0 + k * G < pieces) s.add(ml[k].x, ml[k].y, p[k]);
-    }
-    // The G threads' sums: their exponents to the largest, then in pairs, each of
-    // a pair going on with half of the elements: 15 to 16 exchanges of elements
-    // instead of 16 a step, and the stores spread over the threads (18.6 us against
-    // 19.3 for single tokens of 19 sequences of up to 900 keys, 192 against 196 for
-    // chunks in a window).
-    float top = s.top;
-#pragma unroll
-    for (int o = 1; o < G; o <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-    const float f = s.top == -INFINITY ? 0.f : ex2(s.top - top);
-    float l = s.l * f, v[16];
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      v[4 * q] = s.o[q].x * f, v[4 * q + 1] = s.o[q].y * f, v[4 * q + 2] = s.o[q].z * f, v[4 * q + 3] = s.o[q].w * f;
-    int first = 0;  // of the elements that the thread has
-#pragma unroll
-    for (int o = 1; o < G; o <<= 1) {
-      l += __shfl_xor_sync(kFull, l, o);
-      const bool high = g & o;
-      const int m = 8 / o;  // elements to go on with
-      if (m > 0) {
-#pragma unroll
-        for (int i = 0; i < m; ++i) v[i] = (high ? v[i + m] : v[i]) + __shfl_xor_sync(kFull, high ? v[i] : v[i + m], o);
-        first += high ? m : 0;
-      } else {
-        v[0] += __shfl_xor_sync(kFull, v[0], o);
-      }
-    }
-    if (x >= n) continue;
-    const float inv = (l > 0.f ? 1.f / l : l) * a.v_scale;  // (NaN stays)
-    const int64_t token = unit.token + r / a.group;
-    const int head = h * a.group + r % a.group;
-    T* out = static_cast<T*>(a.out.d_data) + token * a.out.token_stride + head * a.out.head_stride + 16 * column;
-    if constexpr (G == 1) {
-      uint32_t y[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) y[q] = Type<T>::pack(v[2 * q] * inv, v[2 * q + 1] * inv);
-      store16(a, out, y);
-    } else if constexpr (G <= 8) {
-#pragma unroll
-      for (int q = 0; q < 8 / G; ++q)
-        reinterpret_cast<uint32_t*>(out + first)[q] = Type<T>::pack(v[2 * q] * inv, v[2 * q + 1] * inv);
-    } else if (g < 16) {
-      // (element 0 is the low half)
-      reinterpret_cast<uint16_t*>(out)[first] = (uint16_t)Type<T>::pack(v[0] * inv, 0.f);
-    }
-    if (a.lse && column == 0 && g == 0)
-      a.lse[token * a.hq + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
-  }
-}
-
-// The blocks in turn for the units that several CTAs share, so that one such
-// unit (a chunk over a long sequence: 9 MB of pieces) has them all. Bound by the
-// latency of its reads: 10 us for 150 units of 252 rows in two pieces (49 MB), 6
-// for 4 units of 8 rows in 38, 3.5 for none.
+// Bound by the latency of its reads: 10 us for 150 units of 252 rows in two pieces (49
+// MB), 6 for 4 units of 8 rows in 38, 3.5 for none.
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_constant__ AttentionArgs a) {
   // (the plan was done before the kernel that this one waits for)
@@ -1335,13 +1190,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
   }
   pdl_enter();
   if (block >= blocks) return;
-  // Chunks have two or three pieces of many rows, single tokens many of few.
-  if (s.n_last <= 4)
-    join<T, 1>(a, s.last, s.h1, c1, s.n_last, block, blocks);
-  else if (s.n_last <= 16)
-    join<T, 8>(a, s.last, s.h1, c1, s.n_last, block, blocks);
-  else
-    join<T, 32>(a, s.last, s.h1, c1, s.n_last, block, blocks);
+  join_unit<T>(a, s, c1, block, blocks, threadIdx.x);
 }
 
 constexpr size_t smem_bytes(int halves, bool four) {
@@ -1391,10 +1240,10 @@ bool limits() {
   return set((const void*)k_paged_attention<T, 1, kFour>, 1) && set((const void*)k_paged_attention<T, 2, kFour>, 2);
 }
 
-// The attention and its join; `a` has the caches, the rest is set here.
+// The attention and, with `joins`, its join; `a` has the caches, the rest is set here.
 template <bool kFour>
 int launch_attention(smetric_kv* kv, AttentionArgs& a, const smetric_heads& q, float scale, const smetric_heads& out,
-                     float* d_lse, smetric_stream_t stream) {
+                     float* d_lse, bool joins, smetric_stream_t stream) {
   const smetric_kv_config& c = kv->cfg;
   {
     const cuuint64_t dims[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.num_q_heads, (cuuint64_t)kv->n_tokens};
@@ -1428,10 +1277,10 @@ int launch_attention(smetric_kv* kv, AttentionArgs& a, const smetric_heads& q, f
   auto kern = c.dtype == SMETRIC_BF16
                   ? (halves == 2 ? k_paged_attention<__nv_bfloat16, 2, kFour> : k_paged_attention<__nv_bfloat16, 1, kFour>)
                   : (halves == 2 ? k_paged_attention<__half, 2, kFour> : k_paged_attention<__half, 1, kFour>);
-  kv->launches += 2;
+  kv->launches += 1 + joins;
   const int rc = launch_k(kern, dim3((unsigned)kv->num_sms), dim3(kThreads), smem_bytes(halves, kFour),
                           reinterpret_cast<cudaStream_t>(stream), true, a);
-  if (rc) return rc;
+  if (rc || !joins) return rc;
   auto join = c.dtype == SMETRIC_BF16 ? k_paged_join<__nv_bfloat16> : k_paged_join<__half>;
   return launch_k(join, dim3((unsigned)kv->num_sms * kJoinBlocks), dim3(kJoinThreads), 0,
                   reinterpret_cast<cudaStream_t>(stream), true, a);
@@ -1452,7 +1301,7 @@ int smetric::attention_many_rows(smetric_kv* kv, const smetric_kvq_cache& k_cach
   a.v4 = v_cache;
   a.v_scale = std::ldexp(1.f, v_cache.exp);
   a.clears = !kv->few.rows;
-  return launch_attention<true>(kv, a, q, std::ldexp(scale, k_cache.exp), out, d_lse, stream);
+  return launch_attention<true>(kv, a, q, std::ldexp(scale, k_cache.exp), out, d_lse, !kv->one_join, stream);
 }
 
 extern "C" {
@@ -1481,7 +1330,7 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
   }
   a.v_scale = 1.f;
   a.clears = true;
-  return launch_attention<false>(kv, a, q, scale, out, d_lse, stream);
+  return launch_attention<false>(kv, a, q, scale, out, d_lse, true, stream);
 }
 
 }  // extern "C"

@@ -71,7 +71,7 @@ struct PlanArgs {
   const int32_t* kv_lens;
   const int32_t* pages;
   int32_t max_pages, page_size;
-  int64_t pages_stride, num_pages;
+  int64_t pages_stride, num_pages, max_new;
   int32_t window, ctas, sets;
   PlanSet set[2];
   KvPlan* plan;
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(const __grid_constant_
     int bad = 0;
     for (int32_t r = threadIdx.x; r < a.n; r += blockDim.x) {
       const int64_t lo = a.off[r], hi = a.off[r + 1], kv = a.kv_lens[r];
-      bad |= lo < 0 || hi < lo || hi > a.n_tokens || kv < hi - lo || kv > (int64_t)a.max_pages * a.page_size;
+      bad |= lo < 0 || hi < lo || hi > a.n_tokens || hi - lo > a.max_new || kv < hi - lo || kv > (int64_t)a.max_pages * a.page_size;
     }
     bad = __syncthreads_or(bad);
     if (threadIdx.x == 0 && blockIdx.x == 0) {
@@ -812,11 +812,18 @@ int smetric_kv_destroy(smetric_kv* kv) {
 int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests, int64_t n_tokens,
                     const int32_t* d_kv_lens, const int32_t* d_pages, int32_t max_pages, int64_t pages_stride,
                     int32_t window, smetric_stream_t stream) {
+  return smetric_kv_plan_up_to(kv, d_offsets, n_requests, n_tokens, d_kv_lens, d_pages, max_pages, pages_stride, window,
+                               INT64_MAX, stream);
+}
+
+int smetric_kv_plan_up_to(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests, int64_t n_tokens,
+                          const int32_t* d_kv_lens, const int32_t* d_pages, int32_t max_pages, int64_t pages_stride,
+                          int32_t window, int64_t max_new, smetric_stream_t stream) {
   CallRange range("smetric_kv_plan");
   int rc = check_device(kv);
   if (rc) return rc;
   if (n_requests < 0 || n_requests > kv->cfg.max_batch_requests || n_tokens < 0 ||
-      n_tokens > kv->cfg.max_batch_tokens || max_pages < 0 || pages_stride < max_pages || window < 0 ||
+      n_tokens > kv->cfg.max_batch_tokens || max_pages < 0 || pages_stride < max_pages || window < 0 || max_new < 0 ||
       (n_requests > 0 && (!d_offsets || !d_kv_lens || (max_pages > 0 && !d_pages))) || !aligned(d_offsets) ||
       !aligned(d_kv_lens) || !aligned(d_pages))
     return SMETRIC_ERR_INVALID_ARG;
@@ -831,14 +838,22 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
   a.page_size = kv->cfg.page_size;
   a.pages_stride = pages_stride;
   a.num_pages = kv->cfg.num_pages;
+  a.max_new = max_new;
   a.window = window > 0 ? window : INT32_MAX;
   a.ctas = kv->num_sms;
   a.plan = kv->plan;
   a.tokens = kv->tokens;
   const KvFew& f = kv->few;
-  // A step of single tokens (or of requests with nothing new among them) goes to
-  // the few-row kernel whole, so that the other need not be launched.
-  const bool all_few = f.rows && n_tokens <= n_requests;
+  // A request's own tokens decide which kernel takes it: a chunk of 200 tokens on a prefix
+  // of 24k among 255 requests without tokens takes 89 us with the chunks' kernel, 492 a
+  // token at a time with the other. Where no request can have more tokens than the few-row
+  // kernel takes, the chunks' kernel need not be launched. A batch of no more tokens than requests (a decoding step,
+  // or few chunks among many requests without tokens) may have chunks; probably it has
+  // none, and then a launch for both joins costs less than two: 64 single tokens over 2k
+  // to 48k keys take 171 us without the chunks' kernel, 174 with it and one join, 177 with
+  // two; chunks of up to 700 tokens among single ones 222 with one, 217 with two.
+  const bool all_few = f.rows && std::min<int64_t>(n_tokens, max_new) <= f.tokens;
+  const bool one_join = f.rows && !all_few && n_tokens <= n_requests;
   a.sets = f.rows ? 2 : 1;
   PlanSet& s = a.set[0];
   s.units = kv->units;
@@ -847,7 +862,7 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
   s.shares = kv->shares;
   s.split = kv->split;
   s.n_split = &kv->plan->n_split;
-  s.over = all_few ? INT32_MAX : f.rows ? f.tokens : 0;
+  s.over = f.rows ? f.tokens : 0;
   s.up_to = INT32_MAX;
   s.per = 2 * kv->tile_tokens, s.one = kv->tile_tokens;
   s.tile = kTile, s.heads = kv->cfg.num_kv_heads;
@@ -874,7 +889,7 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
     w.split = f.split;
     w.n_split = &kv->plan->n_split_few;
     w.over = 0;
-    w.up_to = all_few ? INT32_MAX : f.tokens;
+    w.up_to = f.tokens;
     w.per = w.one = f.tokens;
     w.tile = kFewTile, w.heads = f.blocks;
     // In tiles of one key head: a unit's ends (pages and queries on their way, the joined
@@ -891,6 +906,7 @@ int smetric_kv_plan(smetric_kv* kv, const int64_t* d_offsets, int32_t n_requests
   if (rc) return rc;
   kv->planned = true;
   kv->all_few = all_few;
+  kv->one_join = one_join;
   kv->n_tokens = n_tokens;
   kv->pages = d_pages;
   kv->pages_stride = pages_stride;

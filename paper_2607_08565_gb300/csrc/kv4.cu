@@ -5,7 +5,8 @@
 //   k_kv4_read      rows of positions in 16 bits.
 //   k_kv4_few       one CTA an SM, each with the share of the batch that the plan gave
 //                   it.
-//   k_kv4_few_join  joins the pieces of the units that several CTAs share.
+//   k_kv4_join      joins the pieces of the units that several CTAs share (and those of
+//                   the chunks' kernel, where it probably has none).
 //
 // An element is code * scale * 2^exp: 4 bits (e2m1) and, for 16 of them, 8 (e4m3). Code
 // times scale has 6 bits and lies within 2^-10 .. 2,688: exact in half precision, in
@@ -20,6 +21,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "attention_join.cuh"
 #include "call_range.cuh"
 #include "kv_impl.cuh"
 #include "launch.cuh"
@@ -198,7 +200,21 @@ __global__ void __launch_bounds__(kReadThreads) k_kv4_read(const __grid_constant
 
 // ---- attention of few rows ----
 
+// The pieces of the chunks' kernel, for the join.
+struct ManyJoin {
+  smetric_heads out;
+  float* lse;
+  const KvShare* shares;
+  const int32_t* split;
+  float* part;
+  float2* part_ml;
+  int32_t hq, group, tile_tokens, D;
+  float v_scale;
+  bool wide;  // outputs can be stored in pieces of 32 bytes
+};
+
 struct FewArgs {
+  ManyJoin many;
   smetric_kvq_cache k, v;
   smetric_heads q, out;
   float* lse;
@@ -273,11 +289,6 @@ struct FewWalk {
   }
 };
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
@@ -833,21 +844,11 @@ constexpr int kFewJoin = 512;
 constexpr int kFewPieces = 8;
 
 template <int D, int NB>
-__global__ void __launch_bounds__(kFewJoin) k_kv4_few_join(const __grid_constant__ FewArgs a) {
+__device__ __forceinline__ void join_few(const FewArgs& a, const KvShare& s, int c1, int block, int blocks) {
   constexpr int kRows = 8 * NB, kWarps = kFewJoin / 32;
   __shared__ float4 sums[kWarps][D / 4];
   __shared__ float2 stats[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  // (the plan was done before the kernel that this one waits for)
-  const int units = a.plan->n_split_few, blocks = units ? gridDim.x / units : 0, block = units ? blockIdx.x / units : 0;
-  KvShare s = {};
-  int c1 = 0;
-  if (block < blocks) {
-    c1 = a.split[blockIdx.x % units];
-    s = a.shares[c1];
-  }
-  pdl_enter();
-  if (block >= blocks) return;
   const KvUnit& u = s.last;
   const int unit_rows = u.tokens * a.group, rows = min(a.heads, a.hk - s.h1 * a.heads) * unit_rows, n = s.n_last;
   const bool holds = lane < D / 4;
@@ -937,6 +938,33 @@ __global__ void __launch_bounds__(kFewJoin) k_kv4_few_join(const __grid_constant
   }
 }
 
+// The units that several CTAs share; with kMany those of the chunks' kernel too.
+template <int D, int NB, bool kMany>
+__global__ void __launch_bounds__(kFewJoin) k_kv4_join(const __grid_constant__ FewArgs a) {
+  // (the plan was done before the kernel that this one waits for)
+  const auto find = [](int units, const int32_t* split, const KvShare* shares, int at, int n, KvShare& s, int& c1, int& block, int& blocks) {
+    blocks = units ? n / units : 0, block = units ? at / units : 0;
+    if (block >= blocks) return;
+    c1 = split[at % units];
+    s = shares[c1];
+  };
+  constexpr int kParts = kFewJoin / kJoinThreads;  // a block is as many for the units of many rows
+  KvShare few = {}, many = {};
+  int few_c1 = 0, few_block, few_blocks, many_c1 = 0, many_block = 0, many_blocks = 0;
+  find(a.plan->n_split_few, a.split, a.shares, blockIdx.x, gridDim.x, few, few_c1, few_block, few_blocks);
+  if (kMany)
+    find(a.plan->n_split, a.many.split, a.many.shares, blockIdx.x * kParts + threadIdx.x / kJoinThreads, gridDim.x * kParts, many, many_c1,
+         many_block, many_blocks);
+  pdl_enter();
+  if (few_block < few_blocks) join_few<D, NB>(a, few, few_c1, few_block, few_blocks);
+  if (kMany && many_block < many_blocks) {
+    if (a.bf16)
+      join_unit<__nv_bfloat16>(a.many, many, many_c1, many_block, many_blocks, threadIdx.x % kJoinThreads);
+    else
+      join_unit<__half>(a.many, many, many_c1, many_block, many_blocks, threadIdx.x % kJoinThreads);
+  }
+}
+
 template <int D, int NB>
 bool few_limit() {
   return cudaFuncSetAttribute((const void*)k_kv4_few<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(D, 8 * NB)) ==
@@ -947,7 +975,7 @@ int launch_few(smetric_kv* kv, const FewArgs& a, cudaStream_t s) {
   int rc = launch_k(k_kv4_few<D, NB>, dim3((unsigned)kv->num_sms), dim3(few_heads(8 * NB) * 32), (size_t)few_smem(D, 8 * NB), s, true, a);
   if (rc) return rc;
   kv->launches += 2;
-  return launch_k(k_kv4_few_join<D, NB>, dim3((unsigned)kv->num_sms * 2), dim3(kFewJoin), 0, s, true, a);
+  return launch_k(kv->one_join ? k_kv4_join<D, NB, true> : k_kv4_join<D, NB, false>, dim3((unsigned)kv->num_sms * 2), dim3(kFewJoin), 0, s, true, a);
 }
 
 }  // namespace
@@ -1041,6 +1069,18 @@ int smetric_kvq_attention(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq
   a.v_scale = std::ldexp(1.f, v_cache.exp);
   a.bf16 = c.dtype == SMETRIC_BF16;
   a.status = kv->status;
+  a.many.out = out;
+  a.many.lse = d_lse;
+  a.many.shares = kv->shares;
+  a.many.split = kv->split;
+  a.many.part = kv->part;
+  a.many.part_ml = kv->part_ml;
+  a.many.hq = a.hq;
+  a.many.group = kv->group;
+  a.many.tile_tokens = kv->tile_tokens;
+  a.many.D = c.head_dim;
+  a.many.v_scale = a.v_scale;
+  a.many.wide = !(reinterpret_cast<uintptr_t>(out.d_data) & 31) && out.token_stride % 16 == 0 && out.head_stride % 16 == 0;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const bool one = kv->few.rows == 8;
   switch (c.head_dim) {

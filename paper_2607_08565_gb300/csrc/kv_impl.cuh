@@ -96,7 +96,8 @@ struct smetric_kv {
   smetric::KvFew few;
   // of the last plan
   bool planned;
-  bool all_few;  // every unit is the few-row kernel's
+  bool all_few;   // every unit is the few-row kernel's
+  bool one_join;  // its join is the chunks' kernel's too
   int64_t n_tokens;
   const int32_t* pages;
   int64_t pages_stride;
@@ -110,7 +111,8 @@ int check_device(const smetric_kv* kv);
 // Sets the attention kernels' shared-memory limits; false on a CUDA error.
 bool attention_limits(bool four);
 bool few_limits();
-// Attention over caches in 4 bits of the plan's requests of more rows than few.rows.
+// Attention over caches in 4 bits of the plan's requests of more rows than few.rows; with
+// one_join its shared units are left to the few-row kernel's join.
 int attention_many_rows(smetric_kv* kv, const smetric_kvq_cache& k_cache, const smetric_kvq_cache& v_cache,
                         const smetric_heads& q, float scale, const smetric_heads& out, float* d_lse,
                         smetric_stream_t stream);
