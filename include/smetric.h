@@ -713,7 +713,7 @@ int smetric_qk_norm_rope(smetric_kv* kv, smetric_heads q, smetric_heads k, const
  * Single tokens, chunks and whole prompts may share a batch. Scores, softmax
  * and sums are held in 32 bits; the softmax's weights are rounded to dtype for
  * the product with the values. A token of no request gets out = 0 and
- * lse = -inf. scale is finite and > 0. d_lse: NULL or float [n_tokens,
+ * lse = -inf. scale is > 0 and scale * log2 e finite. d_lse: NULL or float [n_tokens,
  * num_q_heads]. out must not overlap q. Values at masked positions of a
  * request's own length must be finite; what lies past its length or before
  * its window may be anything. A row whose largest score is 2^27 or more in
@@ -753,7 +753,7 @@ int smetric_kvq_read(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq_cach
  * row, which is exact for elements of 2^-17 of the row's largest and more (smaller
  * ones are rounded to multiples of up to 2^-24 of it), and the softmax's weights are
  * rounded to half precision (to within 2^-32 of the row's largest where they are
- * below 2^-21 of it). scale * 2^exp of the keys is finite and > 0; scores of
+ * below 2^-21 of it). scale * 2^exp of the keys is > 0, and finite times log2 e; scores of
  * 2^27 and more may latch OVERFLOW. Scales at masked positions of a request's own
  * length must not be NaN; what lies past its length or before its window may be
  * anything. */

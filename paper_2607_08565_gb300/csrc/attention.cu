@@ -1311,7 +1311,7 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
   CallRange range("smetric_paged_attention");
   int rc = check_device(kv);
   if (rc) return rc;
-  if (four_bits(kv) || !kv->planned || !std::isfinite(scale) || !(scale > 0.f) || !cache_ok(cache) || !heads_ok(q, kv->n_tokens) ||
+  if (four_bits(kv) || !kv->planned || !scale_ok(scale) || !cache_ok(cache) || !heads_ok(q, kv->n_tokens) ||
       !heads_ok(out, kv->n_tokens) || (reinterpret_cast<uintptr_t>(d_lse) & 3))
     return SMETRIC_ERR_INVALID_ARG;
   if (kv->n_tokens == 0) return SMETRIC_OK;

@@ -1034,8 +1034,7 @@ int smetric_kvq_attention(smetric_kv* kv, smetric_kvq_cache k_cache, smetric_kvq
   if (rc) return rc;
   const smetric_kv_config& c = kv->cfg;
   if (!four_bits(kv) || !kv->planned || !cache4_ok(k_cache, c.head_dim) || !cache4_ok(v_cache, c.head_dim) ||
-      !std::isfinite(std::ldexp(scale, k_cache.exp)) || !(std::ldexp(scale, k_cache.exp) > 0.f) ||
-      !heads_ok(q, kv->n_tokens) || !heads_ok(out, kv->n_tokens) || (reinterpret_cast<uintptr_t>(d_lse) & 3))
+      !scale_ok(std::ldexp(scale, k_cache.exp)) || !heads_ok(q, kv->n_tokens) || !heads_ok(out, kv->n_tokens) || (reinterpret_cast<uintptr_t>(d_lse) & 3))
     return SMETRIC_ERR_INVALID_ARG;
   if (kv->n_tokens == 0) return SMETRIC_OK;
   if (!kv->all_few) {

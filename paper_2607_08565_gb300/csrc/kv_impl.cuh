@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <cmath>
 
 #include "smetric_impl.cuh"
 
@@ -157,5 +158,7 @@ template <typename E>
 bool aligned(const E* p) {
   return reinterpret_cast<uintptr_t>(p) % sizeof(E) == 0;
 }
+// A scale of scores that the kernels can multiply by, as exponents of 2.
+inline bool scale_ok(float scale) { return scale > 0.f && std::isfinite(scale * 1.4426950408889634f); }
 inline bool four_bits(const smetric_kv* kv) { return kv->cfg.flags & SMETRIC_KV_4BIT; }
 }  // namespace smetric
