@@ -589,8 +589,8 @@ __device__ __forceinline__ void convert_row(SharedFour* sh, uint32_t nq, uint32_
 // 128-byte swizzle, 32 rows each: a conversion for two codes and a product with their
 // scale, both exact (2 and 4 bits). A tile's keys and values are laid out alike. They
 // also convert an item's query tiles (kQueries), when they find them there between two
-// of its tiles, and after its fourth (or last) at the latest: the ring takes so many, and
-// all before are used up without the queries.
+// of its tiles, and after as many as the ring takes (or its last) at the latest: all
+// before are used up without the queries.
 template <int HALVES, bool kQueries>
 __device__ __forceinline__ void convert_tiles(const AttentionArgs& a, SharedFour* sh, Walk w, uint32_t q_smem, uint32_t ring,
                                               uint32_t staging) {

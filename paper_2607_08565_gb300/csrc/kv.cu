@@ -770,7 +770,7 @@ int smetric_kv_create(const smetric_kv_config* cfg, smetric_kv** out) {
     KvFew& f = kv->few;
     f.rows = kv->group <= 8 ? 8 : 16;
     f.tokens = f.rows / kv->group;
-    f.blocks = (c.num_kv_heads + few_heads(f.rows) - 1) / few_heads(f.rows);
+    f.blocks = (c.num_kv_heads + kFewWarps - 1) / kFewWarps;
     f.heads = (c.num_kv_heads + f.blocks - 1) / f.blocks;
   }
   unsigned char* mem = nullptr;

@@ -238,16 +238,16 @@ constexpr float kLift = 7.f;   // weights up to 2^(kLift + kSlack): half precisi
 constexpr float kSlack = 8.f;  // log2 of how far scores may pass the reference
 
 __host__ __device__ constexpr int stage_bytes(int D) { return 2 * kFewTile * (D / 2 + scale_bytes(D)); }
-__host__ __device__ constexpr int stages(int D, int rows) {
-  return 225 * 1024 / (few_heads(rows) * stage_bytes(D)) < 8 ? 225 * 1024 / (few_heads(rows) * stage_bytes(D)) : 8;
+__host__ __device__ constexpr int stages(int D) {
+  return 225 * 1024 / (kFewWarps * stage_bytes(D)) < 8 ? 225 * 1024 / (kFewWarps * stage_bytes(D)) : 8;
 }
-__host__ __device__ constexpr int ring_bytes(int D, int rows) { return few_heads(rows) * stages(D, rows) * stage_bytes(D); }
+__host__ __device__ constexpr int ring_bytes(int D) { return kFewWarps * stages(D) * stage_bytes(D); }
 // A row of a warp's sums in shared memory, in floats: 4 past a multiple of 32, so that
 // the rows of the lanes that store together lie in other banks.
 __host__ __device__ constexpr int sum_row(int D) { return D + 4; }
 __host__ __device__ constexpr int few_smem(int D, int rows) {
-  const int sums = few_heads(rows) * rows * (sum_row(D) + 2) * 4;
-  return ring_bytes(D, rows) > sums ? ring_bytes(D, rows) : sums;
+  const int sums = kFewWarps * rows * (sum_row(D) + 2) * 4;
+  return ring_bytes(D) > sums ? ring_bytes(D) : sums;
 }
 static_assert(few_smem(128, 8) <= 232448 && few_smem(128, 16) <= 232448 && few_smem(32, 8) <= 232448, "227 KB");
 
@@ -432,8 +432,8 @@ __device__ __forceinline__ void write_row(const FewArgs& a, const KvUnit& u, int
 // 12 warps of 168 registers: 16 of 128 took 178 us for the 64 tokens, 20 of 96 239, 8 of
 // 255 205. The next tile's scores computed beside this tile's weights took 186.
 template <int D, int NB>
-__global__ void __launch_bounds__(few_heads(8 * NB) * 32, 1) k_kv4_few(const __grid_constant__ FewArgs a) {
-  constexpr int kWarps = few_heads(8 * NB), kRows = 8 * NB, kStages = stages(D, kRows), kStage = stage_bytes(D);
+__global__ void __launch_bounds__(kFewWarps * 32, 1) k_kv4_few(const __grid_constant__ FewArgs a) {
+  constexpr int kWarps = kFewWarps, kRows = 8 * NB, kStages = stages(D), kStage = stage_bytes(D);
   constexpr int W = D / 32;               // words of codes a lane has of a key, and half words of a value
   constexpr int kCodes = kFewTile * D / 2, kScales = kFewTile * scale_bytes(D), SB = scale_bytes(D);
   extern __shared__ __align__(128) unsigned char smem[];
@@ -972,7 +972,7 @@ bool few_limit() {
 }
 template <int D, int NB>
 int launch_few(smetric_kv* kv, const FewArgs& a, cudaStream_t s) {
-  int rc = launch_k(k_kv4_few<D, NB>, dim3((unsigned)kv->num_sms), dim3(few_heads(8 * NB) * 32), (size_t)few_smem(D, 8 * NB), s, true, a);
+  int rc = launch_k(k_kv4_few<D, NB>, dim3((unsigned)kv->num_sms), dim3(kFewWarps * 32), (size_t)few_smem(D, 8 * NB), s, true, a);
   if (rc) return rc;
   kv->launches += 2;
   return launch_k(kv->one_join ? k_kv4_join<D, NB, true> : k_kv4_join<D, NB, false>, dim3((unsigned)kv->num_sms * 2), dim3(kFewJoin), 0, s, true, a);

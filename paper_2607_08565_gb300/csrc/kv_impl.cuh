@@ -62,7 +62,7 @@ struct __align__(16) KvShare {
 // kFewTile keys.
 constexpr int kFewTile = 32;
 // Its warps, and so the key heads of a block at most.
-__host__ __device__ constexpr int few_heads(int rows) { return rows == 8 ? 12 : 12; }
+constexpr int kFewWarps = 12;
 struct KvFew {
   int rows;    // 8, 16, or 0: no such kernel (more than 16 query heads per key head)
   int tokens;  // rows / group
@@ -130,8 +130,8 @@ inline bool cache_ok(const smetric_kv_cache& c) {
 }
 // What scores are multiplied by, of a row that was divided by a power of two: a normal
 // number, as 0 times the -inf of a key that is not seen is NaN, and infinity times the
-// score 0 is. (A row of zeros has the power 2^-126. Scores are below 2^23 before, so that
-// those below 2^-103 after it may be any so small.)
+// score 0 is. (A row of zeros has the power 2^-126. Scores are below 2^35 before, so that
+// those below 2^-91 after it may be any so small.)
 __device__ __forceinline__ float score_factor(float c) { return fminf(fmaxf(c, FLT_MIN), FLT_MAX); }
 // A reference exponent, score * factor - lift rounded up, so that no weight passes
 // 2^(lift + slack): weights are of exactly this reference, and the largest one's is

@@ -12,9 +12,11 @@ namespace smetric {
 // Programmatic dependent launch: a kernel launched with programmatic stream
 // serialisation is set up while its predecessor still runs and waits here
 // until that predecessor has finished and its writes are visible (a no-op for
-// an ordinary launch). But for k_paged_attention, whose CTAs leave no room for
-// its successor's, no kernel triggers its successor early: successors waiting on
-// the SMs during a kernel's run measured slower.
+// an ordinary launch). But for the attention kernels, k_paged_attention and
+// k_kv4_few, whose CTAs leave no room for their successors', no kernel triggers its
+// successor early: successors waiting on the SMs during a kernel's run measured
+// slower. These two do so when they are past their own wait, as their joins read the
+// plan before theirs.
 __device__ __forceinline__ void pdl_enter() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
 
 // Launches a kernel; with pdl the launch may begin while the previous kernel
