@@ -197,14 +197,24 @@ __device__ void plan_units(const PlanArgs& a, const PlanSet& s) {
         if (--x.h1 < 0) x.h1 = s.heads - 1, --x.u1;
         x.t1 = s.units[x.u1].te;
       }
-      const auto same = [&](int i, int32_t u, int32_t h) {
-        return i <= ctas && su[i] == u && sh[i] == h && u < U && st[i] > s.units[u].tb;
-      };
       x.last = s.units[x.u1];
+      const int32_t u1 = x.u1, h1 = x.h1, tb = x.last.tb;
+      const auto same = [&](int i) { return i <= ctas && su[i] == u1 && sh[i] == h1 && u1 < U && st[i] > tb; };
+      // Boundaries in a row have it: their number in steps that double, then halve. (One by
+      // one, and asking for the unit's first tile each time, the plan of one token over
+      // 24,577 keys, which 152 CTAs share, took 22.9 us with caches in 4 bits.)
+      int some = 0;
       x.n_last = 1;
-      while (same(c + x.n_last, x.u1, x.h1)) ++x.n_last;
+      while (same(c + x.n_last)) some = x.n_last, x.n_last *= 2;
+      while (x.n_last - some > 1) {
+        const int mid = (some + x.n_last) / 2;
+        if (same(c + mid))
+          some = mid;
+        else
+          x.n_last = mid;
+      }
       // (their order decides which blocks join them, not how)
-      if (x.n_last > 1 && !same(c, x.u1, x.h1)) s.split[atomicAdd(&n_split, 1)] = c;
+      if (x.n_last > 1 && !same(c)) s.split[atomicAdd(&n_split, 1)] = c;
     }
     s.shares[c] = x;
   }
