@@ -69,7 +69,7 @@ class Instance:
             table[r, :len(pages)] = torch.tensor(pages, dtype=torch.int32)
         offsets = torch.tensor([0] + new).cumsum(0).to(dev)
         lens = torch.tensor([len(p) for p in prompts], dtype=torch.int32, device=dev)
-        self.kv.plan(offsets, lens, table.to(dev), sum(new))
+        self.kv.plan(offsets, lens, table.to(dev), sum(new), max_new=max(new))
         tokens = torch.cat([torch.tensor(p[len(p) - n:]) for p, n in zip(prompts, new)]).to(dev)
         out = layer(self.kv, self.cache, tokens)
         self.kv.check()

@@ -568,10 +568,10 @@ int64_t smetric_launch_count(const smetric_index* idx);
  * aligned pointers and strides that are multiples of 8 elements, arrays of
  * whole numbers and d_lse the alignment of their elements.
  *
- * A cache in 4 bits holds 3.6 times the tokens. Of each head of each token it
- * has head_dim codes, two a byte (the even element in the low four bits): a
- * sign, two bits of exponent and one of mantissa (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4
- * and 6); and for every 16 elements a scale of 8 bits (e4m3). An element is
+ * A cache in 4 bits holds 3.6 times the tokens (3.4 with heads of 96 elements, 3.2
+ * of 32, whose scales are padded). Of each head of each token it has head_dim
+ * codes, two a byte (the even element in the low four bits): a sign, two bits of
+ * exponent and one of mantissa (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4 and 6); and for every 16 elements a scale of 8 bits (e4m3). An element is
  *   code * scale * 2^exp,
  * with one exp for all keys and one for all values. smetric_kvq_append writes
  * it, smetric_kvq_attention attends over it and smetric_kvq_read reads it back;
@@ -726,7 +726,8 @@ int smetric_paged_attention(smetric_kv* kv, smetric_kv_cache cache, smetric_head
  * y = x / 2^exp, the scale s is the e4m3 number nearest to max|y| / 6 (at most
  * 448), and a code the e2m1 number nearest to y / s (at most 6 in magnitude;
  * where s is 0 the codes are), halves to even in both. So elements up to 2,688 *
- * 2^exp are held to within a sixth of their group's largest. A NaN makes its 16
+ * 2^exp are held to within a fifth of their group's largest (a sixth, and what the
+ * scale is rounded up by), or 0.006 * 2^exp where that is more. A NaN makes its 16
  * elements NaN; an infinite one is held as 2,688 * 2^exp. (A 32-bit value within 2^-20
  * of its size of the border between two numbers may go to either.) Two tokens with one
  * slot may leave a mixture of both. */

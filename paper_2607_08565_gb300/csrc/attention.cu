@@ -35,22 +35,22 @@
 // with the values and its half's next scores (2 x 512 on the tensor cores), 2,840
 // cycles for two query tiles and a key tile: 2,048 tokens over 65,000 (32 query
 // heads) take 1,566 us, 1,415 TFLOP/s, with the cap, and 1,360 to 1,440 us in
-// runs too short for it. A thread spills 112 bytes and loads 136 (of all roles).
+// runs too short for it. A thread spills 116 bytes and loads 136 (of all roles).
 //
 // Caches in 4 bits (kFour) go the same way with other hands: warp 0 copies tiles of codes
 // with TMA, 2 their scales (8 bytes a row are too few for TMA), 3 the query tiles; 12-15
 // turn codes into tiles of the ring, in half precision, which all products take; and the
 // softmax's warps write the output. Queries in bf16 become half precision, divided by a
-// power of two for each row, by 12-15 too. 2,048 tokens over 65,000 take 1,372 us, 1,620
-// TFLOP/s (1,480 with the power cap), 3,000 cycles for two query tiles and a key tile:
+// power of two for each row, by 12-15 too. 2,048 tokens over 65,000 take 1,380 us, 1,605
+// TFLOP/s (1,554 with the power cap), 3,000 cycles for two query tiles and a key tile:
 // the weights have 11 bits instead of 8, memory moves a quarter. What conversions cost is
-// issue slots (54 %, where 16-bit caches take 38): a tile's softmax takes 1,700 cycles
+// issue slots (54 %, where 16-bit caches take 40): a tile's softmax takes 1,700 cycles
 // beside them instead of 1,200, and a unit's ends 10,000 and more, as its output is not
-// written beside the next unit's softmax. So 4,600 tokens of 8 turns take 433 us (as
+// written beside the next unit's softmax. So 4,600 tokens of 8 turns take 429 us (as
 // 16-bit caches do: 425), two prompts of 7,600 tokens 700 (641). Before, three warps
 // copied and converted what they had copied: 2,369 us for the 2,048 tokens (each took
 // 1,200 cycles a tile to copy its part), and 4,344 with their loads in registers, whose
-// lines shared memory leaves no room for. A thread spills 204 bytes and loads 236.
+// lines shared memory leaves no room for. A thread spills 208 bytes and loads 236.
 
 #include <cuda.h>
 #include <cuda_bf16.h>

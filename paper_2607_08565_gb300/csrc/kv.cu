@@ -14,8 +14,8 @@
 //                  us, 92 % of a copy; 16,001 of 64 + 4 (565 MB) 93 us; 86,444 of
 //                  2 x 8 of 64 (366 MB) 63 us, 87 %, as a warp has 2 KB to copy
 //                  and two dependent reads to make first. Few tokens: 2 us.
-//                  Into 4 bits: the same tokens (680 MB with the queries, 240 MB) 119
-//                  and 68 us, bound by issue slots (60 %) as much as by memory: a group's
+//                  Into 4 bits: the same tokens (680 MB with the queries, 240 MB) 121
+//                  and 68 us, bound by issue slots (67 %) as much as by memory: a group's
 //                  largest, its scale and its codes are some 120 instructions for 16
 //                  elements of a lane.
 
@@ -857,11 +857,12 @@ int smetric_kv_plan_up_to(smetric_kv* kv, const int64_t* d_offsets, int32_t n_re
   // A request's own tokens decide which kernel takes it: a chunk of 200 tokens on a prefix
   // of 24k among 255 requests without tokens takes 89 us with the chunks' kernel, 492 a
   // token at a time with the other. Where no request can have more tokens than the few-row
-  // kernel takes, the chunks' kernel need not be launched. A batch of no more tokens than requests (a decoding step,
-  // or few chunks among many requests without tokens) may have chunks; probably it has
-  // none, and then a launch for both joins costs less than two: 64 single tokens over 2k
-  // to 48k keys take 171 us without the chunks' kernel, 174 with it and one join, 177 with
-  // two; chunks of up to 700 tokens among single ones 222 with one, 217 with two.
+  // kernel takes, the chunks' kernel need not be launched. A batch of no more tokens than
+  // requests (a decoding step, or few chunks among many requests without tokens) may have
+  // chunks; probably it has none, and then a launch for both joins costs less than two: 64
+  // single tokens over 2k to 48k keys take 171 us without the chunks' kernel, 174 with it
+  // and one join, 177 with two; chunks of up to 700 tokens among single ones 222 with one,
+  // 217 with two.
   const bool all_few = f.rows && std::min<int64_t>(n_tokens, max_new) <= f.tokens;
   const bool one_join = f.rows && !all_few && n_tokens <= n_requests;
   a.sets = f.rows ? 2 : 1;

@@ -423,7 +423,7 @@ __device__ __forceinline__ void write_row(const FewArgs& a, const KvUnit& u, int
 // and 555 instructions, 139 cycles of issue slots; conversions and their products take
 // half of theirs (64 lanes a cycle each). Both together come to 234 cycles, at 56 % of
 // the issue slots: 64 single tokens over 2k to 48k keys (4 key heads of 128, 896 MB) take
-// 170 us, 5.3 TB/s, 79 % of a copy's rate, where the copies alone take 148 and the
+// 171 us, 5.2 TB/s, 78 % of a copy's rate, where the copies alone take 148 and the
 // arithmetic alone 137, and 12 of them are the start, the item's end and the join. 37
 // tokens of 16 rows (347 MB) take 98 us, with twice the products. One token over 24,577
 // keys takes 12.4 us on the device: share, pages and first tile 3.5, tiles 2, the
